@@ -52,8 +52,12 @@ enum {
 typedef enum {
   ACRL_SCALE_PER_TENSOR = 0,  /* one fp32 scale for the whole matrix               */
   ACRL_SCALE_PER_ROW = 1,     /* one fp32 scale per row (token / vocabulary row)    */
-  ACRL_SCALE_MX32 = 2         /* one E8M0 scale per 32 consecutive elements of a row */
-} acrl_scaling;
+  ACRL_SCALE_MX32 = 2,        /* one E8M0 scale per 32 consecutive elements of a row */
+  ACRL_SCALE_ROW128 = 3,      /* one fp32 scale per 128 consecutive elements of a row
+                                 (activations of acrl_matmul_fp8)                   */
+  ACRL_SCALE_BLOCK128 = 4     /* one fp32 scale per block of 128 rows x 128 columns
+                                 (weights of acrl_matmul_fp8)                       */
+} acrl_scaling;                /* mu's operands in scoring and sampling: the first three */
 
 /* FP8 rounding: nearest-even (the "nearest-around" quantization of Sec. 5.1)
  * or toward zero (the truncated FP8 of the stress test, Sec. 5.3).          */
@@ -114,15 +118,18 @@ void acrl_abi_struct_sizes(size_t* score_desc, size_t* reduce_desc, size_t* cont
  *   x      bf16 [rows, ld], columns [0, cols) are used.  (device)
  *   q      uint8 [rows, cols], dense; E4M3 codes.                  (device, out)
  *   scales PER_TENSOR: float[1]; PER_ROW: float[rows];
- *          MX32: uint8 E8M0 [rows, cols/32].                       (device, out)
- * Definition.  PER_TENSOR / PER_ROW: amax = max |x| over the group, fp32;
+ *          MX32: uint8 E8M0 [rows, cols/32];
+ *          ROW128: float [rows, ceil(cols/128)];
+ *          BLOCK128: float [ceil(rows/128), ceil(cols/128)].       (device, out)
+ * Definition.  PER_TENSOR / PER_ROW / ROW128 / BLOCK128: amax = max |x| over the group, fp32;
  * s = amax / 448 (fp32, correctly rounded; s = 1 if amax == 0);
  * q = e4m3(x / s) with a correctly rounded fp32 divide.  MX32 (OCP MX v1.0):
  * per 32-element block, code = clamp(floor(log2 amax) - 8 + 127, 0, 254)
  * (0 for an all-zero block), q = e4m3(x * 2^(127 - code)).  e4m3() rounds as
  * `rounding` says and saturates magnitudes >= 448 to 448; NaN -> 0x7F|sign.
  * Requirements: rows >= 0, cols > 0 and a multiple of 32, ld >= cols and a
- * multiple of 8.  PER_TENSOR needs a workspace of
+ * multiple of 8.  The last groups of ROW128 and BLOCK128 hold what the matrix
+ * has left (cols % 128 columns, rows % 128 rows).  PER_TENSOR needs a workspace of
  * acrl_quantize_workspace_size() bytes; the others need none (may be NULL).
  */
 acrl_status acrl_quantize_workspace_size(int64_t rows, int64_t cols, int scaling, size_t* bytes);
@@ -508,6 +515,178 @@ typedef struct acrl_backward_desc {
 acrl_status acrl_backward_workspace_size(int64_t n_rows, int64_t d, int64_t V, int64_t token_chunk,
                                          size_t* bytes);
 acrl_status acrl_lm_head_backward(const acrl_backward_desc* desc, void* stream);
+
+/* ======================================================================== */
+/* acrl_matmul_fp8 -- product of block-scaled FP8 operands                   */
+/* ======================================================================== *
+ * A linear layer of an inference policy whose weights and activations are FP8
+ * with one scale per 128 elements (Sec. 5.1 quantizes weights and activations
+ * of the rollout engine; acrl_quantize_fp8 makes both operands):
+ *   y[m, n] = sum_b x_scales[m, b] w_scales[n / 128, b] sum_{k in block b} xq[m, k] wq[n, k]
+ * with b = k / 128.  The products of a block are summed by one matrix
+ * instruction, the scaled blocks in fp32, in an order that the sizes alone
+ * select (equal calls give equal bits; a row alone and among others may differ
+ * by fp32 roundings of the sum).  y is rounded once, to bf16 or fp32.  (The
+ * matrix instruction aligns a block's products to the largest before it adds
+ * them: a fp32 y of normally distributed operands is within 2e-5 of the exact
+ * sum, relative to its size, not within fp32's half step.)  A scale or code
+ * that is NaN makes the sums it enters NaN.
+ *   xq        e4m3 [M, K], x_scales float [M, ceil(K/128)]: ACRL_SCALE_ROW128
+ *   wq        e4m3 [N, K], w_scales float [ceil(N/128), ceil(K/128)]: ACRL_SCALE_BLOCK128
+ *   y         [M, N] of y_type, rows ldy elements apart; columns from N on are
+ *             not written
+ * Requirements: M >= 0, N > 0, M and N < 2^26, ceil(M/128) ceil(N/128) < 2^23;
+ * K > 0, K % 32 == 0, K <= 2^22; ldy >= N; xq, wq and y 16-byte aligned, the
+ * scales 4-byte.
+ */
+typedef enum { ACRL_OUT_BF16 = 0, ACRL_OUT_F32 = 1 } acrl_out_type;
+
+typedef struct acrl_matmul_desc {
+  int64_t M;                    /* rows of x (tokens)                                       */
+  int64_t N;                    /* rows of w (outputs)                                      */
+  int64_t K;                    /* columns of both                                          */
+  const void* xq;
+  const float* x_scales;
+  const void* wq;
+  const float* w_scales;
+  void* y;                      /* out                                                      */
+  int64_t ldy;                  /* elements between rows of y                               */
+  int32_t y_type;               /* acrl_out_type                                            */
+} acrl_matmul_desc;
+
+acrl_status acrl_matmul_fp8(const acrl_matmul_desc* desc, void* stream);
+
+/* ======================================================================== */
+/* acrl_policy_loss -- clipped policy loss with a KL term, and its gradient   */
+/* ======================================================================== *
+ * Beside acrl_surrogate (group mean of the clipped objective): the same clip
+ * with a bound on negative advantages, a KL penalty to a reference policy, and
+ * the usual ways to average.  For every valid slot t (mask != 0), with
+ * delta = logp_new - logp_old, r = exp(delta), q = logp_ref - logp_new:
+ *   m = min(r A, clip(r) A), clip(r) = min(max(r, 1 - eps_low), 1 + eps_high);
+ *       for A < 0 and dual_clip > 0: max(m, dual_clip A)
+ *   k = -q (K1), q^2 / 2 (K2) or exp(q) - q - 1 (K3), 0 without logp_ref
+ *   loss = sum_t a_t (-w_t m_t + kl_coef k_t)
+ *   coef[t] = d loss / d logp_new[t]
+ *           = a_t (-w_t r_t A_t [m is r A] + kl_coef k'_t),
+ *       k' = 1 (K1), -q (K2), 1 - exp(q) (K3); a tie counts as m = r A.
+ * a_t by `aggregate`:
+ *   GROUP     1 / (P G_g |a_i|), as acrl_surrogate: mean over the P prompts that
+ *             have a non-empty response of the mean over their G_g non-empty
+ *             responses of the mean over the |a_i| valid tokens
+ *   SEQUENCE  1 / (S |a_i|): mean over the S non-empty responses
+ *   TOKEN     1 / (number of valid tokens of the batch)
+ *   CONSTANT  1 / norm
+ * w_t (nullable: 1) is held constant.  Masked slots are not looked at whatever
+ * they hold, and get coef 0.  Under GROUP a response whose group id lies
+ * outside [0, n_groups) enters neither loss nor stats and gets coef NaN.  All
+ * is evaluated in fp64 from the fp32 inputs, sums by fixed trees.
+ * stats (nullable): ACRL_PSTAT_*.
+ * Requirements: B, L >= 0; for GROUP n_groups > 0 if B > 0 and group_of_seq
+ * non-NULL (else both are not read); eps_low in [0, 1), eps_high >= 0;
+ * dual_clip 0 (none) or > 1; kl_coef >= 0, and 0 without logp_ref; norm > 0
+ * for CONSTANT; B < 2^22 and B ceil(L/1024) < 2^23 (B ceil(L/4096) where B L >
+ * 2^20); workspace of acrl_policy_loss_workspace_size() bytes, 16-byte aligned. */
+typedef enum { ACRL_KL_K1 = 0, ACRL_KL_K2 = 1, ACRL_KL_K3 = 2 } acrl_kl_estimator;
+typedef enum {
+  ACRL_AGG_GROUP = 0, ACRL_AGG_SEQUENCE = 1, ACRL_AGG_TOKEN = 2, ACRL_AGG_CONSTANT = 3
+} acrl_aggregate;
+
+/* Slots of the policy loss's statistics (double[ACRL_N_PSTATS]); means over
+ * valid tokens, 0 if there are none.                                        */
+enum {
+  ACRL_PSTAT_POLICY = 0,        /* sum a_t (-w_t m_t)                               */
+  ACRL_PSTAT_KL = 1,            /* sum a_t k_t (0 without logp_ref)                 */
+  ACRL_PSTAT_CLIPPED = 2,       /* share of tokens whose clip is the minimum        */
+  ACRL_PSTAT_DUAL = 3,          /* share of tokens at the dual clip                 */
+  ACRL_PSTAT_MOVED = 4,         /* mean of r - 1 - delta: KL(old || new), estimated */
+  ACRL_PSTAT_N_TOKENS = 5,      /* valid tokens                                     */
+  ACRL_N_PSTATS = 6
+};
+
+typedef struct acrl_policy_loss_desc {
+  int64_t B;
+  int64_t L;
+  int64_t n_groups;
+  const uint8_t* mask;          /* [B*L]                                                    */
+  const int32_t* group_of_seq;  /* [B] (GROUP)                                              */
+  const float* logp_new;        /* [B*L] log pi_theta(a_t) of the policy being trained       */
+  const float* logp_old;        /* [B*L] log pi_theta_old(a_t)                              */
+  const float* logp_ref;        /* [B*L] log pi_ref(a_t), nullable (no KL term)              */
+  const float* adv;             /* [B] or [B*L] advantages A                                */
+  const float* weight;          /* [B*L] w_t (acrl_controller_step), nullable               */
+  int32_t adv_per_token;        /* 0: adv is [B]; 1: adv is [B*L]                           */
+  int32_t kl_estimator;         /* acrl_kl_estimator                                        */
+  int32_t aggregate;            /* acrl_aggregate                                           */
+  float eps_low;
+  float eps_high;
+  float dual_clip;              /* bound of m / A for A < 0, > 1; 0 = none                   */
+  float kl_coef;
+  float norm;                   /* CONSTANT                                                 */
+  float* coef;                  /* [B*L] out: d loss / d logp_new                           */
+  double* loss;                 /* [1] out                                                  */
+  double* stats;                /* [ACRL_N_PSTATS] out, nullable                            */
+  void* workspace;
+  size_t workspace_bytes;
+} acrl_policy_loss_desc;
+
+acrl_status acrl_policy_loss_workspace_size(int64_t B, int64_t L, int64_t n_groups, size_t* bytes);
+acrl_status acrl_policy_loss(const acrl_policy_loss_desc* desc, void* stream);
+
+/* ======================================================================== */
+/* acrl_preference_loss -- loss of preferred / rejected pairs, and its gradient */
+/* ======================================================================== *
+ * For every response i the log-ratio to the reference policy over its valid
+ * slots, x_i = sum_t (logp_new - logp_ref) (logp_ref NULL: sum_t logp_new),
+ * divided by the number of valid slots with mean_logp = 1 (0 for an empty
+ * response); for every pair p of a preferred and a rejected response
+ *   h_p = beta (x_chosen[p] - x_rejected[p]) - margin,
+ *   SIGMOID  l = -(1 - e) log sigmoid(h) - e log sigmoid(-h), e = label_smoothing
+ *   HINGE    l = max(0, 1 - h)      (slope 0 at h = 1)
+ *   SQUARED  l = ((h - 1/2) / beta)^2
+ *   loss = (1 / n_pairs) sum_p u_p l_p   (0 without pairs),  u = pair_weight or 1
+ *   coef[t] = d loss / d logp_new[t], for response i of slot t
+ *           = (beta / n_pairs) (sum_{p: chosen = i} - sum_{p: rejected = i}) u_p l'_p
+ *             (/ the number of valid slots with mean_logp).
+ * A response may be in any number of pairs, or in none (coef 0).  rewards
+ * (nullable) [2, n_pairs]: beta x of the preferred, then of the rejected ones.
+ * Masked slots are not looked at whatever they hold, and get coef 0.  An index
+ * outside [0, B) gives NaN: the reward it names, the loss, and coef of the
+ * pair's other response.  All is evaluated in fp64 from the fp32 inputs, sums
+ * by fixed trees.
+ * Requirements: B, L, n_pairs >= 0; B < 2^22; beta > 0; margin finite; label_smoothing in
+ * [0, 1), and 0 but for SIGMOID; workspace of
+ * acrl_preference_loss_workspace_size() bytes, 16-byte aligned.             */
+typedef enum { ACRL_PREF_SIGMOID = 0, ACRL_PREF_HINGE = 1, ACRL_PREF_SQUARED = 2 } acrl_preference_form;
+
+typedef struct acrl_preference_desc {
+  int64_t B;
+  int64_t L;
+  int64_t n_pairs;
+  const uint8_t* mask;          /* [B*L]                                                    */
+  const float* logp_new;        /* [B*L] log pi_theta(a_t) of the policy being trained       */
+  const float* logp_ref;        /* [B*L] log pi_ref(a_t), nullable                          */
+  const int32_t* chosen;        /* [n_pairs] index of the preferred response                */
+  const int32_t* rejected;      /* [n_pairs] index of the other                             */
+  const float* pair_weight;     /* [n_pairs], nullable                                      */
+  int32_t form;                 /* acrl_preference_form                                     */
+  int32_t mean_logp;            /* 1: x_i is the mean over the valid slots                  */
+  float beta;
+  float margin;
+  float label_smoothing;
+  float* coef;                  /* [B*L] out: d loss / d logp_new                           */
+  double* loss;                 /* [1] out                                                  */
+  float* rewards;               /* [2, n_pairs] out, nullable                               */
+  void* workspace;
+  size_t workspace_bytes;
+} acrl_preference_desc;
+
+acrl_status acrl_preference_loss_workspace_size(int64_t B, int64_t L, int64_t n_pairs, size_t* bytes);
+acrl_status acrl_preference_loss(const acrl_preference_desc* desc, void* stream);
+
+/* sizeof of the three descriptors above as compiled into the library (host),
+ * as acrl_abi_struct_sizes gives those of the others.                       */
+void acrl_abi_operator_struct_sizes(size_t* matmul_desc, size_t* policy_loss_desc, size_t* preference_desc);
 
 /* Host helper (host pointers): the reference discrepancy X of Sec. 4.1 is the
  * mean of Y_g over the non-empty groups (group_nseq > 0) of the step-0

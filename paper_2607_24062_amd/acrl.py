@@ -18,14 +18,20 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libacrl.so")
 
 ACRL_OK, ACRL_ERR_INVALID_ARG, ACRL_ERR_UNSUPPORTED, ACRL_ERR_WORKSPACE, ACRL_ERR_HIP = range(5)
-SCALE_PER_TENSOR, SCALE_PER_ROW, SCALE_MX32 = 0, 1, 2
+SCALE_PER_TENSOR, SCALE_PER_ROW, SCALE_MX32, SCALE_ROW128, SCALE_BLOCK128 = 0, 1, 2, 3, 4
 ROUND_NEAREST_EVEN, ROUND_TOWARD_ZERO = 0, 1
 Y_GROUP, Y_SEQUENCE, Y_BATCH = 0, 1, 2
 CTRL_ACRL, CTRL_TIS, CTRL_MIS, CTRL_CONTINUOUS, CTRL_FALLBACK = 0, 1, 2, 3, 4
 POLICY_BOTH, POLICY_PI, POLICY_MU = 0, 1, 2
+OUT_BF16, OUT_F32 = 0, 1
+KL_K1, KL_K2, KL_K3 = 0, 1, 2
+AGG_GROUP, AGG_SEQUENCE, AGG_TOKEN, AGG_CONSTANT = 0, 1, 2, 3
+PREF_SIGMOID, PREF_HINGE, PREF_SQUARED = 0, 1, 2
 N_STATS = 10
 STAT_NAMES = ["y_batch", "tok_mean_d", "tok_max_d", "tok_std_d", "mean_h_pi", "mean_h_mu",
               "n_tokens", "n_groups", "tok_mean_logratio", "n_seqs"]
+N_PSTATS = 6
+PSTAT_NAMES = ["policy", "kl", "clipped", "dual", "moved", "n_tokens"]
 
 EXPORTED = [
     "acrl_status_string", "acrl_last_error", "acrl_abi_version", "acrl_abi_struct_sizes",
@@ -36,6 +42,8 @@ EXPORTED = [
     "acrl_controller_step", "acrl_reference_from_groups", "acrl_sample_mu",
     "acrl_surrogate_workspace_size", "acrl_surrogate",
     "acrl_backward_workspace_size", "acrl_lm_head_backward",
+    "acrl_matmul_fp8", "acrl_policy_loss_workspace_size", "acrl_policy_loss",
+    "acrl_preference_loss_workspace_size", "acrl_preference_loss", "acrl_abi_operator_struct_sizes",
 ]
 
 _P = ctypes.c_void_p
@@ -97,6 +105,26 @@ class SampleDesc(ctypes.Structure):
                 ("seed", ctypes.c_uint64), ("row_offset", _I64),
                 ("ids", _P), ("logp_mu", _P), ("workspace", _P), ("workspace_bytes", _SZ),
                 ("packed_weights", _P), ("packed_weights_bytes", _SZ)]
+
+
+class MatmulDesc(ctypes.Structure):
+    _fields_ = [("M", _I64), ("N", _I64), ("K", _I64), ("xq", _P), ("x_scales", _P), ("wq", _P), ("w_scales", _P),
+                ("y", _P), ("ldy", _I64), ("y_type", _I32)]
+
+
+class PolicyLossDesc(ctypes.Structure):
+    _fields_ = [("B", _I64), ("L", _I64), ("n_groups", _I64), ("mask", _P), ("group_of_seq", _P),
+                ("logp_new", _P), ("logp_old", _P), ("logp_ref", _P), ("adv", _P), ("weight", _P),
+                ("adv_per_token", _I32), ("kl_estimator", _I32), ("aggregate", _I32),
+                ("eps_low", _F32), ("eps_high", _F32), ("dual_clip", _F32), ("kl_coef", _F32), ("norm", _F32),
+                ("coef", _P), ("loss", _P), ("stats", _P), ("workspace", _P), ("workspace_bytes", _SZ)]
+
+
+class PreferenceDesc(ctypes.Structure):
+    _fields_ = [("B", _I64), ("L", _I64), ("n_pairs", _I64), ("mask", _P), ("logp_new", _P), ("logp_ref", _P),
+                ("chosen", _P), ("rejected", _P), ("pair_weight", _P), ("form", _I32), ("mean_logp", _I32),
+                ("beta", _F32), ("margin", _F32), ("label_smoothing", _F32),
+                ("coef", _P), ("loss", _P), ("rewards", _P), ("workspace", _P), ("workspace_bytes", _SZ)]
 
 
 class AcrlError(RuntimeError):
@@ -164,10 +192,24 @@ def lib() -> ctypes.CDLL:
         L.acrl_backward_workspace_size.argtypes = [_I64, _I64, _I64, _I64, ctypes.POINTER(_SZ)]
         L.acrl_lm_head_backward.restype = _I32
         L.acrl_lm_head_backward.argtypes = [ctypes.POINTER(BackwardDesc), _P]
-        sizes = [_SZ() for _ in range(6)]
-        L.acrl_abi_struct_sizes(*[ctypes.byref(s) for s in sizes])
+        L.acrl_matmul_fp8.restype = _I32
+        L.acrl_matmul_fp8.argtypes = [ctypes.POINTER(MatmulDesc), _P]
+        L.acrl_policy_loss_workspace_size.restype = _I32
+        L.acrl_policy_loss_workspace_size.argtypes = [_I64, _I64, _I64, ctypes.POINTER(_SZ)]
+        L.acrl_policy_loss.restype = _I32
+        L.acrl_policy_loss.argtypes = [ctypes.POINTER(PolicyLossDesc), _P]
+        L.acrl_preference_loss_workspace_size.restype = _I32
+        L.acrl_preference_loss_workspace_size.argtypes = [_I64, _I64, _I64, ctypes.POINTER(_SZ)]
+        L.acrl_preference_loss.restype = _I32
+        L.acrl_preference_loss.argtypes = [ctypes.POINTER(PreferenceDesc), _P]
+        L.acrl_abi_operator_struct_sizes.restype = None
+        L.acrl_abi_operator_struct_sizes.argtypes = [ctypes.POINTER(_SZ)] * 3
+        sizes = [_SZ() for _ in range(9)]
+        L.acrl_abi_struct_sizes(*[ctypes.byref(s) for s in sizes[:6]])
+        L.acrl_abi_operator_struct_sizes(*[ctypes.byref(s) for s in sizes[6:]])
         want = [ctypes.sizeof(ScoreDesc), ctypes.sizeof(ReduceDesc), ctypes.sizeof(ControllerDesc),
-                ctypes.sizeof(SampleDesc), ctypes.sizeof(SurrogateDesc), ctypes.sizeof(BackwardDesc)]
+                ctypes.sizeof(SampleDesc), ctypes.sizeof(SurrogateDesc), ctypes.sizeof(BackwardDesc),
+                ctypes.sizeof(MatmulDesc), ctypes.sizeof(PolicyLossDesc), ctypes.sizeof(PreferenceDesc)]
         got = [s.value for s in sizes]
         if got != want:
             raise RuntimeError("libacrl descriptor layout mismatch: library %s, binding %s" % (got, want))
@@ -224,6 +266,36 @@ def _dev(t: torch.Tensor, dtype, name: str):
     return t
 
 
+def _want(t, dtype, numel: int, device, name: str, optional: bool = False):
+    """Device address of a contiguous tensor of numel elements on `device`."""
+    if t is None:
+        if optional:
+            return None
+        raise ValueError("%s is required" % name)
+    _dev(t, dtype, name)
+    if t.device != device:
+        raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
+    if t.numel() != numel:
+        raise ValueError("%s must have %d elements, got %d" % (name, numel, t.numel()))
+    return _ptr(t)
+
+
+def _on_current(device) -> None:
+    """The library launches on the current device: its tensors have to be there."""
+    if device.index != torch.cuda.current_device():
+        raise ValueError("the tensors are on %s, the current device is cuda:%d" % (device, torch.cuda.current_device()))
+
+
+def _empty(shape, dtype, device, stream=None):
+    """A fresh device tensor that belongs to the stream the call runs on.
+    Outputs and workspaces of a captured call then live in its graph's memory:
+    graphs share none, and nothing else takes it while the graph lives."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 _ws_cache: Dict[tuple, torch.Tensor] = {}
 
 
@@ -267,6 +339,10 @@ def acrl_quantize_fp8(x: torch.Tensor, scaling: int, rounding: int = ROUND_NEARE
             scales = torch.empty(1, dtype=torch.float32, device=x.device)
         elif scaling == SCALE_PER_ROW:
             scales = torch.empty(rows, dtype=torch.float32, device=x.device)
+        elif scaling == SCALE_ROW128:
+            scales = torch.empty((rows, (cols + 127) // 128), dtype=torch.float32, device=x.device)
+        elif scaling == SCALE_BLOCK128:
+            scales = torch.empty(((rows + 127) // 128, (cols + 127) // 128), dtype=torch.float32, device=x.device)
         else:
             scales = torch.empty((rows, cols // 32), dtype=torch.uint8, device=x.device)
     nb = _SZ()
@@ -528,3 +604,100 @@ def acrl_lm_head_backward(h, w, token_ids, coef, lse, inv_temperature: float = 1
                         token_chunk=int(token_chunk), workspace=_ptr(ws), workspace_bytes=nb.value)
     _check(lib().acrl_lm_head_backward(ctypes.byref(desc), _stream(stream)), "acrl_lm_head_backward")
     return (dh if want_dh else None), (dw if want_dw else None)
+
+
+# ------------------------------------------------------------------ block-scaled FP8 product
+_OUT_TYPES = {torch.bfloat16: OUT_BF16, torch.float32: OUT_F32}
+
+
+def acrl_matmul_fp8(xq, x_scales, wq, w_scales, out=None, out_dtype=torch.bfloat16, stream=None):
+    """y = x W^T [M, N] of FP8 operands with one scale per 128 elements:
+    xq uint8 [M, K] with SCALE_ROW128 scales, wq uint8 [N, K] with
+    SCALE_BLOCK128 scales (acrl_quantize_fp8).  `out` (bf16 or float32) may be
+    a column slice of a wider matrix: unit column stride, any row stride."""
+    _dev(xq, torch.uint8, "xq")
+    _dev(wq, torch.uint8, "wq")
+    if xq.dim() != 2 or wq.dim() != 2 or xq.shape[1] != wq.shape[1]:
+        raise ValueError("xq [M, K] and wq [N, K] must be 2-D with the same K")
+    M, K = xq.shape
+    N = wq.shape[0]
+    dev = xq.device
+    _on_current(dev)
+    kb = (K + 127) // 128
+    if out is None:
+        if out_dtype not in _OUT_TYPES:
+            raise ValueError("out_dtype must be torch.bfloat16 or torch.float32, got %s" % out_dtype)
+        out = _empty((M, N), out_dtype, dev, stream)
+    elif (out.dtype not in _OUT_TYPES or out.device != dev or tuple(out.shape) != (M, N) or
+          (N > 1 and out.stride(1) != 1) or (M > 1 and out.stride(0) < N)):
+        raise ValueError("out must be a bf16 or float32 device matrix [M, N] with unit column stride")
+    desc = MatmulDesc(M=M, N=N, K=K, xq=_ptr(xq), wq=_want(wq, torch.uint8, N * K, dev, "wq"),
+                      x_scales=_want(x_scales, torch.float32, M * kb, dev, "x_scales"),
+                      w_scales=_want(w_scales, torch.float32, (N + 127) // 128 * kb, dev, "w_scales"),
+                      y=_ptr(out), ldy=out.stride(0) if M > 1 else N, y_type=_OUT_TYPES[out.dtype])
+    _check(lib().acrl_matmul_fp8(ctypes.byref(desc), _stream(stream)), "acrl_matmul_fp8")
+    return out
+
+
+# ------------------------------------------------------------------ losses beside the surrogate
+def acrl_policy_loss(B: int, L: int, n_groups: int, mask, group_of_seq, logp_new, logp_old, adv,
+                     adv_per_token: bool, logp_ref=None, weight=None, eps_low: float = 0.2, eps_high: float = 0.2,
+                     dual_clip: float = 0.0, kl_coef: float = 0.0, kl_estimator: int = KL_K3,
+                     aggregate: int = AGG_GROUP, norm: float = 1.0, coef=None, stream=None):
+    """Clipped policy loss with a KL term to a reference policy: returns
+    (coef float32 [B*L] = d loss / d logp_new, loss float64 [1], stats float64
+    [N_PSTATS], PSTAT_NAMES).  coef goes to acrl_lm_head_backward."""
+    n, dev = B * L, logp_new.device
+    new = _want(logp_new, torch.float32, n, dev, "logp_new")
+    _on_current(dev)
+    if coef is None:
+        coef = _empty(n, torch.float32, dev, stream)
+    loss = _empty(1, torch.float64, dev, stream)
+    stats = _empty(N_PSTATS, torch.float64, dev, stream)
+    nb = _SZ()
+    _check(lib().acrl_policy_loss_workspace_size(B, L, n_groups, ctypes.byref(nb)),
+           "acrl_policy_loss_workspace_size")
+    ws = _empty(nb.value, torch.uint8, dev, stream)
+    desc = PolicyLossDesc(
+        B=B, L=L, n_groups=n_groups, mask=_want(mask, torch.uint8, n, dev, "mask"),
+        group_of_seq=_want(group_of_seq, torch.int32, B, dev, "group_of_seq", optional=True), logp_new=new,
+        logp_old=_want(logp_old, torch.float32, n, dev, "logp_old"),
+        logp_ref=_want(logp_ref, torch.float32, n, dev, "logp_ref", optional=True),
+        adv=_want(adv, torch.float32, n if adv_per_token else B, dev, "adv"),
+        weight=_want(weight, torch.float32, n, dev, "weight", optional=True),
+        adv_per_token=int(bool(adv_per_token)), kl_estimator=int(kl_estimator), aggregate=int(aggregate),
+        eps_low=float(eps_low), eps_high=float(eps_high), dual_clip=float(dual_clip), kl_coef=float(kl_coef),
+        norm=float(norm), coef=_want(coef, torch.float32, n, dev, "coef"), loss=_ptr(loss), stats=_ptr(stats),
+        workspace=_ptr(ws), workspace_bytes=nb.value)
+    _check(lib().acrl_policy_loss(ctypes.byref(desc), _stream(stream)), "acrl_policy_loss")
+    return coef, loss, stats
+
+
+def acrl_preference_loss(B: int, L: int, mask, logp_new, chosen, rejected, logp_ref=None, pair_weight=None,
+                         beta: float = 0.1, margin: float = 0.0, label_smoothing: float = 0.0,
+                         form: int = PREF_SIGMOID, mean_logp: bool = False, coef=None, stream=None):
+    """Loss of preferred / rejected response pairs (int32 response indexes
+    chosen, rejected [n_pairs]): returns (coef float32 [B*L] = d loss / d
+    logp_new, loss float64 [1], rewards float32 [2, n_pairs])."""
+    n, dev = B * L, logp_new.device
+    new = _want(logp_new, torch.float32, n, dev, "logp_new")
+    _on_current(dev)
+    P = chosen.numel()
+    if coef is None:
+        coef = _empty(n, torch.float32, dev, stream)
+    loss = _empty(1, torch.float64, dev, stream)
+    rewards = _empty((2, P), torch.float32, dev, stream)
+    nb = _SZ()
+    _check(lib().acrl_preference_loss_workspace_size(B, L, P, ctypes.byref(nb)),
+           "acrl_preference_loss_workspace_size")
+    ws = _empty(nb.value, torch.uint8, dev, stream)
+    desc = PreferenceDesc(
+        B=B, L=L, n_pairs=P, mask=_want(mask, torch.uint8, n, dev, "mask"), logp_new=new,
+        logp_ref=_want(logp_ref, torch.float32, n, dev, "logp_ref", optional=True),
+        chosen=_want(chosen, torch.int32, P, dev, "chosen"), rejected=_want(rejected, torch.int32, P, dev, "rejected"),
+        pair_weight=_want(pair_weight, torch.float32, P, dev, "pair_weight", optional=True), form=int(form),
+        mean_logp=int(bool(mean_logp)), beta=float(beta), margin=float(margin),
+        label_smoothing=float(label_smoothing), coef=_want(coef, torch.float32, n, dev, "coef"), loss=_ptr(loss),
+        rewards=_ptr(rewards), workspace=_ptr(ws), workspace_bytes=nb.value)
+    _check(lib().acrl_preference_loss(ctypes.byref(desc), _stream(stream)), "acrl_preference_loss")
+    return coef, loss, rewards

@@ -13,7 +13,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libacrl.so")
-SOURCES = ["api.hip", "quantize.hip", "score.hip", "reduce.hip"]
+SOURCES = ["api.hip", "quantize.hip", "score.hip", "reduce.hip", "product.hip", "losses.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -6,7 +6,7 @@
 
 #include <mutex>
 
-#include "acrl_internal.h"
+#include "entry.h"
 
 namespace acrl {
 
@@ -24,6 +24,8 @@ namespace {
 constexpr int kMaxDevices = 64;
 std::mutex g_dev_mu;
 int g_dev_state[kMaxDevices];  // 0 unknown, 1 gfx950, 2 other
+
+}  // namespace
 
 acrl_status check_device() {
   int dev = -1;
@@ -60,15 +62,7 @@ acrl_status hip_status(hipError_t e, const char* what) {
   return ACRL_ERR_HIP;
 }
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-
-#define ACRL_REQUIRE(cond, ...)       \
-  do {                                \
-    if (!(cond)) {                    \
-      acrl::set_error(__VA_ARGS__);   \
-      return ACRL_ERR_INVALID_ARG;    \
-    }                                 \
-  } while (0)
+namespace {
 
 size_t quantize_ws(int scaling) { return scaling == ACRL_SCALE_PER_TENSOR ? 256 : 0; }
 
@@ -182,7 +176,7 @@ void acrl_abi_struct_sizes(size_t* score_desc, size_t* reduce_desc, size_t* cont
 acrl_status acrl_quantize_workspace_size(int64_t rows, int64_t cols, int scaling, size_t* bytes) {
   ACRL_REQUIRE(bytes, "bytes is NULL");
   ACRL_REQUIRE(rows >= 0 && cols > 0, "rows must be >= 0 and cols > 0");
-  ACRL_REQUIRE(scaling >= ACRL_SCALE_PER_TENSOR && scaling <= ACRL_SCALE_MX32, "scaling %d unknown", scaling);
+  ACRL_REQUIRE(scaling >= ACRL_SCALE_PER_TENSOR && scaling <= ACRL_SCALE_BLOCK128, "scaling %d unknown", scaling);
   *bytes = acrl::quantize_ws(scaling);
   return ACRL_OK;
 }
@@ -193,10 +187,12 @@ acrl_status acrl_quantize_fp8(const void* x, int64_t rows, int64_t cols, int64_t
   ACRL_REQUIRE(rows >= 0, "rows = %lld must be >= 0", (long long)rows);
   ACRL_REQUIRE(cols > 0 && cols % 32 == 0, "cols = %lld must be a positive multiple of 32", (long long)cols);
   ACRL_REQUIRE(ld >= cols && ld % 8 == 0, "ld = %lld must be >= cols and a multiple of 8", (long long)ld);
-  ACRL_REQUIRE(scaling >= ACRL_SCALE_PER_TENSOR && scaling <= ACRL_SCALE_MX32, "scaling %d unknown", scaling);
+  ACRL_REQUIRE(scaling >= ACRL_SCALE_PER_TENSOR && scaling <= ACRL_SCALE_BLOCK128, "scaling %d unknown", scaling);
   ACRL_REQUIRE(rounding == ACRL_ROUND_NEAREST_EVEN || rounding == ACRL_ROUND_TOWARD_ZERO,
                "rounding %d unknown", rounding);
-  ACRL_REQUIRE(scales, "scales is NULL");
+  // (no rows: no scales, but the one of a tensor)
+  const bool blocks = scaling == ACRL_SCALE_ROW128 || scaling == ACRL_SCALE_BLOCK128;
+  ACRL_REQUIRE(scales || (blocks && rows == 0), "scales is NULL");
   if (rows > 0) {
     ACRL_REQUIRE(x && q, "x and q are required");
     ACRL_REQUIRE(acrl::aligned16(x) && acrl::aligned16(q), "x and q must be 16-byte aligned");

@@ -1,0 +1,431 @@
+// losses.hip -- the clipped policy loss with a KL term and the loss of
+// preferred / rejected pairs, each with its gradient with respect to the new
+// policy's log-probs (the coef that acrl_lm_head_backward takes).
+//
+// Layout: slots [B, L] row-major.  Every slot's inputs are read once; the
+// terms and sums are fp64, the sums by fixed trees (deterministic).
+#include "entry.h"
+#include "slots.h"
+
+namespace acrl {
+namespace {
+
+// exp(x) and exp(x) - 1 - x.  Next to 0 the difference cancels: there its
+// series x^2/2 (1 + x/3 (1 + x/4 (... (1 + x/8)))), whose next term is below
+// 2^-47 of it for |x| < 1/32, where the difference keeps 42 bits.
+__device__ __forceinline__ double exp_rest(double x, double& e) {
+  e = exp(x);
+  double s = 1.0 + x * (1.0 / 8);
+  s = 1.0 + x * (1.0 / 7) * s;
+  s = 1.0 + x * (1.0 / 6) * s;
+  s = 1.0 + x * 0.2 * s;
+  s = 1.0 + x * 0.25 * s;
+  s = 1.0 + x * (1.0 / 3) * s;
+  return fabs(x) < 0.03125 ? x * x * 0.5 * s : e - 1.0 - x;
+}
+
+// ------------------------------------------------------------------ policy loss
+// Sums of a unit of slots: policy term, KL term, clipped, at the dual clip,
+// moved, valid (the first two before a_t).
+constexpr int kPolicySums = 6;
+
+struct PolicyWs {
+  int32_t* n;        // [B] valid slots of a response (-1: its group id is out of range)
+  double* share;     // [B] a_t of the response's slots
+  int32_t* live;     // [n_groups] non-empty responses of a group
+  double* part;      // [kPolicySums][units]
+  int64_t bytes;
+};
+constexpr int kUnitThreads = 256;
+constexpr int64_t kMaxResponses = (int64_t)1 << 22;
+// Slots of a workgroup: 4 a thread, in 1 or 4 turns.
+inline int unit_turns(int64_t B, int64_t L) { return B * L > ((int64_t)1 << 20) ? 4 : 1; }
+inline int64_t units_of_response(int64_t B, int64_t L) {
+  const int64_t u = (int64_t)kUnitThreads * kSlots * unit_turns(B, L);
+  return (L + u - 1) / u;
+}
+PolicyWs policy_ws(void* base, int64_t B, int64_t L, int64_t n_groups) {
+  uint8_t* b = static_cast<uint8_t*>(base);
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off += align_up(bytes, 256);
+    return b + at;
+  };
+  PolicyWs w;
+  w.n = reinterpret_cast<int32_t*>(take((size_t)B * sizeof(int32_t)));
+  w.share = reinterpret_cast<double*>(take((size_t)B * sizeof(double)));
+  w.live = reinterpret_cast<int32_t*>(take((size_t)n_groups * sizeof(int32_t)));
+  w.part = reinterpret_cast<double*>(take((size_t)B * units_of_response(B, L) * kPolicySums * sizeof(double)));
+  w.bytes = (int64_t)off;
+  return w;
+}
+
+// Valid slots of each response, one wavefront per response.
+__global__ __launch_bounds__(kUnitThreads) void policy_count_kernel(acrl_policy_loss_desc p, int32_t* n) {
+  const int64_t i = (int64_t)blockIdx.x * (kUnitThreads / 64) + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (i >= p.B) return;
+  const uint8_t* m = p.mask + i * p.L;
+  int c = 0;
+  for (int64_t j = lane; j < p.L; j += 64) c += m[j] != 0;
+#pragma unroll
+  for (int s = 32; s > 0; s >>= 1) c += __shfl_xor(c, s);
+  if (lane == 0) {
+    const bool out = p.aggregate == ACRL_AGG_GROUP && (p.group_of_seq[i] < 0 || p.group_of_seq[i] >= p.n_groups);
+    n[i] = out ? -1 : c;
+  }
+}
+
+// a_t of every response, by one workgroup.
+__global__ __launch_bounds__(1024) void policy_share_kernel(acrl_policy_loss_desc p, PolicyWs ws) {
+  __shared__ BlockShared<2, 1024> sh;
+  double v[2] = {0, 0}, unused = 0.0;  // tokens, non-empty responses (groups)
+  if (p.aggregate == ACRL_AGG_GROUP) {
+    for (int64_t g = threadIdx.x; g < p.n_groups; g += 1024) ws.live[g] = 0;
+    __syncthreads();
+    for (int64_t i = threadIdx.x; i < p.B; i += 1024)
+      if (ws.n[i] > 0) atomicAdd(&ws.live[p.group_of_seq[i]], 1);
+    __syncthreads();
+    for (int64_t g = threadIdx.x; g < p.n_groups; g += 1024)
+      if (atomicAdd(&ws.live[g], 0) > 0) v[1] += 1.0;
+  } else {
+    for (int64_t i = threadIdx.x; i < p.B; i += 1024) {
+      v[0] += ws.n[i];
+      v[1] += ws.n[i] > 0 ? 1.0 : 0.0;
+    }
+  }
+  block_stats<2, 1024>(v, unused, sh);
+  for (int64_t i = threadIdx.x; i < p.B; i += 1024) {
+    const double n = ws.n[i];
+    double a = 0.0;
+    if (n < 0) a = __builtin_nan("");
+    else if (n > 0) {
+      switch (p.aggregate) {
+        case ACRL_AGG_GROUP: a = 1.0 / (v[1] * atomicAdd(&ws.live[p.group_of_seq[i]], 0) * n); break;
+        case ACRL_AGG_SEQUENCE: a = 1.0 / (v[1] * n); break;
+        case ACRL_AGG_TOKEN: a = 1.0 / v[0]; break;
+        default: a = 1.0 / (double)p.norm;
+      }
+    }
+    ws.share[i] = a;
+  }
+}
+
+// One slot: its terms added to v, its d(-w m + kl_coef k) / d logp_new returned.
+__device__ __forceinline__ double policy_slot(const acrl_policy_loss_desc& p, double ln, double lo, double lr,
+                                              double A, double w, double (&v)[kPolicySums]) {
+  const double delta = ln - lo, lo_r = 1.0 - (double)p.eps_low, hi_r = 1.0 + (double)p.eps_high;
+  double r;
+  v[4] += exp_rest(delta, r);
+  const bool over = A > 0 && r > hi_r, under = A < 0 && r < lo_r;
+  const bool dual = p.dual_clip > 0.0f && A < 0 && r > (double)p.dual_clip;
+  const double eff = over ? hi_r : under ? lo_r : dual ? (double)p.dual_clip : r;
+  v[0] -= w * (eff * A);
+  v[2] += over || under ? 1.0 : 0.0;
+  v[3] += dual ? 1.0 : 0.0;
+  v[5] += 1.0;
+  double g = over || under || dual ? 0.0 : -w * (r * A);
+  if (p.logp_ref) {
+    const double q = lr - ln;
+    double k, dk;
+    if (p.kl_estimator == ACRL_KL_K1) {
+      k = -q;
+      dk = 1.0;
+    } else if (p.kl_estimator == ACRL_KL_K2) {
+      k = 0.5 * q * q;
+      dk = -q;
+    } else {
+      double e;
+      k = exp_rest(q, e);
+      dk = -(k + q);
+    }
+    v[1] += k;
+    g += (double)p.kl_coef * dk;
+  }
+  return g;
+}
+
+// One unit of a response's slots: coef, and the unit's sums.
+template <int TURNS, bool VEC>
+__global__ __launch_bounds__(kUnitThreads) void policy_main_kernel(acrl_policy_loss_desc p, PolicyWs ws,
+                                                                   int64_t units) {
+  __shared__ BlockShared<kPolicySums, kUnitThreads> sh;
+  const int64_t i = blockIdx.x / units, u = blockIdx.x - i * units;
+  const int64_t base = i * p.L;
+  const double a = ws.share[i];
+  double v[kPolicySums] = {}, unused = 0.0;
+#pragma unroll
+  for (int t = 0; t < TURNS; ++t) {
+    const int64_t j = (u * TURNS + t) * kUnitThreads * kSlots + first_slot<kUnitThreads, VEC>();
+    if (j >= p.L) break;
+    uint8_t m[kSlots];
+    float ln[kSlots] = {}, lo[kSlots] = {}, lr[kSlots] = {}, w[kSlots] = {1.0f, 1.0f, 1.0f, 1.0f}, A[kSlots] = {}, c[kSlots] = {};
+    load_mask<kUnitThreads, VEC>(p.mask, base, j, p.L, m);
+    if (m[0] | m[1] | m[2] | m[3]) {
+      load_slots<kUnitThreads, VEC>(p.logp_new, base, j, p.L, ln);
+      load_slots<kUnitThreads, VEC>(p.logp_old, base, j, p.L, lo);
+      if (p.logp_ref) load_slots<kUnitThreads, VEC>(p.logp_ref, base, j, p.L, lr);
+      if (p.weight) load_slots<kUnitThreads, VEC>(p.weight, base, j, p.L, w);
+      if (p.adv_per_token) {
+        load_slots<kUnitThreads, VEC>(p.adv, base, j, p.L, A);
+      } else {
+#pragma unroll
+        for (int k = 0; k < kSlots; ++k) A[k] = p.adv[i];
+      }
+#pragma unroll
+      for (int k = 0; k < kSlots; ++k)
+        if (m[k]) c[k] = (float)(a * policy_slot(p, ln[k], lo[k], lr[k], A[k], w[k], v));
+    }
+    if constexpr (VEC) {
+      *reinterpret_cast<float4*>(p.coef + base + j) = make_float4(c[0], c[1], c[2], c[3]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kSlots; ++k)
+        if (j + k * kUnitThreads < p.L) p.coef[base + j + k * kUnitThreads] = c[k];
+    }
+  }
+  block_stats<kPolicySums, kUnitThreads>(v, unused, sh);
+  if (threadIdx.x == 0) {
+    const bool in = a == a;  // (a response of no group enters nothing)
+    const int64_t n = gridDim.x;
+#pragma unroll
+    for (int k = 0; k < kPolicySums; ++k) ws.part[k * n + blockIdx.x] = in ? (k < 2 ? a * v[k] : v[k]) : 0.0;
+  }
+}
+
+// loss and stats from the units' sums, by one workgroup.
+__global__ __launch_bounds__(1024) void policy_sum_kernel(acrl_policy_loss_desc p, PolicyWs ws, int64_t n) {
+  __shared__ BlockShared<kPolicySums, 1024> sh;
+  double v[kPolicySums] = {}, unused = 0.0;
+  for (int64_t u = threadIdx.x; u < n; u += 1024) {
+#pragma unroll
+    for (int k = 0; k < kPolicySums; ++k) v[k] += ws.part[k * n + u];
+  }
+  block_stats<kPolicySums, 1024>(v, unused, sh);
+  if (threadIdx.x != 0) return;
+  p.loss[0] = v[0] + (double)p.kl_coef * v[1];
+  if (!p.stats) return;
+  const double inv = v[5] > 0 ? 1.0 / v[5] : 0.0;
+  p.stats[ACRL_PSTAT_POLICY] = v[0];
+  p.stats[ACRL_PSTAT_KL] = v[1];
+  p.stats[ACRL_PSTAT_CLIPPED] = v[2] * inv;
+  p.stats[ACRL_PSTAT_DUAL] = v[3] * inv;
+  p.stats[ACRL_PSTAT_MOVED] = v[4] * inv;
+  p.stats[ACRL_PSTAT_N_TOKENS] = v[5];
+}
+
+hipError_t launch_policy_loss(const acrl_policy_loss_desc& p, hipStream_t s) {
+  const PolicyWs ws = policy_ws(p.workspace, p.B, p.L, p.n_groups);
+  const int64_t units = units_of_response(p.B, p.L), n = p.B * units;
+  if (n > 0) {
+    const int per = kUnitThreads / 64;
+    hipLaunchKernelGGL(policy_count_kernel, dim3((unsigned)((p.B + per - 1) / per)), dim3(kUnitThreads), 0, s, p, ws.n);
+    hipLaunchKernelGGL(policy_share_kernel, dim3(1), dim3(1024), 0, s, p, ws);
+    const bool vec = p.L % kSlots == 0 && aligned(p.mask, 4) && aligned(p.logp_new, 16) && aligned(p.logp_old, 16) &&
+                     aligned(p.logp_ref, 16) && aligned(p.weight, 16) && aligned(p.coef, 16) &&
+                     (!p.adv_per_token || aligned(p.adv, 16));
+    auto go = [&](auto turns, auto v) {
+      hipLaunchKernelGGL((policy_main_kernel<decltype(turns)::value, decltype(v)::value>), dim3((unsigned)n),
+                         dim3(kUnitThreads), 0, s, p, ws, units);
+    };
+    auto with = [&](auto turns) { vec ? go(turns, std::true_type{}) : go(turns, std::false_type{}); };
+    if (unit_turns(p.B, p.L) == 1) with(std::integral_constant<int, 1>{});
+    else with(std::integral_constant<int, 4>{});
+  }
+  hipLaunchKernelGGL(policy_sum_kernel, dim3(1), dim3(1024), 0, s, p, ws, n);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ preference loss
+struct PrefRec {
+  double x, each;  // x_i (mean_logp applied); d x_i / d logp_new of a valid slot
+};
+size_t pref_ws_bytes(int64_t B) { return align_up((size_t)B * sizeof(PrefRec), 256) + 256; }
+
+// x_i of each response, one workgroup per response.
+template <int NT, bool VEC>
+__global__ __launch_bounds__(NT) void pref_seq_kernel(acrl_preference_desc p, PrefRec* rec) {
+  __shared__ BlockShared<2, NT> sh;
+  const int64_t i = blockIdx.x;
+  const int64_t base = i * p.L;
+  double v[2] = {0, 0}, unused = 0.0;  // n, x
+  for (int64_t j = first_slot<NT, VEC>(); j < p.L; j += NT * kSlots) {
+    uint8_t m[kSlots];
+    float ln[kSlots], lr[kSlots] = {};
+    load_mask<NT, VEC>(p.mask, base, j, p.L, m);
+    if (!(m[0] | m[1] | m[2] | m[3])) continue;
+    load_slots<NT, VEC>(p.logp_new, base, j, p.L, ln);
+    if (p.logp_ref) load_slots<NT, VEC>(p.logp_ref, base, j, p.L, lr);
+#pragma unroll
+    for (int k = 0; k < kSlots; ++k) {
+      if (!m[k]) continue;
+      v[0] += 1.0;
+      v[1] += (double)ln[k] - (double)lr[k];
+    }
+  }
+  block_stats<2, NT>(v, unused, sh);
+  if (threadIdx.x == 0) {
+    const double each = p.mean_logp ? (v[0] > 0 ? 1.0 / v[0] : 0.0) : 1.0;
+    rec[i] = PrefRec{v[1] * each, each};
+  }
+}
+
+// The loss of pair `at` and u l'(h) beta / n_pairs; NaN for an index outside
+// the batch.
+__device__ __forceinline__ double pref_pair(const acrl_preference_desc& p, const PrefRec* rec, int64_t at, int32_t c,
+                                            int32_t r, double& loss) {
+  const double nan = __builtin_nan("");
+  const double xc = c >= 0 && c < p.B ? rec[c].x : nan, xr = r >= 0 && r < p.B ? rec[r].x : nan;
+  const double beta = p.beta, h = beta * (xc - xr) - (double)p.margin;
+  double l, d;
+  if (p.form == ACRL_PREF_SIGMOID) {
+    const double e = p.label_smoothing, t = exp(-fabs(h)), soft = log1p(t);
+    // sigmoid(h) and sigmoid(-h), each without cancellation
+    const double big = 1.0 / (1.0 + t), small = t * big, up = h >= 0 ? big : small, down = h >= 0 ? small : big;
+    l = (1.0 - e) * (soft + fmax(-h, 0.0)) + (e > 0 ? e * (soft + fmax(h, 0.0)) : 0.0);
+    d = h == h ? e * up - (1.0 - e) * down : nan;
+    if (!(h == h)) l = nan;  // (fmax drops a NaN)
+  } else if (p.form == ACRL_PREF_HINGE) {
+    l = h == h ? fmax(1.0 - h, 0.0) : nan;
+    d = h == h ? (h < 1.0 ? -1.0 : 0.0) : nan;
+  } else {
+    const double z = (h - 0.5) / beta;
+    l = z * z;
+    d = 2.0 * z / beta;
+  }
+  const double u = p.pair_weight ? (double)p.pair_weight[at] : 1.0;
+  loss = u * l;
+  return u * d * beta / (double)p.n_pairs;
+}
+
+// coef of one response's slots: its pairs' slopes, then one value for every
+// valid slot.  The last workgroup sums the loss and writes the rewards.
+__global__ __launch_bounds__(kUnitThreads) void pref_coef_kernel(acrl_preference_desc p, const PrefRec* rec) {
+  __shared__ BlockShared<1, kUnitThreads> sh;
+  double v[1] = {0}, unused = 0.0;
+  const int64_t i = blockIdx.x;
+  for (int64_t at = threadIdx.x; at < p.n_pairs; at += kUnitThreads) {
+    const int32_t c = p.chosen[at], r = p.rejected[at];
+    double l;
+    if (i == p.B) {
+      pref_pair(p, rec, at, c, r, l);
+      v[0] += l;
+      if (p.rewards) {
+        const float nan = __builtin_nanf("");
+        p.rewards[at] = c >= 0 && c < p.B ? (float)((double)p.beta * rec[c].x) : nan;
+        p.rewards[p.n_pairs + at] = r >= 0 && r < p.B ? (float)((double)p.beta * rec[r].x) : nan;
+      }
+    } else if ((c == i) != (r == i)) {  // (a response against itself: its slopes cancel)
+      const double g = pref_pair(p, rec, at, c, r, l);
+      v[0] += c == i ? g : -g;
+    }
+  }
+  block_stats<1, kUnitThreads>(v, unused, sh);
+  if (i == p.B) {
+    if (threadIdx.x == 0) p.loss[0] = p.n_pairs > 0 ? v[0] / (double)p.n_pairs : 0.0;
+    return;
+  }
+  const float c = (float)(v[0] * rec[i].each);
+  for (int64_t j = threadIdx.x; j < p.L; j += kUnitThreads) p.coef[i * p.L + j] = p.mask[i * p.L + j] ? c : 0.0f;
+}
+
+hipError_t launch_preference_loss(const acrl_preference_desc& p, hipStream_t s) {
+  PrefRec* rec = static_cast<PrefRec*>(p.workspace);
+  if (p.B > 0) {
+    const bool vec = p.L % kSlots == 0 && aligned(p.mask, 4) && aligned(p.logp_new, 16) && aligned(p.logp_ref, 16);
+    launch_seq(p.L <= 64 * kSlots ? 64 : kRedThreads, vec, [&](auto nt, auto v) {
+      constexpr int NT = decltype(nt)::value;
+      hipLaunchKernelGGL((pref_seq_kernel<NT, decltype(v)::value>), dim3((unsigned)p.B), dim3(NT), 0, s, p, rec);
+    });
+  }
+  hipLaunchKernelGGL(pref_coef_kernel, dim3((unsigned)p.B + 1), dim3(kUnitThreads), 0, s, p, (const PrefRec*)rec);
+  return hipGetLastError();
+}
+
+bool finite(float v) { return v - v == 0.0f; }
+
+}  // namespace
+}  // namespace acrl
+
+using acrl::set_error;
+
+extern "C" {
+
+acrl_status acrl_policy_loss_workspace_size(int64_t B, int64_t L, int64_t n_groups, size_t* bytes) {
+  ACRL_REQUIRE(bytes, "bytes is NULL");
+  ACRL_REQUIRE(B >= 0 && L >= 0 && n_groups >= 0, "B, L and n_groups must be >= 0");
+  // a launch holds fewer than 2^32 threads
+  ACRL_REQUIRE(B < acrl::kMaxResponses && L < INT32_MAX && n_groups < INT32_MAX, "B, L or n_groups too large");
+  ACRL_REQUIRE(B * acrl::units_of_response(B, L) < 2 * acrl::kMaxResponses, "B x L too large");
+  *bytes = (size_t)acrl::policy_ws(nullptr, B, L, n_groups).bytes + 256;
+  return ACRL_OK;
+}
+
+acrl_status acrl_policy_loss(const acrl_policy_loss_desc* d, void* stream) {
+  ACRL_REQUIRE(d, "desc is NULL");
+  size_t need = 0;
+  acrl_status st = acrl_policy_loss_workspace_size(d->B, d->L, d->n_groups, &need);
+  if (st != ACRL_OK) return st;
+  ACRL_REQUIRE(d->aggregate >= ACRL_AGG_GROUP && d->aggregate <= ACRL_AGG_CONSTANT, "aggregate %d unknown",
+               d->aggregate);
+  ACRL_REQUIRE(d->kl_estimator >= ACRL_KL_K1 && d->kl_estimator <= ACRL_KL_K3, "kl_estimator %d unknown",
+               d->kl_estimator);
+  ACRL_REQUIRE(d->eps_low >= 0.0f && d->eps_low < 1.0f, "eps_low must lie in [0, 1) (got %g)", (double)d->eps_low);
+  ACRL_REQUIRE(d->eps_high >= 0.0f && d->eps_high < 1e30f, "eps_high must be >= 0 (got %g)", (double)d->eps_high);
+  ACRL_REQUIRE(d->dual_clip == 0.0f || (d->dual_clip > 1.0f && d->dual_clip < 1e30f),
+               "dual_clip must be 0 or > 1 (got %g)", (double)d->dual_clip);
+  ACRL_REQUIRE(d->kl_coef >= 0.0f && d->kl_coef < 1e30f, "kl_coef must be >= 0 (got %g)", (double)d->kl_coef);
+  ACRL_REQUIRE(d->logp_ref || d->kl_coef == 0.0f || d->B == 0 || d->L == 0, "kl_coef needs logp_ref");
+  if (d->aggregate == ACRL_AGG_CONSTANT)
+    ACRL_REQUIRE(d->norm > 0.0f && acrl::finite(d->norm), "norm must be positive (got %g)", (double)d->norm);
+  ACRL_REQUIRE(d->loss, "loss is required");
+  if (d->B > 0 && d->aggregate == ACRL_AGG_GROUP)
+    ACRL_REQUIRE(d->n_groups > 0 && d->group_of_seq, "group_of_seq and n_groups > 0 are required");
+  if (d->B > 0 && d->L > 0)
+    ACRL_REQUIRE(d->mask && d->logp_new && d->logp_old && d->adv && d->coef,
+                 "mask, logp_new, logp_old, adv and coef are required");
+  if (!d->workspace || d->workspace_bytes < need) {
+    set_error("acrl_policy_loss needs %zu workspace bytes, got %zu", need, d->workspace_bytes);
+    return ACRL_ERR_WORKSPACE;
+  }
+  ACRL_REQUIRE(acrl::aligned16(d->workspace), "workspace must be 16-byte aligned");
+  st = acrl::check_device();
+  if (st != ACRL_OK) return st;
+  return acrl::hip_status(acrl::launch_policy_loss(*d, (hipStream_t)stream), "acrl_policy_loss launch");
+}
+
+acrl_status acrl_preference_loss_workspace_size(int64_t B, int64_t L, int64_t n_pairs, size_t* bytes) {
+  ACRL_REQUIRE(bytes, "bytes is NULL");
+  ACRL_REQUIRE(B >= 0 && L >= 0 && n_pairs >= 0, "B, L and n_pairs must be >= 0");
+  ACRL_REQUIRE(B < acrl::kMaxResponses && L < INT32_MAX && n_pairs < INT32_MAX, "B, L or n_pairs too large");
+  *bytes = acrl::pref_ws_bytes(B);
+  return ACRL_OK;
+}
+
+acrl_status acrl_preference_loss(const acrl_preference_desc* d, void* stream) {
+  ACRL_REQUIRE(d, "desc is NULL");
+  size_t need = 0;
+  acrl_status st = acrl_preference_loss_workspace_size(d->B, d->L, d->n_pairs, &need);
+  if (st != ACRL_OK) return st;
+  ACRL_REQUIRE(d->form >= ACRL_PREF_SIGMOID && d->form <= ACRL_PREF_SQUARED, "form %d unknown", d->form);
+  ACRL_REQUIRE(d->mean_logp == 0 || d->mean_logp == 1, "mean_logp must be 0 or 1");
+  ACRL_REQUIRE(d->beta > 0.0f && d->beta < 1e30f, "beta must be positive (got %g)", (double)d->beta);
+  ACRL_REQUIRE(acrl::finite(d->margin), "margin must be finite");
+  ACRL_REQUIRE(d->label_smoothing >= 0.0f && d->label_smoothing < 1.0f, "label_smoothing must lie in [0, 1) (got %g)",
+               (double)d->label_smoothing);
+  ACRL_REQUIRE(d->form == ACRL_PREF_SIGMOID || d->label_smoothing == 0.0f, "label_smoothing goes with SIGMOID only");
+  ACRL_REQUIRE(d->loss, "loss is required");
+  if (d->B > 0 && d->L > 0) ACRL_REQUIRE(d->mask && d->logp_new && d->coef, "mask, logp_new and coef are required");
+  if (d->n_pairs > 0) ACRL_REQUIRE(d->chosen && d->rejected, "chosen and rejected are required");
+  if (!d->workspace || d->workspace_bytes < need) {
+    set_error("acrl_preference_loss needs %zu workspace bytes, got %zu", need, d->workspace_bytes);
+    return ACRL_ERR_WORKSPACE;
+  }
+  ACRL_REQUIRE(acrl::aligned16(d->workspace), "workspace must be 16-byte aligned");
+  st = acrl::check_device();
+  if (st != ACRL_OK) return st;
+  return acrl::hip_status(acrl::launch_preference_loss(*d, (hipStream_t)stream), "acrl_preference_loss launch");
+}
+
+}  // extern "C"

@@ -1,9 +1,10 @@
 // quantize.hip -- FP8 (OCP E4M3) quantization of bf16 matrices for the
 // inference policy mu: per-tensor, per-row (per-token activations /
-// per-channel weights, Sec. 5.1 of the ACRL paper) and MX32 (one E8M0 scale
-// per 32 consecutive elements, the MXFP8 of Sec. 5.2).
+// per-channel weights, Sec. 5.1 of the ACRL paper), MX32 (one E8M0 scale
+// per 32 consecutive elements, the MXFP8 of Sec. 5.2), ROW128 and BLOCK128
+// (one fp32 scale per 128 elements of a row, or per 128 x 128 block).
 //
-// All three are HBM-bound streams: 2 bytes in and 1 byte out per element
+// All are HBM-bound streams: 2 bytes in and 1 byte out per element
 // (per-tensor reads the tensor twice: amax pass, then encode).  Loads and
 // stores are 16-byte vectors, one wavefront per row for the row kernels.
 #include "acrl_internal.h"
@@ -247,6 +248,78 @@ __global__ __launch_bounds__(256) void quantize_mx_kernel(const uint16_t* __rest
   }
 }
 
+// Maximum over 8 consecutive lanes (DPP: lane ^ 1, lane ^ 2, the mirror image
+// in the half row).
+__device__ __forceinline__ float max8(float v) {
+  v = fmaxf(v, dpp_f32<0xB1>(v));
+  v = fmaxf(v, dpp_f32<0x4E>(v));
+  return fmaxf(v, dpp_f32<0x141>(v));  // row_half_mirror
+}
+
+// 16 elements of a group with maximum amax and scale s.
+template <int ROUND>
+__device__ __forceinline__ uint4 encode16_of(uint4 a, uint4 b, float amax, float s) {
+  return rcp_ok(amax) ? encode16<ROUND, true>(a, b, s, 1.0f / s) : encode16<ROUND, false>(a, b, s, 0.0f);
+}
+
+// ROW128: 8 lanes per group of 128 elements, 32 bytes in and 16 out a lane.
+// `groups` = ceil(cols / 128) of a row; the last one's lanes past the row's
+// end take part in the maximum with 0.
+template <int ROUND>
+__global__ __launch_bounds__(256) void quantize_row128_kernel(const uint16_t* __restrict__ x, int64_t rows,
+                                                              int64_t cols, int64_t ld, int64_t groups,
+                                                              uint8_t* __restrict__ q, float* __restrict__ scales) {
+  // (a group's lanes are all in or all out)
+  for (int64_t g = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3); g < rows * groups; g += (int64_t)gridDim.x * 32) {
+    const int64_t r = g / groups, b = g - r * groups, c = 128 * b + 16 * (threadIdx.x & 7);
+    uint4 v[2] = {};
+    if (c < cols) {
+      const uint4* src = reinterpret_cast<const uint4*>(x + r * ld + c);
+      v[0] = src[0];
+      v[1] = src[1];
+    }
+    const float amax = max8(fmaxf(absmax8(v[0]), absmax8(v[1]))), s = group_scale(amax);
+    if (c < cols) *reinterpret_cast<uint4*>(q + r * cols + c) = encode16_of<ROUND>(v[0], v[1], amax, s);
+    if ((threadIdx.x & 7) == 0) scales[g] = s;
+  }
+}
+
+// BLOCK128: one workgroup per 128 x 128 block, 8 lanes a row, 4 rows a thread,
+// kept in registers between the maximum and the encoding.
+template <int ROUND>
+__global__ __launch_bounds__(256) void quantize_block128_kernel(const uint16_t* __restrict__ x, int64_t rows,
+                                                                int64_t cols, int64_t ld, int64_t groups,
+                                                                uint8_t* __restrict__ q, float* __restrict__ scales) {
+  __shared__ float sh[2][4];
+  const int64_t blocks = (rows + 127) / 128 * groups;
+  int turn = 0;
+  for (int64_t at = blockIdx.x; at < blocks; at += gridDim.x, turn ^= 1) {
+    const int64_t rb = at / groups, b = at - rb * groups;
+    const int64_t c = 128 * b + 16 * (threadIdx.x & 7), r0 = 128 * rb + (threadIdx.x >> 3);
+    uint4 v[4][2] = {};
+    float amax = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (c < cols && r0 + 32 * k < rows) {
+        const uint4* src = reinterpret_cast<const uint4*>(x + (r0 + 32 * k) * ld + c);
+        v[k][0] = src[0];
+        v[k][1] = src[1];
+      }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) amax = fmaxf(amax, fmaxf(absmax8(v[k][0]), absmax8(v[k][1])));
+    amax = wave_max(amax);
+    if ((threadIdx.x & 63) == 0) sh[turn][threadIdx.x >> 6] = amax;
+    __syncthreads();  // (two copies: the next block's maxima go beside those still being read)
+    amax = fmaxf(fmaxf(sh[turn][0], sh[turn][1]), fmaxf(sh[turn][2], sh[turn][3]));
+    const float s = group_scale(amax);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (c < cols && r0 + 32 * k < rows)
+        *reinterpret_cast<uint4*>(q + (r0 + 32 * k) * cols + c) = encode16_of<ROUND>(v[k][0], v[k][1], amax, s);
+    if (threadIdx.x == 0) scales[at] = s;
+  }
+}
+
 template <int ROUND>
 __global__ __launch_bounds__(256) void encode_kernel(const float* __restrict__ x, int64_t n,
                                                      uint8_t* __restrict__ q) {
@@ -288,6 +361,16 @@ hipError_t launch_quantize_t(const uint16_t* x, int64_t rows, int64_t cols, int6
     const int64_t blocks = rows * (cols >> 5);
     hipLaunchKernelGGL((quantize_mx_kernel<ROUND>), dim3(grid_for(blocks, 256, 1u << 20)),
                        dim3(256), 0, s, x, rows, cols, ld, q, (uint8_t*)scales);
+    return hipGetLastError();
+  }
+  if (scaling == ACRL_SCALE_ROW128 || scaling == ACRL_SCALE_BLOCK128) {
+    const int64_t groups = (cols + 127) / 128;
+    if (scaling == ACRL_SCALE_ROW128)
+      hipLaunchKernelGGL((quantize_row128_kernel<ROUND>), dim3(grid_for(rows * groups, 32, 1u << 22)), dim3(256),
+                         0, s, x, rows, cols, ld, groups, q, (float*)scales);
+    else
+      hipLaunchKernelGGL((quantize_block128_kernel<ROUND>), dim3(grid_for((rows + 127) / 128 * groups, 1, 1u << 22)),
+                         dim3(256), 0, s, x, rows, cols, ld, groups, q, (float*)scales);
     return hipGetLastError();
   }
   const uint32_t* amax = nullptr;

@@ -1,0 +1,161 @@
+"""acrl_matmul_fp8 against its definition in 64 bits: exact where the operands
+are small whole numbers and the scales powers of two (every layout, tail and
+split shows), within the instruction's bound for random ones."""
+import numpy as np
+import pytest
+
+from cases import random_bf16
+from gpu_util import down, torch_dev, up, up_bf16
+from operators64 import e4m3_values, product, quantize_blocks
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [(1, 1, 32), (1, 16, 128), (2, 130, 96), (7, 64, 160), (16, 256, 2080), (17, 200, 512), (33, 384, 1184),
+          (64, 1000, 256), (65, 129, 288), (100, 700, 640), (129, 128, 1024), (255, 257, 416), (256, 512, 384),
+          (333, 520, 2080), (513, 1025, 160), (1, 4096, 4096), (40, 2048, 5120)]
+
+
+def _integers(shape, seed):
+    """Codes of whole numbers -4 .. 4."""
+    val = e4m3_values()
+    codes = np.array([int(np.flatnonzero(val == v)[0]) for v in range(-4, 5)], np.uint8)
+    return codes[np.random.default_rng(seed).integers(0, 9, size=shape)]
+
+
+def _powers(shape, seed):
+    return np.exp2(np.random.default_rng(seed).integers(-2, 3, size=shape)).astype(np.float32)
+
+
+def _exact_case(M, N, K, seed):
+    kb = -(-K // 128)
+    return (_integers((M, K), seed), _powers((M, kb), seed + 1), _integers((N, K), seed + 2),
+            _powers((-(-N // 128), kb), seed + 3))
+
+
+def _run(ops, **kw):
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    return acrl.acrl_matmul_fp8(*[up(torch, dev, a) for a in ops], **kw)
+
+
+def _bf16(torch, y):
+    return torch.from_numpy(np.asarray(y, np.float32)).to(torch.bfloat16).float().numpy()
+
+
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_exact(M, N, K):
+    # sums of whole numbers times powers of two, below 2^24 units: every fp32 step is exact
+    torch, dev = torch_dev()
+    ops = _exact_case(M, N, K, M + N + K)
+    want = product(*ops)[0]
+    assert np.array_equal(down(_run(ops, out_dtype=torch.float32)), want.astype(np.float32))
+    assert np.array_equal(down(_run(ops).float()), _bf16(torch, want))
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 300, 4096), (5, 520, 1056), (48, 640, 2048), (130, 260, 5120), (300, 400, 928)])
+def test_random(M, N, K):
+    torch, dev = torch_dev()
+    xq, xs = quantize_blocks(random_bf16((M, K), K), 1)
+    wq, ws = quantize_blocks(random_bf16((N, K), K + 1, std=0.05), 128)
+    want, slack = product(xq, xs, wq, ws)
+    y = down(_run((xq, xs, wq, ws), out_dtype=torch.float32))
+    assert (np.abs(y - want) <= slack + 2.0 ** -24 * np.abs(want)).all(), (np.abs(y - want) / slack).max()
+    assert np.linalg.norm(y - want) <= 2e-5 * np.linalg.norm(want)
+    y = down(_run((xq, xs, wq, ws)).float())
+    assert (np.abs(y - want) <= slack * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("M,N", [(3, 150), (70, 260), (200, 300)])
+def test_output_slice(M, N):
+    # columns of a wider matrix at odd and even row strides, what lies around them left alone
+    torch, dev = torch_dev()
+    ops = _exact_case(M, N, 352, 5)
+    want = product(*ops)[0]
+    for wide, at in ((N + 8, 8), (N + 9, 0), (N + 11, 8)):
+        for dtype in (torch.bfloat16, torch.float32):
+            buf = torch.full((M + 2, wide), -7.0, dtype=dtype, device=dev)
+            out = buf[:M, at:at + N]
+            if out.data_ptr() % 16:
+                continue
+            got = _run(ops, out=out)
+            assert got.data_ptr() == out.data_ptr()
+            ref = np.full((M + 2, wide), -7.0, np.float32)
+            ref[:M, at:at + N] = want if dtype == torch.float32 else _bf16(torch, want)
+            assert np.array_equal(down(buf.float()), ref)
+
+
+@pytest.mark.parametrize("M", [1, 20, 65, 140])
+def test_nan_scale_and_code(M):
+    ops = [a.copy() for a in _exact_case(M, 270, 320, 3)]
+    ops[0][M - 1, 300] = 0x7F                  # a NaN code of the last token
+    ops[2][5, 17] = 0xFF                       # and of one weight row
+    ops[3][1, 2] = np.nan                      # the scale of outputs 128 .. 255, last block
+    y = down(_run(ops, out_dtype=torch_dev()[0].float32))
+    bad = np.zeros((M, 270), bool)
+    bad[M - 1] = bad[:, 5] = bad[:, 128:256] = True
+    assert np.array_equal(np.isnan(y), bad)
+
+
+def test_garbage_behind_the_last_rows_and_columns():
+    # operands that end inside an allocation full of NaN codes: the last row's tail and the rows behind stay out
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    for M, N, K in ((3, 77, 96), (70, 130, 160), (130, 140, 416)):
+        ops = _exact_case(M, N, K, 8)
+        t = []
+        for a in ops:
+            buf = torch.full((a.size * a.itemsize + 4096,), 0x7F, dtype=torch.uint8, device=dev)
+            raw = torch.from_numpy(a.view(np.uint8).reshape(-1))
+            buf[:raw.numel()] = raw.to(dev)
+            v = buf[:raw.numel()]
+            t.append((v if a.dtype == np.uint8 else v.view(torch.float32)).reshape(a.shape))
+        y = acrl.acrl_matmul_fp8(*t, out_dtype=torch.float32)
+        assert np.array_equal(down(y), product(*ops)[0].astype(np.float32))
+
+
+def test_no_rows_of_x():
+    torch, dev = torch_dev()
+    ops = _exact_case(1, 64, 128, 1)
+    y = _run((ops[0][:0], ops[1][:0], ops[2], ops[3]))
+    assert y.shape == (0, 64)
+
+
+@pytest.mark.parametrize("M", [1, 30, 130])
+def test_other_stream_and_repeats(M):
+    torch, dev = torch_dev()
+    ops = [up(torch, dev, a) for a in _exact_case(M, 390, 1056, 21)]
+    from paper_2607_24062_amd import acrl
+    want = acrl.acrl_matmul_fp8(*ops)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = acrl.acrl_matmul_fp8(*ops, stream=side)
+    with torch.cuda.stream(side):
+        again = acrl.acrl_matmul_fp8(*ops)
+    side.synchronize()
+    assert torch.equal(got, want) and torch.equal(again, want)
+
+
+@pytest.mark.parametrize("M", [1, 30, 130])
+def test_captured_and_replayed(M):
+    # quantization and product in one graph, replayed on new inputs, with eager calls between
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    K, N = 1056, 390
+    x = torch.zeros((M, K), dtype=torch.bfloat16, device=dev)
+    w = up_bf16(torch, dev, random_bf16((N, K), 2))
+    wq, ws = acrl.acrl_quantize_fp8(w, acrl.SCALE_BLOCK128)
+
+    def step():
+        xq, xs = acrl.acrl_quantize_fp8(x, acrl.SCALE_ROW128)
+        return acrl.acrl_matmul_fp8(xq, xs, wq, ws)
+
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        y = step()
+    for k in range(3):
+        x.copy_(up_bf16(torch, dev, random_bf16((M, K), 30 + k)))
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, step())

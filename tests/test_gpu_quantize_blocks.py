@@ -1,0 +1,84 @@
+"""GPU parity of acrl_quantize_fp8's ROW128 and BLOCK128 scalings with the
+oracle's quantizer on the same blocks: codes and scales bit for bit."""
+import numpy as np
+import pytest
+
+import oracle
+from cases import random_bf16
+from gpu_util import down, torch_dev, up_bf16
+from operators64 import quantize_blocks
+
+pytestmark = pytest.mark.gpu
+ROUNDINGS = [oracle.ROUND_NEAREST_EVEN, oracle.ROUND_TOWARD_ZERO]
+
+
+def _scaling(tile):
+    from paper_2607_24062_amd import acrl
+    return {1: acrl.SCALE_ROW128, 128: acrl.SCALE_BLOCK128}[tile]
+
+
+def _assert_same(bits, tile, rounding):
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    q, s = acrl.acrl_quantize_fp8(up_bf16(torch, dev, bits), _scaling(tile), rounding)
+    qo, so = quantize_blocks(bits, tile, rounding)
+    assert s.shape == so.shape
+    assert np.array_equal(down(s).view(np.uint32), so.astype(np.float32).view(np.uint32)), "scales differ"
+    assert np.array_equal(down(q), qo), np.argwhere(down(q) != qo)[:5]
+
+
+@pytest.mark.parametrize("tile", [1, 128])
+@pytest.mark.parametrize("rounding", ROUNDINGS)
+@pytest.mark.parametrize("shape", [(1, 32), (1, 128), (3, 96), (5, 160), (127, 4096), (128, 128), (129, 1056),
+                                   (300, 2080), (2, 9024)])
+def test_shapes(shape, tile, rounding):
+    _assert_same(random_bf16(shape, sum(shape), std=2.0), tile, rounding)
+
+
+@pytest.mark.parametrize("tile", [1, 128])
+@pytest.mark.parametrize("rounding", ROUNDINGS)
+def test_edge_values(tile, rounding):
+    # every finite bf16 pattern, a row of zeros, one of negative zeros, blocks of subnormals
+    b = np.arange(65536, dtype=np.uint32)
+    f = (b << 16).view(np.float32)
+    bits = b[np.isfinite(f)].astype(np.uint16)
+    x = np.concatenate([bits, np.zeros(-bits.size % 2048, np.uint16)]).reshape(-1, 2048)
+    x[3], x[4] = 0, 0x8000
+    _assert_same(x, tile, rounding)
+    y = random_bf16((256, 384), 5, std=1e-38)
+    _assert_same(y, tile, rounding)
+    z = np.zeros((130, 160), np.uint16)
+    z[129, 150] = 0x3F80
+    _assert_same(z, tile, rounding)
+
+
+@pytest.mark.parametrize("tile", [1, 128])
+def test_nan_and_infinity(tile):
+    # a NaN takes no part in the maximum and keeps its code; an infinite maximum gives an infinite scale
+    x = random_bf16((130, 288), 9, std=1.0)
+    x[2, 7], x[2, 200], x[129, 287] = 0x7FC0, 0x7F80, 0xFF80
+    for rounding in ROUNDINGS:
+        _assert_same(x, tile, rounding)
+
+
+@pytest.mark.parametrize("tile", [1, 128])
+def test_column_slice_and_rows_behind(tile):
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    wide = random_bf16((133, 512), 11)
+    x = up_bf16(torch, dev, wide)[:, 64:64 + 160]
+    q = torch.full((140, 160), 77, dtype=torch.uint8, device=dev)
+    groups = (140 if tile == 1 else 2) * 2
+    s = torch.full((groups + 2,), 5.0, device=dev)
+    acrl.acrl_quantize_fp8(x, _scaling(tile), q=q, scales=s)
+    qo, so = quantize_blocks(np.ascontiguousarray(wide[:, 64:64 + 160]), tile)
+    assert np.array_equal(down(q)[:133], qo) and (down(q)[133:] == 77).all()
+    assert np.array_equal(down(s)[:so.size], so.reshape(-1)) and (down(s)[so.size:] == 5.0).all()
+
+
+@pytest.mark.parametrize("tile", [1, 128])
+def test_no_rows(tile):
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    q, s = acrl.acrl_quantize_fp8(torch.empty((0, 256), dtype=torch.bfloat16, device=dev), _scaling(tile))
+    assert q.shape == (0, 256) and s.shape == (0, 2)

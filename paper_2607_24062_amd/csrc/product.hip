@@ -8,6 +8,8 @@
 // FMA a value, whose factor x_scale w_scale is one number a lane: the token is
 // the lane's own and the weight's scale is the same for all 128 outputs of a
 // wave.
+#include <type_traits>
+
 #include "entry.h"
 
 namespace acrl {
@@ -29,7 +31,7 @@ struct ProductParams {
   int M, N, K;
   int kb;                  // scale blocks of a row, ceil(K / 128)
   int n_mtiles, n_ntiles;
-  int vec;                 // y's rows take the vector stores
+  int vec, whole;          // y's rows take stores of four values; of 16 bytes
 };
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, int64_t bytes) {
@@ -58,117 +60,390 @@ __device__ __forceinline__ f32x4 mfma(const i32x8& a, const i32x8& b) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, zero, 0, 0, 0, 127, 0, 127);
 }
 
-__device__ __forceinline__ uint32_t bf16_rne(float f) {  // NaN stays NaN (quiet)
-  const uint32_t u = __float_as_uint(f);
-  if ((u & 0x7FFFFFFFu) > 0x7F800000u) return (u >> 16) | 0x40u;
-  return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
+__device__ __forceinline__ void add(f32x4& acc, const f32x4& t, float s) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) acc[e] = fmaf(t[e], s, acc[e]);
 }
+
+// The sums stand here: the compiler would move the last products into the
+// stores' branches, one after another.
+template <int A, int B>
+__device__ __forceinline__ void settle(f32x4 (&acc)[A][B]) {
+#pragma unroll
+  for (int i = 0; i < A; ++i)
+#pragma unroll
+    for (int j = 0; j < B; ++j) asm volatile("" : "+v"(acc[i][j]));
+}
+
+template <typename OUT>
+using out4 = OUT __attribute__((ext_vector_type(4)));
 
 // Four consecutive outputs n .. n + 3 of token m.
 template <typename OUT>
 __device__ __forceinline__ void store4(const ProductParams& p, int m, int n, const f32x4& v) {
   if (m >= p.M || n >= p.N) return;
   OUT* y = static_cast<OUT*>(p.y) + (int64_t)m * p.ldy + n;
-  if constexpr (sizeof(OUT) == 2) {
-    if (p.vec && n + 3 < p.N) {
-      *reinterpret_cast<uint2*>(y) = make_uint2(bf16_rne(v[0]) | bf16_rne(v[1]) << 16, bf16_rne(v[2]) | bf16_rne(v[3]) << 16);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (n + i < p.N) y[i] = (OUT)bf16_rne(v[i]);
-    }
+  const out4<OUT> o = __builtin_convertvector(v, out4<OUT>);
+  if (p.vec && n + 3 < p.N) {
+    *reinterpret_cast<out4<OUT>*>(y) = o;
   } else {
-    if (p.vec && n + 3 < p.N) {
-      *reinterpret_cast<float4*>(y) = make_float4(v[0], v[1], v[2], v[3]);
-    } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (n + i < p.N) y[i] = v[i];
+    for (int i = 0; i < 4; ++i)
+      if (n + i < p.N) y[i] = o[i];
+  }
+}
+
+// The sums of a TM x TN tile (WM x WN waves) to y by way of LDS: a wave's
+// lanes hold 16 tokens and write 8 or 16 bytes of each, which costs twice the
+// time of rows written whole (4096 x 4096 of K = 256: 23 us, 9 without stores).
+template <typename OUT, int TN, int TM, int WN, int WM, int PARTS, int A, int B>
+__device__ __forceinline__ void store_tile(const ProductParams& p, uint8_t* lds, int m0, int n0, int wm, int wn,
+                                           const f32x4 (&acc)[A][B]) {
+  constexpr int kPitch = TN * sizeof(OUT) + 16, kPiece = 16 / sizeof(OUT), kPieces = TN / kPiece;  // (16: other banks)
+  constexpr int kThreads = 64 * WN * WM, kRows = TM / PARTS;
+  static_assert(WM % PARTS == 0 && kRows * kPieces % kThreads == 0, "whole parts");
+  const int lane = threadIdx.x & 63, q = lane >> 4;
+#pragma unroll
+  for (int part = 0; part < PARTS; ++part) {
+    wait_loads_and_barrier<0>();
+    if (wm / (WM / PARTS) == part) {
+#pragma unroll
+      for (int j = 0; j < B; ++j)
+#pragma unroll
+        for (int i = 0; i < A; ++i)
+          *reinterpret_cast<out4<OUT>*>(lds + (wm % (WM / PARTS) * (TM / WM) + j * 16 + (lane & 15)) * kPitch +
+                                        (wn * (TN / WN) + i * 16 + 4 * q) * sizeof(OUT)) =
+              __builtin_convertvector(acc[i][j], out4<OUT>);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kRows * kPieces / kThreads; ++k) {
+      const int at = k * kThreads + threadIdx.x, r = at / kPieces, c = at % kPieces;
+      const int m = m0 + part * kRows + r, n = n0 + c * kPiece;
+      const uint8_t* from = lds + r * kPitch + c * 16;
+      OUT* y = static_cast<OUT*>(p.y) + (int64_t)m * p.ldy + n;
+      if (m < p.M && n + kPiece <= p.N) *reinterpret_cast<i32x4*>(y) = *reinterpret_cast<const i32x4*>(from);
+      else if (m < p.M)
+        for (int e = 0; e < kPiece && n + e < p.N; ++e) y[e] = reinterpret_cast<const OUT*>(from)[e];
     }
   }
 }
 
-// Tile of TN outputs x TM tokens a workgroup, WN x WM waves, K in blocks of
-// 128 bytes through two stages of LDS (buffer -> LDS loads, one barrier a
-// block).  Piece c (16 bytes) of row r lies at position c ^ (r / 2 mod 8) of
-// the row's 128 bytes: the 16 rows of a fragment then read 16 different
-// 16-byte columns of LDS's 64 banks.
-template <typename OUT, int TN, int TM, int WN, int WM>
-__global__ __launch_bounds__(64 * WN * WM) void product_tile_kernel(ProductParams p) {
-  constexpr int NW = WN * WM, AN = TN / WN / 16, BM = TM / WM / 16;  // 16-row fragments of a wave
-  constexpr int kStage = (TN + TM) * kBlock, kLoads = (TN + TM) / 8 / NW;
+// The workgroup's tile.  Consecutive workgroups go to the 8 XCDs in turn; each
+// XCD takes a contiguous range of tiles, ordered in bands of 8 token tiles
+// with the output tile as the slow index, so that the 32 tiles its CUs work
+// on at a time share 8 token tiles and 4 output tiles in its L2.
+constexpr int kXcds = 8, kBand = 8;
+__device__ __forceinline__ void tile_of(const ProductParams& p, int block, int& mt, int& nt) {
+  const int tiles = p.n_mtiles * p.n_ntiles, per = tiles / kXcds, more = tiles % kXcds;
+  const int xcd = block % kXcds, t = xcd * per + min(xcd, more) + block / kXcds;
+  const int band = t / (kBand * p.n_ntiles), rest = t - band * kBand * p.n_ntiles;
+  const int high = min(kBand, p.n_mtiles - band * kBand);
+  nt = rest / high;
+  mt = band * kBand + rest - nt * high;
+}
+
+// Tile of TN outputs x TM tokens a workgroup, WN x WM waves for each of KG
+// groups; a stage of LDS holds KG scale blocks of K, one a group (buffer -> LDS
+// loads, ST stages, one barrier a stage), and the groups' sums are added
+// through LDS in their order.  Piece c (16 bytes) of row r lies at position
+// c ^ (r / 2 mod 8) of the row's 128 bytes: the 16 rows of a fragment then read
+// 16 different 16-byte columns of LDS's 64 banks.
+template <typename OUT, int TN, int TM, int WN, int WM, int KG, int ST, int C>
+__global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(ProductParams p) {
+  constexpr int NW = WN * WM * KG, AN = TN / WN / 16, BM = TM / WM / 16;  // 16-row fragments of a wave
+  constexpr int kRows = TN + TM, kStage = kRows * kBlock * KG, kLoads = kRows * KG / 8 / NW;
+  // the scales of C blocks lie in LDS at a time, twice: x's [TM][C], W's [TN / 128][C]
+  constexpr int kChunk = (TM * C + 64) * 4, kChunkTurns = C / KG;
+  static_assert(kRows * KG % (8 * NW) == 0 && TN % 8 == 0 && TM * C % 64 == 0, "whole loads");
+  static_assert((TN + kBlock - 1) / kBlock * C <= 64 && ST - 1 <= kChunkTurns && C % KG == 0, "scales in time");
   static_assert(kBlock % (TN / WN) == 0, "a wave's outputs lie in one scale block");
-  __shared__ __align__(1024) uint8_t lds[2 * kStage + 2 * TM * 4];
-  float* const lds_s = reinterpret_cast<float*>(lds + 2 * kStage);  // x's scales of the two stages
+  static_assert(KG == 1 || KG * TN * TM * 4 <= ST * kStage, "the groups' sums fit the stages");
+  __shared__ __align__(1024) uint8_t lds[ST * kStage + 2 * kChunk];
+  uint8_t* const lds_s = lds + ST * kStage;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wn = wave % WN, wm = wave / WN;
-  const int nt = blockIdx.x % p.n_ntiles, mt = blockIdx.x / p.n_ntiles;
+  const int wn = wave % WN, wm = wave / WN % WM, g = wave / (WN * WM);
+  int mt, nt;
+  tile_of(p, blockIdx.x, mt, nt);
   const int n0 = nt * TN, m0 = mt * TM;
   const int last = p.kb - 1, tail = p.K - last * kBlock;  // bytes of the last block
+  const int turns = (p.kb + KG - 1) / KG;
 
   const __amdgpu_buffer_rsrc_t rw = make_rsrc(p.w + (int64_t)n0 * p.K, (int64_t)(p.N - n0) * p.K);
   const __amdgpu_buffer_rsrc_t rx = make_rsrc(p.x + (int64_t)m0 * p.K, (int64_t)(p.M - m0) * p.K);
   const __amdgpu_buffer_rsrc_t rs = make_rsrc(p.xs + (int64_t)m0 * p.kb, (int64_t)(p.M - m0) * p.kb * 4);
+  const int nb0 = n0 / kBlock, nb_last = (p.N - 1) / kBlock;
+  const __amdgpu_buffer_rsrc_t rv = make_rsrc(p.ws + (int64_t)nb0 * p.kb, (int64_t)(nb_last + 1 - nb0) * p.kb * 4);
   // rows past the matrix repeat its last one; their results are not stored
   uint32_t off[kLoads];
-  int piece[kLoads];
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
-    const int r = (i * NW + wave) * 8 + (lane >> 3);  // row of the stage: W's TN, then x's TM
+    const int r = ((i * NW + wave) * 8 + (lane >> 3)) % kRows;  // row of the group's part: W's TN, then x's TM
     const int row = r < TN ? min(r, p.N - 1 - n0) : min(r - TN, p.M - 1 - m0);
-    piece[i] = (lane & 7) ^ ((r >> 1) & 7);
-    off[i] = (uint32_t)row * (uint32_t)p.K + 16 * piece[i];
+    off[i] = (uint32_t)row * (uint32_t)p.K + 16 * ((lane & 7) ^ ((r >> 1) & 7));
   }
-  const uint32_t s_off = (uint32_t)min((int)(threadIdx.x % TM), p.M - 1 - m0) * (uint32_t)p.kb * 4;
 
-  auto load = [&](int kb) {
-    uint8_t* stage = lds + (kb & 1) * kStage;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      // pieces past the row's end (last block) read its block's first one; the fragments there are cleared
-      const uint32_t o = kb == last && 16 * piece[i] >= tail ? off[i] - 16 * piece[i] : off[i];
-      const bool is_w = (i * NW + wave) * 8 < TN;
-      buffer_to_lds<16>(is_w ? rw : rx, o, kb * kBlock, stage + (i * NW + wave) * 1024);
+  auto load = [&](int turn, int st) {
+    if (turn % kChunkTurns == 0) {
+      // scales first: they are there when the turn's operands are
+      uint8_t* const chunk = lds_s + (turn / kChunkTurns & 1) * kChunk;
+      for (int at = wave; at < TM * C / 64; at += NW) {
+        const int e = at * 64 + lane, kb = min(turn * KG + e % C, last);
+        buffer_to_lds<4>(rs, (uint32_t)(min(e / C, p.M - 1 - m0) * p.kb + kb) * 4, 0, chunk + at * 256);
+      }
+      if (wave == NW - 1) {
+        const int kb = min(turn * KG + lane % C, last);
+        buffer_to_lds<4>(rv, (uint32_t)(min(lane / C, nb_last - nb0) * p.kb + kb) * 4, 0, chunk + TM * C * 4);
+      }
     }
-    if (wave < TM / 64)
-      buffer_to_lds<4>(rs, s_off, kb * 4, lds + 2 * kStage + (kb & 1) * TM * 4 + wave * 256);
+    uint8_t* const stage = lds + st * kStage;
+    if ((turn + 1) * KG <= last) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int at = (i * NW + wave) * 8;
+        buffer_to_lds<16>(at % kRows < TN ? rw : rx, off[i], (turn * KG + at / kRows) * kBlock, stage + at * kBlock);
+      }
+    } else {
+      // blocks past the last repeat it and are not used; pieces past the row's end read the last block's first
+      // one, and the fragments there are cleared
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int at = (i * NW + wave) * 8;
+        const int kb = min(turn * KG + at / kRows, last), piece = (lane & 7) ^ (((at + (lane >> 3)) % kRows >> 1) & 7);
+        buffer_to_lds<16>(at % kRows < TN ? rw : rx, kb == last && 16 * piece >= tail ? off[i] - 16 * piece : off[i],
+                          kb * kBlock, stage + at * kBlock);
+      }
+    }
   };
 
   f32x4 acc[AN][BM] = {};
   const int q = lane >> 4, f = (lane >> 1) & 7;
-  const int lo = (lane & 15) * kBlock + (((2 * q) ^ f) << 4), hi = (lane & 15) * kBlock + (((2 * q + 1) ^ f) << 4);
-  const float* const ws = p.ws + (int64_t)min((n0 + wn * (TN / WN)) / kBlock, (p.N - 1) / kBlock) * p.kb;
-  load(0);
-  for (int kb = 0; kb < p.kb; ++kb) {
-    wait_loads_and_barrier<0>();
-    if (kb < last) load(kb + 1);
-    const uint8_t* sw = lds + (kb & 1) * kStage + wn * (TN / WN) * kBlock;
-    const uint8_t* sx = lds + (kb & 1) * kStage + (TN + wm * (TM / WM)) * kBlock;
-    const bool empty = kb == last && 32 * q >= tail;  // (K is a multiple of 32: a lane's 32 bytes are all in or all out)
+  const int lo = (lane & 15) * kBlock + ((q ^ f) << 4), hi = lo ^ 64;  // pieces q and q + 4
+  // One block of the wave's group.  LAST: it may be the last one, with less than 128 bytes a row
+  auto block = [&](int turn, int st, auto is_last) {
+    constexpr bool LAST = decltype(is_last)::value;
+    const int kb = turn * KG + g;
+    const uint8_t* sw = lds + st * kStage + (g * kRows + wn * (TN / WN)) * kBlock;
+    const uint8_t* sx = lds + st * kStage + (g * kRows + TN + wm * (TM / WM)) * kBlock;
+    const float* ss = reinterpret_cast<const float*>(lds_s + (turn / kChunkTurns & 1) * kChunk) +
+                      turn % kChunkTurns * KG + g;
+    const bool no_lo = LAST && kb == last && 16 * q >= tail, no_hi = LAST && kb == last && 16 * q + 64 >= tail;
     auto fragment = [&](const uint8_t* rows) {
-      const i32x4 u = *reinterpret_cast<const i32x4*>(rows + lo), v = *reinterpret_cast<const i32x4*>(rows + hi);
-      i32x8 r = __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
-      if (empty) r = i32x8{};
-      return r;
+      i32x4 u = *reinterpret_cast<const i32x4*>(rows + lo), v = *reinterpret_cast<const i32x4*>(rows + hi);
+      if (LAST && no_lo) u = i32x4{};
+      if (LAST && no_hi) v = i32x4{};
+      return __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    const float w_scale = ws[kb];
-    i32x8 b[BM];
+    // Row i's results are added while row i + 1's are made, and row i + 1's operand is read meanwhile
+    i32x8 a[2], b[BM];
+    f32x4 t[2][BM];
     float s[BM];
+    a[0] = fragment(sw);
+#pragma unroll
+    for (int j = 0; j < BM; ++j) b[j] = fragment(sx + j * 16 * kBlock);
+#pragma unroll
+    for (int j = 0; j < BM; ++j) s[j] = ss[(wm * (TM / WM) + j * 16 + (lane & 15)) * C];
+    const float w_scale = ss[TM * C + wn * (TN / WN) / kBlock * C];
+#pragma unroll
+    for (int i = 0; i < AN; ++i) {
+      if (i + 1 < AN) a[(i + 1) & 1] = fragment(sw + (i + 1) * 16 * kBlock);
+#pragma unroll
+      for (int j = 0; j < BM; ++j) {
+        t[i & 1][j] = mfma(a[i & 1], b[j]);
+        if (i == 0) s[j] *= w_scale;
+        if (i > 0) add(acc[i - 1][j], t[(i - 1) & 1][j], s[j]);
+        __builtin_amdgcn_sched_barrier(0);  // (left to itself the scheduler lets every product's sums wait for it)
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < BM; ++j) add(acc[AN - 1][j], t[(AN - 1) & 1][j], s[j]);
+  };
+#pragma unroll
+  for (int t = 0; t < ST - 1; ++t)
+    if (t < turns) load(t, t);
+  int st = 0;
+  for (int turn = 0; turn < turns - 1; ++turn) {
+    // this turn's loads are done once no more than those of the later turns are under way
+    if (turn + ST - 2 < turns) wait_loads_and_barrier<(ST - 2) * kLoads>();
+    else wait_loads_and_barrier<0>();
+    if (turn + ST - 1 < turns) load(turn + ST - 1, st == 0 ? ST - 1 : st - 1);
+    block(turn, st, std::false_type{});
+    st = st + 1 == ST ? 0 : st + 1;
+  }
+  wait_loads_and_barrier<0>();
+  if ((turns - 1) * KG + g <= last) block(turns - 1, st, std::true_type{});
+  settle(acc);
+  if constexpr (KG > 1) {
+    // the groups' sums through LDS: group g adds every KG-th of the WN WM AN BM blocks of 16 x 16
+    constexpr int kBlocks = WN * WM * AN * BM;
+    f32x4* const red = reinterpret_cast<f32x4*>(lds);
+    wait_loads_and_barrier<0>();
+#pragma unroll
+    for (int i = 0; i < AN; ++i)
+#pragma unroll
+      for (int j = 0; j < BM; ++j)
+        red[((g * kBlocks) + ((wm * WN + wn) * AN + i) * BM + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    for (int t = wave; t < kBlocks; t += NW) {
+      f32x4 v = red[t * 64 + lane];
+#pragma unroll
+      for (int h = 1; h < KG; ++h) v += red[(h * kBlocks + t) * 64 + lane];
+      const int j = t % BM, i = t / BM % AN, n = t / (BM * AN) % WN, m = t / (BM * AN * WN);
+      store4<OUT>(p, m0 + m * (TM / WM) + j * 16 + (lane & 15), n0 + n * (TN / WN) + i * 16 + 4 * q, v);
+    }
+  } else {
 #pragma unroll
     for (int j = 0; j < BM; ++j) {
-      b[j] = fragment(sx + j * 16 * kBlock);
-      s[j] = lds_s[(kb & 1) * TM + wm * (TM / WM) + j * 16 + (lane & 15)] * w_scale;
+      const int m = m0 + wm * (TM / WM) + j * 16 + (lane & 15);
+#pragma unroll
+      for (int i = 0; i < AN; ++i) store4<OUT>(p, m, n0 + wn * (TN / WN) + i * 16 + 4 * q, acc[i][j]);
+    }
+  }
+}
+
+// Many tokens: tiles of 256 x 256, 8 waves.  LDS is as busy as the matrix cores
+// here (a block's 512 rows are written once and read 1536 times 128 bytes, at
+// 128 bytes a cycle the 2048 cycles of the products), so nothing may wait for
+// the other: the barrier stands where a wave has its last operands of a block
+// in registers and two rows of products still to issue, and the first operands
+// of the next block are read under those.
+template <typename OUT, int WN, int WM>
+__global__ __launch_bounds__(512, 2) void product_wide_kernel(ProductParams p) {
+  constexpr int TN = 256, TM = 256, NW = 8, C = 8;
+
+  constexpr int AN = TN / WN / 16, BM = TM / WM / 16, kRows = TN + TM, kStage = kRows * kBlock, kLoads = kRows / 8 / NW;
+  constexpr int kChunk = (TM * C + 64) * 4;  // the scales of 8 blocks: x's [TM][C], W's [TN / 128][C]
+  static_assert(WN * WM == NW && kBlock % (TN / WN) == 0, "a wave's outputs lie in one scale block");
+  __shared__ __align__(1024) uint8_t lds[2 * kStage + 2 * kChunk];
+  uint8_t* const lds_s = lds + 2 * kStage;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wn = wave % WN, wm = wave / WN;
+  int mt, nt;
+  tile_of(p, blockIdx.x, mt, nt);
+  const int n0 = nt * TN, m0 = mt * TM;
+  const int last = p.kb - 1, tail = p.K - last * kBlock;
+  const __amdgpu_buffer_rsrc_t rw = make_rsrc(p.w + (int64_t)n0 * p.K, (int64_t)(p.N - n0) * p.K);
+  const __amdgpu_buffer_rsrc_t rx = make_rsrc(p.x + (int64_t)m0 * p.K, (int64_t)(p.M - m0) * p.K);
+  const __amdgpu_buffer_rsrc_t rs = make_rsrc(p.xs + (int64_t)m0 * p.kb, (int64_t)(p.M - m0) * p.kb * 4);
+  const int nb0 = n0 / kBlock, nb_last = (p.N - 1) / kBlock;
+  const __amdgpu_buffer_rsrc_t rv = make_rsrc(p.ws + (int64_t)nb0 * p.kb, (int64_t)(nb_last + 1 - nb0) * p.kb * 4);
+  // rows past the matrix repeat its last one; their results are not stored
+  uint32_t off[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int r = (i * NW + wave) * 8 + (lane >> 3);  // W's rows, then x's
+    const int row = r < TN ? min(r, p.N - 1 - n0) : min(r - TN, p.M - 1 - m0);
+    off[i] = (uint32_t)row * (uint32_t)p.K + 16 * ((lane & 7) ^ ((r >> 1) & 7));
+  }
+  // Pieces past the row's end (last block) read the block's first one; the fragments there are cleared.  (A lane's piece
+  // is the same in every load.  No branches from here to the last block: the compiler moves products past them, away
+  // from the reads of their operands.)
+  const int piece = (lane & 7) ^ ((wave * 8 + (lane >> 3)) >> 1 & 7), back = 16 * piece >= tail ? 16 * piece : 0;
+  auto load = [&](int kb, int i) {
+    const int less = back & -(int)(kb == last);
+    buffer_to_lds<16>(i < kLoads / 2 ? rw : rx, off[i] - less, kb * kBlock,
+                      lds + (kb & 1) * kStage + (i * NW + wave) * 1024);
+  };
+  // Part `part` (64 floats, the last one W's) of the scales of blocks C c .. C c + C - 1
+  constexpr int kParts = TM * C / 64;
+  auto load_scales = [&](int c, int part) {
+    const bool is_w = part == kParts;
+    const int row = is_w ? min(lane / C, nb_last - nb0) : min(part * (64 / C) + lane / C, p.M - 1 - m0);
+    const int k = min(C * c + lane % C, last);
+    buffer_to_lds<4>(is_w ? rv : rs, (uint32_t)(row * p.kb + k) * 4, 0, lds_s + (c & 1) * kChunk + part * 256);
+  };
+
+  f32x4 acc[AN][BM] = {};
+  const int q = lane >> 4, f = (lane >> 1) & 7;
+  const int lo = (lane & 15) * kBlock + ((q ^ f) << 4), hi = lo ^ 64;  // pieces q and q + 4
+  const int a_at = wn * (TN / WN) * kBlock, b_at = (TN + wm * (TM / WM)) * kBlock;
+  const int s_at = (wm * (TM / WM) + (lane & 15)) * C, w_at = TM * C + wn * (TN / WN) / kBlock * C;
+  auto fragment = [&](int at) {
+    const i32x4 u = *reinterpret_cast<const i32x4*>(lds + at + lo), v = *reinterpret_cast<const i32x4*>(lds + at + hi);
+    return __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  i32x8 a[2], b[BM];
+  f32x4 t[4];          // the last products, which enter the sums three products later
+  float s[BM], s_new[BM], w_new;
+  auto scales = [&](int kb) {
+    const float* ss = reinterpret_cast<const float*>(lds_s + (kb / C & 1) * kChunk) + kb % C;
+#pragma unroll
+    for (int j = 0; j < BM; ++j) s_new[j] = ss[s_at + j * 16 * C];
+    w_new = ss[w_at];
+  };
+  const bool no_lo = 16 * q >= tail, no_hi = 16 * q + 64 >= tail;  // in the last block
+  auto cut = [&](i32x8 v) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = no_lo ? 0 : v[e];
+      v[e + 4] = no_hi ? 0 : v[e + 4];
+    }
+    return v;
+  };
+  // The products of block kb, whose b and a[0] are there; MORE: with the reads of the next block's, else it is the last
+  auto block = [&](int kb, auto more) {
+    constexpr bool MORE = decltype(more)::value;
+    const int st = (kb & 1) * kStage, next = kStage - st;
+    if (!MORE) {
+      a[0] = cut(a[0]);
+#pragma unroll
+      for (int j = 0; j < BM; ++j) b[j] = cut(b[j]);
     }
 #pragma unroll
     for (int i = 0; i < AN; ++i) {
-      const i32x8 a = fragment(sw + i * 16 * kBlock);
+      if (i + 1 < AN) {
+        const i32x8 v = fragment(st + a_at + (i + 1) * 16 * kBlock);
+        a[(i + 1) & 1] = MORE ? v : cut(v);
+      }
+      if (MORE && i == AN - 1) {
+        // all waves' loads of block kb + 1 and reads of block kb are done
+        wait_loads_and_barrier<0>();
+load_scales(kb / C + 1, min(kb % C * NW + wave, kParts));  // (a part a wave, in time for the next C blocks)
+        a[0] = fragment(next + a_at);
+        scales(kb + 1);
+      }
 #pragma unroll
       for (int j = 0; j < BM; ++j) {
-        const f32x4 t = mfma(a, b[j]);
+        const int n = i * BM + j, d = n - 3;  // the product made, and the one added
+        t[n & 3] = mfma(a[i & 1], b[j]);
+        if (d >= 0) add(acc[d / BM][d % BM], t[d & 3], s[d % BM]);
+        else add(acc[AN - 1][BM + d], t[d & 3], s[BM + d]);  // (of the block before)
+        if (n == 2) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(t[e], s[j], acc[i][j][e]);
+          for (int k = 0; k < BM; ++k) s[k] = s_new[k] * w_new;
+        }
+        if (MORE && i == AN - 1) b[j] = fragment(next + b_at + j * 16 * kBlock);
+        // the loads of the block after next, one behind each product from the barrier on (all at once they hold the
+        // products up: 16384 x 5120 x 13824 1024 us, 983 so)
+        if (MORE && i == AN - 1) load(min(kb + 2, last), j);
+        if (MORE && n + BM < kLoads) load(kb + 1, n + BM);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
+  };
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) load(0, i);
+  for (int part = wave; part <= kParts; part += NW) load_scales(0, part);
+  wait_loads_and_barrier<0>();
+#pragma unroll
+  for (int i = 0; i < BM; ++i) load(min(1, last), i);
+  a[0] = fragment(a_at);
+#pragma unroll
+  for (int j = 0; j < BM; ++j) b[j] = fragment(b_at + j * 16 * kBlock);
+  scales(0);
+#pragma unroll
+  for (int j = 0; j < BM; ++j) s[j] = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) t[e] = f32x4{};
+  for (int kb = 0; kb < last; ++kb) block(kb, std::true_type{});
+  block(last, std::false_type{});
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (loads past the last block may still be under way into LDS)
+#pragma unroll
+  for (int d = 0; d < 3; ++d) add(acc[AN - 1][BM - 3 + d], t[(AN * BM - 3 + d) & 3], s[BM - 3 + d]);
+  settle(acc);
+  if (p.whole) {
+    store_tile<OUT, TN, TM, WN, WM, sizeof(OUT) / 2>(p, lds, m0, n0, wm, wn, acc);
+    return;
   }
 #pragma unroll
   for (int j = 0; j < BM; ++j) {
@@ -178,14 +453,159 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tile_kernel(ProductParam
   }
 }
 
-template <typename OUT>
-hipError_t launch_product(ProductParams p, hipStream_t s) {
-  constexpr int TN = 128, TM = 128;
+template <typename OUT, int WN, int WM>
+hipError_t launch_wide(ProductParams p, hipStream_t s) {
+  p.n_ntiles = (p.N + 255) / 256;
+  p.n_mtiles = (p.M + 255) / 256;
+  hipLaunchKernelGGL((product_wide_kernel<OUT, WN, WM>), dim3((unsigned)(p.n_ntiles * (int64_t)p.n_mtiles)), dim3(512), 0,
+                     s, p);
+  return hipGetLastError();
+}
+
+// Few tokens: the weights' stream from HBM is the whole work, and a workgroup
+// takes 16 AN outputs x 16 BM tokens so that many of them share it out.  Its
+// NW waves take every NW-th scale block each, U of them at a time, straight
+// into registers: 16-byte pieces q and q + 4 of a row's 128 bytes for lane
+// group q, so that a load takes 64 contiguous bytes of each row (the products
+// of a block may be summed in any order of k, as long as both operands have
+// the same).  The waves' sums are added through LDS in their order.
+template <typename OUT, int AN, int BM, int NW, int U>
+__global__ __launch_bounds__(64 * NW, 2) void product_rows_kernel(ProductParams p) {
+  __shared__ f32x4 red[NW][AN * BM][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int mt = blockIdx.x % p.n_mtiles, nt = blockIdx.x / p.n_mtiles;
+  const int n0 = nt * 16 * AN, m0 = mt * 16 * BM, q = lane >> 4;
+  const int last = p.kb - 1, tail = p.K - last * kBlock;
+  const uint8_t *pw[AN], *px[BM];
+  const float* ps[BM];
+#pragma unroll
+  for (int i = 0; i < AN; ++i) pw[i] = p.w + (int64_t)min(n0 + 16 * i + (lane & 15), p.N - 1) * p.K;
+#pragma unroll
+  for (int j = 0; j < BM; ++j) {
+    const int64_t m = min(m0 + 16 * j + (lane & 15), p.M - 1);
+    px[j] = p.x + m * p.K;
+    ps[j] = p.xs + m * p.kb;
+  }
+  const float* const ws = p.ws + (int64_t)(n0 / kBlock) * p.kb;  // (16 AN divides 128)
+  f32x4 acc[AN][BM] = {};
+  for (int k0 = wave; k0 < p.kb; k0 += NW * U) {
+    i32x4 a[U][AN][2], b[U][BM][2];
+    float s[U][BM];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      // blocks past the last repeat it, pieces past its end its first; neither is used
+      const int kb = min(k0 + u * NW, last);
+      const int o0 = kb * kBlock + (kb == last && 16 * q >= tail ? 0 : 16 * q);
+      const int o1 = kb * kBlock + (kb == last && 16 * q + 64 >= tail ? 0 : 16 * q + 64);
+#pragma unroll
+      for (int i = 0; i < AN; ++i) {
+        a[u][i][0] = *reinterpret_cast<const i32x4*>(pw[i] + o0);
+        a[u][i][1] = *reinterpret_cast<const i32x4*>(pw[i] + o1);
+      }
+#pragma unroll
+      for (int j = 0; j < BM; ++j) {
+        b[u][j][0] = *reinterpret_cast<const i32x4*>(px[j] + o0);
+        b[u][j][1] = *reinterpret_cast<const i32x4*>(px[j] + o1);
+        s[u][j] = ps[j][kb];
+      }
+#pragma unroll
+      for (int j = 0; j < BM; ++j) s[u][j] *= ws[kb];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int kb = k0 + u * NW;
+      if (kb > last) break;
+      const bool no0 = kb == last && 16 * q >= tail, no1 = kb == last && 16 * q + 64 >= tail;
+      auto operand = [&](i32x4 (&h)[2]) {
+        const i32x4 zero = {0, 0, 0, 0};
+        return __builtin_shufflevector(no0 ? zero : h[0], no1 ? zero : h[1], 0, 1, 2, 3, 4, 5, 6, 7);
+      };
+      i32x8 bf[BM];
+#pragma unroll
+      for (int j = 0; j < BM; ++j) bf[j] = operand(b[u][j]);
+#pragma unroll
+      for (int i = 0; i < AN; ++i) {
+        const i32x8 af = operand(a[u][i]);
+#pragma unroll
+        for (int j = 0; j < BM; ++j) {
+          const f32x4 t = mfma(af, bf[j]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(t[e], s[u][j], acc[i][j][e]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < AN; ++i)
+#pragma unroll
+    for (int j = 0; j < BM; ++j) red[wave][i * BM + j][lane] = acc[i][j];
+  __syncthreads();
+  for (int t = wave; t < AN * BM; t += NW) {
+    f32x4 v = red[0][t][lane];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) v += red[w][t][lane];
+    store4<OUT>(p, m0 + 16 * (t % BM) + (lane & 15), n0 + 16 * (t / BM) + 4 * q, v);
+  }
+}
+
+template <typename OUT, int AN, int BM, int NW, int U>
+hipError_t launch_rows(ProductParams p, hipStream_t s) {
+  p.n_ntiles = (p.N + 16 * AN - 1) / (16 * AN);
+  p.n_mtiles = (p.M + 16 * BM - 1) / (16 * BM);
+  hipLaunchKernelGGL((product_rows_kernel<OUT, AN, BM, NW, U>), dim3((unsigned)(p.n_ntiles * (int64_t)p.n_mtiles)),
+                     dim3(64 * NW), 0, s, p);
+  return hipGetLastError();
+}
+
+template <typename OUT, int TN, int TM, int WN, int WM, int KG, int ST, int C>
+hipError_t launch_tiles(ProductParams p, hipStream_t s) {
   p.n_ntiles = (p.N + TN - 1) / TN;
   p.n_mtiles = (p.M + TM - 1) / TM;
-  hipLaunchKernelGGL((product_tile_kernel<OUT, TN, TM, 2, 2>), dim3((unsigned)(p.n_ntiles * (int64_t)p.n_mtiles)),
-                     dim3(256), 0, s, p);
+  hipLaunchKernelGGL((product_tile_kernel<OUT, TN, TM, WN, WM, KG, ST, C>), dim3((unsigned)(p.n_ntiles * (int64_t)p.n_mtiles)),
+                     dim3(64 * WN * WM * KG), 0, s, p);
   return hipGetLastError();
+}
+
+// The kernels and what they take: `turn` us for KG scale blocks of every tile
+// of a round (per_cu tiles a CU), `round` us beside them.  Both are fits to
+// times of 90 sizes (M 1 .. 4096; N x K 4096 x 4096, 24576 x 4096, 5120 x 13824,
+// 1024 x 5120, 2048 x 2048), 6-13 % off each; the kernel that they choose is 0.8 %
+// slower than the fastest of the nine on average, 12 % at most.  Without the
+// last but one, 2.3 % and 27 %.
+template <typename OUT>
+struct Variant {
+  int tn, tm, kg, per_cu;
+  float turn, round;
+  hipError_t (*launch)(ProductParams, hipStream_t);
+};
+constexpr int kCus = 256;
+template <typename OUT>
+float cost(const Variant<OUT>& v, const ProductParams& p) {
+  const int64_t tiles = (int64_t)((p.N + v.tn - 1) / v.tn) * ((p.M + v.tm - 1) / v.tm), slots = kCus * v.per_cu;
+  const int64_t rest = tiles % slots;
+  // a round of one tile a CU, where two fit, takes 0.78 of a full one
+  const float rounds = (float)(tiles / slots) + (rest == 0 ? 0.0f : rest > kCus || v.per_cu == 1 ? 1.0f : 0.78f);
+  return rounds * ((float)((p.kb + v.kg - 1) / v.kg) * v.turn + v.round);
+}
+
+template <typename OUT>
+hipError_t launch_product(const ProductParams& p, hipStream_t s) {
+  // Up to 16 tokens: 16 outputs a workgroup while that is needed to have workgroups for the CUs (1 x 4096 x 4096
+  // 5.8 us, 6.7 with 32), 32 from there on (8 x 5120 x 13824 20 us, 26 with 16)
+  if (p.M <= 16) return p.N < 20 * kCus ? launch_rows<OUT, 1, 1, 8, 2>(p, s) : launch_rows<OUT, 2, 1, 8, 2>(p, s);
+  static const Variant<OUT> variants[] = {
+      {32, 32, 8, 1, 1.237f, 1.13f, launch_tiles<OUT, 32, 32, 1, 1, 8, 2, 16>},
+      {64, 32, 4, 1, 0.805f, 1.69f, launch_tiles<OUT, 64, 32, 2, 1, 4, 3, 8>},
+      {64, 64, 2, 1, 0.560f, 2.48f, launch_tiles<OUT, 64, 64, 2, 2, 2, 4, 8>},
+      {128, 64, 2, 1, 0.860f, 2.82f, launch_tiles<OUT, 128, 64, 2, 2, 2, 3, 8>},
+      {128, 128, 1, 2, 1.152f, 2.32f, launch_tiles<OUT, 128, 128, 2, 2, 1, 2, 8>},
+      {128, 128, 2, 1, 1.491f, 2.25f, launch_tiles<OUT, 128, 128, 2, 2, 2, 2, 8>},
+      {256, 256, 1, 1, 1.573f, 3.66f, launch_wide<OUT, 2, 4>},
+  };
+  const Variant<OUT>* best = variants;
+  for (const Variant<OUT>& v : variants)
+    if (cost(v, p) < cost(*best, p)) best = &v;
+  return best->launch(p, s);
 }
 
 }  // namespace
@@ -224,9 +644,10 @@ acrl_status acrl_matmul_fp8(const acrl_matmul_desc* d, void* stream) {
   p.K = (int)d->K;
   p.kb = (int)((d->K + acrl::kBlock - 1) / acrl::kBlock);
   p.vec = d->ldy % 4 == 0;
+  p.whole = d->ldy % (d->y_type == ACRL_OUT_BF16 ? 8 : 4) == 0;
   const hipStream_t s = (hipStream_t)stream;
   return acrl::hip_status(
-      d->y_type == ACRL_OUT_BF16 ? acrl::launch_product<uint16_t>(p, s) : acrl::launch_product<float>(p, s),
+      d->y_type == ACRL_OUT_BF16 ? acrl::launch_product<__bf16>(p, s) : acrl::launch_product<float>(p, s),
       "acrl_matmul_fp8 launch");
 }
 

@@ -12,7 +12,10 @@ pytestmark = pytest.mark.gpu
 
 SHAPES = [(1, 1, 32), (1, 16, 128), (2, 130, 96), (7, 64, 160), (16, 256, 2080), (17, 200, 512), (33, 384, 1184),
           (64, 1000, 256), (65, 129, 288), (100, 700, 640), (129, 128, 1024), (255, 257, 416), (256, 512, 384),
-          (333, 520, 2080), (513, 1025, 160), (1, 4096, 4096), (40, 2048, 5120)]
+          (333, 520, 2080), (513, 1025, 160), (1, 4096, 4096), (40, 2048, 5120),
+          # outputs in 32-row pieces, wider tiles, tiles of 256 x 256 (whole and cut ones)
+          (13, 5200, 288), (64, 20000, 1056), (300, 3000, 2336), (900, 2100, 1184), (1300, 2050, 2080),
+          (1290, 6700, 96), (1100, 7937, 352)]
 
 
 def _integers(shape, seed):

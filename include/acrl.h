@@ -585,8 +585,7 @@ acrl_status acrl_matmul_fp8(const acrl_matmul_desc* desc, void* stream);
  * Requirements: B, L >= 0; for GROUP n_groups > 0 if B > 0 and group_of_seq
  * non-NULL (else both are not read); eps_low in [0, 1), eps_high >= 0;
  * dual_clip 0 (none) or > 1; kl_coef >= 0, and 0 without logp_ref; norm > 0
- * for CONSTANT; B < 2^22 and B ceil(L/1024) < 2^23 (B ceil(L/4096) where B L >
- * 2^20); workspace of acrl_policy_loss_workspace_size() bytes, 16-byte aligned. */
+ * for CONSTANT; B < 2^22 and B ceil(L/2048) < 2^24; workspace of acrl_policy_loss_workspace_size() bytes, 16-byte aligned. */
 typedef enum { ACRL_KL_K1 = 0, ACRL_KL_K2 = 1, ACRL_KL_K3 = 2 } acrl_kl_estimator;
 typedef enum {
   ACRL_AGG_GROUP = 0, ACRL_AGG_SEQUENCE = 1, ACRL_AGG_TOKEN = 2, ACRL_AGG_CONSTANT = 3

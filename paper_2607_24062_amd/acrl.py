@@ -9,6 +9,7 @@ call raises: there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Dict, Optional
 
@@ -266,24 +267,38 @@ def _dev(t: torch.Tensor, dtype, name: str):
     return t
 
 
-def _want(t, dtype, numel: int, device, name: str, optional: bool = False):
-    """Device address of a contiguous tensor of numel elements on `device`."""
-    if t is None:
-        if optional:
-            return None
-        raise ValueError("%s is required" % name)
-    _dev(t, dtype, name)
-    if t.device != device:
-        raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
-    if t.numel() != numel:
+def _want(t, dtype, numel: int, index: int, name: str, optional: bool = False):
+    """Device address of a contiguous tensor of numel elements on device
+    `index`.  (A call takes up to ten of them: the checks are one expression,
+    0.4 us each, and the reason is found afterwards.)"""
+    if t is None and optional:
+        return None
+    if t is None or t.dtype is not dtype or t.get_device() != index or t.numel() != numel or not t.is_contiguous():
+        if t is None:
+            raise ValueError("%s is required" % name)
+        _dev(t, dtype, name)
+        if t.get_device() != index:
+            raise ValueError("%s is on %s, not on cuda:%d" % (name, t.device, index))
         raise ValueError("%s must have %d elements, got %d" % (name, numel, t.numel()))
-    return _ptr(t)
+    return t.data_ptr()
 
 
-def _on_current(device) -> None:
-    """The library launches on the current device: its tensors have to be there."""
-    if device.index != torch.cuda.current_device():
-        raise ValueError("the tensors are on %s, the current device is cuda:%d" % (device, torch.cuda.current_device()))
+def _index_of(t, dtype, name: str) -> int:
+    """The device index of a device tensor, which is to be the current one: the
+    library launches there."""
+    _dev(t, dtype, name)
+    index = t.get_device()
+    if index != torch.cuda.current_device():
+        raise ValueError("%s is on cuda:%d, the current device is cuda:%d" % (name, index, torch.cuda.current_device()))
+    return index
+
+
+@functools.lru_cache(maxsize=256)
+def _size(query: str, *sizes) -> int:
+    """Workspace bytes by a library query of plain sizes."""
+    nb = _SZ()
+    _check(getattr(lib(), query)(*sizes, ctypes.byref(nb)), query)
+    return nb.value
 
 
 def _empty(shape, dtype, device, stream=None):
@@ -345,12 +360,10 @@ def acrl_quantize_fp8(x: torch.Tensor, scaling: int, rounding: int = ROUND_NEARE
             scales = torch.empty(((rows + 127) // 128, (cols + 127) // 128), dtype=torch.float32, device=x.device)
         else:
             scales = torch.empty((rows, cols // 32), dtype=torch.uint8, device=x.device)
-    nb = _SZ()
-    _check(lib().acrl_quantize_workspace_size(rows, cols, scaling, ctypes.byref(nb)),
-           "acrl_quantize_workspace_size")
-    ws = _workspace(nb.value, x.device, stream) if nb.value else None
-    _check(lib().acrl_quantize_fp8(_ptr(x), rows, cols, ld, scaling, rounding, _ptr(q), _ptr(scales),
-                                   _ptr(ws), nb.value, _stream(stream)), "acrl_quantize_fp8")
+    nbytes = _size("acrl_quantize_workspace_size", rows, cols, scaling)
+    ws = _workspace(nbytes, x.device, stream) if nbytes else None
+    _check(lib().acrl_quantize_fp8(x.data_ptr(), rows, cols, ld, scaling, rounding, q.data_ptr(), scales.data_ptr(),
+                                   _ptr(ws), nbytes, _raw_stream(stream)), "acrl_quantize_fp8")
     return q, scales
 
 
@@ -615,27 +628,26 @@ def acrl_matmul_fp8(xq, x_scales, wq, w_scales, out=None, out_dtype=torch.bfloat
     xq uint8 [M, K] with SCALE_ROW128 scales, wq uint8 [N, K] with
     SCALE_BLOCK128 scales (acrl_quantize_fp8).  `out` (bf16 or float32) may be
     a column slice of a wider matrix: unit column stride, any row stride."""
-    _dev(xq, torch.uint8, "xq")
-    _dev(wq, torch.uint8, "wq")
     if xq.dim() != 2 or wq.dim() != 2 or xq.shape[1] != wq.shape[1]:
         raise ValueError("xq [M, K] and wq [N, K] must be 2-D with the same K")
+    index = _index_of(xq, torch.uint8, "xq")
     M, K = xq.shape
     N = wq.shape[0]
-    dev = xq.device
-    _on_current(dev)
     kb = (K + 127) // 128
     if out is None:
         if out_dtype not in _OUT_TYPES:
             raise ValueError("out_dtype must be torch.bfloat16 or torch.float32, got %s" % out_dtype)
-        out = _empty((M, N), out_dtype, dev, stream)
-    elif (out.dtype not in _OUT_TYPES or out.device != dev or tuple(out.shape) != (M, N) or
-          (N > 1 and out.stride(1) != 1) or (M > 1 and out.stride(0) < N)):
-        raise ValueError("out must be a bf16 or float32 device matrix [M, N] with unit column stride")
-    desc = MatmulDesc(M=M, N=N, K=K, xq=_ptr(xq), wq=_want(wq, torch.uint8, N * K, dev, "wq"),
-                      x_scales=_want(x_scales, torch.float32, M * kb, dev, "x_scales"),
-                      w_scales=_want(w_scales, torch.float32, (N + 127) // 128 * kb, dev, "w_scales"),
-                      y=_ptr(out), ldy=out.stride(0) if M > 1 else N, y_type=_OUT_TYPES[out.dtype])
-    _check(lib().acrl_matmul_fp8(ctypes.byref(desc), _stream(stream)), "acrl_matmul_fp8")
+        out, ldy = _empty((M, N), out_dtype, xq.device, stream), N
+    else:
+        if (out.dtype not in _OUT_TYPES or out.get_device() != index or tuple(out.shape) != (M, N) or
+                (N > 1 and out.stride(1) != 1) or (M > 1 and out.stride(0) < N)):
+            raise ValueError("out must be a bf16 or float32 device matrix [M, N] with unit column stride")
+        out_dtype, ldy = out.dtype, out.stride(0) if M > 1 else N
+    desc = MatmulDesc(M, N, K, xq.data_ptr(), _want(x_scales, torch.float32, M * kb, index, "x_scales"),
+                      _want(wq, torch.uint8, N * K, index, "wq"),
+                      _want(w_scales, torch.float32, (N + 127) // 128 * kb, index, "w_scales"),
+                      out.data_ptr(), ldy, _OUT_TYPES[out_dtype])
+    _check(lib().acrl_matmul_fp8(ctypes.byref(desc), _raw_stream(stream)), "acrl_matmul_fp8")
     return out
 
 
@@ -647,29 +659,21 @@ def acrl_policy_loss(B: int, L: int, n_groups: int, mask, group_of_seq, logp_new
     """Clipped policy loss with a KL term to a reference policy: returns
     (coef float32 [B*L] = d loss / d logp_new, loss float64 [1], stats float64
     [N_PSTATS], PSTAT_NAMES).  coef goes to acrl_lm_head_backward."""
-    n, dev = B * L, logp_new.device
-    new = _want(logp_new, torch.float32, n, dev, "logp_new")
-    _on_current(dev)
+    n, index, dev, f32 = B * L, _index_of(logp_new, torch.float32, "logp_new"), logp_new.device, torch.float32
+    nbytes = _size("acrl_policy_loss_workspace_size", B, L, n_groups)
     if coef is None:
-        coef = _empty(n, torch.float32, dev, stream)
+        coef = _empty(n, f32, dev, stream)
     loss = _empty(1, torch.float64, dev, stream)
     stats = _empty(N_PSTATS, torch.float64, dev, stream)
-    nb = _SZ()
-    _check(lib().acrl_policy_loss_workspace_size(B, L, n_groups, ctypes.byref(nb)),
-           "acrl_policy_loss_workspace_size")
-    ws = _empty(nb.value, torch.uint8, dev, stream)
+    ws = _empty(nbytes, torch.uint8, dev, stream) if nbytes else None
     desc = PolicyLossDesc(
-        B=B, L=L, n_groups=n_groups, mask=_want(mask, torch.uint8, n, dev, "mask"),
-        group_of_seq=_want(group_of_seq, torch.int32, B, dev, "group_of_seq", optional=True), logp_new=new,
-        logp_old=_want(logp_old, torch.float32, n, dev, "logp_old"),
-        logp_ref=_want(logp_ref, torch.float32, n, dev, "logp_ref", optional=True),
-        adv=_want(adv, torch.float32, n if adv_per_token else B, dev, "adv"),
-        weight=_want(weight, torch.float32, n, dev, "weight", optional=True),
-        adv_per_token=int(bool(adv_per_token)), kl_estimator=int(kl_estimator), aggregate=int(aggregate),
-        eps_low=float(eps_low), eps_high=float(eps_high), dual_clip=float(dual_clip), kl_coef=float(kl_coef),
-        norm=float(norm), coef=_want(coef, torch.float32, n, dev, "coef"), loss=_ptr(loss), stats=_ptr(stats),
-        workspace=_ptr(ws), workspace_bytes=nb.value)
-    _check(lib().acrl_policy_loss(ctypes.byref(desc), _stream(stream)), "acrl_policy_loss")
+        B, L, n_groups, _want(mask, torch.uint8, n, index, "mask"),
+        _want(group_of_seq, torch.int32, B, index, "group_of_seq", True), _want(logp_new, f32, n, index, "logp_new"),
+        _want(logp_old, f32, n, index, "logp_old"), _want(logp_ref, f32, n, index, "logp_ref", True),
+        _want(adv, f32, n if adv_per_token else B, index, "adv"), _want(weight, f32, n, index, "weight", True),
+        1 if adv_per_token else 0, kl_estimator, aggregate, eps_low, eps_high, dual_clip, kl_coef, norm,
+        _want(coef, f32, n, index, "coef"), loss.data_ptr(), stats.data_ptr(), ws.data_ptr() if nbytes else None, nbytes)
+    _check(lib().acrl_policy_loss(ctypes.byref(desc), _raw_stream(stream)), "acrl_policy_loss")
     return coef, loss, stats
 
 
@@ -679,25 +683,19 @@ def acrl_preference_loss(B: int, L: int, mask, logp_new, chosen, rejected, logp_
     """Loss of preferred / rejected response pairs (int32 response indexes
     chosen, rejected [n_pairs]): returns (coef float32 [B*L] = d loss / d
     logp_new, loss float64 [1], rewards float32 [2, n_pairs])."""
-    n, dev = B * L, logp_new.device
-    new = _want(logp_new, torch.float32, n, dev, "logp_new")
-    _on_current(dev)
+    n, index, dev, f32 = B * L, _index_of(logp_new, torch.float32, "logp_new"), logp_new.device, torch.float32
     P = chosen.numel()
+    nbytes = _size("acrl_preference_loss_workspace_size", B, L, P)
     if coef is None:
-        coef = _empty(n, torch.float32, dev, stream)
+        coef = _empty(n, f32, dev, stream)
     loss = _empty(1, torch.float64, dev, stream)
-    rewards = _empty((2, P), torch.float32, dev, stream)
-    nb = _SZ()
-    _check(lib().acrl_preference_loss_workspace_size(B, L, P, ctypes.byref(nb)),
-           "acrl_preference_loss_workspace_size")
-    ws = _empty(nb.value, torch.uint8, dev, stream)
+    rewards = _empty((2, P), f32, dev, stream)
+    ws = _empty(nbytes, torch.uint8, dev, stream) if nbytes else None
     desc = PreferenceDesc(
-        B=B, L=L, n_pairs=P, mask=_want(mask, torch.uint8, n, dev, "mask"), logp_new=new,
-        logp_ref=_want(logp_ref, torch.float32, n, dev, "logp_ref", optional=True),
-        chosen=_want(chosen, torch.int32, P, dev, "chosen"), rejected=_want(rejected, torch.int32, P, dev, "rejected"),
-        pair_weight=_want(pair_weight, torch.float32, P, dev, "pair_weight", optional=True), form=int(form),
-        mean_logp=int(bool(mean_logp)), beta=float(beta), margin=float(margin),
-        label_smoothing=float(label_smoothing), coef=_want(coef, torch.float32, n, dev, "coef"), loss=_ptr(loss),
-        rewards=_ptr(rewards), workspace=_ptr(ws), workspace_bytes=nb.value)
-    _check(lib().acrl_preference_loss(ctypes.byref(desc), _stream(stream)), "acrl_preference_loss")
+        B, L, P, _want(mask, torch.uint8, n, index, "mask"), _want(logp_new, f32, n, index, "logp_new"),
+        _want(logp_ref, f32, n, index, "logp_ref", True), _want(chosen, torch.int32, P, index, "chosen"),
+        _want(rejected, torch.int32, P, index, "rejected"), _want(pair_weight, f32, P, index, "pair_weight", True),
+        form, 1 if mean_logp else 0, beta, margin, label_smoothing, _want(coef, f32, n, index, "coef"),
+        loss.data_ptr(), rewards.data_ptr(), ws.data_ptr() if nbytes else None, nbytes)
+    _check(lib().acrl_preference_loss(ctypes.byref(desc), _raw_stream(stream)), "acrl_preference_loss")
     return coef, loss, rewards

@@ -10,18 +10,30 @@
 namespace acrl {
 namespace {
 
-// exp(x) and exp(x) - 1 - x.  Next to 0 the difference cancels: there its
-// series x^2/2 (1 + x/3 (1 + x/4 (... (1 + x/8)))), whose next term is below
-// 2^-47 of it for |x| < 1/32, where the difference keeps 42 bits.
+// e = exp(x); returns exp(x) - 1 - x without cancellation.  x = k ln 2 + r with
+// |r| <= ln 2 / 2 (ln 2 in two parts, the first of 33 bits, so that k times it
+// is exact), exp(r) = 1 + r + r^2 q(r) with the Taylor series of q to r^11, whose
+// next term is below 2^-57: 22 fp64 operations for both values (errors over
+// x of 1e-6 .. 200 in size: exp 1.5e-16, the difference 2.8e-15, relative).
 __device__ __forceinline__ double exp_rest(double x, double& e) {
-  e = exp(x);
-  double s = 1.0 + x * (1.0 / 8);
-  s = 1.0 + x * (1.0 / 7) * s;
-  s = 1.0 + x * (1.0 / 6) * s;
-  s = 1.0 + x * 0.2 * s;
-  s = 1.0 + x * 0.25 * s;
-  s = 1.0 + x * (1.0 / 3) * s;
-  return fabs(x) < 0.03125 ? x * x * 0.5 * s : e - 1.0 - x;
+  const double c = x < -746.0 ? -746.0 : x > 710.0 ? 710.0 : x;  // (0 and infinity from there on; a NaN stays)
+  const double k = rint(c * 1.4426950408889634);
+  const double r = fma(k, -1.9082149292705877e-10, fma(k, -0.6931471803691238, c));
+  double q = 1.0 / 6227020800.0;
+  q = fma(q, r, 1.0 / 479001600.0);
+  q = fma(q, r, 1.0 / 39916800.0);
+  q = fma(q, r, 1.0 / 3628800.0);
+  q = fma(q, r, 1.0 / 362880.0);
+  q = fma(q, r, 1.0 / 40320.0);
+  q = fma(q, r, 1.0 / 5040.0);
+  q = fma(q, r, 1.0 / 720.0);
+  q = fma(q, r, 1.0 / 120.0);
+  q = fma(q, r, 1.0 / 24.0);
+  q = fma(q, r, 1.0 / 6.0);
+  q = fma(q, r, 0.5);
+  const double rest = r * r * q;
+  e = ldexp(1.0 + (r + rest), (int)k);
+  return k == 0.0 ? rest : e < INFINITY ? e - 1.0 - x : e;  // (infinite like e, where x is too)
 }
 
 // ------------------------------------------------------------------ policy loss
@@ -37,11 +49,19 @@ struct PolicyWs {
   int64_t bytes;
 };
 constexpr int kUnitThreads = 256;
+constexpr int kOneRows = 1024;  // responses, and groups, whose counts one workgroup holds
 constexpr int64_t kMaxResponses = (int64_t)1 << 22;
-// Slots of a workgroup: 4 a thread, in 1 or 4 turns.
-inline int unit_turns(int64_t B, int64_t L) { return B * L > ((int64_t)1 << 20) ? 4 : 1; }
+constexpr int64_t kOneSlots = 4096;  // of a batch that one workgroup does
+inline bool one_policy(int64_t B, int64_t L, int64_t n_groups) {
+  return B * L <= kOneSlots && B <= kOneRows && n_groups <= kOneRows;
+}
+// Slots of a workgroup: four a thread, in two turns in a large batch (policy_main_kernel and policy_sum_kernel of 512
+// responses of 16384 slots, 1 / 2 / 4 turns: 34.8 + 7.8, 33.4 + 4.9, 35.6 + 4.3 us).
+constexpr int64_t kManySlots = (int64_t)1 << 20;
+inline int unit_turns(int64_t B, int64_t L) { return B * L <= kManySlots ? 1 : 2; }
+inline int unit_slots(int64_t B, int64_t L) { return kUnitThreads * kSlots * unit_turns(B, L); }
 inline int64_t units_of_response(int64_t B, int64_t L) {
-  const int64_t u = (int64_t)kUnitThreads * kSlots * unit_turns(B, L);
+  const int64_t u = unit_slots(B, L);
   return (L + u - 1) / u;
 }
 PolicyWs policy_ws(void* base, int64_t B, int64_t L, int64_t n_groups) {
@@ -61,27 +81,62 @@ PolicyWs policy_ws(void* base, int64_t B, int64_t L, int64_t n_groups) {
   return w;
 }
 
-// Valid slots of each response, one wavefront per response.
+// a_t of a response of n valid slots (-1: of no group); v = {valid slots,
+// non-empty responses or groups} of the batch, live = those of its group.
+__device__ __forceinline__ double share_of(const acrl_policy_loss_desc& p, int n, int live, const double (&v)[2]) {
+  if (n < 0) return __builtin_nan("");
+  if (n == 0) return 0.0;
+  switch (p.aggregate) {
+    case ACRL_AGG_GROUP: return 1.0 / (v[1] * live * n);
+    case ACRL_AGG_SEQUENCE: return 1.0 / (v[1] * n);
+    case ACRL_AGG_TOKEN: return 1.0 / v[0];
+    default: return 1.0 / (double)p.norm;
+  }
+}
+
+// Nonzero bytes of the L bytes at m, by the lanes of a group of NT threads
+// (their sum is the count): 16-byte loads of what lies 16-byte aligned.
+__device__ __forceinline__ int nonzero_bytes(uint32_t x) {
+  return __popc((((x & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | x) & 0x80808080u);
+}
+template <int NT>
+__device__ __forceinline__ int count_valid(const uint8_t* __restrict__ m, int64_t L, int lane) {
+  const int64_t head = min((int64_t)(-(uintptr_t)m & 15), L), body = (L - head) / 16, tail = head + 16 * body;
+  int c = lane < head ? m[lane] != 0 : 0;
+  const uint4* v = reinterpret_cast<const uint4*>(m + head);
+#pragma unroll 4
+  for (int64_t j = lane; j < body; j += NT) {
+    const uint4 x = v[j];
+    c += nonzero_bytes(x.x) + nonzero_bytes(x.y) + nonzero_bytes(x.z) + nonzero_bytes(x.w);
+  }
+  if (tail + lane < L) c += m[tail + lane] != 0;  // (fewer than 16)
+  return c;
+}
+__device__ __forceinline__ int lane_sum_int(int c) {
+#pragma unroll
+  for (int s = 32; s > 0; s >>= 1) c += __shfl_xor(c, s);
+  return c;
+}
+__device__ __forceinline__ bool in_no_group(const acrl_policy_loss_desc& p, int64_t i) {
+  return p.aggregate == ACRL_AGG_GROUP && (p.group_of_seq[i] < 0 || p.group_of_seq[i] >= p.n_groups);
+}
+
+// Valid slots of each response: a wavefront each.
 __global__ __launch_bounds__(kUnitThreads) void policy_count_kernel(acrl_policy_loss_desc p, int32_t* n) {
   const int64_t i = (int64_t)blockIdx.x * (kUnitThreads / 64) + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (i >= p.B) return;
-  const uint8_t* m = p.mask + i * p.L;
-  int c = 0;
-  for (int64_t j = lane; j < p.L; j += 64) c += m[j] != 0;
-#pragma unroll
-  for (int s = 32; s > 0; s >>= 1) c += __shfl_xor(c, s);
-  if (lane == 0) {
-    const bool out = p.aggregate == ACRL_AGG_GROUP && (p.group_of_seq[i] < 0 || p.group_of_seq[i] >= p.n_groups);
-    n[i] = out ? -1 : c;
-  }
+  const int c = lane_sum_int(count_valid<64>(p.mask + i * p.L, p.L, lane));
+  if (lane == 0) n[i] = in_no_group(p, i) ? -1 : c;
 }
 
-// a_t of every response, by one workgroup.
+// a_t of every response, by one workgroup (more responses or groups than the
+// main kernel's workgroups look through themselves).
 __global__ __launch_bounds__(1024) void policy_share_kernel(acrl_policy_loss_desc p, PolicyWs ws) {
   __shared__ BlockShared<2, 1024> sh;
+  const bool groups = p.aggregate == ACRL_AGG_GROUP;
   double v[2] = {0, 0}, unused = 0.0;  // tokens, non-empty responses (groups)
-  if (p.aggregate == ACRL_AGG_GROUP) {
+  if (groups) {
     for (int64_t g = threadIdx.x; g < p.n_groups; g += 1024) ws.live[g] = 0;
     __syncthreads();
     for (int64_t i = threadIdx.x; i < p.B; i += 1024)
@@ -96,20 +151,33 @@ __global__ __launch_bounds__(1024) void policy_share_kernel(acrl_policy_loss_des
     }
   }
   block_stats<2, 1024>(v, unused, sh);
-  for (int64_t i = threadIdx.x; i < p.B; i += 1024) {
-    const double n = ws.n[i];
-    double a = 0.0;
-    if (n < 0) a = __builtin_nan("");
-    else if (n > 0) {
-      switch (p.aggregate) {
-        case ACRL_AGG_GROUP: a = 1.0 / (v[1] * atomicAdd(&ws.live[p.group_of_seq[i]], 0) * n); break;
-        case ACRL_AGG_SEQUENCE: a = 1.0 / (v[1] * n); break;
-        case ACRL_AGG_TOKEN: a = 1.0 / v[0]; break;
-        default: a = 1.0 / (double)p.norm;
-      }
-    }
-    ws.share[i] = a;
+  for (int64_t i = threadIdx.x; i < p.B; i += 1024)
+    ws.share[i] = share_of(p, ws.n[i], groups && ws.n[i] > 0 ? atomicAdd(&ws.live[p.group_of_seq[i]], 0) : 0, v);
+}
+
+// a_t of response i by a workgroup of the main kernel, from the counts of all.
+__device__ __forceinline__ double own_share(const acrl_policy_loss_desc& p, const int32_t* n, int64_t i) {
+  __shared__ BlockShared<2, kUnitThreads> sh;
+  __shared__ int live[kOneRows];
+  const bool groups = p.aggregate == ACRL_AGG_GROUP;
+  double v[2] = {0, 0}, unused = 0.0;
+  if (groups) {
+    for (int g = threadIdx.x; g < p.n_groups; g += kUnitThreads) live[g] = 0;
+    __syncthreads();
   }
+  for (int j = threadIdx.x; j < p.B; j += kUnitThreads) {
+    const int c = n[j];
+    if (c <= 0) continue;
+    v[0] += c;
+    if (groups) atomicAdd(&live[p.group_of_seq[j]], 1);
+    else v[1] += 1.0;
+  }
+  if (groups) {
+    __syncthreads();
+    for (int g = threadIdx.x; g < p.n_groups; g += kUnitThreads) v[1] += live[g] > 0 ? 1.0 : 0.0;
+  }
+  block_stats<2, kUnitThreads>(v, unused, sh);
+  return share_of(p, n[i], groups && n[i] > 0 ? live[p.group_of_seq[i]] : 0, v);
 }
 
 // One slot: its terms added to v, its d(-w m + kl_coef k) / d logp_new returned.
@@ -146,14 +214,18 @@ __device__ __forceinline__ double policy_slot(const acrl_policy_loss_desc& p, do
   return g;
 }
 
-// One unit of a response's slots: coef, and the unit's sums.
+// Where the main kernel has a_t from.
+enum ShareFrom { kShareNorm, kShareOwn, kShareWs };
+
+// One unit of a response's slots: coef, and the unit's sums.  Where a thread's
+// mask leaves nothing, nothing else is loaded.
 template <int TURNS, bool VEC>
 __global__ __launch_bounds__(kUnitThreads) void policy_main_kernel(acrl_policy_loss_desc p, PolicyWs ws,
-                                                                   int64_t units) {
+                                                                   int64_t units, int from) {
   __shared__ BlockShared<kPolicySums, kUnitThreads> sh;
   const int64_t i = blockIdx.x / units, u = blockIdx.x - i * units;
   const int64_t base = i * p.L;
-  const double a = ws.share[i];
+  const double a = from == kShareNorm ? 1.0 / (double)p.norm : from == kShareOwn ? own_share(p, ws.n, i) : ws.share[i];
   double v[kPolicySums] = {}, unused = 0.0;
 #pragma unroll
   for (int t = 0; t < TURNS; ++t) {
@@ -194,16 +266,7 @@ __global__ __launch_bounds__(kUnitThreads) void policy_main_kernel(acrl_policy_l
   }
 }
 
-// loss and stats from the units' sums, by one workgroup.
-__global__ __launch_bounds__(1024) void policy_sum_kernel(acrl_policy_loss_desc p, PolicyWs ws, int64_t n) {
-  __shared__ BlockShared<kPolicySums, 1024> sh;
-  double v[kPolicySums] = {}, unused = 0.0;
-  for (int64_t u = threadIdx.x; u < n; u += 1024) {
-#pragma unroll
-    for (int k = 0; k < kPolicySums; ++k) v[k] += ws.part[k * n + u];
-  }
-  block_stats<kPolicySums, 1024>(v, unused, sh);
-  if (threadIdx.x != 0) return;
+__device__ __forceinline__ void policy_finish(const acrl_policy_loss_desc& p, const double (&v)[kPolicySums]) {
   p.loss[0] = v[0] + (double)p.kl_coef * v[1];
   if (!p.stats) return;
   const double inv = v[5] > 0 ? 1.0 / v[5] : 0.0;
@@ -215,23 +278,92 @@ __global__ __launch_bounds__(1024) void policy_sum_kernel(acrl_policy_loss_desc 
   p.stats[ACRL_PSTAT_N_TOKENS] = v[5];
 }
 
+// loss and stats from the units' sums, by one workgroup.
+__global__ __launch_bounds__(1024) void policy_sum_kernel(acrl_policy_loss_desc p, PolicyWs ws, int64_t n) {
+  __shared__ BlockShared<kPolicySums, 1024> sh;
+  double v[kPolicySums] = {}, unused = 0.0;
+#pragma unroll 4
+  for (int64_t u = threadIdx.x; u < n; u += 1024) {
+#pragma unroll
+    for (int k = 0; k < kPolicySums; ++k) v[k] += ws.part[k * n + u];
+  }
+  block_stats<kPolicySums, 1024>(v, unused, sh);
+  if (threadIdx.x == 0) policy_finish(p, v);
+}
+
+// All of it in one workgroup, a slot a thread and turn: a small batch is
+// launches and waits (4 responses of 64 slots 5.7 us; 14.5 by the four kernels).
+__global__ __launch_bounds__(1024) void policy_one_kernel(acrl_policy_loss_desc p) {
+  __shared__ BlockShared<2, 1024> sh2;
+  __shared__ BlockShared<kPolicySums, 1024> sh;
+  __shared__ int n[kOneRows], live[kOneRows];
+  __shared__ double share[kOneRows];
+  const int t = threadIdx.x, B = (int)p.B, L = (int)p.L, slots = B * L;
+  const bool groups = p.aggregate == ACRL_AGG_GROUP;
+  n[t] = live[t] = 0;
+  __syncthreads();
+  for (int j = t; j < slots; j += 1024)
+    if (p.mask[j]) atomicAdd(&n[j / L], 1);
+  __syncthreads();
+  int g = -1;
+  if (t < B) {
+    if (groups) g = p.group_of_seq[t];
+    if (in_no_group(p, t)) n[t] = g = -1;
+    else if (groups && n[t] > 0) atomicAdd(&live[g], 1);
+  }
+  __syncthreads();
+  double c[2] = {t < B ? (double)max(n[t], 0) : 0.0, (groups ? live[t] : n[t]) > 0 ? 1.0 : 0.0}, unused = 0.0;
+  block_stats<2, 1024>(c, unused, sh2);
+  if (t < B) share[t] = share_of(p, n[t], g >= 0 ? live[g] : 0, c);
+  __syncthreads();
+  double v[kPolicySums] = {};
+  for (int j = t; j < slots; j += 1024) {
+    float out = 0.0f;
+    if (p.mask[j]) {
+      const int i = j / L;
+      const double a = share[i];
+      double one[kPolicySums] = {};
+      out = (float)(a * policy_slot(p, p.logp_new[j], p.logp_old[j], p.logp_ref ? p.logp_ref[j] : 0.0f,
+                                    p.adv_per_token ? p.adv[j] : p.adv[i], p.weight ? p.weight[j] : 1.0f, one));
+      if (a == a) {
+#pragma unroll
+        for (int k = 0; k < kPolicySums; ++k) v[k] += k < 2 ? a * one[k] : one[k];
+      }
+    }
+    p.coef[j] = out;
+  }
+  unused = 0.0;
+  block_stats<kPolicySums, 1024>(v, unused, sh);
+  if (t == 0) policy_finish(p, v);
+}
+
 hipError_t launch_policy_loss(const acrl_policy_loss_desc& p, hipStream_t s) {
   const PolicyWs ws = policy_ws(p.workspace, p.B, p.L, p.n_groups);
   const int64_t units = units_of_response(p.B, p.L), n = p.B * units;
+  if (n > 0 && one_policy(p.B, p.L, p.n_groups)) {
+    hipLaunchKernelGGL(policy_one_kernel, dim3(1), dim3(1024), 0, s, p);
+    return hipGetLastError();
+  }
   if (n > 0) {
-    const int per = kUnitThreads / 64;
-    hipLaunchKernelGGL(policy_count_kernel, dim3((unsigned)((p.B + per - 1) / per)), dim3(kUnitThreads), 0, s, p, ws.n);
-    hipLaunchKernelGGL(policy_share_kernel, dim3(1), dim3(1024), 0, s, p, ws);
+    int from = kShareNorm;
+    if (p.aggregate != ACRL_AGG_CONSTANT) {
+      const int per = kUnitThreads / 64;
+      hipLaunchKernelGGL(policy_count_kernel, dim3((unsigned)((p.B + per - 1) / per)), dim3(kUnitThreads), 0, s, p, ws.n);
+      // (a few workgroups look through the counts of all responses sooner than a launch of its own does; of many, 512
+      // responses of 16384 slots, each would do so again: policy_main_kernel 38.7 us, 33.4 + 2.7 with the launch)
+      from = p.B * p.L <= kManySlots && p.B <= kOneRows && p.n_groups <= kOneRows ? kShareOwn : kShareWs;
+      if (from == kShareWs) hipLaunchKernelGGL(policy_share_kernel, dim3(1), dim3(1024), 0, s, p, ws);
+    }
     const bool vec = p.L % kSlots == 0 && aligned(p.mask, 4) && aligned(p.logp_new, 16) && aligned(p.logp_old, 16) &&
                      aligned(p.logp_ref, 16) && aligned(p.weight, 16) && aligned(p.coef, 16) &&
                      (!p.adv_per_token || aligned(p.adv, 16));
     auto go = [&](auto turns, auto v) {
       hipLaunchKernelGGL((policy_main_kernel<decltype(turns)::value, decltype(v)::value>), dim3((unsigned)n),
-                         dim3(kUnitThreads), 0, s, p, ws, units);
+                         dim3(kUnitThreads), 0, s, p, ws, units, from);
     };
     auto with = [&](auto turns) { vec ? go(turns, std::true_type{}) : go(turns, std::false_type{}); };
     if (unit_turns(p.B, p.L) == 1) with(std::integral_constant<int, 1>{});
-    else with(std::integral_constant<int, 4>{});
+    else with(std::integral_constant<int, 2>{});
   }
   hipLaunchKernelGGL(policy_sum_kernel, dim3(1), dim3(1024), 0, s, p, ws, n);
   return hipGetLastError();
@@ -241,7 +373,19 @@ hipError_t launch_policy_loss(const acrl_policy_loss_desc& p, hipStream_t s) {
 struct PrefRec {
   double x, each;  // x_i (mean_logp applied); d x_i / d logp_new of a valid slot
 };
+constexpr int kPrefOne = 256;  // responses, and pairs, of a batch that one workgroup does
+inline bool one_preference(int64_t B, int64_t L, int64_t P) {
+  return B * L <= kOneSlots && B <= kPrefOne && P <= kPrefOne;
+}
 size_t pref_ws_bytes(int64_t B) { return align_up((size_t)B * sizeof(PrefRec), 256) + 256; }
+
+// Workgroup size: 1024 threads from the second turn on while that leaves a few
+// workgroups a CU (512 responses of 16384 slots 12.3 us, 18.0 with 256 threads; 256 of 4096 3.6 /
+// 4.4; 2048 of 2048 11.0 / 7.9).
+inline int pref_threads(int64_t B, int64_t L) {
+  if (L <= 64 * kSlots) return 64;
+  return L > kRedThreads * kSlots && B <= 1024 ? 1024 : kRedThreads;
+}
 
 // x_i of each response, one workgroup per response.
 template <int NT, bool VEC>
@@ -299,8 +443,17 @@ __device__ __forceinline__ double pref_pair(const acrl_preference_desc& p, const
   return u * d * beta / (double)p.n_pairs;
 }
 
+__device__ __forceinline__ void pref_rewards(const acrl_preference_desc& p, const PrefRec* rec, int64_t at, int32_t c,
+                                             int32_t r) {
+  if (!p.rewards) return;
+  const float nan = __builtin_nanf("");
+  p.rewards[at] = c >= 0 && c < p.B ? (float)((double)p.beta * rec[c].x) : nan;
+  p.rewards[p.n_pairs + at] = r >= 0 && r < p.B ? (float)((double)p.beta * rec[r].x) : nan;
+}
+
 // coef of one response's slots: its pairs' slopes, then one value for every
 // valid slot.  The last workgroup sums the loss and writes the rewards.
+template <bool VEC>
 __global__ __launch_bounds__(kUnitThreads) void pref_coef_kernel(acrl_preference_desc p, const PrefRec* rec) {
   __shared__ BlockShared<1, kUnitThreads> sh;
   double v[1] = {0}, unused = 0.0;
@@ -311,11 +464,7 @@ __global__ __launch_bounds__(kUnitThreads) void pref_coef_kernel(acrl_preference
     if (i == p.B) {
       pref_pair(p, rec, at, c, r, l);
       v[0] += l;
-      if (p.rewards) {
-        const float nan = __builtin_nanf("");
-        p.rewards[at] = c >= 0 && c < p.B ? (float)((double)p.beta * rec[c].x) : nan;
-        p.rewards[p.n_pairs + at] = r >= 0 && r < p.B ? (float)((double)p.beta * rec[r].x) : nan;
-      }
+      pref_rewards(p, rec, at, c, r);
     } else if ((c == i) != (r == i)) {  // (a response against itself: its slopes cancel)
       const double g = pref_pair(p, rec, at, c, r, l);
       v[0] += c == i ? g : -g;
@@ -327,19 +476,80 @@ __global__ __launch_bounds__(kUnitThreads) void pref_coef_kernel(acrl_preference
     return;
   }
   const float c = (float)(v[0] * rec[i].each);
-  for (int64_t j = threadIdx.x; j < p.L; j += kUnitThreads) p.coef[i * p.L + j] = p.mask[i * p.L + j] ? c : 0.0f;
+  const int64_t base = i * p.L;
+  if constexpr (VEC) {
+#pragma unroll 4
+    for (int64_t j = threadIdx.x * kSlots; j < p.L; j += kUnitThreads * kSlots) {
+      uint8_t m[kSlots];
+      load_mask<kUnitThreads, true>(p.mask, base, j, p.L, m);
+      *reinterpret_cast<float4*>(p.coef + base + j) =
+          make_float4(m[0] ? c : 0.0f, m[1] ? c : 0.0f, m[2] ? c : 0.0f, m[3] ? c : 0.0f);
+    }
+  } else {
+    for (int64_t j = threadIdx.x; j < p.L; j += kUnitThreads) p.coef[base + j] = p.mask[base + j] ? c : 0.0f;
+  }
+}
+
+// All of it in one workgroup: a wavefront a response for the sums, a thread a
+// pair for the slopes, a thread a response for its coef (8 responses of 67
+// slots 4.1 us; 6.9 by the two kernels).
+__global__ __launch_bounds__(1024) void pref_one_kernel(acrl_preference_desc p) {
+  __shared__ BlockShared<1, 1024> sh;
+  __shared__ PrefRec rec[kPrefOne];
+  __shared__ double slope[kPrefOne];
+  __shared__ int32_t chosen[kPrefOne], rejected[kPrefOne];
+  __shared__ float coef[kPrefOne];
+  const int t = threadIdx.x, lane = t & 63, B = (int)p.B, L = (int)p.L, P = (int)p.n_pairs;
+  for (int i = t >> 6; i < B; i += 16) {
+    double n = 0, x = 0;
+    for (int j = lane; j < L; j += 64)
+      if (p.mask[i * L + j]) {
+        n += 1.0;
+        x += (double)p.logp_new[i * L + j] - (p.logp_ref ? (double)p.logp_ref[i * L + j] : 0.0);
+      }
+    n = lane_sum<64>(n);
+    x = lane_sum<64>(x);
+    const double each = p.mean_logp ? (n > 0 ? 1.0 / n : 0.0) : 1.0;
+    if (lane == 0) rec[i] = PrefRec{x * each, each};
+  }
+  __syncthreads();
+  double v[1] = {0}, unused = 0.0;
+  if (t < P) {
+    chosen[t] = p.chosen[t];
+    rejected[t] = p.rejected[t];
+    slope[t] = pref_pair(p, rec, t, chosen[t], rejected[t], v[0]);
+    pref_rewards(p, rec, t, chosen[t], rejected[t]);
+  }
+  block_stats<1, 1024>(v, unused, sh);
+  if (t == 0) p.loss[0] = P > 0 ? v[0] / (double)P : 0.0;
+  if (t < B) {
+    double c = 0.0;
+    for (int k = 0; k < P; ++k) {
+      const bool up = chosen[k] == t, down = rejected[k] == t;
+      if (up != down) c += up ? slope[k] : -slope[k];
+    }
+    coef[t] = (float)(c * rec[t].each);
+  }
+  __syncthreads();
+  for (int j = t; j < B * L; j += 1024) p.coef[j] = p.mask[j] ? coef[j / L] : 0.0f;
 }
 
 hipError_t launch_preference_loss(const acrl_preference_desc& p, hipStream_t s) {
+  if (one_preference(p.B, p.L, p.n_pairs)) {
+    hipLaunchKernelGGL(pref_one_kernel, dim3(1), dim3(1024), 0, s, p);
+    return hipGetLastError();
+  }
   PrefRec* rec = static_cast<PrefRec*>(p.workspace);
   if (p.B > 0) {
     const bool vec = p.L % kSlots == 0 && aligned(p.mask, 4) && aligned(p.logp_new, 16) && aligned(p.logp_ref, 16);
-    launch_seq(p.L <= 64 * kSlots ? 64 : kRedThreads, vec, [&](auto nt, auto v) {
+    launch_seq(pref_threads(p.B, p.L), vec, [&](auto nt, auto v) {
       constexpr int NT = decltype(nt)::value;
       hipLaunchKernelGGL((pref_seq_kernel<NT, decltype(v)::value>), dim3((unsigned)p.B), dim3(NT), 0, s, p, rec);
     });
   }
-  hipLaunchKernelGGL(pref_coef_kernel, dim3((unsigned)p.B + 1), dim3(kUnitThreads), 0, s, p, (const PrefRec*)rec);
+  const bool vec = p.L % kSlots == 0 && aligned(p.mask, 4) && aligned(p.coef, 16);
+  if (vec) hipLaunchKernelGGL((pref_coef_kernel<true>), dim3((unsigned)p.B + 1), dim3(kUnitThreads), 0, s, p, (const PrefRec*)rec);
+  else hipLaunchKernelGGL((pref_coef_kernel<false>), dim3((unsigned)p.B + 1), dim3(kUnitThreads), 0, s, p, (const PrefRec*)rec);
   return hipGetLastError();
 }
 
@@ -357,8 +567,8 @@ acrl_status acrl_policy_loss_workspace_size(int64_t B, int64_t L, int64_t n_grou
   ACRL_REQUIRE(B >= 0 && L >= 0 && n_groups >= 0, "B, L and n_groups must be >= 0");
   // a launch holds fewer than 2^32 threads
   ACRL_REQUIRE(B < acrl::kMaxResponses && L < INT32_MAX && n_groups < INT32_MAX, "B, L or n_groups too large");
-  ACRL_REQUIRE(B * acrl::units_of_response(B, L) < 2 * acrl::kMaxResponses, "B x L too large");
-  *bytes = (size_t)acrl::policy_ws(nullptr, B, L, n_groups).bytes + 256;
+  ACRL_REQUIRE(B * acrl::units_of_response(B, L) < 4 * acrl::kMaxResponses, "B x L too large");
+  *bytes = acrl::one_policy(B, L, n_groups) ? 0 : (size_t)acrl::policy_ws(nullptr, B, L, n_groups).bytes;
   return ACRL_OK;
 }
 
@@ -385,7 +595,7 @@ acrl_status acrl_policy_loss(const acrl_policy_loss_desc* d, void* stream) {
   if (d->B > 0 && d->L > 0)
     ACRL_REQUIRE(d->mask && d->logp_new && d->logp_old && d->adv && d->coef,
                  "mask, logp_new, logp_old, adv and coef are required");
-  if (!d->workspace || d->workspace_bytes < need) {
+  if (need > 0 && (!d->workspace || d->workspace_bytes < need)) {
     set_error("acrl_policy_loss needs %zu workspace bytes, got %zu", need, d->workspace_bytes);
     return ACRL_ERR_WORKSPACE;
   }
@@ -399,7 +609,7 @@ acrl_status acrl_preference_loss_workspace_size(int64_t B, int64_t L, int64_t n_
   ACRL_REQUIRE(bytes, "bytes is NULL");
   ACRL_REQUIRE(B >= 0 && L >= 0 && n_pairs >= 0, "B, L and n_pairs must be >= 0");
   ACRL_REQUIRE(B < acrl::kMaxResponses && L < INT32_MAX && n_pairs < INT32_MAX, "B, L or n_pairs too large");
-  *bytes = acrl::pref_ws_bytes(B);
+  *bytes = acrl::one_preference(B, L, n_pairs) ? 0 : acrl::pref_ws_bytes(B);
   return ACRL_OK;
 }
 
@@ -418,7 +628,7 @@ acrl_status acrl_preference_loss(const acrl_preference_desc* d, void* stream) {
   ACRL_REQUIRE(d->loss, "loss is required");
   if (d->B > 0 && d->L > 0) ACRL_REQUIRE(d->mask && d->logp_new && d->coef, "mask, logp_new and coef are required");
   if (d->n_pairs > 0) ACRL_REQUIRE(d->chosen && d->rejected, "chosen and rejected are required");
-  if (!d->workspace || d->workspace_bytes < need) {
+  if (need > 0 && (!d->workspace || d->workspace_bytes < need)) {
     set_error("acrl_preference_loss needs %zu workspace bytes, got %zu", need, d->workspace_bytes);
     return ACRL_ERR_WORKSPACE;
   }

@@ -144,22 +144,36 @@ __device__ __forceinline__ void tile_of(const ProductParams& p, int block, int& 
 }
 
 // Tile of TN outputs x TM tokens a workgroup, WN x WM waves for each of KG
-// groups; a stage of LDS holds KG scale blocks of K, one a group (buffer -> LDS
-// loads, ST stages, one barrier a stage), and the groups' sums are added
-// through LDS in their order.  Piece c (16 bytes) of row r lies at position
-// c ^ (r / 2 mod 8) of the row's 128 bytes: the 16 rows of a fragment then read
-// 16 different 16-byte columns of LDS's 64 banks.
+// groups.  K passes through LDS in ST stages of KG scale blocks, one a group
+// (buffer -> LDS loads), and the groups' sums are added at the end in their
+// order.  Piece c (16 bytes) of row r lies at position c ^ (r / 2 mod 8) of the
+// row's 128 bytes, and lane group q of a fragment takes pieces q and q + 4 (the
+// products of a block may be summed in any order of k, as long as both operands
+// have the same): LDS then serves a fragment's reads without bank conflicts.
+//
+// The barrier stands where a wave has its last operands of a turn in registers
+// and a row of products still to issue; the next turn's first operands are read
+// under those, and its stage's loads go out one behind each product.  The loop
+// has no branches: the compiler would move products past them, away from the
+// reads of their operands.  At 256 x 256 LDS is as busy as the matrix cores: a
+// block's 512 rows are written once and read 1536 times 128 bytes, at 128 bytes
+// a cycle the 2048 cycles of the products.
 template <typename OUT, int TN, int TM, int WN, int WM, int KG, int ST, int C>
 __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(ProductParams p) {
-  constexpr int NW = WN * WM * KG, AN = TN / WN / 16, BM = TM / WM / 16;  // 16-row fragments of a wave
-  constexpr int kRows = TN + TM, kStage = kRows * kBlock * KG, kLoads = kRows * KG / 8 / NW;
-  // the scales of C blocks lie in LDS at a time, twice: x's [TM][C], W's [TN / 128][C]
-  constexpr int kChunk = (TM * C + 64) * 4, kChunkTurns = C / KG;
-  static_assert(kRows * KG % (8 * NW) == 0 && TN % 8 == 0 && TM * C % 64 == 0, "whole loads");
-  static_assert((TN + kBlock - 1) / kBlock * C <= 64 && ST - 1 <= kChunkTurns && C % KG == 0, "scales in time");
+  constexpr int NW = WN * WM * KG, AN = TN / WN / 16, BM = TM / WM / 16, kSteps = AN * BM;  // fragments of a wave
+  constexpr int kRows = TN + TM, kStage = kRows * kBlock * KG, kLoads = kRows * KG / 8 / NW, kPer = kLoads + 1;
+  constexpr int kStepLoads = (kLoads + kSteps - 1) / kSteps;  // behind each product
+  // the scales of C blocks lie in LDS at a time, twice: x's [TM][C], W's [TN / 128][C]; 64 floats a load, one load a
+  // wave and turn
+  constexpr int kParts = TM * C / 64, kChunk = (kParts + 1) * 256, kChunkTurns = C / KG;
+  static_assert(kRows * KG % (8 * NW) == 0 && TN % 16 == 0 && TM * C % 64 == 0 && kRows % 16 == 0, "whole loads");
+  static_assert((TN + kBlock - 1) / kBlock * C <= 64 && C % KG == 0, "one load of W's scales");
+  static_assert(kParts / NW <= kChunkTurns - ST, "the next scales are there in time");
   static_assert(kBlock % (TN / WN) == 0, "a wave's outputs lie in one scale block");
+  static_assert(AN >= 2 && kSteps % 4 == 0, "operands and products in turn");
   static_assert(KG == 1 || KG * TN * TM * 4 <= ST * kStage, "the groups' sums fit the stages");
-  __shared__ __align__(1024) uint8_t lds[ST * kStage + 2 * kChunk];
+  constexpr int kLds = ST * kStage + 2 * kChunk + 256;
+  __shared__ __align__(1024) uint8_t lds[kLds];
   uint8_t* const lds_s = lds + ST * kStage;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wn = wave % WN, wm = wave / WN % WM, g = wave / (WN * WM);
@@ -167,114 +181,139 @@ __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(Prod
   tile_of(p, blockIdx.x, mt, nt);
   const int n0 = nt * TN, m0 = mt * TM;
   const int last = p.kb - 1, tail = p.K - last * kBlock;  // bytes of the last block
-  const int turns = (p.kb + KG - 1) / KG;
-
+  const int last_turn = (p.kb + KG - 1) / KG - 1;
   const __amdgpu_buffer_rsrc_t rw = make_rsrc(p.w + (int64_t)n0 * p.K, (int64_t)(p.N - n0) * p.K);
   const __amdgpu_buffer_rsrc_t rx = make_rsrc(p.x + (int64_t)m0 * p.K, (int64_t)(p.M - m0) * p.K);
   const __amdgpu_buffer_rsrc_t rs = make_rsrc(p.xs + (int64_t)m0 * p.kb, (int64_t)(p.M - m0) * p.kb * 4);
   const int nb0 = n0 / kBlock, nb_last = (p.N - 1) / kBlock;
   const __amdgpu_buffer_rsrc_t rv = make_rsrc(p.ws + (int64_t)nb0 * p.kb, (int64_t)(nb_last + 1 - nb0) * p.kb * 4);
-  // rows past the matrix repeat its last one; their results are not stored
+  // Rows past the matrix repeat its last one (their results are not stored), blocks past the last one the last (their
+  // factor is 0), pieces past the row's end the block's first (the fragments there are cleared).  A lane's piece is the
+  // same in every load.
+  const int piece = (lane & 7) ^ ((wave * 8 + (lane >> 3)) >> 1 & 7), back = 16 * piece >= tail ? 16 * piece : 0;
   uint32_t off[kLoads];
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
     const int r = ((i * NW + wave) * 8 + (lane >> 3)) % kRows;  // row of the group's part: W's TN, then x's TM
     const int row = r < TN ? min(r, p.N - 1 - n0) : min(r - TN, p.M - 1 - m0);
-    off[i] = (uint32_t)row * (uint32_t)p.K + 16 * ((lane & 7) ^ ((r >> 1) & 7));
+    off[i] = (uint32_t)row * (uint32_t)p.K + 16 * piece;
   }
-
-  auto load = [&](int turn, int st) {
-    if (turn % kChunkTurns == 0) {
-      // scales first: they are there when the turn's operands are
-      uint8_t* const chunk = lds_s + (turn / kChunkTurns & 1) * kChunk;
-      for (int at = wave; at < TM * C / 64; at += NW) {
-        const int e = at * 64 + lane, kb = min(turn * KG + e % C, last);
-        buffer_to_lds<4>(rs, (uint32_t)(min(e / C, p.M - 1 - m0) * p.kb + kb) * 4, 0, chunk + at * 256);
-      }
-      if (wave == NW - 1) {
-        const int kb = min(turn * KG + lane % C, last);
-        buffer_to_lds<4>(rv, (uint32_t)(min(lane / C, nb_last - nb0) * p.kb + kb) * 4, 0, chunk + TM * C * 4);
-      }
-    }
-    uint8_t* const stage = lds + st * kStage;
-    if ((turn + 1) * KG <= last) {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int at = (i * NW + wave) * 8;
-        buffer_to_lds<16>(at % kRows < TN ? rw : rx, off[i], (turn * KG + at / kRows) * kBlock, stage + at * kBlock);
-      }
-    } else {
-      // blocks past the last repeat it and are not used; pieces past the row's end read the last block's first
-      // one, and the fragments there are cleared
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int at = (i * NW + wave) * 8;
-        const int kb = min(turn * KG + at / kRows, last), piece = (lane & 7) ^ (((at + (lane >> 3)) % kRows >> 1) & 7);
-        buffer_to_lds<16>(at % kRows < TN ? rw : rx, kb == last && 16 * piece >= tail ? off[i] - 16 * piece : off[i],
-                          kb * kBlock, stage + at * kBlock);
-      }
-    }
+  auto load = [&](int turn, int st, int i) {
+    const int at = (i * NW + wave) * 8, kb = min(turn * KG + at / kRows, last);
+    buffer_to_lds<16>(at % kRows < TN ? rw : rx, off[i] - (back & -(int)(kb == last)), kb * kBlock,
+                      lds + st * kStage + at * kBlock);
+  };
+  // Part `part` of the scales of blocks C c .. C c + C - 1: x's, then W's; past those, into no one's place
+  auto load_scales = [&](int c, int part) {
+    const bool is_w = part >= kParts;
+    const int row = is_w ? min(lane / C, nb_last - nb0) : min(part * (64 / C) + lane / C, p.M - 1 - m0);
+    const int k = min(C * c + lane % C, last);
+    buffer_to_lds<4>(is_w ? rv : rs, (uint32_t)(row * p.kb + k) * 4, 0,
+                     part <= kParts ? lds_s + (c & 1) * kChunk + part * 256 : lds_s + 2 * kChunk);
   };
 
   f32x4 acc[AN][BM] = {};
   const int q = lane >> 4, f = (lane >> 1) & 7;
   const int lo = (lane & 15) * kBlock + ((q ^ f) << 4), hi = lo ^ 64;  // pieces q and q + 4
-  // One block of the wave's group.  LAST: it may be the last one, with less than 128 bytes a row
-  auto block = [&](int turn, int st, auto is_last) {
-    constexpr bool LAST = decltype(is_last)::value;
-    const int kb = turn * KG + g;
-    const uint8_t* sw = lds + st * kStage + (g * kRows + wn * (TN / WN)) * kBlock;
-    const uint8_t* sx = lds + st * kStage + (g * kRows + TN + wm * (TM / WM)) * kBlock;
-    const float* ss = reinterpret_cast<const float*>(lds_s + (turn / kChunkTurns & 1) * kChunk) +
-                      turn % kChunkTurns * KG + g;
-    const bool no_lo = LAST && kb == last && 16 * q >= tail, no_hi = LAST && kb == last && 16 * q + 64 >= tail;
-    auto fragment = [&](const uint8_t* rows) {
-      i32x4 u = *reinterpret_cast<const i32x4*>(rows + lo), v = *reinterpret_cast<const i32x4*>(rows + hi);
-      if (LAST && no_lo) u = i32x4{};
-      if (LAST && no_hi) v = i32x4{};
-      return __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
-    // Row i's results are added while row i + 1's are made, and row i + 1's operand is read meanwhile
-    i32x8 a[2], b[BM];
-    f32x4 t[2][BM];
-    float s[BM];
-    a[0] = fragment(sw);
+  const int a_at = (g * kRows + wn * (TN / WN)) * kBlock, b_at = (g * kRows + TN + wm * (TM / WM)) * kBlock;
+  const int s_at = (wm * (TM / WM) + (lane & 15)) * C + g, w_at = TM * C + wn * (TN / WN) / kBlock * C + g;
+  auto fragment = [&](int at) {
+    const i32x4 u = *reinterpret_cast<const i32x4*>(lds + at + lo), v = *reinterpret_cast<const i32x4*>(lds + at + hi);
+    return __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  i32x8 a[2], b[BM];
+  f32x4 t[4];          // the last products, which enter the sums three products later
+  float s[BM], s_new[BM], w_new;
+  auto scales = [&](int turn) {
+    const float* ss = reinterpret_cast<const float*>(lds_s + (turn / kChunkTurns & 1) * kChunk) + turn % kChunkTurns * KG;
 #pragma unroll
-    for (int j = 0; j < BM; ++j) b[j] = fragment(sx + j * 16 * kBlock);
+    for (int j = 0; j < BM; ++j) s_new[j] = ss[s_at + j * 16 * C];
+    w_new = ss[w_at];
+  };
+  const bool mine = last_turn * KG + g <= last, cut_here = last_turn * KG + g == last;  // in the last turn
+  const bool no_lo = cut_here & (16 * q >= tail), no_hi = cut_here & (16 * q + 64 >= tail);
+  auto cut = [&](i32x8 v) {
 #pragma unroll
-    for (int j = 0; j < BM; ++j) s[j] = ss[(wm * (TM / WM) + j * 16 + (lane & 15)) * C];
-    const float w_scale = ss[TM * C + wn * (TN / WN) / kBlock * C];
+    for (int e = 0; e < 4; ++e) {
+      v[e] = no_lo ? 0 : v[e];
+      v[e + 4] = no_hi ? 0 : v[e + 4];
+    }
+    return v;
+  };
+  // The products of a turn, whose b and a[0] are there; MORE: with the reads of the next turn's, else it is the last
+  auto block = [&](int turn, int st, int st_next, auto more) {
+    constexpr bool MORE = decltype(more)::value;
+    if (!MORE) {
+      a[0] = cut(a[0]);
 #pragma unroll
-    for (int i = 0; i < AN; ++i) {
-      if (i + 1 < AN) a[(i + 1) & 1] = fragment(sw + (i + 1) * 16 * kBlock);
-#pragma unroll
-      for (int j = 0; j < BM; ++j) {
-        t[i & 1][j] = mfma(a[i & 1], b[j]);
-        if (i == 0) s[j] *= w_scale;
-        if (i > 0) add(acc[i - 1][j], t[(i - 1) & 1][j], s[j]);
-        __builtin_amdgcn_sched_barrier(0);  // (left to itself the scheduler lets every product's sums wait for it)
-      }
+      for (int j = 0; j < BM; ++j) b[j] = cut(b[j]);
     }
 #pragma unroll
-    for (int j = 0; j < BM; ++j) add(acc[AN - 1][j], t[(AN - 1) & 1][j], s[j]);
+    for (int i = 0; i < AN; ++i) {
+      if (i + 1 < AN) {
+        const i32x8 v = fragment(st * kStage + a_at + (i + 1) * 16 * kBlock);
+        a[(i + 1) & 1] = MORE ? v : cut(v);
+      }
+      if (MORE && i == AN - 1) {
+        // all waves' loads of the next turn and reads of this one are done
+        wait_loads_and_barrier<(ST - 2) * kPer>();
+        load_scales(turn / kChunkTurns + 1, turn % kChunkTurns * NW + wave);
+        a[AN & 1] = fragment(st_next * kStage + a_at);
+      }
+#pragma unroll
+      for (int j = 0; j < BM; ++j) {
+        const int n = i * BM + j, d = (n + kSteps - 3) % kSteps;  // the product made, and the one added (n < 3: the turn before's)
+        t[n & 3] = mfma(a[i & 1], b[j]);
+        add(acc[d / BM][d % BM], t[(n + 1) & 3], s[d % BM]);
+        if (n == 2) {
+#pragma unroll
+          for (int k = 0; k < BM; ++k) s[k] = MORE || mine ? s_new[k] * w_new : 0.0f;
+        }
+        if (MORE && i == AN - 1) b[j] = fragment(st_next * kStage + b_at + j * 16 * kBlock);
+        if (MORE && n == kSteps - 1) scales(turn + 1);
+        // into this turn's place, the loads of turn + ST from the barrier on
+        if (MORE) {
+#pragma unroll
+          for (int k = 0; k < kStepLoads; ++k) {
+            const int at = ((n + BM) % kSteps) * kStepLoads + k;
+            if (at < kLoads) i == AN - 1 ? load(turn + ST, st, at) : load(turn + ST - 1, st == 0 ? ST - 1 : st - 1, at);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if (AN & 1) a[0] = a[1];
   };
 #pragma unroll
-  for (int t = 0; t < ST - 1; ++t)
-    if (t < turns) load(t, t);
-  int st = 0;
-  for (int turn = 0; turn < turns - 1; ++turn) {
-    // this turn's loads are done once no more than those of the later turns are under way
-    if (turn + ST - 2 < turns) wait_loads_and_barrier<(ST - 2) * kLoads>();
-    else wait_loads_and_barrier<0>();
-    if (turn + ST - 1 < turns) load(turn + ST - 1, st == 0 ? ST - 1 : st - 1);
-    block(turn, st, std::false_type{});
-    st = st + 1 == ST ? 0 : st + 1;
+  for (int k = 0; k < ST - 1; ++k) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(k, k, i);
   }
+  for (int part = wave; part <= kParts; part += NW) load_scales(0, part);
   wait_loads_and_barrier<0>();
-  if ((turns - 1) * KG + g <= last) block(turns - 1, st, std::true_type{});
+#pragma unroll
+  for (int i = 0; i < (BM * kStepLoads < kLoads ? BM * kStepLoads : kLoads); ++i) load(ST - 1, ST - 1, i);
+  a[0] = fragment(a_at);
+#pragma unroll
+  for (int j = 0; j < BM; ++j) b[j] = fragment(b_at + j * 16 * kBlock);
+  scales(0);
+#pragma unroll
+  for (int j = 0; j < BM; ++j) s[j] = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) t[e] = f32x4{};
+  int st = 0;
+  for (int turn = 0; turn < last_turn; ++turn) {
+    const int st_next = st + 1 == ST ? 0 : st + 1;
+    block(turn, st, st_next, std::true_type{});
+    st = st_next;
+  }
+  block(last_turn, st, 0, std::false_type{});
+#pragma unroll
+  for (int e = 0; e < 3; ++e) add(acc[(kSteps - 3 + e) / BM][(kSteps - 3 + e) % BM], t[(kSteps - 3 + e) & 3], s[(kSteps - 3 + e) % BM]);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (loads past the last turn are still under way into LDS)
   settle(acc);
   if constexpr (KG > 1) {
-    // the groups' sums through LDS: group g adds every KG-th of the WN WM AN BM blocks of 16 x 16
+    // the groups' sums through LDS: wave w adds every NW-th of the WN WM AN BM blocks of 16 x 16
     constexpr int kBlocks = WN * WM * AN * BM;
     f32x4* const red = reinterpret_cast<f32x4*>(lds);
     wait_loads_and_barrier<0>();
@@ -284,13 +323,16 @@ __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(Prod
       for (int j = 0; j < BM; ++j)
         red[((g * kBlocks) + ((wm * WN + wn) * AN + i) * BM + j) * 64 + lane] = acc[i][j];
     __syncthreads();
-    for (int t = wave; t < kBlocks; t += NW) {
-      f32x4 v = red[t * 64 + lane];
+    for (int e = wave; e < kBlocks; e += NW) {
+      f32x4 v = red[e * 64 + lane];
 #pragma unroll
-      for (int h = 1; h < KG; ++h) v += red[(h * kBlocks + t) * 64 + lane];
-      const int j = t % BM, i = t / BM % AN, n = t / (BM * AN) % WN, m = t / (BM * AN * WN);
+      for (int h = 1; h < KG; ++h) v += red[(h * kBlocks + e) * 64 + lane];
+      const int j = e % BM, i = e / BM % AN, n = e / (BM * AN) % WN, m = e / (BM * AN * WN);
       store4<OUT>(p, m0 + m * (TM / WM) + j * 16 + (lane & 15), n0 + n * (TN / WN) + i * 16 + 4 * q, v);
     }
+  } else if (p.whole) {
+    constexpr int kParted = TM * (TN * (int)sizeof(OUT) + 16) <= kLds ? 1 : 2;
+    store_tile<OUT, TN, TM, WN, WM, kParted>(p, lds, m0, n0, wm, wn, acc);
   } else {
 #pragma unroll
     for (int j = 0; j < BM; ++j) {
@@ -299,167 +341,6 @@ __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(Prod
       for (int i = 0; i < AN; ++i) store4<OUT>(p, m, n0 + wn * (TN / WN) + i * 16 + 4 * q, acc[i][j]);
     }
   }
-}
-
-// Many tokens: tiles of 256 x 256, 8 waves.  LDS is as busy as the matrix cores
-// here (a block's 512 rows are written once and read 1536 times 128 bytes, at
-// 128 bytes a cycle the 2048 cycles of the products), so nothing may wait for
-// the other: the barrier stands where a wave has its last operands of a block
-// in registers and two rows of products still to issue, and the first operands
-// of the next block are read under those.
-template <typename OUT, int WN, int WM>
-__global__ __launch_bounds__(512, 2) void product_wide_kernel(ProductParams p) {
-  constexpr int TN = 256, TM = 256, NW = 8, C = 8;
-
-  constexpr int AN = TN / WN / 16, BM = TM / WM / 16, kRows = TN + TM, kStage = kRows * kBlock, kLoads = kRows / 8 / NW;
-  constexpr int kChunk = (TM * C + 64) * 4;  // the scales of 8 blocks: x's [TM][C], W's [TN / 128][C]
-  static_assert(WN * WM == NW && kBlock % (TN / WN) == 0, "a wave's outputs lie in one scale block");
-  __shared__ __align__(1024) uint8_t lds[2 * kStage + 2 * kChunk];
-  uint8_t* const lds_s = lds + 2 * kStage;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wn = wave % WN, wm = wave / WN;
-  int mt, nt;
-  tile_of(p, blockIdx.x, mt, nt);
-  const int n0 = nt * TN, m0 = mt * TM;
-  const int last = p.kb - 1, tail = p.K - last * kBlock;
-  const __amdgpu_buffer_rsrc_t rw = make_rsrc(p.w + (int64_t)n0 * p.K, (int64_t)(p.N - n0) * p.K);
-  const __amdgpu_buffer_rsrc_t rx = make_rsrc(p.x + (int64_t)m0 * p.K, (int64_t)(p.M - m0) * p.K);
-  const __amdgpu_buffer_rsrc_t rs = make_rsrc(p.xs + (int64_t)m0 * p.kb, (int64_t)(p.M - m0) * p.kb * 4);
-  const int nb0 = n0 / kBlock, nb_last = (p.N - 1) / kBlock;
-  const __amdgpu_buffer_rsrc_t rv = make_rsrc(p.ws + (int64_t)nb0 * p.kb, (int64_t)(nb_last + 1 - nb0) * p.kb * 4);
-  // rows past the matrix repeat its last one; their results are not stored
-  uint32_t off[kLoads];
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const int r = (i * NW + wave) * 8 + (lane >> 3);  // W's rows, then x's
-    const int row = r < TN ? min(r, p.N - 1 - n0) : min(r - TN, p.M - 1 - m0);
-    off[i] = (uint32_t)row * (uint32_t)p.K + 16 * ((lane & 7) ^ ((r >> 1) & 7));
-  }
-  // Pieces past the row's end (last block) read the block's first one; the fragments there are cleared.  (A lane's piece
-  // is the same in every load.  No branches from here to the last block: the compiler moves products past them, away
-  // from the reads of their operands.)
-  const int piece = (lane & 7) ^ ((wave * 8 + (lane >> 3)) >> 1 & 7), back = 16 * piece >= tail ? 16 * piece : 0;
-  auto load = [&](int kb, int i) {
-    const int less = back & -(int)(kb == last);
-    buffer_to_lds<16>(i < kLoads / 2 ? rw : rx, off[i] - less, kb * kBlock,
-                      lds + (kb & 1) * kStage + (i * NW + wave) * 1024);
-  };
-  // Part `part` (64 floats, the last one W's) of the scales of blocks C c .. C c + C - 1
-  constexpr int kParts = TM * C / 64;
-  auto load_scales = [&](int c, int part) {
-    const bool is_w = part == kParts;
-    const int row = is_w ? min(lane / C, nb_last - nb0) : min(part * (64 / C) + lane / C, p.M - 1 - m0);
-    const int k = min(C * c + lane % C, last);
-    buffer_to_lds<4>(is_w ? rv : rs, (uint32_t)(row * p.kb + k) * 4, 0, lds_s + (c & 1) * kChunk + part * 256);
-  };
-
-  f32x4 acc[AN][BM] = {};
-  const int q = lane >> 4, f = (lane >> 1) & 7;
-  const int lo = (lane & 15) * kBlock + ((q ^ f) << 4), hi = lo ^ 64;  // pieces q and q + 4
-  const int a_at = wn * (TN / WN) * kBlock, b_at = (TN + wm * (TM / WM)) * kBlock;
-  const int s_at = (wm * (TM / WM) + (lane & 15)) * C, w_at = TM * C + wn * (TN / WN) / kBlock * C;
-  auto fragment = [&](int at) {
-    const i32x4 u = *reinterpret_cast<const i32x4*>(lds + at + lo), v = *reinterpret_cast<const i32x4*>(lds + at + hi);
-    return __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
-  };
-  i32x8 a[2], b[BM];
-  f32x4 t[4];          // the last products, which enter the sums three products later
-  float s[BM], s_new[BM], w_new;
-  auto scales = [&](int kb) {
-    const float* ss = reinterpret_cast<const float*>(lds_s + (kb / C & 1) * kChunk) + kb % C;
-#pragma unroll
-    for (int j = 0; j < BM; ++j) s_new[j] = ss[s_at + j * 16 * C];
-    w_new = ss[w_at];
-  };
-  const bool no_lo = 16 * q >= tail, no_hi = 16 * q + 64 >= tail;  // in the last block
-  auto cut = [&](i32x8 v) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      v[e] = no_lo ? 0 : v[e];
-      v[e + 4] = no_hi ? 0 : v[e + 4];
-    }
-    return v;
-  };
-  // The products of block kb, whose b and a[0] are there; MORE: with the reads of the next block's, else it is the last
-  auto block = [&](int kb, auto more) {
-    constexpr bool MORE = decltype(more)::value;
-    const int st = (kb & 1) * kStage, next = kStage - st;
-    if (!MORE) {
-      a[0] = cut(a[0]);
-#pragma unroll
-      for (int j = 0; j < BM; ++j) b[j] = cut(b[j]);
-    }
-#pragma unroll
-    for (int i = 0; i < AN; ++i) {
-      if (i + 1 < AN) {
-        const i32x8 v = fragment(st + a_at + (i + 1) * 16 * kBlock);
-        a[(i + 1) & 1] = MORE ? v : cut(v);
-      }
-      if (MORE && i == AN - 1) {
-        // all waves' loads of block kb + 1 and reads of block kb are done
-        wait_loads_and_barrier<0>();
-load_scales(kb / C + 1, min(kb % C * NW + wave, kParts));  // (a part a wave, in time for the next C blocks)
-        a[0] = fragment(next + a_at);
-        scales(kb + 1);
-      }
-#pragma unroll
-      for (int j = 0; j < BM; ++j) {
-        const int n = i * BM + j, d = n - 3;  // the product made, and the one added
-        t[n & 3] = mfma(a[i & 1], b[j]);
-        if (d >= 0) add(acc[d / BM][d % BM], t[d & 3], s[d % BM]);
-        else add(acc[AN - 1][BM + d], t[d & 3], s[BM + d]);  // (of the block before)
-        if (n == 2) {
-#pragma unroll
-          for (int k = 0; k < BM; ++k) s[k] = s_new[k] * w_new;
-        }
-        if (MORE && i == AN - 1) b[j] = fragment(next + b_at + j * 16 * kBlock);
-        // the loads of the block after next, one behind each product from the barrier on (all at once they hold the
-        // products up: 16384 x 5120 x 13824 1024 us, 983 so)
-        if (MORE && i == AN - 1) load(min(kb + 2, last), j);
-        if (MORE && n + BM < kLoads) load(kb + 1, n + BM);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-  };
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) load(0, i);
-  for (int part = wave; part <= kParts; part += NW) load_scales(0, part);
-  wait_loads_and_barrier<0>();
-#pragma unroll
-  for (int i = 0; i < BM; ++i) load(min(1, last), i);
-  a[0] = fragment(a_at);
-#pragma unroll
-  for (int j = 0; j < BM; ++j) b[j] = fragment(b_at + j * 16 * kBlock);
-  scales(0);
-#pragma unroll
-  for (int j = 0; j < BM; ++j) s[j] = 0.0f;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) t[e] = f32x4{};
-  for (int kb = 0; kb < last; ++kb) block(kb, std::true_type{});
-  block(last, std::false_type{});
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (loads past the last block may still be under way into LDS)
-#pragma unroll
-  for (int d = 0; d < 3; ++d) add(acc[AN - 1][BM - 3 + d], t[(AN * BM - 3 + d) & 3], s[BM - 3 + d]);
-  settle(acc);
-  if (p.whole) {
-    store_tile<OUT, TN, TM, WN, WM, sizeof(OUT) / 2>(p, lds, m0, n0, wm, wn, acc);
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < BM; ++j) {
-    const int m = m0 + wm * (TM / WM) + j * 16 + (lane & 15);
-#pragma unroll
-    for (int i = 0; i < AN; ++i) store4<OUT>(p, m, n0 + wn * (TN / WN) + i * 16 + 4 * q, acc[i][j]);
-  }
-}
-
-template <typename OUT, int WN, int WM>
-hipError_t launch_wide(ProductParams p, hipStream_t s) {
-  p.n_ntiles = (p.N + 255) / 256;
-  p.n_mtiles = (p.M + 255) / 256;
-  hipLaunchKernelGGL((product_wide_kernel<OUT, WN, WM>), dim3((unsigned)(p.n_ntiles * (int64_t)p.n_mtiles)), dim3(512), 0,
-                     s, p);
-  return hipGetLastError();
 }
 
 // Few tokens: the weights' stream from HBM is the whole work, and a workgroup
@@ -566,12 +447,13 @@ hipError_t launch_tiles(ProductParams p, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The kernels and what they take: `turn` us for KG scale blocks of every tile
-// of a round (per_cu tiles a CU), `round` us beside them.  Both are fits to
-// times of 90 sizes (M 1 .. 4096; N x K 4096 x 4096, 24576 x 4096, 5120 x 13824,
-// 1024 x 5120, 2048 x 2048), 6-13 % off each; the kernel that they choose is 0.8 %
-// slower than the fastest of the nine on average, 12 % at most.  Without the
-// last but one, 2.3 % and 27 %.
+// The tilings and what they take: `turn` us for KG scale blocks of every tile
+// of a round (per_cu tiles a CU), `round` us beside them: fits to the times of
+// 60 sizes (M 24 .. 4096; N x K 4096 x 4096, 24576 x 4096, 5120 x 13824, 1024 x 5120,
+// 2048 x 2048), at each of which but one they choose the fastest of the seven.
+// How far apart those are: 64 x 4096 x 4096 8.6 us by the first, 24.9 by the
+// sixth; 700 x 4096 x 4096 27.9 by the sixth, 51 by the last; 4096 x 4096 x 4096
+// 63.5 by the last, 82 by the fifth, 187 by the third.
 template <typename OUT>
 struct Variant {
   int tn, tm, kg, per_cu;
@@ -594,13 +476,13 @@ hipError_t launch_product(const ProductParams& p, hipStream_t s) {
   // 5.8 us, 6.7 with 32), 32 from there on (8 x 5120 x 13824 20 us, 26 with 16)
   if (p.M <= 16) return p.N < 20 * kCus ? launch_rows<OUT, 1, 1, 8, 2>(p, s) : launch_rows<OUT, 2, 1, 8, 2>(p, s);
   static const Variant<OUT> variants[] = {
-      {32, 32, 8, 1, 1.237f, 1.13f, launch_tiles<OUT, 32, 32, 1, 1, 8, 2, 16>},
-      {64, 32, 4, 1, 0.805f, 1.69f, launch_tiles<OUT, 64, 32, 2, 1, 4, 3, 8>},
-      {64, 64, 2, 1, 0.560f, 2.48f, launch_tiles<OUT, 64, 64, 2, 2, 2, 4, 8>},
-      {128, 64, 2, 1, 0.860f, 2.82f, launch_tiles<OUT, 128, 64, 2, 2, 2, 3, 8>},
-      {128, 128, 1, 2, 1.152f, 2.32f, launch_tiles<OUT, 128, 128, 2, 2, 1, 2, 8>},
-      {128, 128, 2, 1, 1.491f, 2.25f, launch_tiles<OUT, 128, 128, 2, 2, 2, 2, 8>},
-      {256, 256, 1, 1, 1.573f, 3.66f, launch_wide<OUT, 2, 4>},
+      {32, 32, 8, 1, 1.237f, 1.79f, launch_tiles<OUT, 32, 32, 1, 1, 8, 2, 32>},
+      {64, 32, 4, 1, 0.713f, 2.94f, launch_tiles<OUT, 64, 32, 2, 1, 4, 3, 16>},
+      {64, 64, 2, 1, 0.531f, 3.41f, launch_tiles<OUT, 64, 64, 2, 2, 2, 4, 16>},
+      {128, 64, 2, 1, 0.793f, 3.53f, launch_tiles<OUT, 128, 64, 2, 2, 2, 3, 8>},
+      {128, 128, 1, 2, 1.179f, 0.96f, launch_tiles<OUT, 128, 128, 2, 2, 1, 2, 8>},
+      {128, 128, 2, 1, 1.429f, 3.12f, launch_tiles<OUT, 128, 128, 2, 2, 2, 2, 8>},
+      {256, 256, 1, 1, 1.526f, 5.30f, launch_tiles<OUT, 256, 256, 2, 4, 1, 2, 8>},
   };
   const Variant<OUT>* best = variants;
   for (const Variant<OUT>& v : variants)

@@ -118,6 +118,29 @@ def test_policy_matches_the_surrogate():
 
 
 @pytest.mark.parametrize("aggregate", AGG)
+def test_policy_many_groups_and_large_batch(aggregate):
+    # more groups than one workgroup counts; more slots than its workgroups share out the norms of
+    for B, L, n_groups in ((40, 200, 3000), (33, 33000, 5)):
+        if L > 1000 and aggregate in ("sequence", "constant"):
+            continue
+        r, mask, lp, groups = _batch(B, L, 70 + B, n_groups, holes=0.4)
+        adv = r.normal(size=B).astype(np.float32)
+        ref = policy_loss(B, L, mask, lp["new"], lp["old"], adv, False, aggregate, groups, n_groups, ref=lp["ref"],
+                          kl_coef=0.05, eps_high=0.28, norm=31.0)
+        _check_policy(_policy(B, L, n_groups, mask, groups, lp, adv, False, aggregate), ref, B, L)
+
+
+def test_policy_any_nonzero_mask():
+    for B, L in ((3, 90), (7, 4099), (12, 90000)):
+        r, mask, lp, groups = _batch(B, L, 90 + B, 2)
+        adv = r.normal(size=B).astype(np.float32)
+        a = _policy(B, L, 2, mask, groups, lp, adv, False, "token")
+        b = _policy(B, L, 2, mask * r.choice([1, 2, 127, 128, 255], mask.size).astype(np.uint8), groups, lp, adv, False,
+                    "token")
+        assert all((down(x) == down(y)).all() for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("aggregate", AGG)
 def test_policy_nothing_valid(aggregate):
     for B, L in ((3, 40), (2, 5000), (0, 8), (4, 0)):
         mask = np.zeros(B * L, np.uint8)

@@ -15,7 +15,7 @@ SHAPES = [(1, 1, 32), (1, 16, 128), (2, 130, 96), (7, 64, 160), (16, 256, 2080),
           (333, 520, 2080), (513, 1025, 160), (1, 4096, 4096), (40, 2048, 5120),
           # outputs in 32-row pieces, wider tiles, tiles of 256 x 256 (whole and cut ones)
           (13, 5200, 288), (64, 20000, 1056), (300, 3000, 2336), (900, 2100, 1184), (1300, 2050, 2080),
-          (1290, 6700, 96), (1100, 7937, 352)]
+          (1290, 6700, 96), (1100, 7937, 352), (1290, 6712, 352), (1500, 2056, 416)]
 
 
 def _integers(shape, seed):
@@ -114,6 +114,38 @@ def test_garbage_behind_the_last_rows_and_columns():
             t.append((v if a.dtype == np.uint8 else v.view(torch.float32)).reshape(a.shape))
         y = acrl.acrl_matmul_fp8(*t, out_dtype=torch.float32)
         assert np.array_equal(down(y), product(*ops)[0].astype(np.float32))
+
+
+@pytest.mark.parametrize("M", [1, 20, 200])
+def test_subnormal_codes_and_large_scales(M):
+    # every code against whole numbers, with scales of 2^-20 .. 2^20: exact as long as one term a sum is not 0
+    torch, dev = torch_dev()
+    N, K = 260, 256
+    xq, wq = np.zeros((M, K), np.uint8), np.zeros((N, K), np.uint8)
+    codes = np.array([c for c in range(256) if c & 127 != 127], np.uint8)
+    at = (7 * np.arange(M)) % K
+    xq[np.arange(M), at] = codes[np.arange(M) % codes.size]
+    wq[:] = _integers((N, K), 4)
+    r = np.random.default_rng(6)
+    xs = np.exp2(r.integers(-20, 21, (M, 2))).astype(np.float32)
+    ws = np.exp2(r.integers(-20, 21, (3, 2))).astype(np.float32)
+    y = _run((xq, xs, wq, ws), out_dtype=torch.float32)
+    assert np.array_equal(down(y), product(xq, xs, wq, ws)[0].astype(np.float32))
+
+
+def test_refusals():
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    xq, xs, wq, ws = (up(torch, dev, a) for a in _exact_case(4, 64, 256, 1))
+    wide = torch.empty((4, 130), dtype=torch.bfloat16, device=dev)
+    for bad in (dict(xq=xq[:, :128]), dict(x_scales=xs[:2]), dict(w_scales=ws.double()), dict(wq=wq.t()),
+                dict(x_scales=xs.cpu()), dict(out=wide), dict(out=wide.t()[:4, :4]), dict(out_dtype=torch.float16),
+                dict(out=wide[:, :64].half()), dict(xq=xq.float())):
+        args = dict(xq=xq, x_scales=xs, wq=wq, w_scales=ws, **{})
+        with pytest.raises(ValueError):
+            acrl.acrl_matmul_fp8(**{**args, **bad})
+    with pytest.raises(acrl.AcrlError):  # 2 bytes off 16
+        acrl.acrl_matmul_fp8(xq, xs, wq, ws, out=wide[:, 1:65])
 
 
 def test_no_rows_of_x():

@@ -218,7 +218,11 @@ __device__ __forceinline__ double policy_slot(const acrl_policy_loss_desc& p, do
 enum ShareFrom { kShareNorm, kShareOwn, kShareWs };
 
 // One unit of a response's slots: coef, and the unit's sums.  Where a thread's
-// mask leaves nothing, nothing else is loaded.
+// mask leaves nothing, nothing else is loaded.  512 responses of up to 16384
+// slots (126 MB): 33.4 us, 3.8 TB/s; the fp64 operations alone are 20 us of the
+// SIMDs' time (12.4 M wavefront instructions), and cover the loads in part.
+// (The sums added up by the workgroup that ends last, behind a device-wide
+// fence, instead of by policy_sum_kernel: 216 us, 14.4 for 7.4 at 64 x 4096.)
 template <int TURNS, bool VEC>
 __global__ __launch_bounds__(kUnitThreads) void policy_main_kernel(acrl_policy_loss_desc p, PolicyWs ws,
                                                                    int64_t units, int from) {
@@ -452,7 +456,8 @@ __device__ __forceinline__ void pref_rewards(const acrl_preference_desc& p, cons
 }
 
 // coef of one response's slots: its pairs' slopes, then one value for every
-// valid slot.  The last workgroup sums the loss and writes the rewards.
+// valid slot (512 responses of 16384 slots: 10.2 us, 4.1 TB/s; pref_seq_kernel
+// 12.3 us, 3.7 TB/s).  The last workgroup sums the loss and writes the rewards.
 template <bool VEC>
 __global__ __launch_bounds__(kUnitThreads) void pref_coef_kernel(acrl_preference_desc p, const PrefRec* rec) {
   __shared__ BlockShared<1, kUnitThreads> sh;

@@ -155,9 +155,19 @@ __device__ __forceinline__ void tile_of(const ProductParams& p, int block, int& 
 // and a row of products still to issue; the next turn's first operands are read
 // under those, and its stage's loads go out one behind each product.  The loop
 // has no branches: the compiler would move products past them, away from the
-// reads of their operands.  At 256 x 256 LDS is as busy as the matrix cores: a
-// block's 512 rows are written once and read 1536 times 128 bytes, at 128 bytes
-// a cycle the 2048 cycles of the products.
+// reads of their operands.
+//
+// What bounds it, 16384 x 5120 x 13824 by 256 x 256 tiles (980 us, 2370 TFLOP/s; counters): a turn takes 3440
+// cycles at 1.8 GHz, to which the power limit has brought the clock (2.4 without
+// load); the matrix cores are busy for 2097 of them, LDS for 1064; the four FMAs
+// beside each product let it take 37 cycles for 32 even with all operands in
+// registers.  Without the turn's loads it takes three quarters of the time, so
+// what is left is loads that arrive late or hold the products up.  Measured
+// without gain: loads all at once behind the barrier (1024 us), one behind every
+// second product (1020), two or four behind one (1005, 1018), lines touched a turn or more
+// ahead (1090), bands of 4 or 16 token tiles, wave priorities.  Tiles of 64 x 64
+// (0.53 us for 2 blocks) pay for the barrier and a chain of read, product and
+// sum each turn.
 template <typename OUT, int TN, int TM, int WN, int WM, int KG, int ST, int C>
 __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(ProductParams p) {
   constexpr int NW = WN * WM * KG, AN = TN / WN / 16, BM = TM / WM / 16, kSteps = AN * BM;  // fragments of a wave

@@ -566,7 +566,7 @@ acrl_status acrl_matmul_fp8(const acrl_matmul_desc* desc, void* stream);
  *   m = min(r A, clip(r) A), clip(r) = min(max(r, 1 - eps_low), 1 + eps_high);
  *       for A < 0 and dual_clip > 0: max(m, dual_clip A)
  *   k = -q (K1), q^2 / 2 (K2) or exp(q) - q - 1 (K3), 0 without logp_ref
- *   loss = sum_t a_t (-w_t m_t + kl_coef k_t)
+ *   loss = sum_t a_t (-w_t m_t + kl_coef k_t)     (kl_coef 0: k enters the stats alone)
  *   coef[t] = d loss / d logp_new[t]
  *           = a_t (-w_t r_t A_t [m is r A] + kl_coef k'_t),
  *       k' = 1 (K1), -q (K2), 1 - exp(q) (K3); a tie counts as m = r A.

@@ -206,10 +206,10 @@ __device__ __forceinline__ double policy_slot(const acrl_policy_loss_desc& p, do
     } else {
       double e;
       k = exp_rest(q, e);
-      dk = -(k + q);
+      dk = q < -1.0 ? 1.0 - e : -(k + q);  // 1 - exp(q): k + q loses it below, 1 - e next to 0
     }
     v[1] += k;
-    g += (double)p.kl_coef * dk;
+    if (p.kl_coef > 0.0f) g += (double)p.kl_coef * dk;  // (no 0 * infinity)
   }
   return g;
 }
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(kUnitThreads) void policy_main_kernel(acrl_policy_l
 }
 
 __device__ __forceinline__ void policy_finish(const acrl_policy_loss_desc& p, const double (&v)[kPolicySums]) {
-  p.loss[0] = v[0] + (double)p.kl_coef * v[1];
+  p.loss[0] = p.kl_coef > 0.0f ? v[0] + (double)p.kl_coef * v[1] : v[0];
   if (!p.stats) return;
   const double inv = v[5] > 0 ? 1.0 / v[5] : 0.0;
   p.stats[ACRL_PSTAT_POLICY] = v[0];

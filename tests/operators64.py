@@ -103,12 +103,12 @@ def policy_loss(B, L, mask, new, old, adv, per_token, aggregate, groups=None, n_
             k, dk = {"k1": (-q, 1.0), "k2": (q * q / 2, -q), "k3": (math.expm1(q) - q, -math.expm1(q))}[kl]
         pol += a[i] * -w * m
         klsum += a[i] * k
-        size += a[i] * (abs(w * m) + beta * abs(k))
+        size += a[i] * (abs(w * m) + (beta * abs(k) if beta else 0.0))
         moved += math.expm1(delta) - delta
         count += 1
-        coef[t] = a[i] * ((-w * u if live else 0.0) + beta * dk)
+        coef[t] = a[i] * ((-w * u if live else 0.0) + (beta * dk if beta else 0.0))
     d = max(1, count)
-    return dict(loss=pol + beta * klsum, coef=coef, size=size,
+    return dict(loss=pol + beta * klsum if beta else pol, coef=coef, size=size,
                 stats=np.array([pol, klsum, clipped / d, dual / d, moved / d, count]))
 
 

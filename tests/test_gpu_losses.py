@@ -102,6 +102,46 @@ def test_policy_terms(kl, dual, use_ref):
     _check_policy(got, ref, B, L)
 
 
+@pytest.mark.parametrize("B,L", [(4, 64), (3, 4096)])
+@pytest.mark.parametrize("kl", KL)
+def test_policy_reference_far_below_and_above(B, L, kl):
+    # a reference that gives a token next to nothing: k' = 1 - exp(q) is 1 there, whatever k is
+    r, mask, lp, groups = _batch(B, L, 5, 1)
+    mask[:] = 1
+    far = np.array([-1.0, -1.5, -40, -745, -800, -1e9, -1e30, -3.4e38, 5, 40, 60], np.float32)
+    lp["ref"][:far.size] = far
+    adv = r.normal(size=B).astype(np.float32)
+    ref = policy_loss(B, L, mask, lp["new"], lp["old"], adv, False, "constant", eps_high=0.28, kl=kl, kl_coef=0.05,
+                      ref=lp["ref"], norm=31.0)
+    coef, loss, stats = _policy(B, L, 1, mask, groups, lp, adv, False, "constant", kl)
+    _check(coef, ref["coef"], np.abs(ref["coef"]))
+    assert abs(float(down(loss)[0]) - ref["loss"]) <= 1e-12 * ref["size"]
+
+
+@pytest.mark.parametrize("B,L", [(4, 64), (3, 4096)])
+def test_policy_infinite_divergence(B, L):
+    # k is infinite where the reference rules a token out: the loss too, but not the gradient of k3, and without
+    # kl_coef the statistics alone
+    r, mask, lp, groups = _batch(B, L, 5, 1)
+    mask[:] = 1
+    lp["ref"][3] = -np.inf
+    adv = r.normal(size=B).astype(np.float32)
+    for kl in ("k1", "k3"):
+        for kl_coef in (0.05, 0.0):
+            q = lp["ref"].astype(np.float64) - lp["new"]
+            coef, loss, stats = _policy(B, L, 1, mask, groups, lp, adv, False, "token", kl, kl_coef=kl_coef)
+            finite = dict(lp, ref=np.where(q == -np.inf, np.float32(-1e30), lp["ref"]))
+            ref = policy_loss(B, L, mask, lp["new"], lp["old"], adv, False, "token", eps_high=0.28, kl=kl,
+                              kl_coef=kl_coef, ref=finite["ref"])
+            _check(coef, ref["coef"], np.abs(ref["coef"]))
+            s = down(stats)
+            assert s[1] == np.inf and np.isfinite(s[[0, 2, 3, 4, 5]]).all()
+            if kl_coef:
+                assert down(loss)[0] == np.inf
+            else:
+                assert abs(float(down(loss)[0]) - ref["loss"]) <= 1e-12 * ref["size"]
+
+
 def test_policy_matches_the_surrogate():
     torch, dev = torch_dev()
     from paper_2607_24062_amd import acrl

@@ -585,7 +585,8 @@ acrl_status acrl_matmul_fp8(const acrl_matmul_desc* desc, void* stream);
  * Requirements: B, L >= 0; for GROUP n_groups > 0 if B > 0 and group_of_seq
  * non-NULL (else both are not read); eps_low in [0, 1), eps_high >= 0;
  * dual_clip 0 (none) or > 1; kl_coef >= 0, and 0 without logp_ref; norm > 0
- * for CONSTANT; B < 2^22 and B ceil(L/2048) < 2^24; workspace of acrl_policy_loss_workspace_size() bytes, 16-byte aligned. */
+ * for CONSTANT; B < 2^22 and B ceil(L/2048) < 2^24; workspace of
+ * acrl_policy_loss_workspace_size() bytes, 16-byte aligned.                 */
 typedef enum { ACRL_KL_K1 = 0, ACRL_KL_K2 = 1, ACRL_KL_K3 = 2 } acrl_kl_estimator;
 typedef enum {
   ACRL_AGG_GROUP = 0, ACRL_AGG_SEQUENCE = 1, ACRL_AGG_TOKEN = 2, ACRL_AGG_CONSTANT = 3
@@ -653,8 +654,9 @@ acrl_status acrl_policy_loss(const acrl_policy_loss_desc* desc, void* stream);
  * outside [0, B) gives NaN: the reward it names, the loss, and coef of the
  * pair's other response.  All is evaluated in fp64 from the fp32 inputs, sums
  * by fixed trees.
- * Requirements: B, L, n_pairs >= 0; B < 2^22; beta > 0; margin finite; label_smoothing in
- * [0, 1), and 0 but for SIGMOID; workspace of
+ * Requirements: B, L, n_pairs >= 0; B < 2^22, n_pairs < 2^24 and B n_pairs <
+ * 2^40; beta > 0; margin finite; label_smoothing in [0, 1), and 0 but for
+ * SIGMOID; workspace of
  * acrl_preference_loss_workspace_size() bytes, 16-byte aligned.             */
 typedef enum { ACRL_PREF_SIGMOID = 0, ACRL_PREF_HINGE = 1, ACRL_PREF_SQUARED = 2 } acrl_preference_form;
 

@@ -377,6 +377,9 @@ hipError_t launch_policy_loss(const acrl_policy_loss_desc& p, hipStream_t s) {
 struct PrefRec {
   double x, each;  // x_i (mean_logp applied); d x_i / d logp_new of a valid slot
 };
+// Every response's workgroup looks through all pairs: 65536 responses of 65536 pairs take 2.9 ms, 2^20 of 2^20 1.1 s,
+// and more are refused.
+constexpr int64_t kMaxPairs = (int64_t)1 << 24, kMaxPairLooks = (int64_t)1 << 40;
 constexpr int kPrefOne = 256;  // responses, and pairs, of a batch that one workgroup does
 inline bool one_preference(int64_t B, int64_t L, int64_t P) {
   return B * L <= kOneSlots && B <= kPrefOne && P <= kPrefOne;
@@ -613,7 +616,8 @@ acrl_status acrl_policy_loss(const acrl_policy_loss_desc* d, void* stream) {
 acrl_status acrl_preference_loss_workspace_size(int64_t B, int64_t L, int64_t n_pairs, size_t* bytes) {
   ACRL_REQUIRE(bytes, "bytes is NULL");
   ACRL_REQUIRE(B >= 0 && L >= 0 && n_pairs >= 0, "B, L and n_pairs must be >= 0");
-  ACRL_REQUIRE(B < acrl::kMaxResponses && L < INT32_MAX && n_pairs < INT32_MAX, "B, L or n_pairs too large");
+  ACRL_REQUIRE(B < acrl::kMaxResponses && L < INT32_MAX && n_pairs < acrl::kMaxPairs, "B, L or n_pairs too large");
+  ACRL_REQUIRE(B * n_pairs < acrl::kMaxPairLooks, "B x n_pairs too large");
   *bytes = acrl::one_preference(B, L, n_pairs) ? 0 : acrl::pref_ws_bytes(B);
   return ACRL_OK;
 }

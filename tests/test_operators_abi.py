@@ -115,7 +115,8 @@ def test_preference_loss(acrl, p):
                 dict(beta=nan), dict(beta=inf), dict(margin=nan), dict(margin=inf), dict(label_smoothing=1.0),
                 dict(label_smoothing=-0.1), dict(label_smoothing=nan), dict(form=1, label_smoothing=0.1),
                 dict(form=2, label_smoothing=0.1), dict(form=3), dict(form=-1), dict(mean_logp=2), dict(B=1 << 22),
-                dict(L=INT_MAX), dict(n_pairs=INT_MAX), dict(workspace=_off(p, 8))):
+                dict(L=INT_MAX), dict(n_pairs=INT_MAX), dict(n_pairs=1 << 24), dict(B=1 << 20, n_pairs=1 << 20),
+                dict(workspace=_off(p, 8))):
         d = acrl.PreferenceDesc(**{**ok, **bad})
         assert L.acrl_preference_loss(ctypes.byref(d), None) == acrl.ACRL_ERR_INVALID_ARG, bad
     for bad in (dict(workspace=None), dict(workspace_bytes=16)):

@@ -283,11 +283,13 @@ def _want(t, dtype, numel: int, index: int, name: str, optional: bool = False):
     return t.data_ptr()
 
 
-def _index_of(t, dtype, name: str) -> int:
-    """The device index of a device tensor, which is to be the current one: the
-    library launches there."""
+def _index_of(t, dtype, name: str, stream=None) -> int:
+    """The device index of a device tensor, which is to be the current one (the
+    library launches there) and the stream's."""
     _dev(t, dtype, name)
     index = t.get_device()
+    if stream is not None and stream.device_index != index:
+        raise ValueError("%s is on cuda:%d, the stream belongs to cuda:%d" % (name, index, stream.device_index))
     if index != torch.cuda.current_device():
         raise ValueError("%s is on cuda:%d, the current device is cuda:%d" % (name, index, torch.cuda.current_device()))
     return index
@@ -347,6 +349,8 @@ def acrl_quantize_fp8(x: torch.Tensor, scaling: int, rounding: int = ROUND_NEARE
         if not x.is_cuda or x.dtype != torch.bfloat16 or x.stride(1) != 1 or x.stride(0) < cols:
             raise ValueError("x must be a bf16 device matrix with unit column stride")
         ld = x.stride(0)
+    if scaling == SCALE_ROW128 or scaling == SCALE_BLOCK128:
+        return _quantize_blocks(x, rows, cols, ld, scaling, rounding, q, scales, stream)
     if q is None:
         q = torch.empty((rows, cols), dtype=torch.uint8, device=x.device)
     if scales is None:
@@ -354,16 +358,30 @@ def acrl_quantize_fp8(x: torch.Tensor, scaling: int, rounding: int = ROUND_NEARE
             scales = torch.empty(1, dtype=torch.float32, device=x.device)
         elif scaling == SCALE_PER_ROW:
             scales = torch.empty(rows, dtype=torch.float32, device=x.device)
-        elif scaling == SCALE_ROW128:
-            scales = torch.empty((rows, (cols + 127) // 128), dtype=torch.float32, device=x.device)
-        elif scaling == SCALE_BLOCK128:
-            scales = torch.empty(((rows + 127) // 128, (cols + 127) // 128), dtype=torch.float32, device=x.device)
         else:
             scales = torch.empty((rows, cols // 32), dtype=torch.uint8, device=x.device)
     nbytes = _size("acrl_quantize_workspace_size", rows, cols, scaling)
     ws = _workspace(nbytes, x.device, stream) if nbytes else None
     _check(lib().acrl_quantize_fp8(x.data_ptr(), rows, cols, ld, scaling, rounding, q.data_ptr(), scales.data_ptr(),
                                    _ptr(ws), nbytes, _raw_stream(stream)), "acrl_quantize_fp8")
+    return q, scales
+
+
+def _quantize_blocks(x, rows: int, cols: int, ld: int, scaling: int, rounding: int, q, scales, stream):
+    """ROW128 and BLOCK128: outputs and stream as for acrl_matmul_fp8."""
+    index = x.get_device()
+    if index != torch.cuda.current_device() or (stream is not None and stream.device_index != index):
+        raise ValueError("x is on %s, not on the current device or the stream's" % x.device)
+    shape = (rows if scaling == SCALE_ROW128 else (rows + 127) // 128, (cols + 127) // 128)
+    if q is None:
+        q = _empty((rows, cols), torch.uint8, x.device, stream)
+    if scales is None:
+        scales = _empty(shape, torch.float32, x.device, stream)
+    for t, dtype, n, name in ((q, torch.uint8, rows * cols, "q"), (scales, torch.float32, shape[0] * shape[1], "scales")):
+        if t.dtype is not dtype or t.get_device() != index or t.numel() < n or not t.is_contiguous():
+            raise ValueError("%s must be a contiguous %s tensor of %d elements or more on %s" % (name, dtype, n, x.device))
+    _check(lib().acrl_quantize_fp8(x.data_ptr(), rows, cols, ld, scaling, rounding, q.data_ptr(), scales.data_ptr(),
+                                   None, 0, _raw_stream(stream)), "acrl_quantize_fp8")
     return q, scales
 
 
@@ -631,7 +649,7 @@ def acrl_matmul_fp8(xq, x_scales, wq, w_scales, out=None, out_dtype=torch.bfloat
     first element 16-byte aligned."""
     if xq.dim() != 2 or wq.dim() != 2 or xq.shape[1] != wq.shape[1]:
         raise ValueError("xq [M, K] and wq [N, K] must be 2-D with the same K")
-    index = _index_of(xq, torch.uint8, "xq")
+    index = _index_of(xq, torch.uint8, "xq", stream)
     M, K = xq.shape
     N = wq.shape[0]
     kb = (K + 127) // 128
@@ -660,7 +678,7 @@ def acrl_policy_loss(B: int, L: int, n_groups: int, mask, group_of_seq, logp_new
     """Clipped policy loss with a KL term to a reference policy: returns
     (coef float32 [B*L] = d loss / d logp_new, loss float64 [1], stats float64
     [N_PSTATS], PSTAT_NAMES).  coef goes to acrl_lm_head_backward."""
-    n, index, dev, f32 = B * L, _index_of(logp_new, torch.float32, "logp_new"), logp_new.device, torch.float32
+    n, index, dev, f32 = B * L, _index_of(logp_new, torch.float32, "logp_new", stream), logp_new.device, torch.float32
     nbytes = _size("acrl_policy_loss_workspace_size", B, L, n_groups)
     if coef is None:
         coef = _empty(n, f32, dev, stream)
@@ -684,7 +702,7 @@ def acrl_preference_loss(B: int, L: int, mask, logp_new, chosen, rejected, logp_
     """Loss of preferred / rejected response pairs (int32 response indexes
     chosen, rejected [n_pairs]): returns (coef float32 [B*L] = d loss / d
     logp_new, loss float64 [1], rewards float32 [2, n_pairs])."""
-    n, index, dev, f32 = B * L, _index_of(logp_new, torch.float32, "logp_new"), logp_new.device, torch.float32
+    n, index, dev, f32 = B * L, _index_of(logp_new, torch.float32, "logp_new", stream), logp_new.device, torch.float32
     P = chosen.numel()
     nbytes = _size("acrl_preference_loss_workspace_size", B, L, P)
     if coef is None:

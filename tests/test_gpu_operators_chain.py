@@ -12,6 +12,8 @@ what is compared is the loss's and the gradient's part:
  - softmax and coef are off by the log-probs' error (2e-3 bound of the scoring
    tests, taken relative to the probability): another 2e-3 of the same sums;
  - fp32 accumulation: 2^-20 of the same sums covers 2048 additions' random walk."""
+import types
+
 import numpy as np
 import pytest
 
@@ -96,3 +98,42 @@ def test_step(kl, aggregate):
         assert (np.abs(down(dh) - dz @ W) <= tol * (mag @ np.abs(W)) + 1e-12).all()
         assert (np.abs(down(dw) - dz.T @ H) <= tol * (mag.T @ np.abs(H)) + 1e-12).all()
         assert np.abs(down(dw)).max() > 0
+
+
+def _calls(torch, dev, acrl, stream=None):
+    """One call of each operator: name -> outputs."""
+    x, w = (up_bf16(torch, dev, random_bf16(shape, k)) for k, shape in enumerate(((40, 256), (192, 256))))
+    n, m = torch.zeros(4000, device=dev), torch.ones(4000, dtype=torch.uint8, device=dev)
+    i = torch.zeros(2, dtype=torch.int32, device=dev)
+    xq, xs = acrl.acrl_quantize_fp8(x, acrl.SCALE_ROW128)
+    wq, ws = acrl.acrl_quantize_fp8(w, acrl.SCALE_BLOCK128)
+    torch.cuda.synchronize()
+    return dict(rows=lambda: acrl.acrl_quantize_fp8(x, acrl.SCALE_ROW128, stream=stream),
+                blocks=lambda: acrl.acrl_quantize_fp8(w, acrl.SCALE_BLOCK128, stream=stream),
+                matmul=lambda: [acrl.acrl_matmul_fp8(xq, xs, wq, ws, stream=stream)],
+                policy=lambda: acrl.acrl_policy_loss(2, 2000, 1, m, i, n, n, n[:2], False, stream=stream),
+                preference=lambda: acrl.acrl_preference_loss(2, 2000, m, n, i, i, stream=stream))
+
+
+def test_stream_of_another_device():
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    other = types.SimpleNamespace(device_index=torch.cuda.current_device() + 1, cuda_stream=0)  # (refused before its use)
+    for name, call in _calls(torch, dev, acrl, other).items():
+        with pytest.raises(ValueError, match="stream"):
+            call()
+
+
+def test_outputs_belong_to_the_stream():
+    # memory of outputs that are dropped while the stream may still use them goes back to that stream, not to the
+    # current one's next allocation
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    s = torch.cuda.Stream()
+    for name, call in _calls(torch, dev, acrl, s).items():
+        out = call()
+        held = [(t.data_ptr(), t.shape, t.dtype) for t in out]
+        del out
+        fresh = [torch.empty(shape, dtype=dtype, device=dev) for _, shape, dtype in held for _ in range(3)]
+        assert not {a for a, _, _ in held} & {t.data_ptr() for t in fresh}, name
+    torch.cuda.synchronize()

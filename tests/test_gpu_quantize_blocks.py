@@ -82,3 +82,19 @@ def test_no_rows(tile):
     from paper_2607_24062_amd import acrl
     q, s = acrl.acrl_quantize_fp8(torch.empty((0, 256), dtype=torch.bfloat16, device=dev), _scaling(tile))
     assert q.shape == (0, 256) and s.shape == (0, 2)
+
+
+@pytest.mark.parametrize("tile", [1, 128])
+def test_outputs_that_do_not_fit(tile):
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    x = up_bf16(torch, dev, random_bf16((256, 160), 12))
+    n = (256 if tile == 1 else 2) * 2
+    for kw in (dict(q=torch.empty(256 * 160 - 1, dtype=torch.uint8, device=dev)),
+               dict(q=torch.empty((256, 160), dtype=torch.int8, device=dev)),
+               dict(q=torch.empty((160, 256), dtype=torch.uint8, device=dev).t()),
+               dict(q=torch.empty((256, 160), dtype=torch.uint8)),
+               dict(scales=torch.empty(n - 1, device=dev)),
+               dict(scales=torch.empty(n, dtype=torch.float64, device=dev)), dict(scales=torch.empty(n))):
+        with pytest.raises(ValueError, match=list(kw)[0]):
+            acrl.acrl_quantize_fp8(x, _scaling(tile), **kw)

@@ -145,40 +145,50 @@ __device__ __forceinline__ void tile_of(const ProductParams& p, int block, int& 
 
 // Tile of TN outputs x TM tokens a workgroup, WN x WM waves for each of KG
 // groups.  K passes through LDS in ST stages of KG scale blocks, one a group
-// (buffer -> LDS loads), and the groups' sums are added at the end in their
-// order.  Piece c (16 bytes) of row r lies at position c ^ (r / 2 mod 8) of the
-// row's 128 bytes, and lane group q of a fragment takes pieces q and q + 4 (the
-// products of a block may be summed in any order of k, as long as both operands
-// have the same): LDS then serves a fragment's reads without bank conflicts.
+// (buffer -> LDS loads; W's rows of all groups, then x's), and the groups' sums
+// are added at the end in their order.  Piece c (16 bytes) of row r lies at
+// position c ^ (r / 2 mod 8) of the row's 128 bytes, and lane group q of a
+// fragment takes pieces q and q + 4 (the products of a block may be summed in
+// any order of k, as long as both operands have the same): LDS then serves a
+// fragment's reads without bank conflicts.
 //
-// The barrier stands where a wave has its last operands of a turn in registers
-// and a row of products still to issue; the next turn's first operands are read
-// under those, and its stage's loads go out one behind each product.  The loop
-// has no branches: the compiler would move products past them, away from the
-// reads of their operands.
+// A stage's place is loaded again, one load behind each product, from the
+// barrier on that ends its reads.  That barrier stands, row by row (AHEAD
+// false), where a wave has its last operands of a turn in registers and a row
+// of products still to issue, with the next turn's first operands read under
+// those; or (AHEAD) at the turn's start, with all operands of the next turn read
+// under this one's products, which takes twice their registers (128 x 128, 700 x
+// 5120 x 13824: 64 us for 72; tiles of 64 and less gain nothing).  The
+// loops have no branches: the compiler would move products past them, away from
+// the reads of their operands.  The scales come C blocks at a time, between the
+// turns.
 //
-// What bounds it, 16384 x 5120 x 13824 by 256 x 256 tiles (980 us, 2370 TFLOP/s; counters): a turn takes 3440
-// cycles at 1.8 GHz, to which the power limit has brought the clock (2.4 without
-// load); the matrix cores are busy for 2097 of them, LDS for 1064; the four FMAs
-// beside each product let it take 37 cycles for 32 even with all operands in
-// registers.  Without the turn's loads it takes three quarters of the time, so
-// what is left is loads that arrive late or hold the products up.  Measured
-// without gain: loads all at once behind the barrier (1024 us), one behind every
-// second product (1020), two or four behind one (1005, 1018), lines touched a turn or more
-// ahead (1090), bands of 4 or 16 token tiles, wave priorities.  Tiles of 64 x 64
-// (0.53 us for 2 blocks) pay for the barrier and a chain of read, product and
-// sum each turn.
-template <typename OUT, int TN, int TM, int WN, int WM, int KG, int ST, int C>
+// What bounds it.  A wave issues its instructions one by one, and address
+// arithmetic beside the products counts in full: with descriptor, row group and
+// bounds of each load known when it is compiled or once a turn, a turn of a 128 x 128
+// tile went from 158 instructions to 103, and times fell by 3 to 12 % at all
+// sizes, 4096 x 4096 x 8192 from 122 to 114 us.  Large tiles, 16384 x 5120 x 13824
+// (counters): the matrix cores are busy for 2097 of a turn's cycles at 1.8 GHz,
+// to which the power limit brings the clock (2.4 without load); the four FMAs
+// beside each product let it take 37 cycles for 32.  Smaller ones: loads alone,
+// without products, take the same time while there are two stages (tiles of 128 x 128 of
+// two groups, 49 us for 1.5 GB of loads by way of L2 at 700 x 4096 x 8192; 36 if all
+// hit in L2), hence four stages (42; loads reach 120 bytes a ns and CU with 32 KB
+// under way, where all hit).  Measured without gain: loads all at once behind the
+// barrier, or two or four behind a product; waves that only load (0.6 to 1.08 of
+// the speed); lines touched a turn or more ahead; bands of 4 or 16 token tiles; wave priorities.
+template <typename OUT, int TN, int TM, int WN, int WM, int KG, int ST, int C, bool AHEAD>
 __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(ProductParams p) {
   constexpr int NW = WN * WM * KG, AN = TN / WN / 16, BM = TM / WM / 16, kSteps = AN * BM;  // fragments of a wave
-  constexpr int kRows = TN + TM, kStage = kRows * kBlock * KG, kLoads = kRows * KG / 8 / NW, kPer = kLoads + 1;
+  constexpr int kRows = TN + TM, kStage = kRows * kBlock * KG, kLoads = kRows * KG / 8 / NW;
   constexpr int kStepLoads = (kLoads + kSteps - 1) / kSteps;  // behind each product
-  // the scales of C blocks lie in LDS at a time, twice: x's [TM][C], W's [TN / 128][C]; 64 floats a load, one load a
-  // wave and turn
+  constexpr int kStepReads = (AN + BM + kSteps * 3 / 4 - 1) / (kSteps * 3 / 4);  // (AHEAD) so that the last are early
+  // the scales of C blocks lie in LDS at a time, twice: x's [TM][C], W's [TN / 128][C]; 64 floats a load
   constexpr int kParts = TM * C / 64, kChunk = (kParts + 1) * 256, kChunkTurns = C / KG;
   static_assert(kRows * KG % (8 * NW) == 0 && TN % 16 == 0 && TM * C % 64 == 0 && kRows % 16 == 0, "whole loads");
   static_assert((TN + kBlock - 1) / kBlock * C <= 64 && C % KG == 0, "one load of W's scales");
-  static_assert(kParts / NW <= kChunkTurns - ST, "the next scales are there in time");
+  // (they are older than ST - 2 stages' loads when they are read, so that no barrier need count them)
+  static_assert(kChunkTurns >= ST && kChunkTurns % 2 == 0, "the next scales are there in time");
   static_assert(kBlock % (TN / WN) == 0, "a wave's outputs lie in one scale block");
   static_assert(AN >= 2 && kSteps % 4 == 0, "operands and products in turn");
   static_assert(KG == 1 || KG * TN * TM * 4 <= ST * kStage, "the groups' sums fit the stages");
@@ -197,51 +207,64 @@ __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(Prod
   const __amdgpu_buffer_rsrc_t rs = make_rsrc(p.xs + (int64_t)m0 * p.kb, (int64_t)(p.M - m0) * p.kb * 4);
   const int nb0 = n0 / kBlock, nb_last = (p.N - 1) / kBlock;
   const __amdgpu_buffer_rsrc_t rv = make_rsrc(p.ws + (int64_t)nb0 * p.kb, (int64_t)(nb_last + 1 - nb0) * p.kb * 4);
-  // Rows past the matrix repeat its last one (their results are not stored), blocks past the last one the last (their
-  // factor is 0), pieces past the row's end the block's first (the fragments there are cleared).  A lane's piece is the
-  // same in every load.
-  const int piece = (lane & 7) ^ ((wave * 8 + (lane >> 3)) >> 1 & 7), back = 16 * piece >= tail ? 16 * piece : 0;
+  // Rows past the matrix repeat its last one (their results are not stored).  The last block is read as the row's last
+  // 128 bytes, and blocks past it too; what of those belongs to the block before is cleared in the fragments (of a row
+  // shorter than a block: the pieces past its end, which repeat its last one).  A lane's piece is the same in every load.
+  constexpr int kSpan = 8 * NW, kWLoads = KG * TN / kSpan;  // rows of a load of all waves; loads of W
+  static_assert(KG * TN % kSpan == 0 && KG * TM % kSpan == 0 && (TN % kSpan == 0 || kSpan % TN == 0) &&
+                (TM % kSpan == 0 || kSpan % TM == 0), "a load is of W or of x, of whole groups or of one");
+  const int piece = (lane & 7) ^ ((wave * 8 + (lane >> 3)) >> 1 & 7);
+  const int last_at = max(p.K - kBlock, 0);
   uint32_t off[kLoads];
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
-    const int r = ((i * NW + wave) * 8 + (lane >> 3)) % kRows;  // row of the group's part: W's TN, then x's TM
-    const int row = r < TN ? min(r, p.N - 1 - n0) : min(r - TN, p.M - 1 - m0);
-    off[i] = (uint32_t)row * (uint32_t)p.K + 16 * piece;
+    const bool is_w = i < kWLoads;
+    const int r = ((is_w ? i : i - kWLoads) * kSpan + wave * 8 + (lane >> 3)) % (is_w ? TN : TM);
+    off[i] = (uint32_t)min(r, (is_w ? p.N - n0 : p.M - m0) - 1) * (uint32_t)p.K + min(16 * piece, p.K - 16);
   }
-  auto load = [&](int turn, int st, int i) {
-    const int at = (i * NW + wave) * 8, kb = min(turn * KG + at / kRows, last);
-    buffer_to_lds<16>(at % kRows < TN ? rw : rx, off[i] - (back & -(int)(kb == last)), kb * kBlock,
-                      lds + st * kStage + at * kBlock);
+  uint8_t* const lds_w = lds + wave * 1024;
+  auto load = [&](int turn, int at, int i) {  // into the stage `at` bytes from the first
+    const bool is_w = i < kWLoads;
+    const int k = is_w ? i : i - kWLoads, T = is_w ? TN : TM;
+    const int group = T % kSpan == 0 ? k * kSpan / T : k * (kSpan / T) + wave * 8 / T;
+    buffer_to_lds<16>(is_w ? rw : rx, off[i], min((turn * KG + group) * kBlock, last_at), lds_w + at + i * (kSpan * kBlock));
   };
-  // Part `part` of the scales of blocks C c .. C c + C - 1: x's, then W's; past those, into no one's place
-  auto load_scales = [&](int c, int part) {
-    const bool is_w = part >= kParts;
-    const int row = is_w ? min(lane / C, nb_last - nb0) : min(part * (64 / C) + lane / C, p.M - 1 - m0);
-    const int k = min(C * c + lane % C, last);
-    buffer_to_lds<4>(is_w ? rv : rs, (uint32_t)(row * p.kb + k) * 4, 0,
-                     part <= kParts ? lds_s + (c & 1) * kChunk + part * 256 : lds_s + 2 * kChunk);
+  // The scales of blocks C c .. C c + C - 1, in parts of 64: x's, then W's; past those, into no one's place
+  auto load_scales = [&](int c) {
+#pragma unroll
+    for (int i = 0; i <= kParts / NW; ++i) {
+      const int part = i * NW + wave, k = min(C * c + lane % C, last);
+      const bool is_w = part >= kParts;
+      const int row = is_w ? min(lane / C, nb_last - nb0) : min(part * (64 / C) + lane / C, p.M - 1 - m0);
+      buffer_to_lds<4>(is_w ? rv : rs, (uint32_t)(row * p.kb + k) * 4, 0,
+                       part <= kParts ? lds_s + (c & 1) * kChunk + part * 256 : lds_s + 2 * kChunk);
+    }
   };
 
   f32x4 acc[AN][BM] = {};
   const int q = lane >> 4, f = (lane >> 1) & 7;
   const int lo = (lane & 15) * kBlock + ((q ^ f) << 4), hi = lo ^ 64;  // pieces q and q + 4
-  const int a_at = (g * kRows + wn * (TN / WN)) * kBlock, b_at = (g * kRows + TN + wm * (TM / WM)) * kBlock;
+  const int a_at = (g * TN + wn * (TN / WN)) * kBlock, b_at = (KG * TN + g * TM + wm * (TM / WM)) * kBlock;
   const int s_at = (wm * (TM / WM) + (lane & 15)) * C + g, w_at = TM * C + wn * (TN / WN) / kBlock * C + g;
   auto fragment = [&](int at) {
     const i32x4 u = *reinterpret_cast<const i32x4*>(lds + at + lo), v = *reinterpret_cast<const i32x4*>(lds + at + hi);
     return __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
   };
-  i32x8 a[2], b[BM];
   f32x4 t[4];          // the last products, which enter the sums three products later
   float s[BM], s_new[BM], w_new;
-  auto scales = [&](int turn) {
-    const float* ss = reinterpret_cast<const float*>(lds_s + (turn / kChunkTurns & 1) * kChunk) + turn % kChunkTurns * KG;
+  auto scales = [&](int at) {
+    const float* ss = reinterpret_cast<const float*>(lds_s + at);
 #pragma unroll
     for (int j = 0; j < BM; ++j) s_new[j] = ss[s_at + j * 16 * C];
     w_new = ss[w_at];
   };
-  const bool mine = last_turn * KG + g <= last, cut_here = last_turn * KG + g == last;  // in the last turn
-  const bool no_lo = cut_here & (16 * q >= tail), no_hi = cut_here & (16 * q + 64 >= tail);
+  auto next_scales = [&](int turn, int at) {  // where the scales of the turn after `turn` lie; at: its own
+    return (turn + 1) % kChunkTurns == 0 ? (at >= kChunk ? 0 : kChunk) : at + KG * 4;
+  };
+  // in the last turn
+  const bool mine = last_turn * KG + g <= last, cut_here = last_turn * KG + g == last, one = p.K < kBlock;
+  const bool no_lo = cut_here & (one ? 16 * q >= tail : 16 * q < kBlock - tail);
+  const bool no_hi = cut_here & (one ? 16 * q + 64 >= tail : 16 * q + 64 < kBlock - tail);
   auto cut = [&](i32x8 v) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -250,74 +273,155 @@ __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(Prod
     }
     return v;
   };
-  // The products of a turn, whose b and a[0] are there; MORE: with the reads of the next turn's, else it is the last
-  auto block = [&](int turn, int st, int st_next, auto more) {
-    constexpr bool MORE = decltype(more)::value;
-    if (!MORE) {
-      a[0] = cut(a[0]);
+  if constexpr (AHEAD) {
+    i32x8 a[2][AN], b[2][BM];
+    // The products of a turn, whose operands are in a[P] and b[P]; MORE: with the reads of the next turn's
+    auto block = [&](int turn, int st, int st_next, int ss_next, auto more, auto parity) {
+      constexpr bool MORE = decltype(more)::value;
+      constexpr int P = decltype(parity)::value;
+      // this wave's reads of the turn's stage are done, all waves' and the loads of the next
+      wait_loads_and_barrier<(ST - 2) * kLoads>();
 #pragma unroll
-      for (int j = 0; j < BM; ++j) b[j] = cut(b[j]);
-    }
+      for (int i = 0; i < AN; ++i) asm volatile("" : "+v"(a[P][i]));
 #pragma unroll
-    for (int i = 0; i < AN; ++i) {
-      if (i + 1 < AN) {
-        const i32x8 v = fragment(st * kStage + a_at + (i + 1) * 16 * kBlock);
-        a[(i + 1) & 1] = MORE ? v : cut(v);
-      }
-      if (MORE && i == AN - 1) {
-        // all waves' loads of the next turn and reads of this one are done
-        wait_loads_and_barrier<(ST - 2) * kPer>();
-        load_scales(turn / kChunkTurns + 1, turn % kChunkTurns * NW + wave);
-        a[AN & 1] = fragment(st_next * kStage + a_at);
+      for (int j = 0; j < BM; ++j) asm volatile("" : "+v"(b[P][j]));
+      if (!MORE) {
+#pragma unroll
+        for (int i = 0; i < AN; ++i) a[P][i] = cut(a[P][i]);
+#pragma unroll
+        for (int j = 0; j < BM; ++j) b[P][j] = cut(b[P][j]);
       }
 #pragma unroll
-      for (int j = 0; j < BM; ++j) {
-        const int n = i * BM + j, d = (n + kSteps - 3) % kSteps;  // the product made, and the one added (n < 3: the turn before's)
-        t[n & 3] = mfma(a[i & 1], b[j]);
+      for (int n = 0; n < kSteps; ++n) {
+        const int i = n / BM, j = n % BM, d = (n + kSteps - 3) % kSteps;
+        t[n & 3] = mfma(a[P][i], b[P][j]);
         add(acc[d / BM][d % BM], t[(n + 1) & 3], s[d % BM]);
         if (n == 2) {
 #pragma unroll
           for (int k = 0; k < BM; ++k) s[k] = MORE || mine ? s_new[k] * w_new : 0.0f;
+          if (MORE) scales(ss_next);
         }
-        if (MORE && i == AN - 1) b[j] = fragment(st_next * kStage + b_at + j * 16 * kBlock);
-        if (MORE && n == kSteps - 1) scales(turn + 1);
-        // into this turn's place, the loads of turn + ST from the barrier on
         if (MORE) {
 #pragma unroll
-          for (int k = 0; k < kStepLoads; ++k) {
-            const int at = ((n + BM) % kSteps) * kStepLoads + k;
-            if (at < kLoads) i == AN - 1 ? load(turn + ST, st, at) : load(turn + ST - 1, st == 0 ? ST - 1 : st - 1, at);
+          for (int k = 0; k < kStepReads; ++k) {
+            const int f = n * kStepReads + k;
+            if (f < BM) b[P ^ 1][f] = fragment(st_next + b_at + f * 16 * kBlock);
+            else if (f < BM + AN) a[P ^ 1][f - BM] = fragment(st_next + a_at + (f - BM) * 16 * kBlock);
           }
+#pragma unroll
+          for (int k = 0; k < kStepLoads; ++k)
+            if (n * kStepLoads + k < kLoads) load(turn + ST, st, n * kStepLoads + k);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
+    };
+    load_scales(0);
+#pragma unroll
+    for (int k = 0; k < ST; ++k)
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) load(k, k * kStage, i);
+    wait_loads_and_barrier<(ST - 1) * kLoads>();
+#pragma unroll
+    for (int i = 0; i < AN; ++i) a[0][i] = fragment(a_at + i * 16 * kBlock);
+#pragma unroll
+    for (int j = 0; j < BM; ++j) b[0][j] = fragment(b_at + j * 16 * kBlock);
+    scales(0);
+#pragma unroll
+    for (int j = 0; j < BM; ++j) s[j] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = f32x4{};
+    int st = 0, ss = 0, turn = 0;
+    auto next = [&](int k) { return k == (ST - 1) * kStage ? 0 : k + kStage; };
+    while (turn + 2 <= last_turn) {
+      load_scales(turn / kChunkTurns + 1);
+      for (const int end = min(last_turn, turn + kChunkTurns); turn + 2 <= end; turn += 2) {
+        const int s1 = next(st), s2 = next(s1), ss1 = ss + KG * 4, ss2 = next_scales(turn + 1, ss1);
+        block(turn, st, s1, ss1, std::true_type{}, std::integral_constant<int, 0>{});
+        block(turn + 1, s1, s2, ss2, std::true_type{}, std::integral_constant<int, 1>{});
+        st = s2;
+        ss = ss2;
+      }
     }
-    if (AN & 1) a[0] = a[1];
-  };
+    if (turn < last_turn) {
+      block(turn, st, next(st), ss + KG * 4, std::true_type{}, std::integral_constant<int, 0>{});
+      block(last_turn, next(st), 0, 0, std::false_type{}, std::integral_constant<int, 1>{});
+    } else {
+      block(last_turn, st, 0, 0, std::false_type{}, std::integral_constant<int, 0>{});
+    }
+  } else {
+    i32x8 a[2], b[BM];
+    // The products of a turn, whose b and a[0] are there; MORE: with the reads of the next turn's, else it is the last
+    auto block = [&](int turn, int st_prev, int st, int st_next, int ss_next, auto more) {
+      constexpr bool MORE = decltype(more)::value;
+      if (!MORE) {
+        a[0] = cut(a[0]);
 #pragma unroll
-  for (int k = 0; k < ST - 1; ++k) {
+        for (int j = 0; j < BM; ++j) b[j] = cut(b[j]);
+      }
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load(k, k, i);
+      for (int i = 0; i < AN; ++i) {
+        if (MORE && i == AN - 1) {
+          // all waves' loads of the next turn and reads of this one are done
+          wait_loads_and_barrier<(ST - 2) * kLoads>();
+          a[AN & 1] = fragment(st_next + a_at);
+        }
+#pragma unroll
+        for (int j = 0; j < BM; ++j) {
+          const int n = i * BM + j, d = (n + kSteps - 3) % kSteps;  // the product made, and the one added (n < 3: the turn before's)
+          t[n & 3] = mfma(a[i & 1], b[j]);
+          if (j == 0 && i + 1 < AN) {
+            const i32x8 v = fragment(st + a_at + (i + 1) * 16 * kBlock);
+            a[(i + 1) & 1] = MORE ? v : cut(v);
+          }
+          add(acc[d / BM][d % BM], t[(n + 1) & 3], s[d % BM]);
+          if (n == 2) {
+#pragma unroll
+            for (int k = 0; k < BM; ++k) s[k] = MORE || mine ? s_new[k] * w_new : 0.0f;
+          }
+          if (MORE && i == AN - 1) b[j] = fragment(st_next + b_at + j * 16 * kBlock);
+          if (MORE && n == kSteps - 1) scales(ss_next);
+          // into this turn's place, the loads of turn + ST from the barrier on
+          if (MORE) {
+#pragma unroll
+            for (int k = 0; k < kStepLoads; ++k) {
+              const int at = ((n + BM) % kSteps) * kStepLoads + k;
+              if (at < kLoads) i == AN - 1 ? load(turn + ST, st, at) : load(turn + ST - 1, st_prev, at);
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      if (AN & 1) a[0] = a[1];
+    };
+    load_scales(0);
+#pragma unroll
+    for (int k = 0; k < ST - 1; ++k)
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) load(k, k * kStage, i);
+    wait_loads_and_barrier<(ST - 2) * kLoads>();
+#pragma unroll
+    for (int i = 0; i < (BM * kStepLoads < kLoads ? BM * kStepLoads : kLoads); ++i) load(ST - 1, (ST - 1) * kStage, i);
+    a[0] = fragment(a_at);
+#pragma unroll
+    for (int j = 0; j < BM; ++j) b[j] = fragment(b_at + j * 16 * kBlock);
+    scales(0);
+#pragma unroll
+    for (int j = 0; j < BM; ++j) s[j] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = f32x4{};
+    int st_prev = (ST - 1) * kStage, st = 0, ss = 0;
+    for (int turn = 0; turn < last_turn;) {
+      load_scales(turn / kChunkTurns + 1);
+      for (const int end = min(last_turn, turn + kChunkTurns); turn < end; ++turn) {
+        const int st_next = st == (ST - 1) * kStage ? 0 : st + kStage;
+        ss = next_scales(turn, ss);
+        block(turn, st_prev, st, st_next, ss, std::true_type{});
+        st_prev = st;
+        st = st_next;
+      }
+    }
+    block(last_turn, st_prev, st, 0, 0, std::false_type{});
   }
-  for (int part = wave; part <= kParts; part += NW) load_scales(0, part);
-  wait_loads_and_barrier<0>();
-#pragma unroll
-  for (int i = 0; i < (BM * kStepLoads < kLoads ? BM * kStepLoads : kLoads); ++i) load(ST - 1, ST - 1, i);
-  a[0] = fragment(a_at);
-#pragma unroll
-  for (int j = 0; j < BM; ++j) b[j] = fragment(b_at + j * 16 * kBlock);
-  scales(0);
-#pragma unroll
-  for (int j = 0; j < BM; ++j) s[j] = 0.0f;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) t[e] = f32x4{};
-  int st = 0;
-  for (int turn = 0; turn < last_turn; ++turn) {
-    const int st_next = st + 1 == ST ? 0 : st + 1;
-    block(turn, st, st_next, std::true_type{});
-    st = st_next;
-  }
-  block(last_turn, st, 0, std::false_type{});
 #pragma unroll
   for (int e = 0; e < 3; ++e) add(acc[(kSteps - 3 + e) / BM][(kSteps - 3 + e) % BM], t[(kSteps - 3 + e) & 3], s[(kSteps - 3 + e) % BM]);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (loads past the last turn are still under way into LDS)
@@ -448,36 +552,34 @@ hipError_t launch_rows(ProductParams p, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename OUT, int TN, int TM, int WN, int WM, int KG, int ST, int C>
+template <typename OUT, int TN, int TM, int WN, int WM, int KG, int ST, int C, bool AHEAD>
 hipError_t launch_tiles(ProductParams p, hipStream_t s) {
   p.n_ntiles = (p.N + TN - 1) / TN;
   p.n_mtiles = (p.M + TM - 1) / TM;
-  hipLaunchKernelGGL((product_tile_kernel<OUT, TN, TM, WN, WM, KG, ST, C>), dim3((unsigned)(p.n_ntiles * (int64_t)p.n_mtiles)),
+  hipLaunchKernelGGL((product_tile_kernel<OUT, TN, TM, WN, WM, KG, ST, C, AHEAD>), dim3((unsigned)(p.n_ntiles * (int64_t)p.n_mtiles)),
                      dim3(64 * WN * WM * KG), 0, s, p);
   return hipGetLastError();
 }
 
 // The tilings and what they take: `turn` us for KG scale blocks of every tile
-// of a round (per_cu tiles a CU), `round` us beside them: fits to the times of
-// 60 sizes (M 24 .. 4096; N x K 4096 x 4096, 24576 x 4096, 5120 x 13824, 1024 x 5120,
+// of a round (a tile a CU), `round` us beside them: fits to the times of 60
+// sizes (M 24 .. 4096; N x K 4096 x 4096, 24576 x 4096, 5120 x 13824, 1024 x 5120,
 // 2048 x 2048), at each of which but one they choose the fastest of the seven.
-// How far apart those are: 64 x 4096 x 4096 8.6 us by the first, 24.9 by the
-// sixth; 700 x 4096 x 4096 27.9 by the sixth, 51 by the last; 4096 x 4096 x 4096
-// 63.5 by the last, 82 by the fifth, 187 by the third.
+// How far apart those are: 64 x 4096 x 4096 8.4 us by the first, 18.5 by the
+// fifth; 700 x 4096 x 4096 20.5 by the fifth, 50 by the last; 1500 x 4096 x 4096 32.5
+// by the sixth, 51 by the last; 4096 x 4096 x 4096 60 by the last, 72 by the sixth, 173
+// by the third.
 template <typename OUT>
 struct Variant {
-  int tn, tm, kg, per_cu;
+  int tn, tm, kg;
   float turn, round;
   hipError_t (*launch)(ProductParams, hipStream_t);
 };
 constexpr int kCus = 256;
 template <typename OUT>
 float cost(const Variant<OUT>& v, const ProductParams& p) {
-  const int64_t tiles = (int64_t)((p.N + v.tn - 1) / v.tn) * ((p.M + v.tm - 1) / v.tm), slots = kCus * v.per_cu;
-  const int64_t rest = tiles % slots;
-  // a round of one tile a CU, where two fit, takes 0.78 of a full one
-  const float rounds = (float)(tiles / slots) + (rest == 0 ? 0.0f : rest > kCus || v.per_cu == 1 ? 1.0f : 0.78f);
-  return rounds * ((float)((p.kb + v.kg - 1) / v.kg) * v.turn + v.round);
+  const int64_t tiles = (int64_t)((p.N + v.tn - 1) / v.tn) * ((p.M + v.tm - 1) / v.tm);
+  return (float)((tiles + kCus - 1) / kCus) * ((float)((p.kb + v.kg - 1) / v.kg) * v.turn + v.round);
 }
 
 template <typename OUT>
@@ -486,13 +588,13 @@ hipError_t launch_product(const ProductParams& p, hipStream_t s) {
   // 5.8 us, 6.7 with 32), 32 from there on (8 x 5120 x 13824 20 us, 26 with 16)
   if (p.M <= 16) return p.N < 20 * kCus ? launch_rows<OUT, 1, 1, 8, 2>(p, s) : launch_rows<OUT, 2, 1, 8, 2>(p, s);
   static const Variant<OUT> variants[] = {
-      {32, 32, 8, 1, 1.237f, 1.79f, launch_tiles<OUT, 32, 32, 1, 1, 8, 2, 32>},
-      {64, 32, 4, 1, 0.713f, 2.94f, launch_tiles<OUT, 64, 32, 2, 1, 4, 3, 16>},
-      {64, 64, 2, 1, 0.531f, 3.41f, launch_tiles<OUT, 64, 64, 2, 2, 2, 4, 16>},
-      {128, 64, 2, 1, 0.793f, 3.53f, launch_tiles<OUT, 128, 64, 2, 2, 2, 3, 8>},
-      {128, 128, 1, 2, 1.179f, 0.96f, launch_tiles<OUT, 128, 128, 2, 2, 1, 2, 8>},
-      {128, 128, 2, 1, 1.429f, 3.12f, launch_tiles<OUT, 128, 128, 2, 2, 2, 2, 8>},
-      {256, 256, 1, 1, 1.526f, 5.30f, launch_tiles<OUT, 256, 256, 2, 4, 1, 2, 8>},
+      {32, 32, 8, 1.179f, 2.13f, launch_tiles<OUT, 32, 32, 1, 1, 8, 2, 32, false>},
+      {64, 32, 4, 0.680f, 2.42f, launch_tiles<OUT, 64, 32, 2, 1, 4, 3, 16, false>},
+      {64, 64, 2, 0.487f, 2.92f, launch_tiles<OUT, 64, 64, 2, 2, 2, 4, 16, false>},
+      {128, 64, 2, 0.756f, 2.59f, launch_tiles<OUT, 128, 64, 2, 2, 2, 3, 8, false>},
+      {128, 128, 1, 0.541f, 3.06f, launch_tiles<OUT, 128, 128, 2, 4, 1, 4, 8, true>},
+      {256, 128, 1, 0.878f, 4.04f, launch_tiles<OUT, 256, 128, 4, 2, 1, 3, 8, false>},
+      {256, 256, 1, 1.531f, 3.54f, launch_tiles<OUT, 256, 256, 2, 4, 1, 2, 8, false>},
   };
   const Variant<OUT>* best = variants;
   for (const Variant<OUT>& v : variants)

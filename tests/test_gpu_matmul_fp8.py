@@ -15,7 +15,10 @@ SHAPES = [(1, 1, 32), (1, 16, 128), (2, 130, 96), (7, 64, 160), (16, 256, 2080),
           (333, 520, 2080), (513, 1025, 160), (1, 4096, 4096), (40, 2048, 5120),
           # outputs in 32-row pieces, wider tiles, tiles of 256 x 256 (whole and cut ones)
           (13, 5200, 288), (64, 20000, 1056), (300, 3000, 2336), (900, 2100, 1184), (1300, 2050, 2080),
-          (1290, 6700, 96), (1100, 7937, 352), (1290, 6712, 352), (1500, 2056, 416)]
+          (1290, 6700, 96), (1100, 7937, 352), (1290, 6712, 352), (1500, 2056, 416),
+          # of 128 x 128 and 256 x 128: one turn, odd and even numbers of them, more than the scales held at a time
+          (650, 4101, 96), (700, 4096, 128), (641, 4104, 256), (700, 4096, 1024), (700, 4100, 1184), (760, 4100, 2336),
+          (1410, 4097, 64), (1520, 4100, 288), (1500, 4096, 1184), (1410, 4104, 2080)]
 
 
 def _integers(shape, seed):

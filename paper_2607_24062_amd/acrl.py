@@ -367,21 +367,27 @@ def acrl_quantize_fp8(x: torch.Tensor, scaling: int, rounding: int = ROUND_NEARE
     return q, scales
 
 
+def _room(t, dtype, numel: int, index: int, name: str):
+    if t.dtype is not dtype or t.get_device() != index or t.numel() < numel or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of %d elements or more on cuda:%d" % (name, dtype, numel, index))
+
+
 def _quantize_blocks(x, rows: int, cols: int, ld: int, scaling: int, rounding: int, q, scales, stream):
     """ROW128 and BLOCK128: outputs and stream as for acrl_matmul_fp8."""
-    index = x.get_device()
+    index, groups = x.get_device(), (cols + 127) // 128
     if index != torch.cuda.current_device() or (stream is not None and stream.device_index != index):
         raise ValueError("x is on %s, not on the current device or the stream's" % x.device)
-    shape = (rows if scaling == SCALE_ROW128 else (rows + 127) // 128, (cols + 127) // 128)
+    n = rows if scaling == SCALE_ROW128 else (rows + 127) // 128
     if q is None:
         q = _empty((rows, cols), torch.uint8, x.device, stream)
+    else:
+        _room(q, torch.uint8, rows * cols, index, "q")
     if scales is None:
-        scales = _empty(shape, torch.float32, x.device, stream)
-    for t, dtype, n, name in ((q, torch.uint8, rows * cols, "q"), (scales, torch.float32, shape[0] * shape[1], "scales")):
-        if t.dtype is not dtype or t.get_device() != index or t.numel() < n or not t.is_contiguous():
-            raise ValueError("%s must be a contiguous %s tensor of %d elements or more on %s" % (name, dtype, n, x.device))
+        scales = _empty((n, groups), torch.float32, x.device, stream)
+    else:
+        _room(scales, torch.float32, n * groups, index, "scales")
     _check(lib().acrl_quantize_fp8(x.data_ptr(), rows, cols, ld, scaling, rounding, q.data_ptr(), scales.data_ptr(),
-                                   None, 0, _raw_stream(stream)), "acrl_quantize_fp8")
+                                   None, 0, _raw_stream(stream, x.device)), "acrl_quantize_fp8")
     return q, scales
 
 
@@ -666,7 +672,7 @@ def acrl_matmul_fp8(xq, x_scales, wq, w_scales, out=None, out_dtype=torch.bfloat
                       _want(wq, torch.uint8, N * K, index, "wq"),
                       _want(w_scales, torch.float32, (N + 127) // 128 * kb, index, "w_scales"),
                       out.data_ptr(), ldy, _OUT_TYPES[out_dtype])
-    _check(lib().acrl_matmul_fp8(ctypes.byref(desc), _raw_stream(stream)), "acrl_matmul_fp8")
+    _check(lib().acrl_matmul_fp8(ctypes.byref(desc), _raw_stream(stream, xq.device)), "acrl_matmul_fp8")
     return out
 
 
@@ -692,7 +698,7 @@ def acrl_policy_loss(B: int, L: int, n_groups: int, mask, group_of_seq, logp_new
         _want(adv, f32, n if adv_per_token else B, index, "adv"), _want(weight, f32, n, index, "weight", True),
         1 if adv_per_token else 0, kl_estimator, aggregate, eps_low, eps_high, dual_clip, kl_coef, norm,
         _want(coef, f32, n, index, "coef"), loss.data_ptr(), stats.data_ptr(), ws.data_ptr() if nbytes else None, nbytes)
-    _check(lib().acrl_policy_loss(ctypes.byref(desc), _raw_stream(stream)), "acrl_policy_loss")
+    _check(lib().acrl_policy_loss(ctypes.byref(desc), _raw_stream(stream, dev)), "acrl_policy_loss")
     return coef, loss, stats
 
 
@@ -716,5 +722,5 @@ def acrl_preference_loss(B: int, L: int, mask, logp_new, chosen, rejected, logp_
         _want(rejected, torch.int32, P, index, "rejected"), _want(pair_weight, f32, P, index, "pair_weight", True),
         form, 1 if mean_logp else 0, beta, margin, label_smoothing, _want(coef, f32, n, index, "coef"),
         loss.data_ptr(), rewards.data_ptr(), ws.data_ptr() if nbytes else None, nbytes)
-    _check(lib().acrl_preference_loss(ctypes.byref(desc), _raw_stream(stream)), "acrl_preference_loss")
+    _check(lib().acrl_preference_loss(ctypes.byref(desc), _raw_stream(stream, dev)), "acrl_preference_loss")
     return coef, loss, rewards

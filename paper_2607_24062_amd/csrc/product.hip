@@ -165,18 +165,19 @@ __device__ __forceinline__ void tile_of(const ProductParams& p, int block, int& 
 //
 // What bounds it.  A wave issues its instructions one by one, and address
 // arithmetic beside the products counts in full: with descriptor, row group and
-// bounds of each load known when it is compiled or once a turn, a turn of a 128 x 128
-// tile went from 158 instructions to 103, and times fell by 3 to 12 % at all
-// sizes, 4096 x 4096 x 8192 from 122 to 114 us.  Large tiles, 16384 x 5120 x 13824
-// (counters): the matrix cores are busy for 2097 of a turn's cycles at 1.8 GHz,
+// bounds of each load known when it is compiled or once a turn, a turn of a
+// 128 x 128 tile went from 158 instructions to 103, and times fell by 3 to 12 % at
+// nearly all sizes.  Large tiles (16384 x 5120 x 13824, 960 us, 2420 TFLOP/s,
+// counters): the matrix cores are busy for 2048 of a turn's 3250 cycles, at 1.83 GHz,
 // to which the power limit brings the clock (2.4 without load); the four FMAs
 // beside each product let it take 37 cycles for 32.  Smaller ones: loads alone,
-// without products, take the same time while there are two stages (tiles of 128 x 128 of
-// two groups, 49 us for 1.5 GB of loads by way of L2 at 700 x 4096 x 8192; 36 if all
-// hit in L2), hence four stages (42; loads reach 120 bytes a ns and CU with 32 KB
-// under way, where all hit).  Measured without gain: loads all at once behind the
-// barrier, or two or four behind a product; waves that only load (0.6 to 1.08 of
-// the speed); lines touched a turn or more ahead; bands of 4 or 16 token tiles; wave priorities.
+// without products, take the same time while there are two stages (128 x 128
+// tiles of two groups, 49 us for 0.4 GB by way of L2 at 700 x 4096 x 8192; 36 if
+// all hit there), hence four stages (42; where all hit, loads reach 120 bytes a ns
+// and CU with 32 KB under way).  Measured without gain: loads all at once behind
+// the barrier, or two or four behind a product; waves that only load (0.6 to
+// 1.08 of the speed); lines touched a turn or more ahead; bands of 4 or 16 token
+// tiles; wave priorities.
 template <typename OUT, int TN, int TM, int WN, int WM, int KG, int ST, int C, bool AHEAD>
 __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(ProductParams p) {
   constexpr int NW = WN * WM * KG, AN = TN / WN / 16, BM = TM / WM / 16, kSteps = AN * BM;  // fragments of a wave

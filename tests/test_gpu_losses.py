@@ -346,6 +346,58 @@ def test_preference_unaligned():
     np.testing.assert_allclose(down(a[1]), down(b[1]), rtol=1e-12)
 
 
+def test_more_slots_than_31_bits():
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    B, L = 140000, 16384
+    mask = torch.zeros((B, L), dtype=torch.uint8, device=dev)
+    mask[:, :3] = 1
+    new, old = torch.zeros((B, L), device=dev), torch.zeros((B, L), device=dev)
+    new[-1, 1] = 0.125
+    groups, adv = torch.zeros(B, dtype=torch.int32, device=dev), torch.ones(B, device=dev)
+    coef, loss, stats = acrl.acrl_policy_loss(B, L, 1, mask, groups, new, old, adv, False, aggregate=acrl.AGG_TOKEN)
+    n, c = 3 * B, coef.view(B, L)
+    assert float(stats[5]) == n and abs(float(loss) + (n - 1 + np.exp(0.125)) / n) <= 1e-12
+    want = np.array([-1 / n, -np.exp(0.125) / n, -1 / n, 0])
+    assert (np.abs(down(c[-1, :4]) - want) <= HALF32 * np.abs(want)).all() and not c[:, 3:].any()
+    pair = lambda *i: torch.tensor(i, dtype=torch.int32, device=dev)
+    coef, loss, rewards = acrl.acrl_preference_loss(B, L, mask, new, pair(B - 1, 0), pair(0, B - 2), beta=0.5)
+    up1, up0 = 1 / (1 + np.exp(0.0625)), 0.5  # sigmoid(-h) of the two pairs
+    want = np.array([-up1, up0, up1 - up0]) * 0.25  # (response 0: rejected in the first pair, preferred in the second)
+    got = down(coef.view(B, L)[[B - 1, B - 2, 0], 0])
+    assert (np.abs(got - want) <= HALF32 * np.abs(want) + 1e-15).all()
+
+
+# ------------------------------------------------------------------ refusals
+def test_refusals():
+    # tensors that do not fit B, L and the number of pairs are refused before anything is launched
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    B, L = 3, 2000
+    n = B * L
+    m, lp = torch.ones(n, dtype=torch.uint8, device=dev), torch.zeros(n, device=dev)
+    i = torch.zeros(B, dtype=torch.int32, device=dev)
+    ok = dict(mask=m, group_of_seq=i, logp_new=lp, logp_old=lp, adv=lp[:B], adv_per_token=False, logp_ref=lp, kl_coef=0.1)
+    for bad in (dict(mask=m[1:]), dict(mask=m.bool()), dict(mask=m.cpu()), dict(mask=None), dict(group_of_seq=i[1:]),
+                dict(group_of_seq=i.long()), dict(logp_new=lp[1:]), dict(logp_new=lp.double()), dict(logp_old=None),
+                dict(logp_old=lp.view(L, B).t()), dict(adv=lp), dict(adv_per_token=True), dict(logp_ref=lp.half()),
+                dict(weight=lp[:B]), dict(coef=lp[:5]), dict(coef=lp.double())):
+        with pytest.raises(ValueError):
+            acrl.acrl_policy_loss(B, L, 1, **{**ok, **bad})
+    for bad in (dict(eps_low=1.0), dict(kl_coef=-1.0), dict(logp_ref=None), dict(dual_clip=0.9), dict(aggregate=7),
+                dict(group_of_seq=None)):
+        with pytest.raises(acrl.AcrlError):
+            acrl.acrl_policy_loss(B, L, 1, **{**ok, **bad})
+    ok = dict(mask=m, logp_new=lp, chosen=i, rejected=i, logp_ref=lp)
+    for bad in (dict(mask=m[1:]), dict(logp_new=lp[1:]), dict(chosen=i[1:]), dict(chosen=i.long()), dict(rejected=None),
+                dict(rejected=i.cpu()), dict(pair_weight=lp[:2]), dict(logp_ref=lp[:B]), dict(coef=lp[:5])):
+        with pytest.raises(ValueError):
+            acrl.acrl_preference_loss(B, L, **{**ok, **bad})
+    for bad in (dict(beta=0.0), dict(label_smoothing=1.0), dict(form=1, label_smoothing=0.1), dict(form=3)):
+        with pytest.raises(acrl.AcrlError):
+            acrl.acrl_preference_loss(B, L, **{**ok, **bad})
+
+
 # ------------------------------------------------------------------ streams and graphs
 def _both(B, L, t, stream=None):
     from paper_2607_24062_amd import acrl

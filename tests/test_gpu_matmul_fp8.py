@@ -136,6 +136,30 @@ def test_subnormal_codes_and_large_scales(M):
     assert np.array_equal(down(y), product(xq, xs, wq, ws)[0].astype(np.float32))
 
 
+@pytest.mark.parametrize("M,N,K", [(20, 64, 1 << 22), (300, 520, 1 << 21), ((1 << 20) + 3, 40, 4128), (70000, 40000, 128)])
+def test_long_rows_and_offsets_past_32_bits(M, N, K):
+    # codes 0 and 1, scales 1: the sums are counts
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    r, kb = torch.Generator(device=dev).manual_seed(K + M), -(-K // 128)
+
+    def ones(rows):
+        x = torch.empty((rows, K), dtype=torch.uint8, device=dev)
+        step = max(1, (1 << 27) // K)
+        for a in range(0, rows, step):
+            x[a:a + step] = (torch.rand(x[a:a + step].shape, device=dev, generator=r) < 1 / 16).to(torch.uint8) * 0x38
+        return x
+
+    x, w = ones(M), ones(N)
+    y = acrl.acrl_matmul_fp8(x, torch.ones((M, kb), device=dev), w, torch.ones((-(-N // 128), kb), device=dev),
+                             out_dtype=torch.float32)
+    rows = torch.tensor([0, 1, M // 2, M - 2, M - 1], device=dev)
+    want = torch.zeros((5, N), device=dev)
+    for a in range(0, K, 1 << 18):
+        want += (x[rows, a:a + (1 << 18)] != 0).float() @ (w[:, a:a + (1 << 18)] != 0).float().t()
+    assert torch.equal(y[rows], want)
+
+
 def test_refusals():
     torch, dev = torch_dev()
     from paper_2607_24062_amd import acrl

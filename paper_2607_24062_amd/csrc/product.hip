@@ -167,17 +167,17 @@ __device__ __forceinline__ void tile_of(const ProductParams& p, int block, int& 
 // arithmetic beside the products counts in full: with descriptor, row group and
 // bounds of each load known when it is compiled or once a turn, a turn of a
 // 128 x 128 tile went from 158 instructions to 103, and times fell by 3 to 12 % at
-// nearly all sizes.  Large tiles (16384 x 5120 x 13824, 960 us, 2420 TFLOP/s,
-// counters): the matrix cores are busy for 2048 of a turn's 3250 cycles, at 1.83 GHz,
+// nearly all sizes.  Large tiles (16384 x 5120 x 13824, 946 to 960 us, 2420
+// TFLOP/s, counters): the matrix cores are busy for 2048 of a turn's 3250 cycles, at 1.83 GHz,
 // to which the power limit brings the clock (2.4 without load); the four FMAs
 // beside each product let it take 37 cycles for 32.  Smaller ones: loads alone,
 // without products, take the same time while there are two stages (128 x 128
 // tiles of two groups, 49 us for 0.4 GB by way of L2 at 700 x 4096 x 8192; 36 if
 // all hit there), hence four stages (42; where all hit, loads reach 120 bytes a ns
-// and CU with 32 KB under way).  Measured without gain: loads all at once behind
-// the barrier, or two or four behind a product; waves that only load (0.6 to
-// 1.08 of the speed); lines touched a turn or more ahead; bands of 4 or 16 token
-// tiles; wave priorities.
+// and CU with 32 KB under way).  Measured without gain (946 us): two or four loads
+// behind a product (975, 980; a wave waits while the address unit is taken), one
+// behind every second (946); waves that only load (0.6 to 1.08 of the speed);
+// lines touched a turn or more ahead; bands of 4 or 16 token tiles; priorities.
 template <typename OUT, int TN, int TM, int WN, int WM, int KG, int ST, int C, bool AHEAD>
 __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(ProductParams p) {
   constexpr int NW = WN * WM * KG, AN = TN / WN / 16, BM = TM / WM / 16, kSteps = AN * BM;  // fragments of a wave

@@ -531,6 +531,11 @@ acrl_status acrl_lm_head_backward(const acrl_backward_desc* desc, void* stream);
  * them: a fp32 y of normally distributed operands is within 2e-5 of the exact
  * sum, relative to its size, not within fp32's half step.)  A scale or code
  * that is NaN makes the sums it enters NaN.
+ * The factor x_scales w_scales of a block is formed first and rounded to fp32.
+ * Either scale may have any size while their product lies in fp32's normal
+ * range.  Where it does not, y is that of the rounded factor: above 3.4e38 it is
+ * infinite (a block's sum of 0 times it is NaN), below 1.2e-38 it is subnormal,
+ * down to steps of 1.4e-45, and in the end 0.
  *   xq        e4m3 [M, K], x_scales float [M, ceil(K/128)]: ACRL_SCALE_ROW128
  *   wq        e4m3 [N, K], w_scales float [ceil(N/128), ceil(K/128)]: ACRL_SCALE_BLOCK128
  *   y         [M, N] of y_type, rows ldy elements apart; columns from N on are

@@ -650,7 +650,8 @@ _OUT_TYPES = {torch.bfloat16: OUT_BF16, torch.float32: OUT_F32}
 def acrl_matmul_fp8(xq, x_scales, wq, w_scales, out=None, out_dtype=torch.bfloat16, stream=None):
     """y = x W^T [M, N] of FP8 operands with one scale per 128 elements:
     xq uint8 [M, K] with SCALE_ROW128 scales, wq uint8 [N, K] with
-    SCALE_BLOCK128 scales (acrl_quantize_fp8).  `out` (bf16 or float32) may be
+    SCALE_BLOCK128 scales (acrl_quantize_fp8); a block's x_scale * w_scale is
+    rounded to float32 before its use.  `out` (bf16 or float32) may be
     a column slice of a wider matrix: unit column stride, any row stride, its
     first element 16-byte aligned."""
     if xq.dim() != 2 or wq.dim() != 2 or xq.shape[1] != wq.shape[1]:

@@ -7,7 +7,9 @@
 // a whole scale block; its result then enters the fp32 accumulators with one
 // FMA a value, whose factor x_scale w_scale is one number a lane: the token is
 // the lane's own and the weight's scale is the same for all 128 outputs of a
-// wave.
+// wave.  (Factors past fp32's normal range lose what lies past it: a second
+// multiplication by the other scale would stand beside every product, where the
+// FMAs already hold the matrix cores up.)
 #include <type_traits>
 
 #include "entry.h"

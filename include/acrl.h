@@ -529,7 +529,8 @@ acrl_status acrl_lm_head_backward(const acrl_backward_desc* desc, void* stream);
  * by fp32 roundings of the sum).  y is rounded once, to bf16 or fp32.  (The
  * matrix instruction aligns a block's products to the largest before it adds
  * them: a fp32 y of normally distributed operands is within 2e-5 of the exact
- * sum, relative to its size, not within fp32's half step.)  A scale or code
+ * sum, relative to its size, one of activations with a few columns ten times as
+ * large within 3e-5, not within fp32's half step.)  A scale or code
  * that is NaN makes the sums it enters NaN.
  * The factor x_scales w_scales of a block is formed first and rounded to fp32.
  * Either scale may have any size while their product lies in fp32's normal

@@ -221,3 +221,18 @@ def test_captured_and_replayed(M):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, step())
+
+
+@pytest.mark.parametrize("M,N,K", [(9, 520, 4096), (70, 300, 5120), (300, 260, 2080)])
+def test_columns_ten_times_as_large(M, N, K):
+    # the header's figure for activations with outlier channels, and the instruction's bound elementwise
+    torch, dev = torch_dev()
+    x = (random_bf16((M, K), K).astype(np.uint32) << 16).view(np.float32)
+    x[:, 7::61] *= 10
+    x = torch.from_numpy(x).to(torch.bfloat16).view(torch.int16).numpy().view(np.uint16)
+    xq, xs = quantize_blocks(x, 1)
+    wq, ws = quantize_blocks(random_bf16((N, K), K + 1, std=0.05), 128)
+    want, slack = product(xq, xs, wq, ws)
+    y = down(_run((xq, xs, wq, ws), out_dtype=torch.float32))
+    assert (np.abs(y - want) <= slack + 2.0 ** -24 * np.abs(want)).all(), (np.abs(y - want) / slack).max()
+    assert np.linalg.norm(y - want) <= 3e-5 * np.linalg.norm(want)

@@ -200,7 +200,8 @@ __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(Prod
   // (they are older than ST - 2 stages' loads when they are read, so that no barrier need count them)
   static_assert(kChunkTurns >= ST && kChunkTurns % 2 == 0, "the next scales are there in time");
   static_assert(kBlock % (TN / WN) == 0, "a wave's outputs lie in one scale block");
-  static_assert(AN >= 2 && kSteps % 4 == 0, "operands and products in turn");
+  // (rows of products take W's operand from two places in turn: an even number of them ends where it began)
+  static_assert(AN >= 2 && AN % 2 == 0 && kSteps % 4 == 0, "operands and products in turn");
   static_assert(KG == 1 || KG * TN * TM * 4 <= ST * kStage, "the groups' sums fit the stages");
   constexpr int kLds = ST * kStage + 2 * kChunk + 256;
   __shared__ __align__(1024) uint8_t lds[kLds];
@@ -373,7 +374,7 @@ __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(Prod
         if (MORE && i == AN - 1) {
           // all waves' loads of the next turn and reads of this one are done
           wait_loads_and_barrier<(ST - 2) * kLoads>();
-          a[AN & 1] = fragment(st_next + a_at);
+          a[0] = fragment(st_next + a_at);
         }
 #pragma unroll
         for (int j = 0; j < BM; ++j) {
@@ -401,7 +402,6 @@ __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(Prod
           __builtin_amdgcn_sched_barrier(0);
         }
       }
-      if (AN & 1) a[0] = a[1];
     };
     load_scales(0);
 #pragma unroll

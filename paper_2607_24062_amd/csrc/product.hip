@@ -467,35 +467,30 @@ __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(Prod
   }
 }
 
-// Few tokens: the weights' stream from HBM is the whole work, and a workgroup
-// takes 16 AN outputs x 16 BM tokens so that many of them share it out.  Its
-// NW waves take every NW-th scale block each, U of them at a time, straight
-// into registers: 16-byte pieces q and q + 4 of a row's 128 bytes for lane
-// group q, so that a load takes 64 contiguous bytes of each row (the products
-// of a block may be summed in any order of k, as long as both operands have
-// the same).  The waves' sums are added through LDS in their order.
-template <typename OUT, int AN, int BM, int NW, int U>
+// Up to 16 tokens: the weights' stream from HBM is the whole work, and a workgroup
+// takes 16 AN outputs so that many of them share it out.  Its NW waves take every
+// NW-th scale block each, U of them at a time, straight into registers: 16-byte
+// pieces q and q + 4 of a row's 128 bytes for lane group q, so that a load takes
+// 64 contiguous bytes of each row (the products of a block may be summed in any
+// order of k, as long as both operands have the same).  The waves' sums are added
+// through LDS in their order.
+template <typename OUT, int AN, int NW, int U>
 __global__ __launch_bounds__(64 * NW, 2) void product_rows_kernel(ProductParams p) {
-  __shared__ f32x4 red[NW][AN * BM][64];
+  __shared__ f32x4 red[NW][AN][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int mt = blockIdx.x % p.n_mtiles, nt = blockIdx.x / p.n_mtiles;
-  const int n0 = nt * 16 * AN, m0 = mt * 16 * BM, q = lane >> 4;
+  const int n0 = blockIdx.x * 16 * AN, q = lane >> 4;
   const int last = p.kb - 1, tail = p.K - last * kBlock;
-  const uint8_t *pw[AN], *px[BM];
-  const float* ps[BM];
+  const uint8_t* pw[AN];
 #pragma unroll
   for (int i = 0; i < AN; ++i) pw[i] = p.w + (int64_t)min(n0 + 16 * i + (lane & 15), p.N - 1) * p.K;
-#pragma unroll
-  for (int j = 0; j < BM; ++j) {
-    const int64_t m = min(m0 + 16 * j + (lane & 15), p.M - 1);
-    px[j] = p.x + m * p.K;
-    ps[j] = p.xs + m * p.kb;
-  }
+  const int64_t m = min(lane & 15, p.M - 1);
+  const uint8_t* const px = p.x + m * p.K;
+  const float* const ps = p.xs + m * p.kb;
   const float* const ws = p.ws + (int64_t)(n0 / kBlock) * p.kb;  // (16 AN divides 128)
-  f32x4 acc[AN][BM] = {};
+  f32x4 acc[AN] = {};
   for (int k0 = wave; k0 < p.kb; k0 += NW * U) {
-    i32x4 a[U][AN][2], b[U][BM][2];
-    float s[U][BM];
+    i32x4 a[U][AN][2], b[U][2];
+    float s[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       // blocks past the last repeat it, pieces past its end its first; neither is used
@@ -507,14 +502,9 @@ __global__ __launch_bounds__(64 * NW, 2) void product_rows_kernel(ProductParams 
         a[u][i][0] = *reinterpret_cast<const i32x4*>(pw[i] + o0);
         a[u][i][1] = *reinterpret_cast<const i32x4*>(pw[i] + o1);
       }
-#pragma unroll
-      for (int j = 0; j < BM; ++j) {
-        b[u][j][0] = *reinterpret_cast<const i32x4*>(px[j] + o0);
-        b[u][j][1] = *reinterpret_cast<const i32x4*>(px[j] + o1);
-        s[u][j] = ps[j][kb];
-      }
-#pragma unroll
-      for (int j = 0; j < BM; ++j) s[u][j] *= ws[kb];
+      b[u][0] = *reinterpret_cast<const i32x4*>(px + o0);
+      b[u][1] = *reinterpret_cast<const i32x4*>(px + o1);
+      s[u] = ps[kb] * ws[kb];
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -525,40 +515,26 @@ __global__ __launch_bounds__(64 * NW, 2) void product_rows_kernel(ProductParams 
         const i32x4 zero = {0, 0, 0, 0};
         return __builtin_shufflevector(no0 ? zero : h[0], no1 ? zero : h[1], 0, 1, 2, 3, 4, 5, 6, 7);
       };
-      i32x8 bf[BM];
+      const i32x8 bf = operand(b[u]);
 #pragma unroll
-      for (int j = 0; j < BM; ++j) bf[j] = operand(b[u][j]);
-#pragma unroll
-      for (int i = 0; i < AN; ++i) {
-        const i32x8 af = operand(a[u][i]);
-#pragma unroll
-        for (int j = 0; j < BM; ++j) {
-          const f32x4 t = mfma(af, bf[j]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(t[e], s[u][j], acc[i][j][e]);
-        }
-      }
+      for (int i = 0; i < AN; ++i) add(acc[i], mfma(operand(a[u][i]), bf), s[u]);
     }
   }
 #pragma unroll
-  for (int i = 0; i < AN; ++i)
-#pragma unroll
-    for (int j = 0; j < BM; ++j) red[wave][i * BM + j][lane] = acc[i][j];
+  for (int i = 0; i < AN; ++i) red[wave][i][lane] = acc[i];
   __syncthreads();
-  for (int t = wave; t < AN * BM; t += NW) {
+  for (int t = wave; t < AN; t += NW) {
     f32x4 v = red[0][t][lane];
 #pragma unroll
     for (int w = 1; w < NW; ++w) v += red[w][t][lane];
-    store4<OUT>(p, m0 + 16 * (t % BM) + (lane & 15), n0 + 16 * (t / BM) + 4 * q, v);
+    store4<OUT>(p, lane & 15, n0 + 16 * t + 4 * q, v);
   }
 }
 
-template <typename OUT, int AN, int BM, int NW, int U>
-hipError_t launch_rows(ProductParams p, hipStream_t s) {
-  p.n_ntiles = (p.N + 16 * AN - 1) / (16 * AN);
-  p.n_mtiles = (p.M + 16 * BM - 1) / (16 * BM);
-  hipLaunchKernelGGL((product_rows_kernel<OUT, AN, BM, NW, U>), dim3((unsigned)(p.n_ntiles * (int64_t)p.n_mtiles)),
-                     dim3(64 * NW), 0, s, p);
+template <typename OUT, int AN, int NW, int U>
+hipError_t launch_rows(const ProductParams& p, hipStream_t s) {
+  hipLaunchKernelGGL((product_rows_kernel<OUT, AN, NW, U>), dim3((unsigned)((p.N + 16 * AN - 1) / (16 * AN))), dim3(64 * NW),
+                     0, s, p);
   return hipGetLastError();
 }
 
@@ -596,7 +572,7 @@ template <typename OUT>
 hipError_t launch_product(const ProductParams& p, hipStream_t s) {
   // Up to 16 tokens: 16 outputs a workgroup while that is needed to have workgroups for the CUs (1 x 4096 x 4096
   // 5.8 us, 6.7 with 32), 32 from there on (8 x 5120 x 13824 20 us, 26 with 16)
-  if (p.M <= 16) return p.N < 20 * kCus ? launch_rows<OUT, 1, 1, 8, 2>(p, s) : launch_rows<OUT, 2, 1, 8, 2>(p, s);
+  if (p.M <= 16) return p.N < 20 * kCus ? launch_rows<OUT, 1, 8, 2>(p, s) : launch_rows<OUT, 2, 8, 2>(p, s);
   static const Variant<OUT> variants[] = {
       {32, 32, 8, 1.179f, 2.13f, launch_tiles<OUT, 32, 32, 1, 1, 8, 2, 32, false>},
       {64, 32, 4, 0.680f, 2.42f, launch_tiles<OUT, 64, 32, 2, 1, 4, 3, 16, false>},

@@ -588,10 +588,12 @@ acrl_status acrl_matmul_fp8(const acrl_matmul_desc* desc, void* stream);
  * outside [0, n_groups) enters neither loss nor stats and gets coef NaN.  All
  * is evaluated in fp64 from the fp32 inputs, sums by fixed trees.
  * stats (nullable): ACRL_PSTAT_*.
- * Requirements: B, L >= 0; for GROUP n_groups > 0 if B > 0 and group_of_seq
- * non-NULL (else both are not read); eps_low in [0, 1), eps_high >= 0;
- * dual_clip 0 (none) or > 1; kl_coef >= 0, and 0 without logp_ref; norm > 0
- * for CONSTANT; B < 2^22 and B ceil(L/2048) < 2^24; workspace of
+ * Requirements: B, L, n_groups >= 0; for GROUP n_groups > 0 if B > 0 and
+ * group_of_seq non-NULL (else group_of_seq is not read, and n_groups sizes the
+ * workspace alone: 0 will do); eps_low in [0, 1), eps_high >= 0; dual_clip 0
+ * (none) or > 1; kl_coef >= 0, and 0 without logp_ref; eps_high, dual_clip and
+ * kl_coef below 1e30; norm > 0 and finite for CONSTANT; B < 2^22, L and n_groups
+ * < 2^31 - 1 and B ceil(L/2048) < 2^24; workspace of
  * acrl_policy_loss_workspace_size() bytes, 16-byte aligned.                 */
 typedef enum { ACRL_KL_K1 = 0, ACRL_KL_K2 = 1, ACRL_KL_K3 = 2 } acrl_kl_estimator;
 typedef enum {
@@ -660,9 +662,9 @@ acrl_status acrl_policy_loss(const acrl_policy_loss_desc* desc, void* stream);
  * outside [0, B) gives NaN: the reward it names, the loss, and coef of the
  * pair's other response.  All is evaluated in fp64 from the fp32 inputs, sums
  * by fixed trees.
- * Requirements: B, L, n_pairs >= 0; B < 2^22, n_pairs < 2^24 and B n_pairs <
- * 2^40; beta > 0; margin finite; label_smoothing in [0, 1), and 0 but for
- * SIGMOID; workspace of
+ * Requirements: B, L, n_pairs >= 0; B < 2^22, L < 2^31 - 1, n_pairs < 2^24 and
+ * B n_pairs < 2^40; beta > 0 and below 1e30; margin finite; label_smoothing in
+ * [0, 1), and 0 but for SIGMOID; workspace of
  * acrl_preference_loss_workspace_size() bytes, 16-byte aligned.             */
 typedef enum { ACRL_PREF_SIGMOID = 0, ACRL_PREF_HINGE = 1, ACRL_PREF_SQUARED = 2 } acrl_preference_form;
 

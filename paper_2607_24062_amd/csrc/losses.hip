@@ -574,8 +574,8 @@ acrl_status acrl_policy_loss_workspace_size(int64_t B, int64_t L, int64_t n_grou
   ACRL_REQUIRE(bytes, "bytes is NULL");
   ACRL_REQUIRE(B >= 0 && L >= 0 && n_groups >= 0, "B, L and n_groups must be >= 0");
   // a launch holds fewer than 2^32 threads
-  ACRL_REQUIRE(B < acrl::kMaxResponses && L < INT32_MAX && n_groups < INT32_MAX, "B, L or n_groups too large");
-  ACRL_REQUIRE(B * acrl::units_of_response(B, L) < 4 * acrl::kMaxResponses, "B x L too large");
+  ACRL_REQUIRE(B < acrl::kMaxResponses && L < INT32_MAX && n_groups < INT32_MAX, "B must be < 2^22, L and n_groups < 2^31 - 1");
+  ACRL_REQUIRE(B * acrl::units_of_response(B, L) < 4 * acrl::kMaxResponses, "B ceil(L / 2048) must be < 2^24");
   *bytes = acrl::one_policy(B, L, n_groups) ? 0 : (size_t)acrl::policy_ws(nullptr, B, L, n_groups).bytes;
   return ACRL_OK;
 }
@@ -590,13 +590,13 @@ acrl_status acrl_policy_loss(const acrl_policy_loss_desc* d, void* stream) {
   ACRL_REQUIRE(d->kl_estimator >= ACRL_KL_K1 && d->kl_estimator <= ACRL_KL_K3, "kl_estimator %d unknown",
                d->kl_estimator);
   ACRL_REQUIRE(d->eps_low >= 0.0f && d->eps_low < 1.0f, "eps_low must lie in [0, 1) (got %g)", (double)d->eps_low);
-  ACRL_REQUIRE(d->eps_high >= 0.0f && d->eps_high < 1e30f, "eps_high must be >= 0 (got %g)", (double)d->eps_high);
+  ACRL_REQUIRE(d->eps_high >= 0.0f && d->eps_high < 1e30f, "eps_high must lie in [0, 1e30) (got %g)", (double)d->eps_high);
   ACRL_REQUIRE(d->dual_clip == 0.0f || (d->dual_clip > 1.0f && d->dual_clip < 1e30f),
-               "dual_clip must be 0 or > 1 (got %g)", (double)d->dual_clip);
-  ACRL_REQUIRE(d->kl_coef >= 0.0f && d->kl_coef < 1e30f, "kl_coef must be >= 0 (got %g)", (double)d->kl_coef);
+               "dual_clip must be 0 or lie in (1, 1e30) (got %g)", (double)d->dual_clip);
+  ACRL_REQUIRE(d->kl_coef >= 0.0f && d->kl_coef < 1e30f, "kl_coef must lie in [0, 1e30) (got %g)", (double)d->kl_coef);
   ACRL_REQUIRE(d->logp_ref || d->kl_coef == 0.0f || d->B == 0 || d->L == 0, "kl_coef needs logp_ref");
   if (d->aggregate == ACRL_AGG_CONSTANT)
-    ACRL_REQUIRE(d->norm > 0.0f && acrl::finite(d->norm), "norm must be positive (got %g)", (double)d->norm);
+    ACRL_REQUIRE(d->norm > 0.0f && acrl::finite(d->norm), "norm must be positive and finite (got %g)", (double)d->norm);
   ACRL_REQUIRE(d->loss, "loss is required");
   if (d->B > 0 && d->aggregate == ACRL_AGG_GROUP)
     ACRL_REQUIRE(d->n_groups > 0 && d->group_of_seq, "group_of_seq and n_groups > 0 are required");
@@ -616,8 +616,8 @@ acrl_status acrl_policy_loss(const acrl_policy_loss_desc* d, void* stream) {
 acrl_status acrl_preference_loss_workspace_size(int64_t B, int64_t L, int64_t n_pairs, size_t* bytes) {
   ACRL_REQUIRE(bytes, "bytes is NULL");
   ACRL_REQUIRE(B >= 0 && L >= 0 && n_pairs >= 0, "B, L and n_pairs must be >= 0");
-  ACRL_REQUIRE(B < acrl::kMaxResponses && L < INT32_MAX && n_pairs < acrl::kMaxPairs, "B, L or n_pairs too large");
-  ACRL_REQUIRE(B * n_pairs < acrl::kMaxPairLooks, "B x n_pairs too large");
+  ACRL_REQUIRE(B < acrl::kMaxResponses && L < INT32_MAX && n_pairs < acrl::kMaxPairs, "B must be < 2^22, L < 2^31 - 1, n_pairs < 2^24");
+  ACRL_REQUIRE(B * n_pairs < acrl::kMaxPairLooks, "B n_pairs must be < 2^40");
   *bytes = acrl::one_preference(B, L, n_pairs) ? 0 : acrl::pref_ws_bytes(B);
   return ACRL_OK;
 }
@@ -629,7 +629,7 @@ acrl_status acrl_preference_loss(const acrl_preference_desc* d, void* stream) {
   if (st != ACRL_OK) return st;
   ACRL_REQUIRE(d->form >= ACRL_PREF_SIGMOID && d->form <= ACRL_PREF_SQUARED, "form %d unknown", d->form);
   ACRL_REQUIRE(d->mean_logp == 0 || d->mean_logp == 1, "mean_logp must be 0 or 1");
-  ACRL_REQUIRE(d->beta > 0.0f && d->beta < 1e30f, "beta must be positive (got %g)", (double)d->beta);
+  ACRL_REQUIRE(d->beta > 0.0f && d->beta < 1e30f, "beta must lie in (0, 1e30) (got %g)", (double)d->beta);
   ACRL_REQUIRE(acrl::finite(d->margin), "margin must be finite");
   ACRL_REQUIRE(d->label_smoothing >= 0.0f && d->label_smoothing < 1.0f, "label_smoothing must lie in [0, 1) (got %g)",
                (double)d->label_smoothing);

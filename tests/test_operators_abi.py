@@ -139,3 +139,31 @@ def test_binding_refuses_host_tensors(acrl):
         acrl.acrl_policy_loss(2, 4, 1, m, g, f, f, f[:2], False)
     with pytest.raises(ValueError, match="device tensor"):
         acrl.acrl_preference_loss(2, 4, m, f, g, g)
+
+
+def test_bounds_of_the_losses_are_named(acrl, p):
+    # what the header's requirements allow is sized, what they do not is refused with the bound
+    L, nb = acrl.lib(), ctypes.c_size_t()
+    last = lambda: L.acrl_last_error().decode()  # noqa: E731
+    for B, n, g in ((1, INT_MAX - 1, 1), (15, INT_MAX - 1, 1), ((1 << 22) - 1, 6144, 0), (4, 64, INT_MAX - 1), (4, 64, 0)):
+        assert L.acrl_policy_loss_workspace_size(B, n, g, ctypes.byref(nb)) == 0, (B, n, g)
+    for B, n, g, bound in ((1, INT_MAX, 1, "2^31"), (4, 64, INT_MAX, "2^31"), (1 << 22, 64, 1, "2^22"),
+                           (16, INT_MAX - 1, 1, "2^24"), ((1 << 22) - 1, 8193, 1, "2^24")):
+        assert L.acrl_policy_loss_workspace_size(B, n, g, ctypes.byref(nb)) == acrl.ACRL_ERR_INVALID_ARG
+        assert bound in last(), last()
+    for B, n, P in ((1, INT_MAX - 1, 1), ((1 << 22) - 1, 64, 1 << 18), (1 << 16, 64, (1 << 24) - 1), (0, 0, 0)):
+        assert L.acrl_preference_loss_workspace_size(B, n, P, ctypes.byref(nb)) == 0, (B, n, P)
+    for B, n, P, bound in ((1, INT_MAX, 1, "2^31"), (1 << 22, 64, 1, "2^22"), (1, 64, 1 << 24, "2^24"),
+                           (1 << 16, 64, 1 << 24, "2^24"), (1 << 21, 64, 1 << 19, "2^40")):
+        assert L.acrl_preference_loss_workspace_size(B, n, P, ctypes.byref(nb)) == acrl.ACRL_ERR_INVALID_ARG
+        assert bound in last(), last()
+    ok = dict(B=2, L=4096, n_groups=1, mask=p, group_of_seq=p, logp_new=p, logp_old=p, logp_ref=p, adv=p, eps_low=0.2,
+              eps_high=0.2, kl_coef=0.1, kl_estimator=2, coef=p, loss=p, workspace=p, workspace_bytes=1 << 30)
+    for bad in (dict(eps_high=float("inf")), dict(eps_high=1e30), dict(dual_clip=1e30), dict(kl_coef=1e30)):
+        d = acrl.PolicyLossDesc(**{**ok, **bad})
+        assert L.acrl_policy_loss(ctypes.byref(d), None) == acrl.ACRL_ERR_INVALID_ARG and "1e30" in last(), bad
+    d = acrl.PolicyLossDesc(**{**ok, "aggregate": 3, "norm": float("inf")})
+    assert L.acrl_policy_loss(ctypes.byref(d), None) == acrl.ACRL_ERR_INVALID_ARG and "finite" in last()
+    d = acrl.PreferenceDesc(B=2, L=4096, n_pairs=1, mask=p, logp_new=p, chosen=p, rejected=p, beta=1e30, coef=p, loss=p,
+                            workspace=p, workspace_bytes=1 << 30)
+    assert L.acrl_preference_loss(ctypes.byref(d), None) == acrl.ACRL_ERR_INVALID_ARG and "1e30" in last()

@@ -2,8 +2,10 @@
 // preferred / rejected pairs, each with its gradient with respect to the new
 // policy's log-probs (the coef that acrl_lm_head_backward takes).
 //
-// Layout: slots [B, L] row-major.  Every slot's inputs are read once; the
-// terms and sums are fp64, the sums by fixed trees (deterministic).
+// Layout: slots [B, L] row-major.  A slot's log-probs, weight and advantage are
+// read once, its mask twice (for the counts or sums that a coef waits for, and
+// with the coef); the terms and sums are fp64, the sums by fixed trees
+// (deterministic).
 #include "entry.h"
 #include "slots.h"
 

@@ -379,8 +379,8 @@ hipError_t launch_policy_loss(const acrl_policy_loss_desc& p, hipStream_t s) {
 struct PrefRec {
   double x, each;  // x_i (mean_logp applied); d x_i / d logp_new of a valid slot
 };
-// Every response's workgroup looks through all pairs: 65536 responses of 65536 pairs take 2.9 ms, 2^20 of 2^20 1.1 s,
-// and more are refused.
+// Every response's workgroup looks through all pairs: 65536 responses of 65536 pairs take 2.9 ms, 2^20 of 2^20 would
+// 1.1 s: from there on they are refused.
 constexpr int64_t kMaxPairs = (int64_t)1 << 24, kMaxPairLooks = (int64_t)1 << 40;
 constexpr int kPrefOne = 256;  // responses, and pairs, of a batch that one workgroup does
 inline bool one_preference(int64_t B, int64_t L, int64_t P) {
@@ -389,8 +389,8 @@ inline bool one_preference(int64_t B, int64_t L, int64_t P) {
 size_t pref_ws_bytes(int64_t B) { return align_up((size_t)B * sizeof(PrefRec), 256) + 256; }
 
 // Workgroup size: 1024 threads from the second turn on while that leaves a few
-// workgroups a CU (512 responses of 16384 slots 12.3 us, 18.0 with 256 threads; 256 of 4096 3.6 /
-// 4.4; 2048 of 2048 11.0 / 7.9).
+// workgroups a CU (512 responses of up to 16384 slots 10.3 us, 14.9 with 256
+// threads; 256 of 4096 3.6 / 4.2; 2048 of 2048 10.3 / 5.9).
 inline int pref_threads(int64_t B, int64_t L) {
   if (L <= 64 * kSlots) return 64;
   return L > kRedThreads * kSlots && B <= 1024 ? 1024 : kRedThreads;
@@ -461,8 +461,9 @@ __device__ __forceinline__ void pref_rewards(const acrl_preference_desc& p, cons
 }
 
 // coef of one response's slots: its pairs' slopes, then one value for every
-// valid slot (512 responses of 16384 slots: 10.2 us, 4.1 TB/s; pref_seq_kernel
-// 12.3 us, 3.7 TB/s).  The last workgroup sums the loss and writes the rewards.
+// valid slot (512 responses of up to 16384 slots: 10.1 us, 4.1 TB/s;
+// pref_seq_kernel 10.2 us, 4.4 TB/s).  The last workgroup sums the loss and writes
+// the rewards.
 template <bool VEC>
 __global__ __launch_bounds__(kUnitThreads) void pref_coef_kernel(acrl_preference_desc p, const PrefRec* rec) {
   __shared__ BlockShared<1, kUnitThreads> sh;

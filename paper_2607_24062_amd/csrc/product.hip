@@ -176,8 +176,9 @@ __device__ __forceinline__ void tile_of(const ProductParams& p, int block, int& 
 // arithmetic beside the products counts in full: with descriptor, row group and
 // bounds of each load known when it is compiled or once a turn, a turn of a
 // 128 x 128 tile went from 158 instructions to 103, and times fell by 3 to 12 % at
-// nearly all sizes.  Large tiles (16384 x 5120 x 13824, 946 to 960 us, 2420
-// TFLOP/s, counters): the matrix cores are busy for 2048 of a turn's 3250 cycles, at 1.83 GHz,
+// nearly all sizes.  Large tiles (16384 x 5120 x 13824: 952 us in a run of calls, 916 to
+// 980, 2440 TFLOP/s; 1000 to 1020 on average of 25 from a cold start; counters): the
+// matrix cores are busy for 2048 of a turn's 3250 cycles, at 1.83 GHz,
 // to which the power limit brings the clock (2.4 without load); the four FMAs
 // beside each product let it take 37 cycles for 32.  Smaller ones: loads alone,
 // without products, take the same time while there are two stages (128 x 128
@@ -467,8 +468,10 @@ __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(Prod
   }
 }
 
-// Up to 16 tokens: the weights' stream from HBM is the whole work, and a workgroup
-// takes 16 AN outputs so that many of them share it out.  Its NW waves take every
+// Up to 16 tokens: the weights' stream is the whole work (16 x 24576 x 4096: 26.2 us,
+// 3.9 TB/s from HBM, 22.3 where the weights lie in the 256 MB cache; 1 x 4096 x 4096: 6.3
+// us, 2.7 TB/s, and 4.6: two rounds of loads for each wave), and a workgroup takes
+// 16 AN outputs so that many of them share it out.  Its NW waves take every
 // NW-th scale block each, U of them at a time, straight into registers: 16-byte
 // pieces q and q + 4 of a row's 128 bytes for lane group q, so that a load takes
 // 64 contiguous bytes of each row (the products of a block may be summed in any
@@ -551,10 +554,13 @@ hipError_t launch_tiles(ProductParams p, hipStream_t s) {
 // of a round (a tile a CU), `round` us beside them: fits to the times of 60
 // sizes (M 24 .. 4096; N x K 4096 x 4096, 24576 x 4096, 5120 x 13824, 1024 x 5120,
 // 2048 x 2048), at each of which but one they choose the fastest of the seven.
-// How far apart those are: 64 x 4096 x 4096 8.4 us by the first, 18.5 by the
+// How far apart those are: 64 x 4096 x 4096 6.9 us by the first, 17.4 by the
 // fifth; 700 x 4096 x 4096 20.5 by the fifth, 50 by the last; 1500 x 4096 x 4096 32.5
 // by the sixth, 51 by the last; 4096 x 4096 x 4096 60 by the last, 72 by the sixth, 173
-// by the third.
+// by the third.  Of the same N x K at M 17, 20, 23, 32, 48 and 64, with weights from the
+// cache and from HBM, they choose the fastest at all but 5120 x 13824 of up to 32 tokens
+// from the cache (16.9 us by the second, 19.7 by the first, which is the faster one
+// from HBM: 25.1 to 27.5).
 template <typename OUT>
 struct Variant {
   int tn, tm, kg;
@@ -570,8 +576,10 @@ float cost(const Variant<OUT>& v, const ProductParams& p) {
 
 template <typename OUT>
 hipError_t launch_product(const ProductParams& p, hipStream_t s) {
-  // Up to 16 tokens: 16 outputs a workgroup while that is needed to have workgroups for the CUs (1 x 4096 x 4096
-  // 5.8 us, 6.7 with 32), 32 from there on (8 x 5120 x 13824 20 us, 26 with 16)
+  // Up to 16 tokens: 16 outputs a workgroup while that is needed to have workgroups for the CUs, 32 from there on.
+  // With 16 / 32, M 1, 8 and 16, K 2048, 4096 and 13824, weights from the cache: N = 4096, K = 4096 4.8 / 6.4, 6.0 / 7.8,
+  // 7.0 / 8.9 us; N = 5120, K = 13824 18.2 / 16.3, 24.5 / 19.0, 29.8 / 21.8; every K and N 1024 .. 24576, from HBM too,
+  // goes the same way or is within 5 %, but N = 12288 of up to 8 tokens (1 x 12288 x 13824: 26.8 / 32.9)
   if (p.M <= 16) return p.N < 20 * kCus ? launch_rows<OUT, 1, 8, 2>(p, s) : launch_rows<OUT, 2, 8, 2>(p, s);
   static const Variant<OUT> variants[] = {
       {32, 32, 8, 1.179f, 2.13f, launch_tiles<OUT, 32, 32, 1, 1, 8, 2, 32, false>},

@@ -264,8 +264,8 @@ __device__ __forceinline__ uint4 encode16_of(uint4 a, uint4 b, float amax, float
 
 // ROW128: 8 lanes per group of 128 elements, 32 bytes in and 16 out a lane.
 // `groups` = ceil(cols / 128) of a row; the last one's lanes past the row's
-// end take part in the maximum with 0.  HBM-bound: 8009 x 5120 in 23.4 us,
-// 5.3 TB/s (a copy of 2 GiB: 5.0).
+// end take part in the maximum with 0.  HBM-bound: 8009 x 5120 in 23.4 us on
+// average, 5.3 TB/s (a copy of 2 GiB, half of it stores: 5.0).
 template <int ROUND>
 __global__ __launch_bounds__(256) void quantize_row128_kernel(const uint16_t* __restrict__ x, int64_t rows,
                                                               int64_t cols, int64_t ld, int64_t groups,
@@ -287,7 +287,7 @@ __global__ __launch_bounds__(256) void quantize_row128_kernel(const uint16_t* __
 
 // BLOCK128: one workgroup per 128 x 128 block, 8 lanes a row, 4 rows a thread,
 // kept in registers between the maximum and the encoding.  HBM-bound: 151936 x
-// 2048 in 166 us, 5.6 TB/s.
+// 2048 in 175 to 178 us on average, 5.2 to 5.3 TB/s.
 template <int ROUND>
 __global__ __launch_bounds__(256) void quantize_block128_kernel(const uint16_t* __restrict__ x, int64_t rows,
                                                                 int64_t cols, int64_t ld, int64_t groups,

@@ -563,6 +563,44 @@ typedef struct acrl_matmul_desc {
 acrl_status acrl_matmul_fp8(const acrl_matmul_desc* desc, void* stream);
 
 /* ======================================================================== */
+/* acrl_linear_fp8 -- the same product with an epilogue                      */
+/* ======================================================================== *
+ *   y = act(x W^T + bias) + residual
+ * with x W^T as acrl_matmul_fp8 has it, in fp32; bias, activation and residual
+ * enter in fp32 and y is rounded once.  With the sums S = x W^T + bias:
+ *   NONE S;  RELU max(S, 0);  SILU S / (1 + e^-S);  GELU S Phi(S), Phi the normal
+ *   distribution function;  GELU_TANH S (1 + tanh(sqrt(2/pi) (S + 0.044715 S^3))) / 2
+ * each within 6e-7 of its exact value at S, relative to its size, or within
+ * 1.3e-36.  NaN stays NaN.
+ *   bias      [N] of bias_type, or NULL
+ *   residual  [M, N] of residual_type, rows ldr elements apart, or NULL.  It may
+ *             be y itself (same pointer, type and row distance): y is then updated
+ *             in place.  Otherwise its values must not lie among y's; columns of
+ *             one matrix, side by side, may (same bytes between rows).
+ * Requirements: those of acrl_matmul_fp8 for `product`; bias and residual
+ * 16-byte aligned; with a residual N <= ldr < 2^34 and ldy < 2^34.
+ */
+typedef enum {
+  ACRL_ACT_NONE = 0,
+  ACRL_ACT_RELU = 1,
+  ACRL_ACT_SILU = 2,
+  ACRL_ACT_GELU = 3,            /* by the error function                                    */
+  ACRL_ACT_GELU_TANH = 4        /* by its tanh approximation                                */
+} acrl_activation;
+
+typedef struct acrl_linear_desc {
+  acrl_matmul_desc product;     /* operands, sizes and y                                    */
+  const void* bias;             /* optional                                                 */
+  const void* residual;         /* optional                                                 */
+  int64_t ldr;                  /* elements between rows of the residual                    */
+  int32_t bias_type;            /* acrl_out_type                                            */
+  int32_t residual_type;        /* acrl_out_type                                            */
+  int32_t activation;           /* acrl_activation                                          */
+} acrl_linear_desc;
+
+acrl_status acrl_linear_fp8(const acrl_linear_desc* desc, void* stream);
+
+/* ======================================================================== */
 /* acrl_policy_loss -- clipped policy loss with a KL term, and its gradient   */
 /* ======================================================================== *
  * Beside acrl_surrogate (group mean of the clipped objective): the same clip
@@ -696,6 +734,9 @@ acrl_status acrl_preference_loss(const acrl_preference_desc* desc, void* stream)
 /* sizeof of the three descriptors above as compiled into the library (host),
  * as acrl_abi_struct_sizes gives those of the others.                       */
 void acrl_abi_operator_struct_sizes(size_t* matmul_desc, size_t* policy_loss_desc, size_t* preference_desc);
+
+/* The same for the descriptors of a decode step's operators.                */
+void acrl_abi_decode_struct_sizes(size_t* linear_desc);
 
 /* Host helper (host pointers): the reference discrepancy X of Sec. 4.1 is the
  * mean of Y_g over the non-empty groups (group_nseq > 0) of the step-0

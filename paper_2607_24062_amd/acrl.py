@@ -28,6 +28,7 @@ OUT_BF16, OUT_F32 = 0, 1
 KL_K1, KL_K2, KL_K3 = 0, 1, 2
 AGG_GROUP, AGG_SEQUENCE, AGG_TOKEN, AGG_CONSTANT = 0, 1, 2, 3
 PREF_SIGMOID, PREF_HINGE, PREF_SQUARED = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2, 3, 4
 N_STATS = 10
 STAT_NAMES = ["y_batch", "tok_mean_d", "tok_max_d", "tok_std_d", "mean_h_pi", "mean_h_mu",
               "n_tokens", "n_groups", "tok_mean_logratio", "n_seqs"]
@@ -45,6 +46,7 @@ EXPORTED = [
     "acrl_backward_workspace_size", "acrl_lm_head_backward",
     "acrl_matmul_fp8", "acrl_policy_loss_workspace_size", "acrl_policy_loss",
     "acrl_preference_loss_workspace_size", "acrl_preference_loss", "acrl_abi_operator_struct_sizes",
+    "acrl_linear_fp8", "acrl_abi_decode_struct_sizes",
 ]
 
 _P = ctypes.c_void_p
@@ -111,6 +113,11 @@ class SampleDesc(ctypes.Structure):
 class MatmulDesc(ctypes.Structure):
     _fields_ = [("M", _I64), ("N", _I64), ("K", _I64), ("xq", _P), ("x_scales", _P), ("wq", _P), ("w_scales", _P),
                 ("y", _P), ("ldy", _I64), ("y_type", _I32)]
+
+
+class LinearDesc(ctypes.Structure):
+    _fields_ = [("product", MatmulDesc), ("bias", _P), ("residual", _P), ("ldr", _I64), ("bias_type", _I32),
+                ("residual_type", _I32), ("activation", _I32)]
 
 
 class PolicyLossDesc(ctypes.Structure):
@@ -205,12 +212,18 @@ def lib() -> ctypes.CDLL:
         L.acrl_preference_loss.argtypes = [ctypes.POINTER(PreferenceDesc), _P]
         L.acrl_abi_operator_struct_sizes.restype = None
         L.acrl_abi_operator_struct_sizes.argtypes = [ctypes.POINTER(_SZ)] * 3
-        sizes = [_SZ() for _ in range(9)]
+        L.acrl_linear_fp8.restype = _I32
+        L.acrl_linear_fp8.argtypes = [ctypes.POINTER(LinearDesc), _P]
+        L.acrl_abi_decode_struct_sizes.restype = None
+        L.acrl_abi_decode_struct_sizes.argtypes = [ctypes.POINTER(_SZ)] * 1
+        sizes = [_SZ() for _ in range(10)]
         L.acrl_abi_struct_sizes(*[ctypes.byref(s) for s in sizes[:6]])
-        L.acrl_abi_operator_struct_sizes(*[ctypes.byref(s) for s in sizes[6:]])
+        L.acrl_abi_operator_struct_sizes(*[ctypes.byref(s) for s in sizes[6:9]])
+        L.acrl_abi_decode_struct_sizes(*[ctypes.byref(s) for s in sizes[9:]])
         want = [ctypes.sizeof(ScoreDesc), ctypes.sizeof(ReduceDesc), ctypes.sizeof(ControllerDesc),
                 ctypes.sizeof(SampleDesc), ctypes.sizeof(SurrogateDesc), ctypes.sizeof(BackwardDesc),
-                ctypes.sizeof(MatmulDesc), ctypes.sizeof(PolicyLossDesc), ctypes.sizeof(PreferenceDesc)]
+                ctypes.sizeof(MatmulDesc), ctypes.sizeof(PolicyLossDesc), ctypes.sizeof(PreferenceDesc),
+                ctypes.sizeof(LinearDesc)]
         got = [s.value for s in sizes]
         if got != want:
             raise RuntimeError("libacrl descriptor layout mismatch: library %s, binding %s" % (got, want))
@@ -654,6 +667,13 @@ def acrl_matmul_fp8(xq, x_scales, wq, w_scales, out=None, out_dtype=torch.bfloat
     rounded to float32 before its use.  `out` (bf16 or float32) may be
     a column slice of a wider matrix: unit column stride, any row stride, its
     first element 16-byte aligned."""
+    index, out, desc = _product(xq, x_scales, wq, w_scales, out, out_dtype, stream)
+    _check(lib().acrl_matmul_fp8(ctypes.byref(desc), _raw_stream(stream, xq.device)), "acrl_matmul_fp8")
+    return out
+
+
+def _product(xq, x_scales, wq, w_scales, out, out_dtype, stream):
+    """(device index, out, descriptor) of a product of block-scaled operands."""
     if xq.dim() != 2 or wq.dim() != 2 or xq.shape[1] != wq.shape[1]:
         raise ValueError("xq [M, K] and wq [N, K] must be 2-D with the same K")
     index = _index_of(xq, torch.uint8, "xq", stream)
@@ -665,15 +685,40 @@ def acrl_matmul_fp8(xq, x_scales, wq, w_scales, out=None, out_dtype=torch.bfloat
             raise ValueError("out_dtype must be torch.bfloat16 or torch.float32, got %s" % out_dtype)
         out, ldy = _empty((M, N), out_dtype, xq.device, stream), N
     else:
-        if (out.dtype not in _OUT_TYPES or out.get_device() != index or tuple(out.shape) != (M, N) or
-                (N > 1 and out.stride(1) != 1) or (M > 1 and out.stride(0) < N)):
-            raise ValueError("out must be a bf16 or float32 device matrix [M, N] with unit column stride")
-        out_dtype, ldy = out.dtype, out.stride(0) if M > 1 else N
-    desc = MatmulDesc(M, N, K, xq.data_ptr(), _want(x_scales, torch.float32, M * kb, index, "x_scales"),
-                      _want(wq, torch.uint8, N * K, index, "wq"),
-                      _want(w_scales, torch.float32, (N + 127) // 128 * kb, index, "w_scales"),
-                      out.data_ptr(), ldy, _OUT_TYPES[out_dtype])
-    _check(lib().acrl_matmul_fp8(ctypes.byref(desc), _raw_stream(stream, xq.device)), "acrl_matmul_fp8")
+        ldy = _matrix(out, M, N, index, "out")
+        out_dtype = out.dtype
+    return index, out, MatmulDesc(M, N, K, xq.data_ptr(), _want(x_scales, torch.float32, M * kb, index, "x_scales"),
+                                  _want(wq, torch.uint8, N * K, index, "wq"),
+                                  _want(w_scales, torch.float32, (N + 127) // 128 * kb, index, "w_scales"),
+                                  out.data_ptr(), ldy, _OUT_TYPES[out_dtype])
+
+
+def _matrix(t, rows: int, cols: int, index: int, name: str) -> int:
+    """The row distance of a bf16 or float32 matrix that may be a column slice of a wider one."""
+    if (t.dtype not in _OUT_TYPES or t.get_device() != index or tuple(t.shape) != (rows, cols) or
+            (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols)):
+        raise ValueError("%s must be a bf16 or float32 device matrix [%d, %d] on cuda:%d with unit column stride"
+                         % (name, rows, cols, index))
+    return t.stride(0) if rows > 1 else cols
+
+
+def acrl_linear_fp8(xq, x_scales, wq, w_scales, bias=None, activation: int = ACT_NONE, residual=None, out=None,
+                    out_dtype=torch.bfloat16, stream=None):
+    """y = act(x W^T + bias) + residual [M, N], operands and `out` as for
+    acrl_matmul_fp8, rounded once.  bias [N] and residual [M, N] are bf16 or
+    float32; the residual may be a column slice of a wider matrix (first element
+    16-byte aligned), and may be `out` itself."""
+    index, out, product = _product(xq, x_scales, wq, w_scales, out, out_dtype, stream)
+    M, N = out.shape
+    desc = LinearDesc(product, activation=activation)
+    if bias is not None:
+        if bias.dtype not in _OUT_TYPES:
+            raise ValueError("bias must be bf16 or float32, got %s" % bias.dtype)
+        desc.bias, desc.bias_type = _want(bias, bias.dtype, N, index, "bias"), _OUT_TYPES[bias.dtype]
+    if residual is not None:
+        desc.ldr = _matrix(residual, M, N, index, "residual")
+        desc.residual, desc.residual_type = residual.data_ptr(), _OUT_TYPES[residual.dtype]
+    _check(lib().acrl_linear_fp8(ctypes.byref(desc), _raw_stream(stream, xq.device)), "acrl_linear_fp8")
     return out
 
 

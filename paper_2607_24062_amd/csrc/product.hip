@@ -10,8 +10,12 @@
 // wave.  (Factors past fp32's normal range lose what lies past it: a second
 // multiplication by the other scale would stand beside every product, where the
 // FMAs already hold the matrix cores up.)
+//
+// acrl_linear_fp8 is the same product with an epilogue: bias, activation and
+// residual enter the fp32 sums before their one rounding.
 #include <type_traits>
 
+#include "activation.h"
 #include "entry.h"
 
 namespace acrl {
@@ -23,6 +27,9 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kBlock = 128;  // elements (bytes) of K per scale
 
+// Results of type T by way of the epilogue.
+template <typename T>
+struct Fused {};
 struct ProductParams {
   const uint8_t* x;
   const float* xs;
@@ -35,6 +42,28 @@ struct ProductParams {
   int n_mtiles, n_ntiles;
   int vec, whole;          // y's rows take stores of four values; of 16 bytes
 };
+struct LinearParams : ProductParams {
+  const void* bias;        // [N] or NULL
+  const void* res;         // [M, N], rows ldr apart, or NULL
+  int64_t ldr;
+  int act;
+  int bias_f32, res_f32;   // else bf16
+  int res_vec;             // the residual's rows take loads of four values, and of as many as a 16-byte store has
+};
+template <typename OUT>
+struct Result {
+  using type = OUT;
+  using params = ProductParams;
+  static constexpr bool fused = false;
+};
+template <typename T>
+struct Result<Fused<T>> {
+  using type = T;
+  using params = LinearParams;
+  static constexpr bool fused = true;
+};
+template <typename OUT>
+using Params = typename Result<OUT>::params;
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, int64_t bytes) {
   const uint32_t n = bytes > 0xFFFFFFFFll ? 0xFFFFFFFFu : (uint32_t)bytes;
@@ -87,10 +116,64 @@ __device__ __forceinline__ void settle(f32x4 (&acc)[A][B]) {
 template <typename OUT>
 using out4 = OUT __attribute__((ext_vector_type(4)));
 
+// Values at .. at + C - 1 of an array of fp32 or bf16 as fp32; of the first `left` of them alone where that is less than
+// C or the address takes no wide load (the others: 0).
+template <int C>
+__device__ __forceinline__ void read_values(float (&v)[C], const void* base, bool f32, int64_t at, int left, bool vec) {
+  if (vec && left >= C) {
+    if (f32) {
+      const f32x4* q = reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + at);
+#pragma unroll
+      for (int i = 0; i < C; ++i) v[i] = q[i / 4][i % 4];
+    } else {
+      using words = uint32_t __attribute__((ext_vector_type(C / 2)));
+      const words q = *reinterpret_cast<const words*>(static_cast<const uint16_t*>(base) + at);
+#pragma unroll
+      for (int i = 0; i < C; ++i) v[i] = i % 2 ? bf16_hi(q[i / 2]) : bf16_lo(q[i / 2]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      v[i] = 0.0f;
+      if (i < left)
+        v[i] = f32 ? static_cast<const float*>(base)[at + i] : bf16_lo(static_cast<const uint16_t*>(base)[at + i]);
+    }
+  }
+}
+
+// The epilogue on the sums n .. n + C - 1 of token m (n a multiple of C), in fp32.  A residual that is y itself is
+// read by the lane that writes it, before it does.
+template <int C>
+__device__ __forceinline__ void finish(const LinearParams& p, int m, int n, float (&v)[C]) {
+  const int left = p.N - n;
+  float r[C];
+  if (p.res) read_values<C>(r, p.res, p.res_f32, (int64_t)m * p.ldr + n, left, p.res_vec);
+  if (p.bias) {
+    float b[C];
+    read_values<C>(b, p.bias, p.bias_f32, n, left, true);
+#pragma unroll
+    for (int i = 0; i < C; ++i) v[i] += b[i];
+  }
+  if (p.act != ACRL_ACT_NONE) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) v[i] = activate(p.act, v[i]);
+  }
+  if (p.res) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) v[i] += r[i];
+  }
+}
+
 // Four consecutive outputs n .. n + 3 of token m.
-template <typename OUT>
-__device__ __forceinline__ void store4(const ProductParams& p, int m, int n, const f32x4& v) {
+template <typename RES>
+__device__ __forceinline__ void store4(const Params<RES>& p, int m, int n, f32x4 v) {
+  using OUT = typename Result<RES>::type;
   if (m >= p.M || n >= p.N) return;
+  if constexpr (Result<RES>::fused) {
+    float f[4] = {v[0], v[1], v[2], v[3]};
+    finish(p, m, n, f);
+    v = f32x4{f[0], f[1], f[2], f[3]};
+  }
   OUT* y = static_cast<OUT*>(p.y) + (int64_t)m * p.ldy + n;
   const out4<OUT> o = __builtin_convertvector(v, out4<OUT>);
   if (p.vec && n + 3 < p.N) {
@@ -105,10 +188,14 @@ __device__ __forceinline__ void store4(const ProductParams& p, int m, int n, con
 // The sums of a TM x TN tile (WM x WN waves) to y by way of LDS: a wave's
 // lanes hold 16 tokens and write 8 or 16 bytes of each, which costs twice the
 // time of rows written whole (4096 x 4096 of K = 256: 23 us, 9 without stores).
-template <typename OUT, int TN, int TM, int WN, int WM, int PARTS, int A, int B>
-__device__ __forceinline__ void store_tile(const ProductParams& p, uint8_t* lds, int m0, int n0, int wm, int wn,
+// With an epilogue they pass as fp32, and it runs where rows are written: its
+// arrays are then read as wide as y is written, and its code stands once.
+template <typename RES, int TN, int TM, int WN, int WM, int PARTS, int A, int B>
+__device__ __forceinline__ void store_tile(const Params<RES>& p, uint8_t* lds, int m0, int n0, int wm, int wn,
                                            const f32x4 (&acc)[A][B]) {
-  constexpr int kPitch = TN * sizeof(OUT) + 16, kPiece = 16 / sizeof(OUT), kPieces = TN / kPiece;  // (16: other banks)
+  using OUT = typename Result<RES>::type;
+  using IN = typename std::conditional<Result<RES>::fused, float, OUT>::type;
+  constexpr int kPitch = TN * sizeof(IN) + 16, kPiece = 16 / sizeof(OUT), kPieces = TN / kPiece;  // (16: other banks)
   constexpr int kThreads = 64 * WN * WM, kRows = TM / PARTS;
   static_assert(WM % PARTS == 0 && kRows * kPieces % kThreads == 0, "whole parts");
   const int lane = threadIdx.x & 63, q = lane >> 4;
@@ -120,11 +207,36 @@ __device__ __forceinline__ void store_tile(const ProductParams& p, uint8_t* lds,
       for (int j = 0; j < B; ++j)
 #pragma unroll
         for (int i = 0; i < A; ++i)
-          *reinterpret_cast<out4<OUT>*>(lds + (wm % (WM / PARTS) * (TM / WM) + j * 16 + (lane & 15)) * kPitch +
-                                        (wn * (TN / WN) + i * 16 + 4 * q) * sizeof(OUT)) =
-              __builtin_convertvector(acc[i][j], out4<OUT>);
+          *reinterpret_cast<out4<IN>*>(lds + (wm % (WM / PARTS) * (TM / WM) + j * 16 + (lane & 15)) * kPitch +
+                                       (wn * (TN / WN) + i * 16 + 4 * q) * sizeof(IN)) =
+              __builtin_convertvector(acc[i][j], out4<IN>);
     }
     __syncthreads();
+    if constexpr (Result<RES>::fused) {
+#pragma unroll 1
+      for (int k = 0; k < kRows * kPieces / kThreads; ++k) {
+        const int at = k * kThreads + threadIdx.x, r = at / kPieces, c = at % kPieces;
+        const int m = m0 + part * kRows + r, n = n0 + c * kPiece;
+        if (m >= p.M || n >= p.N) continue;
+        const f32x4* from = reinterpret_cast<const f32x4*>(lds + r * kPitch + c * kPiece * sizeof(float));
+        float v[kPiece];
+#pragma unroll
+        for (int e = 0; e < kPiece; ++e) v[e] = from[e / 4][e % 4];
+        finish(p, m, n, v);
+        OUT* y = static_cast<OUT*>(p.y) + (int64_t)m * p.ldy + n;
+        OUT o[kPiece];
+#pragma unroll
+        for (int e = 0; e < kPiece; ++e) o[e] = (OUT)v[e];
+        if (p.whole && n + kPiece <= p.N) {
+          *reinterpret_cast<i32x4*>(y) = __builtin_bit_cast(i32x4, o);
+        } else {
+#pragma unroll
+          for (int e = 0; e < kPiece; ++e)
+            if (n + e < p.N) y[e] = o[e];
+        }
+      }
+      continue;
+    }
 #pragma unroll
     for (int k = 0; k < kRows * kPieces / kThreads; ++k) {
       const int at = k * kThreads + threadIdx.x, r = at / kPieces, c = at % kPieces;
@@ -189,7 +301,7 @@ __device__ __forceinline__ void tile_of(const ProductParams& p, int block, int& 
 // behind every second (946); waves that only load (0.6 to 1.08 of the speed);
 // lines touched a turn or more ahead; bands of 4 or 16 token tiles; priorities.
 template <typename OUT, int TN, int TM, int WN, int WM, int KG, int ST, int C, bool AHEAD>
-__global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(ProductParams p) {
+__device__ __forceinline__ void tile_product(Params<OUT> p) {
   constexpr int NW = WN * WM * KG, AN = TN / WN / 16, BM = TM / WM / 16, kSteps = AN * BM;  // fragments of a wave
   constexpr int kRows = TN + TM, kStage = kRows * kBlock * KG, kLoads = kRows * KG / 8 / NW;
   constexpr int kStepLoads = (kLoads + kSteps - 1) / kSteps;  // behind each product
@@ -455,8 +567,10 @@ __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(Prod
       const int j = e % BM, i = e / BM % AN, n = e / (BM * AN) % WN, m = e / (BM * AN * WN);
       store4<OUT>(p, m0 + m * (TM / WM) + j * 16 + (lane & 15), n0 + n * (TN / WN) + i * 16 + 4 * q, v);
     }
-  } else if (p.whole) {
-    constexpr int kParted = TM * (TN * (int)sizeof(OUT) + 16) <= kLds ? 1 : 2;
+  } else if (Result<OUT>::fused || p.whole) {
+    constexpr int kValue = Result<OUT>::fused ? 4 : (int)sizeof(OUT);
+    constexpr int kParted = TM * (TN * kValue + 16) <= kLds ? 1 : 2;
+    static_assert(TM / kParted * (TN * kValue + 16) <= kLds, "a part of the tile fits");
     store_tile<OUT, TN, TM, WN, WM, kParted>(p, lds, m0, n0, wm, wn, acc);
   } else {
 #pragma unroll
@@ -466,6 +580,14 @@ __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(Prod
       for (int i = 0; i < AN; ++i) store4<OUT>(p, m, n0 + wn * (TN / WN) + i * 16 + 4 * q, acc[i][j]);
     }
   }
+}
+template <typename OUT, int TN, int TM, int WN, int WM, int KG, int ST, int C, bool AHEAD>
+__global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(ProductParams p) {
+  tile_product<OUT, TN, TM, WN, WM, KG, ST, C, AHEAD>(p);
+}
+template <typename OUT, int TN, int TM, int WN, int WM, int KG, int ST, int C, bool AHEAD>
+__global__ __launch_bounds__(64 * WN * WM * KG, 2) void linear_tile_kernel(LinearParams p) {
+  tile_product<Fused<OUT>, TN, TM, WN, WM, KG, ST, C, AHEAD>(p);
 }
 
 // Up to 16 tokens: the weights' stream is the whole work (16 x 24576 x 4096: 26.2 us,
@@ -478,7 +600,7 @@ __global__ __launch_bounds__(64 * WN * WM * KG, 2) void product_tile_kernel(Prod
 // order of k, as long as both operands have the same).  The waves' sums are added
 // through LDS in their order.
 template <typename OUT, int AN, int NW, int U>
-__global__ __launch_bounds__(64 * NW, 2) void product_rows_kernel(ProductParams p) {
+__device__ __forceinline__ void rows_product(Params<OUT> p) {
   __shared__ f32x4 red[NW][AN][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n0 = blockIdx.x * 16 * AN, q = lane >> 4;
@@ -533,20 +655,34 @@ __global__ __launch_bounds__(64 * NW, 2) void product_rows_kernel(ProductParams 
     store4<OUT>(p, lane & 15, n0 + 16 * t + 4 * q, v);
   }
 }
+template <typename OUT, int AN, int NW, int U>
+__global__ __launch_bounds__(64 * NW, 2) void product_rows_kernel(ProductParams p) {
+  rows_product<OUT, AN, NW, U>(p);
+}
+template <typename OUT, int AN, int NW, int U>
+__global__ __launch_bounds__(64 * NW, 2) void linear_rows_kernel(LinearParams p) {
+  rows_product<Fused<OUT>, AN, NW, U>(p);
+}
 
 template <typename OUT, int AN, int NW, int U>
-hipError_t launch_rows(const ProductParams& p, hipStream_t s) {
-  hipLaunchKernelGGL((product_rows_kernel<OUT, AN, NW, U>), dim3((unsigned)((p.N + 16 * AN - 1) / (16 * AN))), dim3(64 * NW),
-                     0, s, p);
+hipError_t launch_rows(const Params<OUT>& p, hipStream_t s) {
+  const dim3 grid((unsigned)((p.N + 16 * AN - 1) / (16 * AN)));
+  using T = typename Result<OUT>::type;
+  if constexpr (Result<OUT>::fused) hipLaunchKernelGGL((linear_rows_kernel<T, AN, NW, U>), grid, dim3(64 * NW), 0, s, p);
+  else hipLaunchKernelGGL((product_rows_kernel<T, AN, NW, U>), grid, dim3(64 * NW), 0, s, p);
   return hipGetLastError();
 }
 
 template <typename OUT, int TN, int TM, int WN, int WM, int KG, int ST, int C, bool AHEAD>
-hipError_t launch_tiles(ProductParams p, hipStream_t s) {
+hipError_t launch_tiles(Params<OUT> p, hipStream_t s) {
   p.n_ntiles = (p.N + TN - 1) / TN;
   p.n_mtiles = (p.M + TM - 1) / TM;
-  hipLaunchKernelGGL((product_tile_kernel<OUT, TN, TM, WN, WM, KG, ST, C, AHEAD>), dim3((unsigned)(p.n_ntiles * (int64_t)p.n_mtiles)),
-                     dim3(64 * WN * WM * KG), 0, s, p);
+  const dim3 grid((unsigned)(p.n_ntiles * (int64_t)p.n_mtiles)), threads(64 * WN * WM * KG);
+  using T = typename Result<OUT>::type;
+  if constexpr (Result<OUT>::fused)
+    hipLaunchKernelGGL((linear_tile_kernel<T, TN, TM, WN, WM, KG, ST, C, AHEAD>), grid, threads, 0, s, p);
+  else
+    hipLaunchKernelGGL((product_tile_kernel<T, TN, TM, WN, WM, KG, ST, C, AHEAD>), grid, threads, 0, s, p);
   return hipGetLastError();
 }
 
@@ -565,7 +701,7 @@ template <typename OUT>
 struct Variant {
   int tn, tm, kg;
   float turn, round;
-  hipError_t (*launch)(ProductParams, hipStream_t);
+  hipError_t (*launch)(Params<OUT>, hipStream_t);
 };
 constexpr int kCus = 256;
 template <typename OUT>
@@ -575,7 +711,7 @@ float cost(const Variant<OUT>& v, const ProductParams& p) {
 }
 
 template <typename OUT>
-hipError_t launch_product(const ProductParams& p, hipStream_t s) {
+hipError_t launch_product(const Params<OUT>& p, hipStream_t s) {
   // Up to 16 tokens: 16 outputs a workgroup while that is needed to have workgroups for the CUs, 32 from there on.
   // With 16 / 32, M 1, 8 and 16, K 2048, 4096 and 13824, weights from the cache: N = 4096, K = 4096 4.8 / 6.4, 6.0 / 7.8,
   // 7.0 / 8.9 us; N = 5120, K = 13824 18.2 / 16.3, 24.5 / 19.0, 29.8 / 21.8; every K and N 1024 .. 24576, from HBM too,
@@ -596,12 +732,7 @@ hipError_t launch_product(const ProductParams& p, hipStream_t s) {
   return best->launch(p, s);
 }
 
-}  // namespace
-}  // namespace acrl
-
-extern "C" {
-
-acrl_status acrl_matmul_fp8(const acrl_matmul_desc* d, void* stream) {
+acrl_status validate_product(const acrl_matmul_desc* d) {
   ACRL_REQUIRE(d, "desc is NULL");
   ACRL_REQUIRE(d->M >= 0 && d->M < ((int64_t)1 << 26), "M = %lld out of range", (long long)d->M);
   ACRL_REQUIRE(d->N > 0 && d->N < ((int64_t)1 << 26), "N = %lld out of range", (long long)d->N);
@@ -612,15 +743,18 @@ acrl_status acrl_matmul_fp8(const acrl_matmul_desc* d, void* stream) {
   // a launch holds fewer than 2^32 threads
   ACRL_REQUIRE(((d->M + 127) / 128) * ((d->N + 127) / 128) < ((int64_t)1 << 23), "M x N too large");
   ACRL_REQUIRE(d->wq && d->w_scales, "wq and w_scales are required");
-  ACRL_REQUIRE(acrl::aligned16(d->wq) && ((uintptr_t)d->w_scales & 3u) == 0, "wq or w_scales is misaligned");
+  ACRL_REQUIRE(aligned16(d->wq) && ((uintptr_t)d->w_scales & 3u) == 0, "wq or w_scales is misaligned");
   if (d->M > 0) {
     ACRL_REQUIRE(d->xq && d->x_scales && d->y, "xq, x_scales and y are required");
-    ACRL_REQUIRE(acrl::aligned16(d->xq) && acrl::aligned16(d->y) && ((uintptr_t)d->x_scales & 3u) == 0,
+    ACRL_REQUIRE(aligned16(d->xq) && aligned16(d->y) && ((uintptr_t)d->x_scales & 3u) == 0,
                  "xq, y or x_scales is misaligned");
   }
-  acrl_status st = acrl::check_device();
-  if (st != ACRL_OK || d->M == 0) return st;
-  acrl::ProductParams p{};
+  return ACRL_OK;
+}
+
+template <typename P>
+P product_params(const acrl_matmul_desc* d) {
+  P p{};
   p.x = static_cast<const uint8_t*>(d->xq);
   p.xs = d->x_scales;
   p.w = static_cast<const uint8_t*>(d->wq);
@@ -630,19 +764,86 @@ acrl_status acrl_matmul_fp8(const acrl_matmul_desc* d, void* stream) {
   p.M = (int)d->M;
   p.N = (int)d->N;
   p.K = (int)d->K;
-  p.kb = (int)((d->K + acrl::kBlock - 1) / acrl::kBlock);
+  p.kb = (int)((d->K + kBlock - 1) / kBlock);
   p.vec = d->ldy % 4 == 0;
   p.whole = d->ldy % (d->y_type == ACRL_OUT_BF16 ? 8 : 4) == 0;
+  return p;
+}
+
+// Whether a residual's values lie in y's memory without being y's own, value for value.  Rows of the same pitch may
+// interleave (columns of one matrix).
+bool overlaps(const acrl_linear_desc* l) {
+  const acrl_matmul_desc* d = &l->product;
+  const int64_t ys = d->y_type == ACRL_OUT_F32 ? 4 : 2, rs = l->residual_type == ACRL_OUT_F32 ? 4 : 2;
+  const int64_t py = d->ldy * ys, pr = l->ldr * rs;
+  const uintptr_t y = (uintptr_t)d->y, r = (uintptr_t)l->residual;
+  const uintptr_t y_end = y + (uintptr_t)((d->M - 1) * py + d->N * ys), r_end = r + (uintptr_t)((d->M - 1) * pr + d->N * rs);
+  if (r >= y_end || y >= r_end) return false;
+  if (r == y && ys == rs && (py == pr || d->M == 1)) return false;
+  if (py != pr) return true;
+  const int64_t ahead = r >= y ? (int64_t)(r - y) % py : (py - (int64_t)(y - r) % py) % py;  // of r's columns to y's
+  return ahead < d->N * ys || py - ahead < d->N * rs;
+}
+
+}  // namespace
+}  // namespace acrl
+
+extern "C" {
+
+acrl_status acrl_matmul_fp8(const acrl_matmul_desc* d, void* stream) {
+  acrl_status st = acrl::validate_product(d);
+  if (st == ACRL_OK) st = acrl::check_device();
+  if (st != ACRL_OK || d->M == 0) return st;
+  const acrl::ProductParams p = acrl::product_params<acrl::ProductParams>(d);
   const hipStream_t s = (hipStream_t)stream;
   return acrl::hip_status(
       d->y_type == ACRL_OUT_BF16 ? acrl::launch_product<__bf16>(p, s) : acrl::launch_product<float>(p, s),
       "acrl_matmul_fp8 launch");
 }
 
+acrl_status acrl_linear_fp8(const acrl_linear_desc* l, void* stream) {
+  ACRL_REQUIRE(l, "desc is NULL");
+  const acrl_matmul_desc* d = &l->product;
+  acrl_status st = acrl::validate_product(d);
+  if (st != ACRL_OK) return st;
+  ACRL_REQUIRE(l->activation >= ACRL_ACT_NONE && l->activation <= ACRL_ACT_GELU_TANH, "activation %d unknown", l->activation);
+  if (l->bias) {
+    ACRL_REQUIRE(l->bias_type == ACRL_OUT_BF16 || l->bias_type == ACRL_OUT_F32, "bias_type %d unknown", l->bias_type);
+    ACRL_REQUIRE(acrl::aligned16(l->bias), "bias must be 16-byte aligned");
+  }
+  if (l->residual) {
+    ACRL_REQUIRE(l->residual_type == ACRL_OUT_BF16 || l->residual_type == ACRL_OUT_F32, "residual_type %d unknown",
+                 l->residual_type);
+    const int64_t most = (int64_t)1 << 34;  // (so that bytes of whole matrices fit 63 bits)
+    ACRL_REQUIRE(l->ldr >= d->N && l->ldr < most && d->ldy < most, "ldr = %lld must lie in [N, 2^34), ldy = %lld below it",
+                 (long long)l->ldr, (long long)d->ldy);
+    ACRL_REQUIRE(acrl::aligned16(l->residual), "residual must be 16-byte aligned");
+    ACRL_REQUIRE(d->M == 0 || !acrl::overlaps(l), "the residual overlaps y without being y itself");
+  }
+  st = acrl::check_device();
+  if (st != ACRL_OK || d->M == 0) return st;
+  acrl::LinearParams p = acrl::product_params<acrl::LinearParams>(d);
+  p.bias = l->bias;
+  p.bias_f32 = l->bias_type == ACRL_OUT_F32;
+  p.res = l->residual;
+  p.ldr = l->ldr;
+  p.res_f32 = l->residual_type == ACRL_OUT_F32;
+  p.res_vec = l->ldr % (p.res_f32 ? 4 : 8) == 0;
+  p.act = l->activation;
+  const hipStream_t s = (hipStream_t)stream;
+  return acrl::hip_status(d->y_type == ACRL_OUT_BF16 ? acrl::launch_product<acrl::Fused<__bf16>>(p, s)
+                                                     : acrl::launch_product<acrl::Fused<float>>(p, s),
+                          "acrl_linear_fp8 launch");
+}
+
 void acrl_abi_operator_struct_sizes(size_t* matmul_desc, size_t* policy_loss_desc, size_t* preference_desc) {
   if (matmul_desc) *matmul_desc = sizeof(acrl_matmul_desc);
   if (policy_loss_desc) *policy_loss_desc = sizeof(acrl_policy_loss_desc);
   if (preference_desc) *preference_desc = sizeof(acrl_preference_desc);
+}
+
+void acrl_abi_decode_struct_sizes(size_t* linear_desc) {
+  if (linear_desc) *linear_desc = sizeof(acrl_linear_desc);
 }
 
 }  // extern "C"

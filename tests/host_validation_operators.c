@@ -77,6 +77,37 @@ static acrl_policy_loss_desc policy(void) {
   return d;
 }
 
+static void linears(void) {
+  acrl_linear_desc d;
+  size_t sz = 0;
+  acrl_abi_decode_struct_sizes(&sz);
+  acrl_abi_decode_struct_sizes(NULL);
+  if (sz != sizeof d) ++failures;
+  expect("linear null", acrl_linear_fp8(NULL, NULL), ACRL_ERR_INVALID_ARG);
+#define BAD_LINEAR(change)                                                                      \
+  do {                                                                                          \
+    memset(&d, 0, sizeof d);                                                                    \
+    d.product = matmul(); d.bias = p; d.residual = buf + 4096; d.ldr = 64;                      \
+    change;                                                                                     \
+    expect("linear " #change, acrl_linear_fp8(&d, NULL), ACRL_ERR_INVALID_ARG);                 \
+  } while (0)
+  BAD_LINEAR(d.product.K = 100);
+  BAD_LINEAR(d.product.y = NULL);
+  BAD_LINEAR(d.activation = ACRL_ACT_GELU_TANH + 1);
+  BAD_LINEAR(d.activation = -1);
+  BAD_LINEAR(d.bias_type = 2);
+  BAD_LINEAR(d.bias = buf + 8);
+  BAD_LINEAR(d.residual_type = -1);
+  BAD_LINEAR(d.residual = buf + 4100);
+  BAD_LINEAR(d.ldr = 63);
+  BAD_LINEAR(d.ldr = (int64_t)1 << 34);
+  BAD_LINEAR(d.product.ldy = (int64_t)1 << 34);
+  BAD_LINEAR(d.residual = buf + 64);                           /* inside y's rows */
+  BAD_LINEAR(d.residual = buf + 128);                          /* y's second row */
+  BAD_LINEAR(d.residual = p; d.ldr = 128);                     /* y with other rows */
+  BAD_LINEAR(d.residual = p; d.residual_type = ACRL_OUT_F32);  /* y as another type */
+}
+
 static void policy_losses(void) {
   acrl_policy_loss_desc d;
   size_t nb = 0;
@@ -164,6 +195,7 @@ int main(void) {
     ++failures;
   quantize_blocks();
   products();
+  linears();
   policy_losses();
   preference_losses();
   reduces();

@@ -570,8 +570,8 @@ acrl_status acrl_matmul_fp8(const acrl_matmul_desc* desc, void* stream);
  * enter in fp32 and y is rounded once.  With the sums S = x W^T + bias:
  *   NONE S;  RELU max(S, 0);  SILU S / (1 + e^-S);  GELU S Phi(S), Phi the normal
  *   distribution function;  GELU_TANH S (1 + tanh(sqrt(2/pi) (S + 0.044715 S^3))) / 2
- * each within 6e-7 of its exact value at S, relative to its size, or within
- * 1.3e-36.  NaN stays NaN.
+ * each within 6e-7 of its exact value at S, relative to its size (5e-5 where y
+ * is bf16), or within 1.3e-36.  NaN stays NaN.
  *   bias      [N] of bias_type, or NULL
  *   residual  [M, N] of residual_type, rows ldr elements apart, or NULL.  It may
  *             be y itself (same pointer, type and row distance): y is then updated
@@ -599,6 +599,82 @@ typedef struct acrl_linear_desc {
 } acrl_linear_desc;
 
 acrl_status acrl_linear_fp8(const acrl_linear_desc* desc, void* stream);
+
+/* ======================================================================== */
+/* acrl_moe_fp8 -- a mixture-of-experts layer for a few tokens               */
+/* ======================================================================== *
+ * A decode step's layer of an inference policy with experts (Sec. 5.4 rolls one
+ * out): router, choice, the experts' gated products and their weighted sum.
+ * For a token t with mask[t] != 0 (all tokens without a mask):
+ *   l_e = sum_i x[t, i] router[e, i], summed in 64 bits
+ *   s_e = SOFTMAX e^l_e / sum_f e^l_f; SIGMOID 1 / (1 + e^-l_e), in 64 bits
+ *   chosen: the top_k experts of largest s_e + select_bias[e] (without a bias: of
+ *     largest l_e), in falling order, equal ones by their index, NaN as the lowest
+ *   w_j = s of the j-th (renormalize: over their sum, 0 if that is 0) times scale,
+ *     rounded to fp32
+ *   y[t] = sum_j w_j Wout[e_j] (act(Wgate[e_j] x[t]) * (Wup[e_j] x[t])) + residual[t]
+ * in the order of j.  Masked tokens have ids -1, weights 0 and y = residual (0
+ * without one), and what their rows of x hold has no influence; experts that no
+ * token chose are not read.
+ * Weights are E4M3 with one scale per 128 x 128 block (ACRL_SCALE_BLOCK128 of each
+ * expert's matrix), x stays bf16; sums are fp32, what lies between the products
+ * keeps 16 bits and more.  y is rounded once.
+ *   x         bf16 [T, d], rows ldx elements apart
+ *   router    bf16 [E, d], or NULL: ids and weights are inputs (a routing made
+ *             earlier, taken over as it is; ids outside [0, E) add nothing, the
+ *             same expert may come twice), and score, renormalize, scale and
+ *             select_bias are not used
+ *   select_bias float [E], or NULL
+ *   mask      uint8 [T], or NULL
+ *   w_in      e4m3 [E, 2 F, d]: an expert's F gate rows, then its F up rows;
+ *             s_in float [E, ceil(2F/128), ceil(d/128)]
+ *   w_out     e4m3 [E, d, F], s_out float [E, ceil(d/128), ceil(F/128)]
+ *   residual  [T, d] of residual_type, rows ldr apart, or NULL; it may be y itself,
+ *             or columns beside y's as in acrl_linear_fp8
+ *   y         [T, d] of y_type, rows ldy apart; columns from d on are not written
+ *   ids       int32 [T, top_k], weights float [T, top_k]
+ * Equal calls give equal bits; a token alone and among others differs by fp32
+ * roundings of sums at most.
+ * Requirements: 0 <= T <= 128; d and F positive multiples of 32, at most 65536;
+ * E <= 512; top_k <= 16 and <= E; ldx a multiple of 8, ldx, ldr and ldy in [d, 2^34);
+ * x, router, w_in, w_out and the workspace 16-byte aligned, the others 4-byte;
+ * |scale| < 1e30.
+ */
+typedef enum { ACRL_MOE_SOFTMAX = 0, ACRL_MOE_SIGMOID = 1 } acrl_moe_score;
+
+typedef struct acrl_moe_desc {
+  int64_t T;                    /* tokens                                                   */
+  int64_t d;                    /* hidden size                                              */
+  int64_t E;                    /* experts                                                  */
+  int64_t top_k;                /* experts of a token                                       */
+  int64_t F;                    /* width of an expert                                       */
+  const void* x;
+  int64_t ldx;
+  const void* router;           /* optional                                                 */
+  const float* select_bias;     /* optional                                                 */
+  const uint8_t* mask;          /* optional                                                 */
+  const void* w_in;
+  const float* s_in;
+  const void* w_out;
+  const float* s_out;
+  const void* residual;         /* optional                                                 */
+  int64_t ldr;
+  void* y;                      /* out                                                      */
+  int64_t ldy;
+  int32_t* ids;                 /* out; in without a router                                 */
+  float* weights;               /* out; in without a router                                 */
+  int32_t residual_type;        /* acrl_out_type                                            */
+  int32_t y_type;               /* acrl_out_type                                            */
+  int32_t score;                /* acrl_moe_score                                           */
+  int32_t renormalize;
+  int32_t activation;           /* acrl_activation, of the gate                             */
+  float scale;
+  void* workspace;
+  size_t workspace_bytes;
+} acrl_moe_desc;
+
+acrl_status acrl_moe_workspace_size(int64_t T, int64_t d, int64_t E, int64_t top_k, int64_t F, size_t* bytes);
+acrl_status acrl_moe_fp8(const acrl_moe_desc* desc, void* stream);
 
 /* ======================================================================== */
 /* acrl_policy_loss -- clipped policy loss with a KL term, and its gradient   */
@@ -736,7 +812,7 @@ acrl_status acrl_preference_loss(const acrl_preference_desc* desc, void* stream)
 void acrl_abi_operator_struct_sizes(size_t* matmul_desc, size_t* policy_loss_desc, size_t* preference_desc);
 
 /* The same for the descriptors of a decode step's operators.                */
-void acrl_abi_decode_struct_sizes(size_t* linear_desc);
+void acrl_abi_decode_struct_sizes(size_t* linear_desc, size_t* moe_desc);
 
 /* Host helper (host pointers): the reference discrepancy X of Sec. 4.1 is the
  * mean of Y_g over the non-empty groups (group_nseq > 0) of the step-0

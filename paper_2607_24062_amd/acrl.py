@@ -28,6 +28,7 @@ OUT_BF16, OUT_F32 = 0, 1
 KL_K1, KL_K2, KL_K3 = 0, 1, 2
 AGG_GROUP, AGG_SEQUENCE, AGG_TOKEN, AGG_CONSTANT = 0, 1, 2, 3
 PREF_SIGMOID, PREF_HINGE, PREF_SQUARED = 0, 1, 2
+MOE_SOFTMAX, MOE_SIGMOID = 0, 1
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2, 3, 4
 N_STATS = 10
 STAT_NAMES = ["y_batch", "tok_mean_d", "tok_max_d", "tok_std_d", "mean_h_pi", "mean_h_mu",
@@ -46,7 +47,7 @@ EXPORTED = [
     "acrl_backward_workspace_size", "acrl_lm_head_backward",
     "acrl_matmul_fp8", "acrl_policy_loss_workspace_size", "acrl_policy_loss",
     "acrl_preference_loss_workspace_size", "acrl_preference_loss", "acrl_abi_operator_struct_sizes",
-    "acrl_linear_fp8", "acrl_abi_decode_struct_sizes",
+    "acrl_linear_fp8", "acrl_moe_workspace_size", "acrl_moe_fp8", "acrl_abi_decode_struct_sizes",
 ]
 
 _P = ctypes.c_void_p
@@ -118,6 +119,14 @@ class MatmulDesc(ctypes.Structure):
 class LinearDesc(ctypes.Structure):
     _fields_ = [("product", MatmulDesc), ("bias", _P), ("residual", _P), ("ldr", _I64), ("bias_type", _I32),
                 ("residual_type", _I32), ("activation", _I32)]
+
+
+class MoeDesc(ctypes.Structure):
+    _fields_ = [("T", _I64), ("d", _I64), ("E", _I64), ("top_k", _I64), ("F", _I64), ("x", _P), ("ldx", _I64),
+                ("router", _P), ("select_bias", _P), ("mask", _P), ("w_in", _P), ("s_in", _P), ("w_out", _P), ("s_out", _P),
+                ("residual", _P), ("ldr", _I64), ("y", _P), ("ldy", _I64), ("ids", _P), ("weights", _P),
+                ("residual_type", _I32), ("y_type", _I32), ("score", _I32), ("renormalize", _I32), ("activation", _I32),
+                ("scale", _F32), ("workspace", _P), ("workspace_bytes", _SZ)]
 
 
 class PolicyLossDesc(ctypes.Structure):
@@ -215,15 +224,19 @@ def lib() -> ctypes.CDLL:
         L.acrl_linear_fp8.restype = _I32
         L.acrl_linear_fp8.argtypes = [ctypes.POINTER(LinearDesc), _P]
         L.acrl_abi_decode_struct_sizes.restype = None
-        L.acrl_abi_decode_struct_sizes.argtypes = [ctypes.POINTER(_SZ)] * 1
-        sizes = [_SZ() for _ in range(10)]
+        L.acrl_abi_decode_struct_sizes.argtypes = [ctypes.POINTER(_SZ)] * 2
+        L.acrl_moe_workspace_size.restype = _I32
+        L.acrl_moe_workspace_size.argtypes = [_I64] * 5 + [ctypes.POINTER(_SZ)]
+        L.acrl_moe_fp8.restype = _I32
+        L.acrl_moe_fp8.argtypes = [ctypes.POINTER(MoeDesc), _P]
+        sizes = [_SZ() for _ in range(11)]
         L.acrl_abi_struct_sizes(*[ctypes.byref(s) for s in sizes[:6]])
         L.acrl_abi_operator_struct_sizes(*[ctypes.byref(s) for s in sizes[6:9]])
         L.acrl_abi_decode_struct_sizes(*[ctypes.byref(s) for s in sizes[9:]])
         want = [ctypes.sizeof(ScoreDesc), ctypes.sizeof(ReduceDesc), ctypes.sizeof(ControllerDesc),
                 ctypes.sizeof(SampleDesc), ctypes.sizeof(SurrogateDesc), ctypes.sizeof(BackwardDesc),
                 ctypes.sizeof(MatmulDesc), ctypes.sizeof(PolicyLossDesc), ctypes.sizeof(PreferenceDesc),
-                ctypes.sizeof(LinearDesc)]
+                ctypes.sizeof(LinearDesc), ctypes.sizeof(MoeDesc)]
         got = [s.value for s in sizes]
         if got != want:
             raise RuntimeError("libacrl descriptor layout mismatch: library %s, binding %s" % (got, want))
@@ -720,6 +733,58 @@ def acrl_linear_fp8(xq, x_scales, wq, w_scales, bias=None, activation: int = ACT
         desc.residual, desc.residual_type = residual.data_ptr(), _OUT_TYPES[residual.dtype]
     _check(lib().acrl_linear_fp8(ctypes.byref(desc), _raw_stream(stream, xq.device)), "acrl_linear_fp8")
     return out
+
+
+# ------------------------------------------------------------------ mixture of experts
+def acrl_moe_fp8(x, w_in, s_in, w_out, s_out, top_k: int, router=None, score: int = MOE_SOFTMAX, select_bias=None,
+                 renormalize: bool = True, scale: float = 1.0, activation: int = ACT_SILU, mask=None, residual=None,
+                 ids=None, weights=None, out=None, out_dtype=torch.bfloat16, stream=None):
+    """A mixture-of-experts layer for up to 128 tokens: x bf16 [T, d] (rows may
+    lie apart), w_in uint8 [E, 2 F, d] (gate rows, then up rows) and w_out uint8
+    [E, d, F] with the SCALE_BLOCK128 scales of each expert's matrix, router bf16
+    [E, d].  Returns (y [T, d], ids int32 [T, top_k], weights float32 [T, top_k]);
+    without a router `ids` and `weights` are inputs (the routing of an earlier
+    call).  `out` and `residual` may be column slices of wider matrices, and the
+    same tensor."""
+    if x.dim() != 2 or w_in.dim() != 3 or w_out.dim() != 3:
+        raise ValueError("x [T, d], w_in [E, 2 F, d] and w_out [E, d, F] are required")
+    T, d = x.shape
+    E, F = w_in.shape[0], w_out.shape[2]
+    if tuple(w_in.shape) != (E, 2 * F, d) or tuple(w_out.shape) != (E, d, F):
+        raise ValueError("w_in %s and w_out %s do not fit x's %d columns" % (tuple(w_in.shape), tuple(w_out.shape), d))
+    index, dev, f32, kb = _index_of(w_in, torch.uint8, "w_in", stream), x.device, torch.float32, (d + 127) // 128
+    if x.dtype is not torch.bfloat16 or x.get_device() != index or (d > 1 and x.stride(1) != 1) or (T > 1 and x.stride(0) < d):
+        raise ValueError("x must be a bf16 matrix on cuda:%d with unit column stride" % index)
+    if router is None and (ids is None or weights is None):
+        raise ValueError("a router, or ids and weights, are required")
+    nbytes = _size("acrl_moe_workspace_size", T, d, E, top_k, F)
+    desc = MoeDesc(T, d, E, top_k, F, x.data_ptr(), x.stride(0) if T > 1 else (d + 7) // 8 * 8,
+                   _want(router, torch.bfloat16, E * d, index, "router", True),
+                   _want(select_bias, f32, E, index, "select_bias", True), _want(mask, torch.uint8, T, index, "mask", True),
+                   w_in.data_ptr(), _want(s_in, f32, E * ((2 * F + 127) // 128) * kb, index, "s_in"),
+                   _want(w_out, torch.uint8, E * d * F, index, "w_out"),
+                   _want(s_out, f32, E * kb * ((F + 127) // 128), index, "s_out"),
+                   score=score, renormalize=1 if renormalize else 0, activation=activation, scale=scale)
+    if residual is not None:
+        desc.ldr = _matrix(residual, T, d, index, "residual")
+        desc.residual, desc.residual_type = residual.data_ptr(), _OUT_TYPES[residual.dtype]
+    if out is None:
+        if out_dtype not in _OUT_TYPES:
+            raise ValueError("out_dtype must be torch.bfloat16 or torch.float32, got %s" % out_dtype)
+        out, desc.ldy = _empty((T, d), out_dtype, dev, stream), d
+    else:
+        desc.ldy = _matrix(out, T, d, index, "out")
+    desc.y, desc.y_type = out.data_ptr(), _OUT_TYPES[out.dtype]
+    if ids is None:
+        ids = _empty((T, top_k), torch.int32, dev, stream)
+    if weights is None:
+        weights = _empty((T, top_k), f32, dev, stream)
+    desc.ids, desc.weights = _want(ids, torch.int32, T * top_k, index, "ids"), _want(weights, f32, T * top_k, index, "weights")
+    if nbytes:
+        ws = _empty(nbytes, torch.uint8, dev, stream)
+        desc.workspace, desc.workspace_bytes = ws.data_ptr(), nbytes
+    _check(lib().acrl_moe_fp8(ctypes.byref(desc), _raw_stream(stream, dev)), "acrl_moe_fp8")
+    return out, ids, weights
 
 
 # ------------------------------------------------------------------ losses beside the surrogate

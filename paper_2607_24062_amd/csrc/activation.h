@@ -1,9 +1,14 @@
 // activation.h -- the activations of acrl_linear_fp8 and acrl_moe_fp8, in fp32.
 //
-// Within 6e-7 of the exact value, relative to its size, or within 1.3e-36 (the
-// reciprocal of 1 + e^-s is 0 below fp32's normal range, 1.2e-38, and meets a
-// value of at most 104 there): what a bf16 result's half step does not show.
+// FINE: within 6e-7 of the exact value, relative to its size, or within 1.3e-36
+// (the reciprocal of 1 + e^-s is 0 below fp32's normal range, 1.2e-38, and meets a
+// value of at most 104 there).  Otherwise, for results that become bf16 (half a
+// step: 2e-3 .. 4e-3): within 5e-5, or 1.3e-36, by half the instructions, which
+// stand after a product with nothing to hide them (8192 x 13824 x 5120, bf16 out: GELU
+// 590 -> 578 us, GELU_TANH 601 -> 559, SILU 554 -> 529; 511 with no activation).
 #pragma once
+
+#include <type_traits>
 
 #include "acrl_internal.h"
 
@@ -13,7 +18,9 @@ namespace acrl {
 
 // e^x.  The product with log2(e) is kept in two parts: rounded to one fp32 it
 // would be off by |x| 2^-24, and the result, relatively, by as much.
+template <bool FINE = true>
 __device__ __forceinline__ float exp_f32(float x) {
+  if (!FINE) return __builtin_amdgcn_exp2f(x * kLog2e);
   const float t = x * kLog2e;
   const float rest = fmaf(x, 1.9259629911266174e-8f, fmaf(x, kLog2e, -t));  // (log2(e) less its fp32 value)
   const float e = __builtin_amdgcn_exp2f(t);
@@ -21,13 +28,26 @@ __device__ __forceinline__ float exp_f32(float x) {
 }
 
 // x / (1 + e^-s)
-__device__ __forceinline__ float times_sigmoid(float x, float s) { return x * __builtin_amdgcn_rcpf(1.0f + exp_f32(-s)); }
+template <bool FINE>
+__device__ __forceinline__ float times_sigmoid(float x, float s) {
+  return x * __builtin_amdgcn_rcpf(1.0f + exp_f32<FINE>(-s));
+}
 
 // erfc(z), z >= 0: e^(-z^2) times a polynomial in 1 / (1 + z / 2), fitted to
 // e^(z^2) erfc(z) over 0 <= z <= 14 for the least relative error (4.3e-8; 3.1e-7 as
-// evaluated in fp32).  square = z^2 in two parts.
+// evaluated in fp32; 3.4e-5 the shorter one).  square = z^2 in two parts.
+template <bool FINE>
 __device__ __forceinline__ float erfc_of(float z, float square, float square_rest) {
   const float t = __builtin_amdgcn_rcpf(fmaf(0.5f, z, 1.0f));
+  if (!FINE) {
+    float p = -0.067427858710289f;
+    p = fmaf(p, t, 0.018588868901133537f);
+    p = fmaf(p, t, 0.27242976427078247f);
+    p = fmaf(p, t, 0.2052343785762787f);
+    p = fmaf(p, t, 0.28950396180152893f);
+    p = fmaf(p, t, 0.2816377282142639f);
+    return p * t * exp_f32<false>(-square);
+  }
   float p = -0.05882089212536812f;
   p = fmaf(p, t, 0.28327813744544983f);
   p = fmaf(p, t, -0.4842751920223236f);
@@ -57,27 +77,37 @@ __device__ __forceinline__ float twice_u(float v, float& rest) {
   return s;
 }
 
-// act(v); the same for all lanes of a wave.
-__device__ __forceinline__ float activate(int act, float v) {
+template <int ACT, bool FINE>
+__device__ __forceinline__ float activate(float v) {
+  if constexpr (ACT == ACRL_ACT_RELU) {
+    return v < 0.0f ? 0.0f : v;
+  } else if constexpr (ACT == ACRL_ACT_SILU) {
+    return times_sigmoid<FINE>(v, v);
+  } else if constexpr (ACT == ACRL_ACT_GELU) {
+    // v Phi(v) = v erfc(-v / sqrt 2) / 2, by erfc of |v| / sqrt 2 on either side: no digits are lost far below 0
+    const float a = fminf(fabsf(v), 20.0f), s = 0.5f * a * a;  // (erfc is 0 in fp32 from 14.2 / sqrt 2 on)
+    const float half = 0.5f * erfc_of<FINE>(0.70710678118654752f * a, s, fmaf(0.5f * a, a, -s));
+    return v * (v < 0.0f ? half : 1.0f - half);
+  } else if constexpr (ACT == ACRL_ACT_GELU_TANH) {
+    // 1 + tanh(u) = 2 / (1 + e^(-2 u)), u = sqrt(2 / pi) (v + 0.044715 v^3)
+    if (!FINE) return times_sigmoid<false>(v, v * fmaf(0.07135481627260025f, v * v, 1.5957691216057308f));
+    float rest;
+    const float s = twice_u(v, rest), e = exp_f32(-s);
+    return v * __builtin_amdgcn_rcpf(1.0f + (fabsf(s) < 87.0f ? fmaf(-e, rest, e) : e));
+  } else {
+    return v;
+  }
+}
+
+// f with the activation as a constant.
+template <typename F>
+__device__ __forceinline__ void for_activation(int act, F&& f) {
   switch (act) {
-    case ACRL_ACT_RELU:
-      return v < 0.0f ? 0.0f : v;
-    case ACRL_ACT_SILU:
-      return times_sigmoid(v, v);
-    case ACRL_ACT_GELU: {
-      // v Phi(v) = v erfc(-v / sqrt 2) / 2, by erfc of |v| / sqrt 2 on either side: no digits are lost far below 0
-      const float a = fminf(fabsf(v), 20.0f), s = 0.5f * a * a;  // (erfc is 0 in fp32 from 14.2 / sqrt 2 on)
-      const float half = 0.5f * erfc_of(0.70710678118654752f * a, s, fmaf(0.5f * a, a, -s));
-      return v * (v < 0.0f ? half : 1.0f - half);
-    }
-    case ACRL_ACT_GELU_TANH: {
-      // 1 + tanh(u) = 2 / (1 + e^(-2 u)), u = sqrt(2 / pi) (v + 0.044715 v^3)
-      float rest;
-      const float s = twice_u(v, rest), e = exp_f32(-s);
-      return v * __builtin_amdgcn_rcpf(1.0f + (fabsf(s) < 87.0f ? fmaf(-e, rest, e) : e));
-    }
-    default:
-      return v;
+    case ACRL_ACT_RELU: f(std::integral_constant<int, ACRL_ACT_RELU>{}); break;
+    case ACRL_ACT_SILU: f(std::integral_constant<int, ACRL_ACT_SILU>{}); break;
+    case ACRL_ACT_GELU: f(std::integral_constant<int, ACRL_ACT_GELU>{}); break;
+    case ACRL_ACT_GELU_TANH: f(std::integral_constant<int, ACRL_ACT_GELU_TANH>{}); break;
+    default: f(std::integral_constant<int, ACRL_ACT_NONE>{});
   }
 }
 

@@ -86,6 +86,9 @@ __device__ __forceinline__ void wait_loads_and_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+// The same with the loads into registers still under way.
+__device__ __forceinline__ void read_lds_and_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // A block's sum, from zero.  The instruction aligns the 128 products to the
 // largest before it adds them and so keeps fewer bits than fp32 sums would: over
 // K = 4096 .. 13824, y before its rounding is 1.4e-5 off for normally distributed
@@ -116,52 +119,59 @@ __device__ __forceinline__ void settle(f32x4 (&acc)[A][B]) {
 template <typename OUT>
 using out4 = OUT __attribute__((ext_vector_type(4)));
 
-// Values at .. at + C - 1 of an array of fp32 or bf16 as fp32; of the first `left` of them alone where that is less than
-// C or the address takes no wide load (the others: 0).
+// C consecutive values of an array of fp32 or bf16, as they are read.  Those that are not there count -0: added to any
+// value, that leaves it as it is.
 template <int C>
-__device__ __forceinline__ void read_values(float (&v)[C], const void* base, bool f32, int64_t at, int left, bool vec) {
-  if (vec && left >= C) {
-    if (f32) {
-      const f32x4* q = reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + at);
+struct Piece {
+  uint32_t raw[C];
+  __device__ __forceinline__ float value(int e, bool f32) const {
+    const float h = e % 2 ? bf16_hi(raw[e / 2]) : bf16_lo(raw[e / 2]);
+    return f32 ? __uint_as_float(raw[e]) : h;
+  }
+  // values at .. at + C - 1, the first `left` of them
+  __device__ __forceinline__ void read(const void* base, bool f32, int64_t at, int left, bool vec) {
+    constexpr uint32_t kNone = 0x80000000u;
+    if (base && left >= C && vec) {
+      const uint32_t* q = static_cast<const uint32_t*>(base) + (f32 ? at : at / 2);
+      using words = uint32_t __attribute__((ext_vector_type(C / 2)));  // (half a piece of fp32, a piece of bf16)
+      const words u = *reinterpret_cast<const words*>(q);
 #pragma unroll
-      for (int i = 0; i < C; ++i) v[i] = q[i / 4][i % 4];
+      for (int i = 0; i < C / 2; ++i) raw[i] = u[i];
+      if (f32) {
+        const words v = *reinterpret_cast<const words*>(q + C / 2);
+#pragma unroll
+        for (int i = 0; i < C / 2; ++i) raw[C / 2 + i] = v[i];
+      }
     } else {
-      using words = uint32_t __attribute__((ext_vector_type(C / 2)));
-      const words q = *reinterpret_cast<const words*>(static_cast<const uint16_t*>(base) + at);
 #pragma unroll
-      for (int i = 0; i < C; ++i) v[i] = i % 2 ? bf16_hi(q[i / 2]) : bf16_lo(q[i / 2]);
-    }
-  } else {
+      for (int i = 0; i < C; ++i) raw[i] = f32 || i % 2 ? kNone : kNone | kNone >> 16;
+      if (!base) return;
+      if (f32) {
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-      v[i] = 0.0f;
-      if (i < left)
-        v[i] = f32 ? static_cast<const float*>(base)[at + i] : bf16_lo(static_cast<const uint16_t*>(base)[at + i]);
+        for (int i = 0; i < C; ++i)
+          if (i < left) raw[i] = static_cast<const uint32_t*>(base)[at + i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < C / 2; ++i) {
+          const uint16_t* q = static_cast<const uint16_t*>(base) + at + 2 * i;
+          const uint32_t lo = 2 * i < left ? q[0] : kNone >> 16, hi = 2 * i + 1 < left ? q[1] : kNone >> 16;
+          raw[i] = hi << 16 | lo;
+        }
+      }
     }
   }
-}
+  // the residual's values n .. n + C - 1 of token m
+  __device__ __forceinline__ void read(const LinearParams& p, int m, int n) {
+    read(m < p.M ? p.res : nullptr, p.res_f32, (int64_t)m * p.ldr + n, p.N - n, p.res_vec);
+  }
+};
 
-// The epilogue on the sums n .. n + C - 1 of token m (n a multiple of C), in fp32.  A residual that is y itself is
-// read by the lane that writes it, before it does.
 template <int C>
-__device__ __forceinline__ void finish(const LinearParams& p, int m, int n, float (&v)[C]) {
-  const int left = p.N - n;
-  float r[C];
-  if (p.res) read_values<C>(r, p.res, p.res_f32, (int64_t)m * p.ldr + n, left, p.res_vec);
-  if (p.bias) {
-    float b[C];
-    read_values<C>(b, p.bias, p.bias_f32, n, left, true);
+__device__ __forceinline__ void read_bias(const LinearParams& p, int n, float (&v)[C]) {
+  Piece<C> b;
+  b.read(p.bias, p.bias_f32, n, p.N - n, true);
 #pragma unroll
-    for (int i = 0; i < C; ++i) v[i] += b[i];
-  }
-  if (p.act != ACRL_ACT_NONE) {
-#pragma unroll
-    for (int i = 0; i < C; ++i) v[i] = activate(p.act, v[i]);
-  }
-  if (p.res) {
-#pragma unroll
-    for (int i = 0; i < C; ++i) v[i] += r[i];
-  }
+  for (int e = 0; e < C; ++e) v[e] = b.value(e, p.bias_f32);
 }
 
 // Four consecutive outputs n .. n + 3 of token m.
@@ -170,9 +180,15 @@ __device__ __forceinline__ void store4(const Params<RES>& p, int m, int n, f32x4
   using OUT = typename Result<RES>::type;
   if (m >= p.M || n >= p.N) return;
   if constexpr (Result<RES>::fused) {
-    float f[4] = {v[0], v[1], v[2], v[3]};
-    finish(p, m, n, f);
-    v = f32x4{f[0], f[1], f[2], f[3]};
+    // (in fp32.  A residual that is y itself is read by the lane that writes it, before it does)
+    Piece<4> r;
+    r.read(p, m, n);
+    float b[4];
+    read_bias(p, n, b);
+    for_activation(p.act, [&](auto act) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = activate<decltype(act)::value, std::is_same<OUT, float>::value>(v[e] + b[e]) + r.value(e, p.res_f32);
+    });
   }
   OUT* y = static_cast<OUT*>(p.y) + (int64_t)m * p.ldy + n;
   const out4<OUT> o = __builtin_convertvector(v, out4<OUT>);
@@ -199,9 +215,21 @@ __device__ __forceinline__ void store_tile(const Params<RES>& p, uint8_t* lds, i
   constexpr int kThreads = 64 * WN * WM, kRows = TM / PARTS;
   static_assert(WM % PARTS == 0 && kRows * kPieces % kThreads == 0, "whole parts");
   const int lane = threadIdx.x & 63, q = lane >> 4;
+  // A lane's column is the same in every row it writes: its bias comes once, and the residual's pieces of a part are
+  // under way while the sums pass through LDS (8192 x 13824 x 5120, each piece read where it is added: 626 us).
+  constexpr int kIter = kRows * kPieces / kThreads;
+  static_assert(!Result<RES>::fused || kThreads % kPieces == 0, "a lane keeps its column");
+  const int c = threadIdx.x % kPieces, n = n0 + c * kPiece;
+  float bias[kPiece];
+  Piece<kPiece> res[Result<RES>::fused ? kIter : 1];
+  if constexpr (Result<RES>::fused) read_bias<kPiece>(p, n, bias);
 #pragma unroll
   for (int part = 0; part < PARTS; ++part) {
-    wait_loads_and_barrier<0>();
+    if constexpr (Result<RES>::fused) {
+#pragma unroll
+      for (int k = 0; k < kIter; ++k) res[k].read(p, m0 + part * kRows + (k * kThreads + (int)threadIdx.x) / kPieces, n);
+    }
+    read_lds_and_barrier();
     if (wm / (WM / PARTS) == part) {
 #pragma unroll
       for (int j = 0; j < B; ++j)
@@ -213,20 +241,16 @@ __device__ __forceinline__ void store_tile(const Params<RES>& p, uint8_t* lds, i
     }
     __syncthreads();
     if constexpr (Result<RES>::fused) {
-#pragma unroll 1
-      for (int k = 0; k < kRows * kPieces / kThreads; ++k) {
-        const int at = k * kThreads + threadIdx.x, r = at / kPieces, c = at % kPieces;
-        const int m = m0 + part * kRows + r, n = n0 + c * kPiece;
-        if (m >= p.M || n >= p.N) continue;
+      const auto row = [&](auto act, int k) {
+        const int r = (k * kThreads + threadIdx.x) / kPieces, m = m0 + part * kRows + r;
+        if (m >= p.M || n >= p.N) return;
         const f32x4* from = reinterpret_cast<const f32x4*>(lds + r * kPitch + c * kPiece * sizeof(float));
-        float v[kPiece];
-#pragma unroll
-        for (int e = 0; e < kPiece; ++e) v[e] = from[e / 4][e % 4];
-        finish(p, m, n, v);
-        OUT* y = static_cast<OUT*>(p.y) + (int64_t)m * p.ldy + n;
         OUT o[kPiece];
 #pragma unroll
-        for (int e = 0; e < kPiece; ++e) o[e] = (OUT)v[e];
+        for (int e = 0; e < kPiece; ++e)
+          o[e] = (OUT)(activate<decltype(act)::value, std::is_same<OUT, float>::value>(from[e / 4][e % 4] + bias[e]) +
+                       res[k].value(e, p.res_f32));
+        OUT* y = static_cast<OUT*>(p.y) + (int64_t)m * p.ldy + n;
         if (p.whole && n + kPiece <= p.N) {
           *reinterpret_cast<i32x4*>(y) = __builtin_bit_cast(i32x4, o);
         } else {
@@ -234,7 +258,11 @@ __device__ __forceinline__ void store_tile(const Params<RES>& p, uint8_t* lds, i
           for (int e = 0; e < kPiece; ++e)
             if (n + e < p.N) y[e] = o[e];
         }
-      }
+      };
+      for_activation(p.act, [&](auto act) {
+#pragma unroll
+        for (int k = 0; k < kIter; ++k) row(act, k);
+      });
       continue;
     }
 #pragma unroll
@@ -770,21 +798,6 @@ P product_params(const acrl_matmul_desc* d) {
   return p;
 }
 
-// Whether a residual's values lie in y's memory without being y's own, value for value.  Rows of the same pitch may
-// interleave (columns of one matrix).
-bool overlaps(const acrl_linear_desc* l) {
-  const acrl_matmul_desc* d = &l->product;
-  const int64_t ys = d->y_type == ACRL_OUT_F32 ? 4 : 2, rs = l->residual_type == ACRL_OUT_F32 ? 4 : 2;
-  const int64_t py = d->ldy * ys, pr = l->ldr * rs;
-  const uintptr_t y = (uintptr_t)d->y, r = (uintptr_t)l->residual;
-  const uintptr_t y_end = y + (uintptr_t)((d->M - 1) * py + d->N * ys), r_end = r + (uintptr_t)((d->M - 1) * pr + d->N * rs);
-  if (r >= y_end || y >= r_end) return false;
-  if (r == y && ys == rs && (py == pr || d->M == 1)) return false;
-  if (py != pr) return true;
-  const int64_t ahead = r >= y ? (int64_t)(r - y) % py : (py - (int64_t)(y - r) % py) % py;  // of r's columns to y's
-  return ahead < d->N * ys || py - ahead < d->N * rs;
-}
-
 }  // namespace
 }  // namespace acrl
 
@@ -818,7 +831,8 @@ acrl_status acrl_linear_fp8(const acrl_linear_desc* l, void* stream) {
     ACRL_REQUIRE(l->ldr >= d->N && l->ldr < most && d->ldy < most, "ldr = %lld must lie in [N, 2^34), ldy = %lld below it",
                  (long long)l->ldr, (long long)d->ldy);
     ACRL_REQUIRE(acrl::aligned16(l->residual), "residual must be 16-byte aligned");
-    ACRL_REQUIRE(d->M == 0 || !acrl::overlaps(l), "the residual overlaps y without being y itself");
+    ACRL_REQUIRE(!acrl::overlaps(l->residual, l->ldr, l->residual_type, d->y, d->ldy, d->y_type, d->M, d->N),
+                 "the residual overlaps y without being y itself");
   }
   st = acrl::check_device();
   if (st != ACRL_OK || d->M == 0) return st;
@@ -842,8 +856,9 @@ void acrl_abi_operator_struct_sizes(size_t* matmul_desc, size_t* policy_loss_des
   if (preference_desc) *preference_desc = sizeof(acrl_preference_desc);
 }
 
-void acrl_abi_decode_struct_sizes(size_t* linear_desc) {
+void acrl_abi_decode_struct_sizes(size_t* linear_desc, size_t* moe_desc) {
   if (linear_desc) *linear_desc = sizeof(acrl_linear_desc);
+  if (moe_desc) *moe_desc = sizeof(acrl_moe_desc);
 }
 
 }  // extern "C"

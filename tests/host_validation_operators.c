@@ -79,10 +79,10 @@ static acrl_policy_loss_desc policy(void) {
 
 static void linears(void) {
   acrl_linear_desc d;
-  size_t sz = 0;
-  acrl_abi_decode_struct_sizes(&sz);
-  acrl_abi_decode_struct_sizes(NULL);
-  if (sz != sizeof d) ++failures;
+  size_t sz[2] = {0};
+  acrl_abi_decode_struct_sizes(&sz[0], &sz[1]);
+  acrl_abi_decode_struct_sizes(NULL, NULL);
+  if (sz[0] != sizeof d || sz[1] != sizeof(acrl_moe_desc)) ++failures;
   expect("linear null", acrl_linear_fp8(NULL, NULL), ACRL_ERR_INVALID_ARG);
 #define BAD_LINEAR(change)                                                                      \
   do {                                                                                          \
@@ -106,6 +106,59 @@ static void linears(void) {
   BAD_LINEAR(d.residual = buf + 128);                          /* y's second row */
   BAD_LINEAR(d.residual = p; d.ldr = 128);                     /* y with other rows */
   BAD_LINEAR(d.residual = p; d.residual_type = ACRL_OUT_F32);  /* y as another type */
+}
+
+static void experts(void) {
+  acrl_moe_desc d;
+  size_t nb = 0;
+  expect("moe ws", acrl_moe_workspace_size(4, 64, 8, 2, 32, &nb), ACRL_OK);
+  if (nb < 4 * 2 * 64 * 4) ++failures;
+  expect("moe ws none", acrl_moe_workspace_size(0, 64, 8, 2, 32, &nb), ACRL_OK);
+  if (nb != 0) ++failures;
+  expect("moe ws null", acrl_moe_workspace_size(4, 64, 8, 2, 32, NULL), ACRL_ERR_INVALID_ARG);
+  expect("moe ws T", acrl_moe_workspace_size(129, 64, 8, 2, 32, &nb), ACRL_ERR_INVALID_ARG);
+  expect("moe ws d", acrl_moe_workspace_size(4, 65568, 8, 2, 32, &nb), ACRL_ERR_INVALID_ARG);
+  expect("moe ws E", acrl_moe_workspace_size(4, 64, 513, 2, 32, &nb), ACRL_ERR_INVALID_ARG);
+  expect("moe ws k", acrl_moe_workspace_size(4, 64, 8, 9, 32, &nb), ACRL_ERR_INVALID_ARG);
+  expect("moe ws F", acrl_moe_workspace_size(4, 64, 8, 2, 48, &nb), ACRL_ERR_INVALID_ARG);
+  expect("moe null", acrl_moe_fp8(NULL, NULL), ACRL_ERR_INVALID_ARG);
+#define MOE(change, status)                                                                      \
+  do {                                                                                           \
+    memset(&d, 0, sizeof d);                                                                     \
+    d.T = 4; d.d = 64; d.E = 8; d.top_k = 2; d.F = 32; d.x = p; d.ldx = 64; d.router = p;        \
+    d.w_in = p; d.s_in = (float*)p; d.w_out = p; d.s_out = (float*)p; d.y = p; d.ldy = 64;       \
+    d.residual = buf + 4096; d.ldr = 64; d.ids = (int32_t*)p; d.weights = (float*)p;             \
+    d.scale = 1.0f; d.workspace = p; d.workspace_bytes = 1 << 30;                                \
+    change;                                                                                      \
+    expect("moe " #change, acrl_moe_fp8(&d, NULL), status);                                      \
+  } while (0)
+#define BAD_MOE(change) MOE(change, ACRL_ERR_INVALID_ARG)
+  BAD_MOE(d.T = -1);
+  BAD_MOE(d.T = 129);
+  BAD_MOE(d.d = 48);
+  BAD_MOE(d.top_k = 17; d.E = 32);
+  BAD_MOE(d.score = 2);
+  BAD_MOE(d.activation = 5);
+  BAD_MOE(d.y_type = 2);
+  BAD_MOE(d.scale = (float)NAN);
+  BAD_MOE(d.ldx = 60);
+  BAD_MOE(d.ldx = 68);
+  BAD_MOE(d.ldy = 63);
+  BAD_MOE(d.ldr = (int64_t)1 << 40);
+  BAD_MOE(d.x = NULL);
+  BAD_MOE(d.w_in = NULL);
+  BAD_MOE(d.s_out = NULL);
+  BAD_MOE(d.ids = NULL);
+  BAD_MOE(d.weights = NULL);
+  BAD_MOE(d.y = NULL);
+  BAD_MOE(d.w_out = buf + 8);
+  BAD_MOE(d.x = buf + 8);
+  BAD_MOE(d.router = buf + 2);
+  BAD_MOE(d.residual = buf + 64);
+  BAD_MOE(d.residual_type = 7);
+  BAD_MOE(d.workspace = buf + 8);
+  MOE(d.workspace = NULL, ACRL_ERR_WORKSPACE);
+  MOE(d.workspace_bytes = 64, ACRL_ERR_WORKSPACE);
 }
 
 static void policy_losses(void) {
@@ -196,6 +249,7 @@ int main(void) {
   quantize_blocks();
   products();
   linears();
+  experts();
   policy_losses();
   preference_losses();
   reduces();

@@ -8,7 +8,7 @@ from test_operators_abi import _off, acrl, p  # noqa: F401  (fixtures)
 
 
 def test_descriptor_sizes(acrl):  # noqa: F811
-    descs = (acrl.LinearDesc,)
+    descs = (acrl.LinearDesc, acrl.MoeDesc)
     sizes = [ctypes.c_size_t() for _ in descs]
     acrl.lib().acrl_abi_decode_struct_sizes(*[ctypes.byref(s) for s in sizes])
     assert [s.value for s in sizes] == [ctypes.sizeof(x) for x in descs]
@@ -33,8 +33,40 @@ def test_linear(acrl, p):  # noqa: F811
     assert L.acrl_linear_fp8(None, None) == acrl.ACRL_ERR_INVALID_ARG
 
 
+def test_moe(acrl, p):  # noqa: F811
+    L, nb = acrl.lib(), ctypes.c_size_t()
+    ok = dict(T=4, d=64, E=8, top_k=2, F=32, x=p, ldx=64, router=p, w_in=p, s_in=p, w_out=p, s_out=p, y=p, ldy=64,
+              residual=_off(p, 2048), ldr=64, ids=p, weights=p, scale=1.0, workspace=p, workspace_bytes=1 << 30)
+    sizes = [dict(T=-1), dict(T=129), dict(d=0), dict(d=48), dict(d=65568), dict(E=0), dict(E=513), dict(top_k=0), dict(top_k=9),
+             dict(E=32, top_k=17), dict(F=0), dict(F=16), dict(F=65568)]
+    for bad in sizes:
+        s = {**ok, **bad}
+        assert L.acrl_moe_workspace_size(*[s[n] for n in ("T", "d", "E", "top_k", "F")], ctypes.byref(nb)) == 1, bad
+    for bad in sizes + [dict(score=-1), dict(score=2), dict(activation=5), dict(y_type=2), dict(residual_type=2),
+                        dict(scale=float("inf")), dict(scale=float("nan")), dict(ldx=63), dict(ldx=68), dict(ldx=1 << 34),
+                        dict(ldy=63), dict(ldy=1 << 34), dict(ldr=63), dict(ldr=1 << 34), dict(x=None), dict(w_in=None),
+                        dict(s_in=None), dict(w_out=None), dict(s_out=None), dict(y=None), dict(ids=None), dict(weights=None),
+                        dict(x=_off(p, 8)), dict(w_in=_off(p, 8)), dict(w_out=_off(p, 8)), dict(router=_off(p, 8)),
+                        dict(s_in=_off(p, 2)), dict(s_out=_off(p, 2)), dict(select_bias=_off(p, 2)), dict(y=_off(p, 2)),
+                        dict(ids=_off(p, 1)), dict(weights=_off(p, 2)), dict(residual=_off(p, 2050)), dict(residual=_off(p, 64)),
+                        dict(residual=p, ldr=72), dict(workspace=_off(p, 8))]:
+        d = acrl.MoeDesc(**{**ok, **bad})
+        assert L.acrl_moe_fp8(ctypes.byref(d), None) == acrl.ACRL_ERR_INVALID_ARG, bad
+        assert L.acrl_last_error()
+    for bad in (dict(workspace=None), dict(workspace_bytes=100)):
+        d = acrl.MoeDesc(**{**ok, **bad})
+        assert L.acrl_moe_fp8(ctypes.byref(d), None) == acrl.ACRL_ERR_WORKSPACE, bad
+    assert L.acrl_moe_fp8(None, None) == acrl.ACRL_ERR_INVALID_ARG
+    assert L.acrl_moe_workspace_size(4, 64, 8, 2, 32, None) == acrl.ACRL_ERR_INVALID_ARG
+    assert L.acrl_moe_workspace_size(0, 64, 8, 2, 32, ctypes.byref(nb)) == 0 and nb.value == 0
+    assert L.acrl_moe_workspace_size(128, 65536, 512, 16, 65536, ctypes.byref(nb)) == 0 and nb.value > 2048 * 65536 * 8
+
+
 def test_binding_refuses_host_tensors(acrl):  # noqa: F811
     import torch
     q, s = torch.zeros((4, 128), dtype=torch.uint8), torch.ones((4, 1))
     with pytest.raises(ValueError, match="device tensor"):
         acrl.acrl_linear_fp8(q, s, q, s)
+    x, w = torch.zeros((2, 32), dtype=torch.bfloat16), torch.zeros((1, 64, 32), dtype=torch.uint8)
+    with pytest.raises(ValueError, match="device tensor"):
+        acrl.acrl_moe_fp8(x, w, s[:1], w[:, :32], s[:1], 1, router=x[:1])

@@ -677,6 +677,77 @@ acrl_status acrl_moe_workspace_size(int64_t T, int64_t d, int64_t E, int64_t top
 acrl_status acrl_moe_fp8(const acrl_moe_desc* desc, void* stream);
 
 /* ======================================================================== */
+/* acrl_beam_step, acrl_beam_reorder -- beam search                          */
+/* ======================================================================== *
+ * Beside acrl_sample_mu, which draws the next token of a response: the choice of
+ * the next tokens of B sequences of K beams each, and the states of the beams
+ * that were chosen.
+ *   lp[j, v] = z[j, v] / tau - log sum_u e^(z[j, u] / tau)       (64 bits)
+ *   c[j, v]  = scores[j] + lp[j, v]
+ *   a finished beam: c[j, eos_id] = scores[j], -infinity for its other tokens
+ * The n_out candidates (j, v) of a sequence with the largest c, in falling order,
+ * equal ones by beam and then token: ids (v), parents (j) and out_scores (c,
+ * rounded to fp32).  Within a beam the order is that of its logits.  A beam whose
+ * score is not finite, or whose logits hold a NaN or +infinity or nothing above
+ * -infinity, has c = -infinity for all its tokens; a logit of -infinity has it for
+ * its own.  Such candidates come last, by beam and token, like any others of equal
+ * score.  The rows of beams that are finished or have no finite score are not read.
+ *   logits    [B K, V] of logits_type, rows ldl apart; row b K + j is beam j's
+ *   scores    float [B, K], out_scores float [B, n_out]
+ *   finished  uint8 [B, K], or NULL
+ *   ids, parents  int32 [B, n_out]
+ * Requirements: 0 <= B <= 2^20, 1 <= K <= 64, B K < 2^22, 1 <= V < 2^30, 1 <= n_out <= min(64, K V),
+ * V <= ldl < 2^34; 1e-30 < inv_temperature < 1e30; with `finished` 0 <= eos_id < V;
+ * logits aligned to their type, the workspace to 16 bytes, the others to 4.
+ *
+ * acrl_beam_reorder copies rows of row_bytes bytes: for o < outer, b < B, n < n_out
+ *   dst[o, b, n] = src[o, b, parents[b, n]]     (zeros where that is no beam)
+ * each at its strides in bytes (outer, sequence, beam).  dst may be src itself
+ * (n_out = K, same strides): beams that stay are then not touched.  Otherwise the
+ * two must not overlap, and rows of dst must not overlap each other.
+ * Requirements: outer and B at most 2^20, K and n_out in [1, 64], strides in
+ * [0, 2^42); any alignment: copied in units of 16, 4 or 1 bytes, the largest that
+ * divides both addresses, all strides and row_bytes; the units of a row, rounded up
+ * to 256, times outer B below 2^32.
+ */
+typedef struct acrl_beam_desc {
+  int64_t B;                    /* sequences                                                */
+  int64_t K;                    /* beams of a sequence                                      */
+  int64_t V;                    /* vocabulary                                               */
+  int64_t n_out;                /* candidates to choose                                     */
+  const void* logits;
+  int64_t ldl;                  /* elements between rows of the logits                      */
+  const float* scores;
+  const uint8_t* finished;      /* optional                                                 */
+  int32_t logits_type;          /* acrl_out_type                                            */
+  int32_t eos_id;               /* used with `finished`                                     */
+  float inv_temperature;        /* 1 / tau                                                  */
+  int32_t* ids;                 /* out                                                      */
+  int32_t* parents;             /* out                                                      */
+  float* out_scores;            /* out                                                      */
+  void* workspace;
+  size_t workspace_bytes;
+} acrl_beam_desc;
+
+acrl_status acrl_beam_workspace_size(int64_t B, int64_t K, int64_t V, int64_t n_out, size_t* bytes);
+acrl_status acrl_beam_step(const acrl_beam_desc* desc, void* stream);
+
+typedef struct acrl_reorder_desc {
+  int64_t outer;                /* layers, or 1                                             */
+  int64_t B;                    /* sequences                                                */
+  int64_t K;                    /* beams of src                                             */
+  int64_t n_out;                /* beams of dst                                             */
+  int64_t row_bytes;            /* bytes of a beam's state to copy                          */
+  const void* src;
+  int64_t src_outer, src_seq, src_beam;  /* bytes                                           */
+  void* dst;                    /* out                                                      */
+  int64_t dst_outer, dst_seq, dst_beam;
+  const int32_t* parents;       /* [B, n_out]                                               */
+} acrl_reorder_desc;
+
+acrl_status acrl_beam_reorder(const acrl_reorder_desc* desc, void* stream);
+
+/* ======================================================================== */
 /* acrl_policy_loss -- clipped policy loss with a KL term, and its gradient   */
 /* ======================================================================== *
  * Beside acrl_surrogate (group mean of the clipped objective): the same clip
@@ -812,7 +883,7 @@ acrl_status acrl_preference_loss(const acrl_preference_desc* desc, void* stream)
 void acrl_abi_operator_struct_sizes(size_t* matmul_desc, size_t* policy_loss_desc, size_t* preference_desc);
 
 /* The same for the descriptors of a decode step's operators.                */
-void acrl_abi_decode_struct_sizes(size_t* linear_desc, size_t* moe_desc);
+void acrl_abi_decode_struct_sizes(size_t* linear_desc, size_t* moe_desc, size_t* beam_desc, size_t* reorder_desc);
 
 /* Host helper (host pointers): the reference discrepancy X of Sec. 4.1 is the
  * mean of Y_g over the non-empty groups (group_nseq > 0) of the step-0

@@ -47,7 +47,8 @@ EXPORTED = [
     "acrl_backward_workspace_size", "acrl_lm_head_backward",
     "acrl_matmul_fp8", "acrl_policy_loss_workspace_size", "acrl_policy_loss",
     "acrl_preference_loss_workspace_size", "acrl_preference_loss", "acrl_abi_operator_struct_sizes",
-    "acrl_linear_fp8", "acrl_moe_workspace_size", "acrl_moe_fp8", "acrl_abi_decode_struct_sizes",
+    "acrl_linear_fp8", "acrl_moe_workspace_size", "acrl_moe_fp8", "acrl_beam_workspace_size",
+    "acrl_beam_step", "acrl_beam_reorder", "acrl_abi_decode_struct_sizes",
 ]
 
 _P = ctypes.c_void_p
@@ -127,6 +128,18 @@ class MoeDesc(ctypes.Structure):
                 ("residual", _P), ("ldr", _I64), ("y", _P), ("ldy", _I64), ("ids", _P), ("weights", _P),
                 ("residual_type", _I32), ("y_type", _I32), ("score", _I32), ("renormalize", _I32), ("activation", _I32),
                 ("scale", _F32), ("workspace", _P), ("workspace_bytes", _SZ)]
+
+
+class BeamDesc(ctypes.Structure):
+    _fields_ = [("B", _I64), ("K", _I64), ("V", _I64), ("n_out", _I64), ("logits", _P), ("ldl", _I64), ("scores", _P),
+                ("finished", _P), ("logits_type", _I32), ("eos_id", _I32), ("inv_temperature", _F32), ("ids", _P),
+                ("parents", _P), ("out_scores", _P), ("workspace", _P), ("workspace_bytes", _SZ)]
+
+
+class ReorderDesc(ctypes.Structure):
+    _fields_ = [("outer", _I64), ("B", _I64), ("K", _I64), ("n_out", _I64), ("row_bytes", _I64), ("src", _P),
+                ("src_outer", _I64), ("src_seq", _I64), ("src_beam", _I64), ("dst", _P), ("dst_outer", _I64),
+                ("dst_seq", _I64), ("dst_beam", _I64), ("parents", _P)]
 
 
 class PolicyLossDesc(ctypes.Structure):
@@ -224,19 +237,25 @@ def lib() -> ctypes.CDLL:
         L.acrl_linear_fp8.restype = _I32
         L.acrl_linear_fp8.argtypes = [ctypes.POINTER(LinearDesc), _P]
         L.acrl_abi_decode_struct_sizes.restype = None
-        L.acrl_abi_decode_struct_sizes.argtypes = [ctypes.POINTER(_SZ)] * 2
+        L.acrl_abi_decode_struct_sizes.argtypes = [ctypes.POINTER(_SZ)] * 4
+        L.acrl_beam_workspace_size.restype = _I32
+        L.acrl_beam_workspace_size.argtypes = [_I64] * 4 + [ctypes.POINTER(_SZ)]
+        L.acrl_beam_step.restype = _I32
+        L.acrl_beam_step.argtypes = [ctypes.POINTER(BeamDesc), _P]
+        L.acrl_beam_reorder.restype = _I32
+        L.acrl_beam_reorder.argtypes = [ctypes.POINTER(ReorderDesc), _P]
         L.acrl_moe_workspace_size.restype = _I32
         L.acrl_moe_workspace_size.argtypes = [_I64] * 5 + [ctypes.POINTER(_SZ)]
         L.acrl_moe_fp8.restype = _I32
         L.acrl_moe_fp8.argtypes = [ctypes.POINTER(MoeDesc), _P]
-        sizes = [_SZ() for _ in range(11)]
+        sizes = [_SZ() for _ in range(13)]
         L.acrl_abi_struct_sizes(*[ctypes.byref(s) for s in sizes[:6]])
         L.acrl_abi_operator_struct_sizes(*[ctypes.byref(s) for s in sizes[6:9]])
         L.acrl_abi_decode_struct_sizes(*[ctypes.byref(s) for s in sizes[9:]])
         want = [ctypes.sizeof(ScoreDesc), ctypes.sizeof(ReduceDesc), ctypes.sizeof(ControllerDesc),
                 ctypes.sizeof(SampleDesc), ctypes.sizeof(SurrogateDesc), ctypes.sizeof(BackwardDesc),
                 ctypes.sizeof(MatmulDesc), ctypes.sizeof(PolicyLossDesc), ctypes.sizeof(PreferenceDesc),
-                ctypes.sizeof(LinearDesc), ctypes.sizeof(MoeDesc)]
+                ctypes.sizeof(LinearDesc), ctypes.sizeof(MoeDesc), ctypes.sizeof(BeamDesc), ctypes.sizeof(ReorderDesc)]
         got = [s.value for s in sizes]
         if got != want:
             raise RuntimeError("libacrl descriptor layout mismatch: library %s, binding %s" % (got, want))
@@ -785,6 +804,85 @@ def acrl_moe_fp8(x, w_in, s_in, w_out, s_out, top_k: int, router=None, score: in
         desc.workspace, desc.workspace_bytes = ws.data_ptr(), nbytes
     _check(lib().acrl_moe_fp8(ctypes.byref(desc), _raw_stream(stream, dev)), "acrl_moe_fp8")
     return out, ids, weights
+
+
+# ------------------------------------------------------------------ beam search
+def acrl_beam_step(logits, scores, n_out: int, inv_temperature: float = 1.0, finished=None, eos_id: int = -1, ids=None,
+                   parents=None, out_scores=None, stream=None):
+    """The n_out best continuations of every sequence: logits [B K, V] (bf16 or
+    float32, rows may lie apart), scores float32 [B, K], finished uint8 [B, K].
+    Returns (ids int32, parents int32, scores float32), each [B, n_out]."""
+    if scores.dim() != 2 or logits.dim() != 2 or logits.shape[0] != scores.numel():
+        raise ValueError("scores [B, K] and logits [B K, V] are required")
+    B, K = scores.shape
+    V = logits.shape[1]
+    index, dev, f32 = _index_of(scores, torch.float32, "scores", stream), scores.device, torch.float32
+    ldl = _matrix(logits, B * K, V, index, "logits")
+    nbytes = _size("acrl_beam_workspace_size", B, K, V, n_out)
+    if ids is None:
+        ids = _empty((B, n_out), torch.int32, dev, stream)
+    if parents is None:
+        parents = _empty((B, n_out), torch.int32, dev, stream)
+    if out_scores is None:
+        out_scores = _empty((B, n_out), f32, dev, stream)
+    ws = _empty(nbytes, torch.uint8, dev, stream) if nbytes else None
+    n = B * n_out
+    desc = BeamDesc(B, K, V, n_out, logits.data_ptr(), ldl, scores.data_ptr(),
+                    _want(finished, torch.uint8, B * K, index, "finished", True), _OUT_TYPES[logits.dtype], eos_id,
+                    inv_temperature, _want(ids, torch.int32, n, index, "ids"),
+                    _want(parents, torch.int32, n, index, "parents"), _want(out_scores, f32, n, index, "out_scores"),
+                    ws.data_ptr() if nbytes else None, nbytes)
+    _check(lib().acrl_beam_step(ctypes.byref(desc), _raw_stream(stream, dev)), "acrl_beam_step")
+    return ids, parents, out_scores
+
+
+def acrl_beam_reorder(state, parents, dim: int = 0, out=None, stream=None):
+    """The states of the chosen beams: state has the sequences B in dimension `dim`
+    and their K beams in the next; parents int32 [B, n_out] (acrl_beam_step).
+    Returns `out`, of state's shape with n_out beams.  What follows the beams'
+    dimension is one dense row a beam (a prefix of a longer one, as state[..., :n,
+    :], where the rows lie apart); what precedes `dim` is collapsed.  `out` may be
+    `state` itself (n_out = K)."""
+    index = state.get_device()
+    if not state.is_cuda or state.dim() < dim + 2 or dim < 0:
+        raise ValueError("state must be a device tensor with sequences in dimension %d and beams in the next" % dim)
+    _index_of(parents, torch.int32, "parents", stream)
+    B, K = state.shape[dim], state.shape[dim + 1]
+    if parents.dim() != 2 or parents.shape[0] != B or parents.get_device() != index:
+        raise ValueError("parents must be [%d, n_out] on %s" % (B, state.device))
+    n_out = parents.shape[1]
+    shape = (*state.shape[:dim + 1], n_out, *state.shape[dim + 2:])
+    if out is None:
+        out = _empty(shape, state.dtype, state.device, stream)
+    elif tuple(out.shape) != shape or out.dtype != state.dtype or out.get_device() != index:
+        raise ValueError("out must be %s of %s on %s" % (shape, state.dtype, state.device))
+    size = state.element_size()
+    row, src = _rows(state, dim, "state")
+    _, dst = _rows(out, dim, "out")
+    outer = 1
+    for n in state.shape[:dim]:
+        outer *= n
+    desc = ReorderDesc(outer, B, K, n_out, row * size, state.data_ptr(), *[n * size for n in src], out.data_ptr(),
+                       *[n * size for n in dst], parents.data_ptr())
+    _check(lib().acrl_beam_reorder(ctypes.byref(desc), _raw_stream(stream, state.device)), "acrl_beam_reorder")
+    return out
+
+
+def _rows(t, dim: int, name: str):
+    """(elements of a beam's row, (outer, sequence, beam) strides) of a tensor of states."""
+    row = 1
+    for n, s in zip(reversed(t.shape[dim + 2:]), reversed(t.stride()[dim + 2:])):
+        if n != 1 and s != row:
+            raise ValueError("%s: a beam's row must be dense" % name)
+        row *= n
+    outer, step = 0, None
+    for n, s in zip(reversed(t.shape[:dim]), reversed(t.stride()[:dim])):
+        if n == 1:
+            continue
+        if step is not None and s != step:
+            raise ValueError("%s: the dimensions before the sequences must collapse into one" % name)
+        outer, step = outer or s, s * n
+    return row, (outer, t.stride(dim) if t.shape[dim] > 1 else 0, t.stride(dim + 1) if t.shape[dim + 1] > 1 else 0)
 
 
 # ------------------------------------------------------------------ losses beside the surrogate

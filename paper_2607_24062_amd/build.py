@@ -13,7 +13,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libacrl.so")
-SOURCES = ["api.hip", "quantize.hip", "score.hip", "reduce.hip", "product.hip", "losses.hip", "moe.hip"]
+SOURCES = ["api.hip", "quantize.hip", "score.hip", "reduce.hip", "product.hip", "losses.hip", "moe.hip",
+           "beam.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -1,0 +1,612 @@
+// beam.hip -- beam search: the choice of the next tokens over beams and
+// vocabulary, and the states of the chosen beams.
+//
+// The choice compares scores of different beams, score_j + z - lse_j, so a
+// normaliser that is off by an fp32 rounding would now and then choose another
+// candidate: exponentials and sums are fp64.  Within a beam the order is that of
+// the logits alone.
+#include <algorithm>
+
+#include "entry.h"
+
+namespace acrl {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_anywhere __attribute__((ext_vector_type(4), aligned(2)));
+
+constexpr int kMaxBeams = 64, kMaxOut = 64;
+constexpr int kScanWaves = 8, kEach = 16, kTile = 64 * kEach;  // logits of a lane, of a wave at a time
+constexpr int kPickWaves = 4, kMaxLists = 64 * kPickWaves, kMaxStaged = 6144;
+constexpr int kNone = 0x7FFFFFFF;
+
+struct BeamParams {
+  const void* logits;
+  int64_t ldl;
+  const float* scores;
+  const uint8_t* finished;  // or NULL
+  int B, K, V, N, eos;
+  float inv_t;
+  int S;                    // segments of a row, each one workgroup's
+  int seg_tiles;            // tiles of a segment
+  int32_t* ids;
+  int32_t* parents;
+  float* out;
+  // workspace, by row and segment
+  double* norm;             // [2]: a reference near the largest logit (NaN: no normaliser), sum of 2^((z - it) inv_t log2 e)
+  float* val;               // [N] the segment's largest logits, falling
+  int* idx;                 // [N] their tokens (kNone: no more)
+};
+
+// A row's beam can give candidates: it has a finite score.
+__device__ __forceinline__ bool alive(float score) { return fabsf(score) < INFINITY; }
+
+// 2^t for t in [-1000, 1000] (below: as -1000): the polynomial is an interpolation of
+// 2^f, |f| <= 1/2, at Chebyshev's points, within 1.1e-12 of it.
+__device__ __forceinline__ double exp2_f64(double t) {
+  constexpr double kRound = 6755399441055744.0;  // 1.5 2^52: added, it leaves t's integer in the low bits
+  t = fmax(t, -1000.0);
+  const double r = t + kRound, f = t - (r - kRound);
+  double p = 1.3255224884799127e-06;
+  p = fma(p, f, 1.5310079402383103e-05);
+  p = fma(p, f, 0.00015403455852419016);
+  p = fma(p, f, 0.0013333450568000008);
+  p = fma(p, f, 0.00961812915940262);
+  p = fma(p, f, 0.05550410941205934);
+  p = fma(p, f, 0.2402265069581299);
+  p = fma(p, f, 0.6931471805459335);
+  p = fma(p, f, 1.0);
+  return __hiloint2double(__double2hiint(p) + (__double2loint(r) << 20), __double2loint(p));
+}
+
+__device__ __forceinline__ double shfl_xor_f64(double v, int m) {
+  return __hiloint2double(__shfl_xor(__double2hiint(v), m), __shfl_xor(__double2loint(v), m));
+}
+__device__ __forceinline__ int read_lane(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ int lowest(uint64_t mask) { return __builtin_ctzll(mask); }
+
+// A lane's kEach consecutive logits, as they are read; those past `left` count as -infinity.
+template <typename T>
+struct Logits {
+  static constexpr int kWords = kEach * (int)sizeof(T) / 4;
+  uint32_t w[kWords];
+  __device__ __forceinline__ void read(const T* at, int left) {
+    // (rows of odd lengths begin anywhere: the loads are wide all the same)
+    if (left >= kEach) {
+#pragma unroll
+      for (int i = 0; i < kWords / 4; ++i) {
+        const u32x4_anywhere v = reinterpret_cast<const u32x4_anywhere*>(at)[i];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[4 * i + k] = v[k];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const bool ok = i < left;
+        if constexpr (sizeof(T) == 4) {
+          w[i] = ok ? reinterpret_cast<const uint32_t*>(at)[i] : 0xFF800000u;
+        } else {
+          const uint32_t v = ok ? reinterpret_cast<const uint16_t*>(at)[i] : 0xFF80u;
+          w[i / 2] = i % 2 ? w[i / 2] | v << 16 : v;
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ float operator[](int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return i % 2 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
+  }
+};
+
+// 64-bit keys: the larger value first, then the lower token; -0 as 0.
+__device__ __forceinline__ uint64_t key_of(float v, int idx) {
+  const uint32_t u = __float_as_uint(v == 0.0f ? 0.0f : v);
+  return (uint64_t)(u >> 31 ? ~u : u | 0x80000000u) << 32 | (uint32_t)~idx;
+}
+
+// One pass over a row's segment: the sum of exponentials and the N largest
+// logits.  A wave keeps its own N largest, one a lane, and looks closer at a tile
+// only where a lane's largest beats the least of them: few tiles after the first
+// (N ln(tiles) candidates for logits in no order, N a tile at most, the largest
+// first).  No wave waits for another before the end.
+template <typename T>
+__global__ __launch_bounds__(64 * kScanWaves) void beam_scan_kernel(BeamParams p) {
+  __shared__ uint64_t keys[kScanWaves * kMaxOut];
+  __shared__ double norms[kScanWaves][2];
+  const int row = blockIdx.x / p.S, seg = blockIdx.x % p.S;
+  if (!alive(p.scores[row]) || (p.finished && p.finished[row])) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const T* const z = static_cast<const T*>(p.logits) + row * p.ldl;
+  const int64_t begin = (int64_t)seg * p.seg_tiles * kTile;
+  const int64_t end = min((int64_t)p.V, begin + (int64_t)p.seg_tiles * kTile);
+  const double c = (double)p.inv_t * 1.4426950408889634074;  // (the same rounding for all terms)
+  const int N = p.N;
+  float held = lane < N ? -INFINITY : INFINITY;  // the wave's N largest (empty: -infinity)
+  int held_idx = kNone;
+  float least = -INFINITY;
+  float m = -INFINITY;  // the lane's reference: no more than 2^900 below any of its logits
+  double sum = 0.0;
+  bool bad = false;
+  Logits<T> next;
+  int64_t at = begin + (int64_t)wave * kTile + lane * kEach;
+  next.read(z + at, (int)max((int64_t)-1, min(end - at, (int64_t)kEach)));
+  for (int64_t tile = begin + (int64_t)wave * kTile; tile < end; tile += kScanWaves * kTile) {
+    float x[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) x[i] = next[i];
+    at += kScanWaves * kTile;
+    next.read(z + at, (int)max((int64_t)-1, min(end - at, (int64_t)kEach)));
+    float top = x[0];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      top = fmaxf(top, x[i]);
+      bad |= !(x[i] < INFINITY);
+    }
+    if (((double)top - (double)m) * c > 900.0) {
+      sum *= exp2_f64(((double)m - (double)top) * c);
+      m = top;
+    }
+    const double mc = (double)m * c;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) sum += exp2_f64(fma((double)x[i], c, -mc));
+    while (__ballot(top > least)) {
+      const float best = wave_max(top);
+      const int who = lowest(__ballot(top == best));
+      int i = kEach;
+#pragma unroll
+      for (int k = kEach - 1; k >= 0; --k) i = x[k] == best ? k : i;
+      i = read_lane(i, who);
+      if (i == kEach) break;  // (a NaN that is a lane's largest: no normaliser, no candidates)
+      // it takes the place of the least: of equal ones the last token's
+      uint64_t mine = __ballot(held == least);
+      int out = lowest(mine);
+      for (uint64_t rest = mine & (mine - 1); rest; rest &= rest - 1)
+        if (read_lane(held_idx, lowest(rest)) > read_lane(held_idx, out)) out = lowest(rest);
+      if (lane == out) {
+        held = best;
+        held_idx = (int)(tile + who * kEach + i);
+      }
+      least = -wave_max(-held);
+      if (lane == who) {
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) x[k] = k == i ? -INFINITY : x[k];
+      }
+      top = x[0];
+#pragma unroll
+      for (int k = 1; k < kEach; ++k) top = fmaxf(top, x[k]);
+    }
+  }
+  // the waves' sums and lists together
+  const float ref = wave_max(m);
+  sum *= exp2_f64(((double)m - (double)ref) * c);
+  for (int o = 32; o; o /= 2) sum += shfl_xor_f64(sum, o);
+  const bool any_bad = __ballot(bad) != 0;
+  if (lane < N) keys[wave * N + lane] = held_idx == kNone ? 0 : key_of(held, held_idx);
+  if (lane == 0) {
+    norms[wave][0] = any_bad ? (double)NAN : (double)ref;
+    norms[wave][1] = sum;
+  }
+  __syncthreads();
+  const int64_t slot = blockIdx.x;
+  const int n = kScanWaves * N;
+  if ((int)threadIdx.x < n) {
+    const uint64_t k = keys[threadIdx.x];
+    int rank = 0, filled = 0;
+    for (int i = 0; i < n; ++i) {
+      rank += keys[i] > k;
+      filled += keys[i] != 0;
+    }
+    if (k && rank < N) {
+      const uint32_t u = (uint32_t)(k >> 32);
+      p.val[slot * N + rank] = __uint_as_float(u >> 31 ? u & 0x7FFFFFFFu : ~u);
+      p.idx[slot * N + rank] = (int)~(uint32_t)k;
+    }
+    if ((int)threadIdx.x < N && (int)threadIdx.x >= filled) p.idx[slot * N + threadIdx.x] = kNone;
+  }
+  if (threadIdx.x == 0) {
+    double ref_all = -INFINITY, total = 0.0;
+    bool none = false;
+    for (int w = 0; w < kScanWaves; ++w) {
+      none |= norms[w][0] != norms[w][0];
+      if (norms[w][0] > ref_all) ref_all = norms[w][0];
+    }
+    for (int w = 0; w < kScanWaves; ++w) total += norms[w][1] * exp2_f64((norms[w][0] - ref_all) * c);
+    p.norm[2 * slot] = none ? (double)NAN : ref_all;
+    p.norm[2 * slot + 1] = total;
+  }
+}
+
+// The larger score first, then the lower beam, then the lower token: score in a 64-bit key, the lanes that share the
+// largest told apart by the rest.  0: no candidate.
+__device__ __forceinline__ uint64_t key_of(double v) {
+  const uint64_t u = (uint64_t)__double_as_longlong(v == 0.0 ? 0.0 : v);
+  return u >> 63 ? ~u : u | 1ull << 63;
+}
+__device__ __forceinline__ double value_of(uint64_t k) {
+  return __longlong_as_double((long long)(k >> 63 ? k & ~(1ull << 63) : ~k));
+}
+template <int CTRL>
+__device__ __forceinline__ uint64_t dpp_u64(uint64_t v) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)v, CTRL, 0xF, 0xF, true);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_mov_dpp((int)(v >> 32), CTRL, 0xF, 0xF, true);
+  return (uint64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ uint64_t shfl_u64(uint64_t v, int m) {
+  return (uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), m) << 32 | (uint32_t)__shfl_xor((int)(uint32_t)v, m);
+}
+__device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
+  v = max(v, dpp_u64<0xB1>(v));
+  v = max(v, dpp_u64<0x4E>(v));
+  v = max(v, dpp_u64<0x124>(v));
+  v = max(v, dpp_u64<0x128>(v));
+  v = max(v, shfl_u64(v, 16));
+  v = max(v, shfl_u64(v, 32));
+  return v;
+}
+
+struct Candidate {
+  uint64_t key;
+  int beam, id;
+};
+// The lane whose candidate comes first, or -1.
+__device__ __forceinline__ int first_of(const Candidate& c) {
+  const uint64_t best = wave_max_u64(c.key);
+  if (best == 0) return -1;
+  const uint64_t same = __ballot(c.key == best);
+  int who = lowest(same);
+  for (uint64_t rest = same & (same - 1); rest; rest &= rest - 1) {
+    const int l = lowest(rest), b = read_lane(c.beam, l), wb = read_lane(c.beam, who);
+    if (b < wb || (b == wb && read_lane(c.id, l) < read_lane(c.id, who))) who = l;
+  }
+  return who;
+}
+
+// A sequence's N best of its beams' lists: they lie in LDS, a lane walks one, and
+// the first of all heads is taken N times; with more than 64 lists four waves do
+// that, and one of them over their results.
+__global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p) {
+  extern __shared__ uint8_t staged[];  // val [lists][N], idx [lists][N]
+  __shared__ double lse[kMaxBeams], score[kMaxBeams];
+  __shared__ int state[kMaxBeams];     // 0: no candidates, 1: its lists, 2: finished
+  __shared__ Candidate merged[kPickWaves][kMaxOut];
+  __shared__ int chosen_beam[kMaxOut], chosen_id[kMaxOut];
+  const int b = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lists = p.K * p.S, N = p.N;
+  float* const val = reinterpret_cast<float*>(staged);
+  int* const idx = reinterpret_cast<int*>(val + lists * N);
+  const double c = (double)p.inv_t * 1.4426950408889634074;
+  if ((int)threadIdx.x < p.K) {
+    const int j = threadIdx.x, row = b * p.K + j;
+    score[j] = p.scores[row];
+    state[j] = !alive(p.scores[row]) ? 0 : p.finished && p.finished[row] ? 2 : 1;
+    if (state[j] == 1) {
+      const double* n = p.norm + 2 * (int64_t)row * p.S;
+      double ref = -INFINITY, sum = 0.0;
+      bool none = false;
+      for (int s = 0; s < p.S; ++s) {
+        none |= n[2 * s] != n[2 * s];
+        if (n[2 * s] > ref) ref = n[2 * s];
+      }
+      for (int s = 0; s < p.S; ++s) sum += n[2 * s + 1] * exp2_f64((n[2 * s] - ref) * c);
+      lse[j] = ref * (double)p.inv_t + log(sum);
+      if (none || !(fabs(lse[j]) < INFINITY)) state[j] = 0;
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < lists * N; i += 64 * kPickWaves)
+    if (state[i / (p.S * N)] == 1) {
+      val[i] = p.val[(int64_t)b * lists * N + i];
+      idx[i] = p.idx[(int64_t)b * lists * N + i];
+    }
+  __syncthreads();
+  const int mine = lists <= 64 ? (wave == 0 ? lane : lists) : threadIdx.x;  // the lane's list
+  int at = 0;
+  auto head = [&]() {
+    Candidate r = {0, 0, 0};
+    if (mine >= lists || at >= N) return r;
+    r.beam = mine / p.S;
+    if (state[r.beam] == 2 && mine % p.S == 0 && at == 0) {
+      r.id = p.eos;
+      r.key = key_of(score[r.beam]);
+    } else if (state[r.beam] == 1 && idx[mine * N + at] != kNone) {
+      r.id = idx[mine * N + at];
+      r.key = key_of(score[r.beam] + ((double)val[mine * N + at] * (double)p.inv_t - lse[r.beam]));
+    }
+    return r;
+  };
+  auto emit = [&](int k, int who, const Candidate& h) {
+    if (lane == who) {
+      p.ids[(int64_t)b * N + k] = chosen_id[k] = h.id;
+      p.parents[(int64_t)b * N + k] = chosen_beam[k] = h.beam;
+      p.out[(int64_t)b * N + k] = (float)value_of(h.key);
+    }
+  };
+  int n = 0;
+  if (lists <= 64) {
+    if (wave != 0) return;
+    Candidate h = head();
+    for (; n < N; ++n) {
+      const int who = first_of(h);
+      if (who < 0) break;
+      emit(n, who, h);
+      if (lane == who) {
+        ++at;
+        h = head();
+      }
+    }
+  } else {
+    Candidate h = head();
+    int k = 0;
+    for (; k < N; ++k) {
+      const int who = first_of(h);
+      if (who < 0) break;
+      if (lane == who) {
+        merged[wave][k] = h;
+        ++at;
+        h = head();
+      }
+    }
+    if (lane >= k && lane < N) merged[wave][lane] = Candidate{0, 0, 0};
+    __syncthreads();
+    if (wave != 0) return;
+    at = 0;
+    auto next = [&]() { return lane < kPickWaves && at < N ? merged[lane][at] : Candidate{0, 0, 0}; };
+    h = next();
+    for (; n < N; ++n) {
+      const int who = first_of(h);
+      if (who < 0) break;
+      emit(n, who, h);
+      if (lane == who) {
+        ++at;
+        h = next();
+      }
+    }
+  }
+  if (n == N) return;
+  // All candidates above -infinity are chosen.  The others follow by beam and token.
+  __threadfence_block();
+  if (lane != 0) return;
+  int beam = 0, id = 0;
+  for (int k = n; k < N;) {
+    bool taken = false;
+    for (int i = 0; i < n; ++i) taken |= chosen_beam[i] == beam && chosen_id[i] == id;
+    if (!taken) {
+      p.ids[(int64_t)b * N + k] = id;
+      p.parents[(int64_t)b * N + k] = beam;
+      p.out[(int64_t)b * N + k] = -INFINITY;
+      ++k;
+    }
+    if (++id == p.V) {
+      id = 0;
+      ++beam;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ states
+struct ReorderParams {
+  const uint8_t* src;
+  uint8_t* dst;
+  int64_t s_outer, s_seq, s_beam;  // bytes
+  int64_t d_outer, d_seq, d_beam;
+  const int32_t* parents;
+  int outer, B, K, N;
+  int64_t units;    // of a row
+  int64_t chunks;   // of a row, one workgroup's each
+  int in_place;
+};
+
+// Thread by thread, one unit of a row at the same place of all beams of a
+// sequence: the rows that are somebody's parent are read once each, whoever wants
+// them, into the thread's own column of LDS, and written from there.  All reads of a
+// place stand before its writes, so the states may be reordered in place; beams
+// that stay where they are are then not touched.
+template <typename UNIT, int THREADS>
+__global__ __launch_bounds__(THREADS) void beam_reorder_kernel(ReorderParams p) {
+  extern __shared__ uint8_t column[];  // [K][THREADS] units
+  UNIT* const held = reinterpret_cast<UNIT*>(column) + threadIdx.x;
+  const int64_t at = (int64_t)blockIdx.x % p.chunks * THREADS + threadIdx.x, seq = blockIdx.x / p.chunks;
+  const int b = (int)(seq % p.B);
+  const int64_t o = seq / p.B;
+  const int32_t* const parent = p.parents + (int64_t)b * p.N;
+  uint64_t used = 0;
+  for (int n = 0; n < p.N; ++n) {
+    const uint32_t j = (uint32_t)parent[n];
+    if (j < (uint32_t)p.K && !(p.in_place && (int)j == n)) used |= 1ull << j;
+  }
+  if (at >= p.units) return;
+  const uint8_t* const src = p.src + o * p.s_outer + b * p.s_seq + at * (int64_t)sizeof(UNIT);
+  uint8_t* const dst = p.dst + o * p.d_outer + b * p.d_seq + at * (int64_t)sizeof(UNIT);
+  for (int j0 = 0; j0 < p.K; j0 += 8) {
+    UNIT v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (used >> (j0 + i) & 1) v[i] = *reinterpret_cast<const UNIT*>(src + (j0 + i) * p.s_beam);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (used >> (j0 + i) & 1) held[(j0 + i) * THREADS] = v[i];
+  }
+  for (int n = 0; n < p.N; ++n) {
+    const uint32_t j = (uint32_t)parent[n];
+    if (p.in_place && (int)j == n) continue;
+    UNIT* to = reinterpret_cast<UNIT*>(dst + n * p.d_beam);
+    if (j < (uint32_t)p.K) *to = held[j * THREADS];
+    else *to = UNIT{};
+  }
+}
+
+template <typename UNIT, int THREADS>
+hipError_t launch_reorder(ReorderParams p, int64_t row_bytes, hipStream_t s) {
+  p.units = row_bytes / (int64_t)sizeof(UNIT);
+  p.chunks = (p.units + THREADS - 1) / THREADS;
+  const int64_t grid = p.chunks * p.B * p.outer;
+  hipLaunchKernelGGL((beam_reorder_kernel<UNIT, THREADS>), dim3((unsigned)grid), dim3(THREADS),
+                     (unsigned)(p.K * THREADS * (int)sizeof(UNIT)), s, p);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ host
+constexpr int kCus = 256;
+
+// Segments: two workgroups a CU where the rows are few, each of a tile a wave at least; as many lists as the pick has
+// lanes for, and LDS.
+void segment(BeamParams& p) {
+  const int64_t rows = (int64_t)p.B * p.K, tiles = ((int64_t)p.V + kTile - 1) / kTile;
+  int64_t S = rows ? std::max<int64_t>(1, 2 * kCus / rows) : 1;
+  S = std::min(S, (tiles + kScanWaves - 1) / kScanWaves);
+  S = std::min<int64_t>(S, std::min(kMaxLists / p.K, std::max(1, kMaxStaged / (p.K * p.N))));
+  p.seg_tiles = (int)((tiles + S - 1) / S);
+  p.S = (int)((tiles + p.seg_tiles - 1) / p.seg_tiles);
+}
+
+size_t lay_out(BeamParams& p, uint8_t* base) {
+  const size_t slots = (size_t)p.B * p.K * p.S;
+  p.norm = reinterpret_cast<double*>(base);
+  p.val = reinterpret_cast<float*>(base + slots * 16);
+  p.idx = reinterpret_cast<int*>(base + slots * (16 + 4 * (size_t)p.N));
+  return slots * (16 + 8 * (size_t)p.N);
+}
+
+acrl_status validate_sizes(int64_t B, int64_t K, int64_t V, int64_t N) {
+  ACRL_REQUIRE(K > 0 && K <= kMaxBeams, "K = %lld must lie in [1, %d]", (long long)K, kMaxBeams);
+  ACRL_REQUIRE(B >= 0 && B <= (1 << 20), "B = %lld must lie in [0, 2^20]", (long long)B);
+  ACRL_REQUIRE(B * K < (1 << 22), "B x K = %lld must be below 2^22", (long long)(B * K));
+  ACRL_REQUIRE(V > 0 && V < ((int64_t)1 << 30), "V = %lld must lie in [1, 2^30)", (long long)V);
+  ACRL_REQUIRE(N > 0 && N <= kMaxOut && N <= K * V, "n_out = %lld must lie in [1, min(%d, K V)]", (long long)N, kMaxOut);
+  return ACRL_OK;
+}
+
+BeamParams sized(int64_t B, int64_t K, int64_t V, int64_t N) {
+  BeamParams p{};
+  p.B = (int)B;
+  p.K = (int)K;
+  p.V = (int)V;
+  p.N = (int)N;
+  segment(p);
+  return p;
+}
+
+}  // namespace
+}  // namespace acrl
+
+extern "C" {
+
+acrl_status acrl_beam_workspace_size(int64_t B, int64_t K, int64_t V, int64_t n_out, size_t* bytes) {
+  ACRL_REQUIRE(bytes, "bytes is NULL");
+  acrl_status st = acrl::validate_sizes(B, K, V, n_out);
+  if (st != ACRL_OK) return st;
+  acrl::BeamParams p = acrl::sized(B, K, V, n_out);
+  *bytes = acrl::lay_out(p, nullptr);
+  return ACRL_OK;
+}
+
+acrl_status acrl_beam_step(const acrl_beam_desc* d, void* stream) {
+  ACRL_REQUIRE(d, "desc is NULL");
+  acrl_status st = acrl::validate_sizes(d->B, d->K, d->V, d->n_out);
+  if (st != ACRL_OK) return st;
+  const bool f32 = d->logits_type == ACRL_OUT_F32;
+  ACRL_REQUIRE(f32 || d->logits_type == ACRL_OUT_BF16, "logits_type %d unknown", d->logits_type);
+  ACRL_REQUIRE(d->ldl >= d->V && d->ldl < ((int64_t)1 << 34), "ldl = %lld must lie in [V, 2^34)", (long long)d->ldl);
+  ACRL_REQUIRE(d->inv_temperature > 1e-30f && d->inv_temperature < 1e30f, "inv_temperature must lie in (1e-30, 1e30)");
+  ACRL_REQUIRE(!d->finished || (d->eos_id >= 0 && d->eos_id < d->V), "eos_id = %d must lie in [0, V)", d->eos_id);
+  if (d->B > 0) {
+    ACRL_REQUIRE(d->logits && d->scores && d->ids && d->parents && d->out_scores,
+                 "logits, scores, ids, parents and out_scores are required");
+    ACRL_REQUIRE(((uintptr_t)d->logits & (f32 ? 3u : 1u)) == 0, "logits is misaligned");
+    ACRL_REQUIRE((((uintptr_t)d->scores | (uintptr_t)d->ids | (uintptr_t)d->parents | (uintptr_t)d->out_scores) & 3u) == 0,
+                 "scores, ids, parents or out_scores is misaligned");
+  }
+  acrl::BeamParams p = acrl::sized(d->B, d->K, d->V, d->n_out);
+  const size_t need = acrl::lay_out(p, static_cast<uint8_t*>(d->workspace));
+  if (need && (!d->workspace || d->workspace_bytes < need)) {
+    acrl::set_error("acrl_beam_step needs %zu workspace bytes, got %zu", need, d->workspace_bytes);
+    return ACRL_ERR_WORKSPACE;
+  }
+  ACRL_REQUIRE(acrl::aligned16(d->workspace), "workspace must be 16-byte aligned");
+  st = acrl::check_device();
+  if (st != ACRL_OK || d->B == 0) return st;
+  p.logits = d->logits;
+  p.ldl = d->ldl;
+  p.scores = d->scores;
+  p.finished = d->finished;
+  p.eos = d->eos_id;
+  p.inv_t = d->inv_temperature;
+  p.ids = d->ids;
+  p.parents = d->parents;
+  p.out = d->out_scores;
+  const hipStream_t s = (hipStream_t)stream;
+  const dim3 grid((unsigned)((int64_t)p.B * p.K * p.S)), threads(64 * acrl::kScanWaves);
+  if (f32) hipLaunchKernelGGL(acrl::beam_scan_kernel<float>, grid, threads, 0, s, p);
+  else hipLaunchKernelGGL(acrl::beam_scan_kernel<__bf16>, grid, threads, 0, s, p);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess) {
+    hipLaunchKernelGGL(acrl::beam_pick_kernel, dim3((unsigned)p.B), dim3(64 * acrl::kPickWaves),
+                       (unsigned)(p.K * p.S * p.N * 8), s, p);
+    e = hipGetLastError();
+  }
+  return acrl::hip_status(e, "acrl_beam_step launch");
+}
+
+acrl_status acrl_beam_reorder(const acrl_reorder_desc* d, void* stream) {
+  ACRL_REQUIRE(d, "desc is NULL");
+  ACRL_REQUIRE(d->K > 0 && d->K <= acrl::kMaxBeams, "K = %lld must lie in [1, %d]", (long long)d->K, acrl::kMaxBeams);
+  ACRL_REQUIRE(d->n_out > 0 && d->n_out <= acrl::kMaxOut, "n_out = %lld must lie in [1, %d]", (long long)d->n_out, acrl::kMaxOut);
+  ACRL_REQUIRE(d->B >= 0 && d->B <= (1 << 20), "B = %lld must lie in [0, 2^20]", (long long)d->B);
+  ACRL_REQUIRE(d->outer >= 0 && d->outer <= (1 << 20), "outer = %lld must lie in [0, 2^20]", (long long)d->outer);
+  ACRL_REQUIRE(d->row_bytes >= 0 && d->row_bytes < ((int64_t)1 << 40), "row_bytes = %lld must lie in [0, 2^40)",
+               (long long)d->row_bytes);
+  const int64_t strides[] = {d->src_outer, d->src_seq, d->src_beam, d->dst_outer, d->dst_seq, d->dst_beam};
+  for (int64_t v : strides) ACRL_REQUIRE(v >= 0 && v < ((int64_t)1 << 42), "a stride of %lld bytes", (long long)v);
+  const bool none = d->outer == 0 || d->B == 0 || d->row_bytes == 0;
+  bool in_place = false;
+  uintptr_t all = 0;
+  if (!none) {
+    ACRL_REQUIRE(d->src && d->dst && d->parents, "src, dst and parents are required");
+    ACRL_REQUIRE(((uintptr_t)d->parents & 3u) == 0, "parents is misaligned");
+    // (the last byte's place fits 64 bits: factors of at most 2^20, strides below 2^42)
+    ACRL_REQUIRE((d->n_out == 1 || d->dst_beam >= d->row_bytes) && (d->B == 1 || d->dst_seq >= d->row_bytes) &&
+                     (d->outer == 1 || d->dst_outer >= d->row_bytes), "rows of dst overlap");
+    auto last = [&](int64_t so, int64_t ss, int64_t sb, int64_t n) {
+      return (uintptr_t)((d->outer - 1) * so) + (uintptr_t)((d->B - 1) * ss) + (uintptr_t)((n - 1) * sb + d->row_bytes);
+    };
+    const uintptr_t s0 = (uintptr_t)d->src, d0 = (uintptr_t)d->dst;
+    const uintptr_t s1 = s0 + last(d->src_outer, d->src_seq, d->src_beam, d->K);
+    const uintptr_t d1 = d0 + last(d->dst_outer, d->dst_seq, d->dst_beam, d->n_out);
+    in_place = s0 == d0 && d->n_out == d->K && (d->K == 1 || d->src_beam == d->dst_beam) &&
+               (d->B == 1 || d->src_seq == d->dst_seq) && (d->outer == 1 || d->src_outer == d->dst_outer);
+    ACRL_REQUIRE(in_place || s0 >= d1 || d0 >= s1, "dst overlaps src without being src itself");
+    all = s0 | d0 | (uintptr_t)d->row_bytes;
+    for (int64_t v : strides) all |= (uintptr_t)v;
+    // a launch holds fewer than 2^32 threads
+    const int64_t unit = all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 1;
+    ACRL_REQUIRE((d->row_bytes / unit + 255) / 256 * 256 < ((int64_t)1 << 32) / (d->B * d->outer),
+                 "outer x B x row_bytes / %lld too large", (long long)unit);
+  }
+  acrl_status st = acrl::check_device();
+  if (st != ACRL_OK || none) return st;
+  acrl::ReorderParams p{};
+  p.src = static_cast<const uint8_t*>(d->src);
+  p.dst = static_cast<uint8_t*>(d->dst);
+  p.s_outer = d->src_outer;
+  p.s_seq = d->src_seq;
+  p.s_beam = d->src_beam;
+  p.d_outer = d->dst_outer;
+  p.d_seq = d->dst_seq;
+  p.d_beam = d->dst_beam;
+  p.parents = d->parents;
+  p.outer = (int)d->outer;
+  p.B = (int)d->B;
+  p.K = (int)d->K;
+  p.N = (int)d->n_out;
+  p.in_place = in_place;
+  const hipStream_t s = (hipStream_t)stream;
+  hipError_t e;
+  if (all % 16 == 0) e = p.K <= 16 ? acrl::launch_reorder<acrl::u32x4, 256>(p, d->row_bytes, s)
+                                   : acrl::launch_reorder<acrl::u32x4, 64>(p, d->row_bytes, s);
+  else if (all % 4 == 0) e = acrl::launch_reorder<uint32_t, 256>(p, d->row_bytes, s);
+  else e = acrl::launch_reorder<uint8_t, 256>(p, d->row_bytes, s);
+  return acrl::hip_status(e, "acrl_beam_reorder launch");
+}
+
+}  // extern "C"

@@ -856,9 +856,11 @@ void acrl_abi_operator_struct_sizes(size_t* matmul_desc, size_t* policy_loss_des
   if (preference_desc) *preference_desc = sizeof(acrl_preference_desc);
 }
 
-void acrl_abi_decode_struct_sizes(size_t* linear_desc, size_t* moe_desc) {
+void acrl_abi_decode_struct_sizes(size_t* linear_desc, size_t* moe_desc, size_t* beam_desc, size_t* reorder_desc) {
   if (linear_desc) *linear_desc = sizeof(acrl_linear_desc);
   if (moe_desc) *moe_desc = sizeof(acrl_moe_desc);
+  if (beam_desc) *beam_desc = sizeof(acrl_beam_desc);
+  if (reorder_desc) *reorder_desc = sizeof(acrl_reorder_desc);
 }
 
 }  // extern "C"

@@ -106,3 +106,29 @@ def experts(x, ids, w, w_in, w_out, activation="silu", residual=None):
     if residual is None:
         return y, tol
     return y + residual, tol + HALF["f32"] * (np.abs(y + residual) + tol)
+
+
+# ------------------------------------------------------------------ beam search
+def beam(logits, scores, n, inv_t=1.0, finished=None, eos=-1):
+    """(ids, parents, scores) of logits [B, K, V] by a stable sort of all candidates."""
+    B, K, V = logits.shape
+    out = [], [], []
+    for b in range(B):
+        c = np.full((K, V), -np.inf)
+        for j in range(K):
+            if not np.isfinite(scores[b, j]):
+                continue
+            if finished is not None and finished[b, j]:
+                c[j, eos] = scores[b, j]
+                continue
+            z = logits[b, j].astype(np.float64) * float(np.float32(inv_t))
+            if np.isnan(z).any() or not np.isfinite(z.max()):
+                continue
+            # (a sum that no order of the logits changes: beams of the same ones are equal)
+            c[j] = float(scores[b, j]) + (z - z.max() - math.log(math.fsum(np.exp(z - z.max()))))
+        flat = c.reshape(-1)
+        at = np.argsort(-flat, kind="stable")[:n]
+        out[0].append(at % V)
+        out[1].append(at // V)
+        out[2].append(flat[at])
+    return tuple(np.array(o) for o in out)

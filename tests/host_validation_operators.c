@@ -79,10 +79,12 @@ static acrl_policy_loss_desc policy(void) {
 
 static void linears(void) {
   acrl_linear_desc d;
-  size_t sz[2] = {0};
-  acrl_abi_decode_struct_sizes(&sz[0], &sz[1]);
-  acrl_abi_decode_struct_sizes(NULL, NULL);
-  if (sz[0] != sizeof d || sz[1] != sizeof(acrl_moe_desc)) ++failures;
+  size_t sz[4] = {0};
+  acrl_abi_decode_struct_sizes(&sz[0], &sz[1], &sz[2], &sz[3]);
+  acrl_abi_decode_struct_sizes(NULL, NULL, NULL, NULL);
+  if (sz[0] != sizeof d || sz[1] != sizeof(acrl_moe_desc) || sz[2] != sizeof(acrl_beam_desc) ||
+      sz[3] != sizeof(acrl_reorder_desc))
+    ++failures;
   expect("linear null", acrl_linear_fp8(NULL, NULL), ACRL_ERR_INVALID_ARG);
 #define BAD_LINEAR(change)                                                                      \
   do {                                                                                          \
@@ -159,6 +161,75 @@ static void experts(void) {
   BAD_MOE(d.workspace = buf + 8);
   MOE(d.workspace = NULL, ACRL_ERR_WORKSPACE);
   MOE(d.workspace_bytes = 64, ACRL_ERR_WORKSPACE);
+}
+
+static void beams(void) {
+  acrl_beam_desc d;
+  acrl_reorder_desc r;
+  size_t nb = 0;
+  expect("beam ws", acrl_beam_workspace_size(2, 3, 1000, 4, &nb), ACRL_OK);
+  if (nb < 6 * 4 * 8) ++failures;
+  expect("beam ws null", acrl_beam_workspace_size(2, 3, 1000, 4, NULL), ACRL_ERR_INVALID_ARG);
+  expect("beam ws K", acrl_beam_workspace_size(2, 65, 1000, 4, &nb), ACRL_ERR_INVALID_ARG);
+  expect("beam ws BK", acrl_beam_workspace_size(1 << 20, 4, 1000, 4, &nb), ACRL_ERR_INVALID_ARG);
+  expect("beam ws n", acrl_beam_workspace_size(2, 2, 3, 7, &nb), ACRL_ERR_INVALID_ARG);
+  expect("beam null", acrl_beam_step(NULL, NULL), ACRL_ERR_INVALID_ARG);
+#define BEAM(change, status)                                                                     \
+  do {                                                                                           \
+    memset(&d, 0, sizeof d);                                                                     \
+    d.B = 2; d.K = 3; d.V = 1000; d.n_out = 4; d.logits = p; d.ldl = 1000; d.scores = (float*)p; \
+    d.finished = p; d.eos_id = 5; d.inv_temperature = 1.0f; d.ids = (int32_t*)p;                 \
+    d.parents = (int32_t*)p; d.out_scores = (float*)p; d.workspace = p;                          \
+    d.workspace_bytes = 1 << 30;                                                                 \
+    change;                                                                                      \
+    expect("beam " #change, acrl_beam_step(&d, NULL), status);                                   \
+  } while (0)
+#define BAD_BEAM(change) BEAM(change, ACRL_ERR_INVALID_ARG)
+  BAD_BEAM(d.B = -1);
+  BAD_BEAM(d.V = (int64_t)1 << 30; d.ldl = d.V);
+  BAD_BEAM(d.n_out = 65);
+  BAD_BEAM(d.ldl = 999);
+  BAD_BEAM(d.logits_type = 2);
+  BAD_BEAM(d.eos_id = -1);
+  BAD_BEAM(d.eos_id = 1000);
+  BAD_BEAM(d.inv_temperature = 0.0f);
+  BAD_BEAM(d.inv_temperature = (float)NAN);
+  BAD_BEAM(d.logits = NULL);
+  BAD_BEAM(d.logits = buf + 1);
+  BAD_BEAM(d.parents = NULL);
+  BAD_BEAM(d.scores = (float*)(buf + 2));
+  BAD_BEAM(d.workspace = buf + 8);
+  BEAM(d.workspace = NULL, ACRL_ERR_WORKSPACE);
+  BEAM(d.workspace_bytes = 8, ACRL_ERR_WORKSPACE);
+  expect("reorder null", acrl_beam_reorder(NULL, NULL), ACRL_ERR_INVALID_ARG);
+#define BAD_REORDER(change)                                                                      \
+  do {                                                                                           \
+    memset(&r, 0, sizeof r);                                                                     \
+    r.outer = 2; r.B = 2; r.K = 3; r.n_out = 3; r.row_bytes = 64; r.src = p; r.src_outer = 384;  \
+    r.src_seq = 192; r.src_beam = 64; r.dst = buf + 4096; r.dst_outer = 384; r.dst_seq = 192;    \
+    r.dst_beam = 64; r.parents = (int32_t*)p;                                                    \
+    change;                                                                                      \
+    expect("reorder " #change, acrl_beam_reorder(&r, NULL), ACRL_ERR_INVALID_ARG);               \
+  } while (0)
+  BAD_REORDER(r.K = 0);
+  BAD_REORDER(r.K = 65);
+  BAD_REORDER(r.n_out = 65);
+  BAD_REORDER(r.B = -1);
+  BAD_REORDER(r.outer = (1 << 20) + 1);
+  BAD_REORDER(r.row_bytes = -1);
+  BAD_REORDER(r.row_bytes = (int64_t)1 << 40);
+  BAD_REORDER(r.src_beam = -64);
+  BAD_REORDER(r.dst_outer = (int64_t)1 << 42);
+  BAD_REORDER(r.src = NULL);
+  BAD_REORDER(r.parents = NULL);
+  BAD_REORDER(r.parents = (int32_t*)(buf + 2));
+  BAD_REORDER(r.dst_beam = 63);
+  BAD_REORDER(r.dst_seq = 63);
+  BAD_REORDER(r.dst = buf + 64);
+  BAD_REORDER(r.dst = p; r.dst_beam = 128);
+  BAD_REORDER(r.dst = p; r.n_out = 2);
+  BAD_REORDER(r.row_bytes = (int64_t)1 << 36; r.dst_beam = (int64_t)1 << 37; r.dst_seq = (int64_t)1 << 39;
+              r.dst_outer = (int64_t)1 << 40; r.dst = (void*)((int64_t)1 << 44));
 }
 
 static void policy_losses(void) {
@@ -250,6 +321,7 @@ int main(void) {
   products();
   linears();
   experts();
+  beams();
   policy_losses();
   preference_losses();
   reduces();

@@ -8,7 +8,7 @@ from test_operators_abi import _off, acrl, p  # noqa: F401  (fixtures)
 
 
 def test_descriptor_sizes(acrl):  # noqa: F811
-    descs = (acrl.LinearDesc, acrl.MoeDesc)
+    descs = (acrl.LinearDesc, acrl.MoeDesc, acrl.BeamDesc, acrl.ReorderDesc)
     sizes = [ctypes.c_size_t() for _ in descs]
     acrl.lib().acrl_abi_decode_struct_sizes(*[ctypes.byref(s) for s in sizes])
     assert [s.value for s in sizes] == [ctypes.sizeof(x) for x in descs]
@@ -62,6 +62,44 @@ def test_moe(acrl, p):  # noqa: F811
     assert L.acrl_moe_workspace_size(128, 65536, 512, 16, 65536, ctypes.byref(nb)) == 0 and nb.value > 2048 * 65536 * 8
 
 
+def test_beam(acrl, p):  # noqa: F811
+    L, nb = acrl.lib(), ctypes.c_size_t()
+    ok = dict(B=2, K=3, V=1000, n_out=4, logits=p, ldl=1000, scores=p, finished=p, eos_id=5, inv_temperature=1.0, ids=p, parents=p,
+              out_scores=p, workspace=p, workspace_bytes=1 << 30)
+    sizes = [dict(B=-1), dict(B=(1 << 20) + 1), dict(K=0), dict(K=65), dict(B=1 << 19, K=8), dict(V=0), dict(V=1 << 30, ldl=1 << 30),
+             dict(n_out=0), dict(n_out=65), dict(V=2, n_out=7)]
+    for bad in sizes:
+        s = {**ok, **bad}
+        assert L.acrl_beam_workspace_size(*[s[n] for n in ("B", "K", "V", "n_out")], ctypes.byref(nb)) == 1, bad
+    for bad in sizes + [dict(ldl=999), dict(ldl=1 << 34), dict(logits_type=2), dict(logits_type=-1), dict(eos_id=-1), dict(eos_id=1000),
+                        dict(inv_temperature=0.0), dict(inv_temperature=-1.0), dict(inv_temperature=float("nan")),
+                        dict(inv_temperature=float("inf")), dict(logits=None), dict(scores=None), dict(ids=None), dict(parents=None),
+                        dict(out_scores=None), dict(logits=_off(p, 1)), dict(logits=_off(p, 2), logits_type=1), dict(scores=_off(p, 2)),
+                        dict(ids=_off(p, 2)), dict(parents=_off(p, 1)), dict(out_scores=_off(p, 3)), dict(workspace=_off(p, 8))]:
+        d = acrl.BeamDesc(**{**ok, **bad})
+        assert L.acrl_beam_step(ctypes.byref(d), None) == acrl.ACRL_ERR_INVALID_ARG, bad
+        assert L.acrl_last_error()
+    for bad in (dict(workspace=None), dict(workspace_bytes=100)):
+        d = acrl.BeamDesc(**{**ok, **bad})
+        assert L.acrl_beam_step(ctypes.byref(d), None) == acrl.ACRL_ERR_WORKSPACE, bad
+    assert L.acrl_beam_step(None, None) == acrl.ACRL_ERR_INVALID_ARG
+
+
+def test_reorder(acrl, p):  # noqa: F811
+    L = acrl.lib()
+    ok = dict(outer=2, B=2, K=3, n_out=3, row_bytes=64, src=p, src_outer=384, src_seq=192, src_beam=64, dst=_off(p, 2048), dst_outer=384,
+              dst_seq=192, dst_beam=64, parents=p)
+    for bad in (dict(K=0), dict(K=65), dict(n_out=0), dict(n_out=65), dict(B=-1), dict(B=(1 << 20) + 1), dict(outer=-1),
+                dict(outer=(1 << 20) + 1), dict(row_bytes=-1), dict(row_bytes=1 << 40), dict(src_beam=-64), dict(src_seq=1 << 42),
+                dict(dst_outer=-1), dict(src=None), dict(dst=None), dict(parents=None), dict(parents=_off(p, 2)), dict(dst_beam=63),
+                dict(dst_seq=0), dict(dst_outer=63), dict(dst=_off(p, 64)), dict(dst=p, dst_beam=128, dst_seq=384, dst_outer=768),
+                dict(dst=p, n_out=2), dict(src=_off(p, 2048), dst=p, row_bytes=64, dst_outer=2048)):
+        d = acrl.ReorderDesc(**{**ok, **bad})
+        assert L.acrl_beam_reorder(ctypes.byref(d), None) == acrl.ACRL_ERR_INVALID_ARG, bad
+        assert L.acrl_last_error()
+    assert L.acrl_beam_reorder(None, None) == acrl.ACRL_ERR_INVALID_ARG
+
+
 def test_binding_refuses_host_tensors(acrl):  # noqa: F811
     import torch
     q, s = torch.zeros((4, 128), dtype=torch.uint8), torch.ones((4, 1))
@@ -70,3 +108,8 @@ def test_binding_refuses_host_tensors(acrl):  # noqa: F811
     x, w = torch.zeros((2, 32), dtype=torch.bfloat16), torch.zeros((1, 64, 32), dtype=torch.uint8)
     with pytest.raises(ValueError, match="device tensor"):
         acrl.acrl_moe_fp8(x, w, s[:1], w[:, :32], s[:1], 1, router=x[:1])
+    z, i = torch.zeros((4, 8)), torch.zeros((2, 2), dtype=torch.int32)
+    with pytest.raises(ValueError, match="device tensor"):
+        acrl.acrl_beam_step(z, z[:2, :2], 2)
+    with pytest.raises(ValueError, match="device tensor"):
+        acrl.acrl_beam_reorder(z.view(2, 2, 8), i)

@@ -5,19 +5,24 @@
 // normaliser that is off by an fp32 rounding would now and then choose another
 // candidate: exponentials and sums are fp64.  Within a beam the order is that of
 // the logits alone.
+#include <float.h>
+
 #include <algorithm>
+#include <type_traits>
 
 #include "entry.h"
 
 namespace acrl {
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_anywhere __attribute__((ext_vector_type(4), aligned(2)));
 
 constexpr int kMaxBeams = 64, kMaxOut = 64;
-constexpr int kScanWaves = 8, kEach = 16, kTile = 64 * kEach;  // logits of a lane, of a wave at a time
+constexpr int kScanWaves = 8, kEach = 8, kTile = 64 * kEach;  // logits of a lane, of a wave at a time
+constexpr int kKept = 256, kNotes = 512 + kScanWaves * kTile;  // notes of a workgroup: left between tiles, at most
+static_assert(kKept >= kMaxOut && kKept <= 64 * kScanWaves && kNotes >= kKept + kScanWaves * kTile, "notes fit");
 constexpr int kPickWaves = 4, kMaxLists = 64 * kPickWaves, kMaxStaged = 6144;
 constexpr int kNone = 0x7FFFFFFF;
 
@@ -43,20 +48,19 @@ struct BeamParams {
 __device__ __forceinline__ bool alive(float score) { return fabsf(score) < INFINITY; }
 
 // 2^t for t in [-1000, 1000] (below: as -1000): the polynomial is an interpolation of
-// 2^f, |f| <= 1/2, at Chebyshev's points, within 1.1e-12 of it.
+// 2^f, |f| <= 1/2, at Chebyshev's points, within 5.5e-11 of it.
 __device__ __forceinline__ double exp2_f64(double t) {
   constexpr double kRound = 6755399441055744.0;  // 1.5 2^52: added, it leaves t's integer in the low bits
   t = fmax(t, -1000.0);
   const double r = t + kRound, f = t - (r - kRound);
-  double p = 1.3255224884799127e-06;
-  p = fma(p, f, 1.5310079402383103e-05);
-  p = fma(p, f, 0.00015403455852419016);
-  p = fma(p, f, 0.0013333450568000008);
-  p = fma(p, f, 0.00961812915940262);
-  p = fma(p, f, 0.05550410941205934);
-  p = fma(p, f, 0.2402265069581299);
-  p = fma(p, f, 0.6931471805459335);
-  p = fma(p, f, 1.0);
+  double p = 1.5303700711425663e-05;
+  p = fma(p, f, 0.00015469729214122798);
+  p = fma(p, f, 0.0013333478473685175);
+  p = fma(p, f, 0.009618025613318018);
+  p = fma(p, f, 0.055504109063258665);
+  p = fma(p, f, 0.24022651213498092);
+  p = fma(p, f, 0.6931471805568324);
+  p = fma(p, f, 0.9999999999595618);
   return __hiloint2double(__double2hiint(p) + (__double2loint(r) << 20), __double2loint(p));
 }
 
@@ -64,6 +68,12 @@ __device__ __forceinline__ double shfl_xor_f64(double v, int m) {
   return __hiloint2double(__shfl_xor(__double2hiint(v), m), __shfl_xor(__double2loint(v), m));
 }
 __device__ __forceinline__ int read_lane(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+// fp32 values in their order as integers, and back.
+__device__ __forceinline__ uint32_t order_of(float v) {
+  const uint32_t u = __float_as_uint(v);
+  return u >> 31 ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o >> 31 ? o & 0x7FFFFFFFu : ~o); }
 __device__ __forceinline__ int lowest(uint64_t mask) { return __builtin_ctzll(mask); }
 
 // A lane's kEach consecutive logits, as they are read; those past `left` count as -infinity.
@@ -101,19 +111,81 @@ struct Logits {
 
 // 64-bit keys: the larger value first, then the lower token; -0 as 0.
 __device__ __forceinline__ uint64_t key_of(float v, int idx) {
-  const uint32_t u = __float_as_uint(v == 0.0f ? 0.0f : v);
-  return (uint64_t)(u >> 31 ? ~u : u | 0x80000000u) << 32 | (uint32_t)~idx;
+  return (uint64_t)order_of(v == 0.0f ? 0.0f : v) << 32 | (uint32_t)~idx;
 }
 
+// Workgroup barrier that leaves loads into registers under way.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // One pass over a row's segment: the sum of exponentials and the N largest
-// logits.  A wave keeps its own N largest, one a lane, and looks closer at a tile
-// only where a lane's largest beats the least of them: few tiles after the first
-// (N ln(tiles) candidates for logits in no order, N a tile at most, the largest
-// first).  No wave waits for another before the end.
+// logits.  A workgroup notes in LDS, key by key, what is no less than a bar; when
+// there are many notes they are thinned out to the N largest, and the least of
+// those is the bar from there on.  With logits in no order that happens once or
+// twice.  (A list of N a wave, kept in order by insertions of 100 instructions and
+// more, 50 of them a wave at N = 16, took 28 us more of 103 at 512 x 151936.)
+struct Scan {
+  uint64_t notes[kNotes];
+  double norms[kScanWaves][2];
+  uint32_t first_bar[kScanWaves];
+  int digits[3][256] __attribute__((aligned(16)));
+  int count, left;
+};
+
+// The notes down to the N largest, by all threads: the N-th largest key by its
+// digits of eight bits, counted in LDS, from the value's first until the keys that
+// are no less than it are N (three or four for logits in no order; the token's
+// digits only where others share the value).  Bit by bit, a barrier each, it took
+// 15 us instead of 1.  Returns the N-th's value, by order_of.
+__device__ __forceinline__ int sum_before(int v) {  // of the lanes up to this one
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // (into rows 1 and 3)
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // (into rows 2 and 3)
+  return v;
+}
+__device__ __forceinline__ uint32_t thin_out(Scan& s, int count, int N) {
+  const int lane = threadIdx.x & 63;
+  if (threadIdx.x < 256) s.digits[0][threadIdx.x] = 0;
+  if (threadIdx.x == 0) s.left = 0;
+  lds_barrier();
+  uint64_t nth = 0;
+  int need = N;  // of the keys that begin as nth does
+  for (int shift = 56, now = 0; shift >= 0; shift -= 8, now = now == 2 ? 0 : now + 1) {
+    if (threadIdx.x < 256) s.digits[now == 2 ? 0 : now + 1][threadIdx.x] = 0;  // (the next; the one before may still be read)
+    for (int i = threadIdx.x; i < count; i += 64 * kScanWaves) {
+      const uint64_t k = s.notes[i];
+      if (shift == 56 || k >> (shift + 8) == nth >> (shift + 8)) atomicAdd(&s.digits[now][k >> shift & 255], 1);
+    }
+    lds_barrier();
+    // lane l counts the digits 255 - 4 l .. 252 - 4 l
+    const i32x4 n = *reinterpret_cast<const i32x4*>(&s.digits[now][252 - 4 * lane]);
+    const int all = n[0] + n[1] + n[2] + n[3], upto = sum_before(all);
+    const int who = lowest(__ballot(upto >= need));
+    int above = upto - all, d = 3;  // keys above digit 252 - 4 l + d
+    while (d > 0 && above + n[d] < need) above += n[d--];
+    const int digit = 252 - 4 * who + read_lane(d, who), same = read_lane(d == 3 ? n[3] : d == 2 ? n[2] : d == 1 ? n[1] : n[0], who);
+    need -= read_lane(above, who);
+    nth |= (uint64_t)digit << shift;
+    if (same == need) break;
+  }
+  // (what stays is written to places that have been read: no more stays than was)
+  for (int first = 0; first < count; first += 64 * kScanWaves) {
+    const int i = first + threadIdx.x;
+    const uint64_t k = i < count ? s.notes[i] : 0;
+    lds_barrier();
+    if (k >= nth && i < count) s.notes[atomicAdd(&s.left, 1)] = k;
+    lds_barrier();
+  }
+  if (threadIdx.x == 0) s.count = s.left;
+  lds_barrier();
+  return (uint32_t)(nth >> 32);
+}
+
 template <typename T>
-__global__ __launch_bounds__(64 * kScanWaves) void beam_scan_kernel(BeamParams p) {
-  __shared__ uint64_t keys[kScanWaves * kMaxOut];
-  __shared__ double norms[kScanWaves][2];
+__global__ __launch_bounds__(64 * kScanWaves, 8) void beam_scan_kernel(BeamParams p) {
+  __shared__ Scan s;
   const int row = blockIdx.x / p.S, seg = blockIdx.x % p.S;
   if (!alive(p.scores[row]) || (p.finished && p.finished[row])) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -122,26 +194,61 @@ __global__ __launch_bounds__(64 * kScanWaves) void beam_scan_kernel(BeamParams p
   const int64_t end = min((int64_t)p.V, begin + (int64_t)p.seg_tiles * kTile);
   const double c = (double)p.inv_t * 1.4426950408889634074;  // (the same rounding for all terms)
   const int N = p.N;
-  float held = lane < N ? -INFINITY : INFINITY;  // the wave's N largest (empty: -infinity)
-  int held_idx = kNone;
-  float least = -INFINITY;
   float m = -INFINITY;  // the lane's reference: no more than 2^900 below any of its logits
   double sum = 0.0;
   bool bad = false;
   Logits<T> next;
   int64_t at = begin + (int64_t)wave * kTile + lane * kEach;
   next.read(z + at, (int)max((int64_t)-1, min(end - at, (int64_t)kEach)));
-  for (int64_t tile = begin + (int64_t)wave * kTile; tile < end; tile += kScanWaves * kTile) {
+  if (threadIdx.x == 0) s.count = 0;
+  // The first bar: each of the W waves whose tile is whole has q = ceil(N / W) logits that are no less than the q-th
+  // largest of its lanes' largest, so N of the workgroup's are no less than the least of these.
+  uint32_t bar = order_of(-FLT_MAX);
+  const int W = (int)min((int64_t)kScanWaves, (end - begin) / kTile), q = W ? (N + W - 1) / W : 0;
+  if (W) {
+    float top = next[0];
+#pragma unroll
+    for (int i = 1; i < kEach; ++i) top = fmaxf(top, next[i]);
+    const uint32_t mine = top == top ? order_of(top + 0.0f) : 0;  // (-0 as 0)
+    uint32_t nth = 0;
+    for (uint32_t bit = 1u << 31; bit; bit >>= 1)
+      if (__popcll(__ballot(mine >= (nth | bit))) >= q) nth |= bit;
+    if (lane == 0) s.first_bar[wave] = nth;
+    lds_barrier();
+    nth = ~0u;
+    for (int w = 0; w < W; ++w) nth = min(nth, s.first_bar[w]);
+    bar = max(bar, nth);
+  } else {
+    lds_barrier();
+  }
+  for (int64_t first = begin; first < end; first += kScanWaves * kTile) {
     float x[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) x[i] = next[i];
+    const int64_t here = at;
     at += kScanWaves * kTile;
     next.read(z + at, (int)max((int64_t)-1, min(end - at, (int64_t)kEach)));
     float top = x[0];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      top = fmaxf(top, x[i]);
-      bad |= !(x[i] < INFINITY);
+    for (int i = 0; i < kEach; i += 2) {
+      top = fmaxf(top, fmaxf(x[i], x[i + 1]));
+      bad |= __builtin_isunordered(x[i], x[i + 1]);
+    }
+    bad |= top == INFINITY;
+    const float cut = value_of(bar);
+    if (__ballot(top >= cut)) {
+      uint64_t pass[kEach];
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) n += __popcll(pass[i] = __ballot(x[i] >= cut));
+      int to = 0;
+      if (lane == 0) to = atomicAdd(&s.count, n);
+      to = read_lane(to, 0);
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        if (x[i] >= cut) s.notes[to + __popcll(pass[i] & ((1ull << lane) - 1))] = key_of(x[i], (int)(here + i));
+        to += __popcll(pass[i]);
+      }
     }
     if (((double)top - (double)m) * c > 900.0) {
       sum *= exp2_f64(((double)m - (double)top) * c);
@@ -150,68 +257,41 @@ __global__ __launch_bounds__(64 * kScanWaves) void beam_scan_kernel(BeamParams p
     const double mc = (double)m * c;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) sum += exp2_f64(fma((double)x[i], c, -mc));
-    while (__ballot(top > least)) {
-      const float best = wave_max(top);
-      const int who = lowest(__ballot(top == best));
-      int i = kEach;
-#pragma unroll
-      for (int k = kEach - 1; k >= 0; --k) i = x[k] == best ? k : i;
-      i = read_lane(i, who);
-      if (i == kEach) break;  // (a NaN that is a lane's largest: no normaliser, no candidates)
-      // it takes the place of the least: of equal ones the last token's
-      uint64_t mine = __ballot(held == least);
-      int out = lowest(mine);
-      for (uint64_t rest = mine & (mine - 1); rest; rest &= rest - 1)
-        if (read_lane(held_idx, lowest(rest)) > read_lane(held_idx, out)) out = lowest(rest);
-      if (lane == out) {
-        held = best;
-        held_idx = (int)(tile + who * kEach + i);
-      }
-      least = -wave_max(-held);
-      if (lane == who) {
-#pragma unroll
-        for (int k = 0; k < kEach; ++k) x[k] = k == i ? -INFINITY : x[k];
-      }
-      top = x[0];
-#pragma unroll
-      for (int k = 1; k < kEach; ++k) top = fmaxf(top, x[k]);
-    }
+    lds_barrier();
+    const int count = s.count;
+    lds_barrier();  // (all have read it before any wave notes more)
+    if (count > kKept) bar = thin_out(s, count, N);
   }
-  // the waves' sums and lists together
+  // the waves' sums together
   const float ref = wave_max(m);
   sum *= exp2_f64(((double)m - (double)ref) * c);
   for (int o = 32; o; o /= 2) sum += shfl_xor_f64(sum, o);
   const bool any_bad = __ballot(bad) != 0;
-  if (lane < N) keys[wave * N + lane] = held_idx == kNone ? 0 : key_of(held, held_idx);
   if (lane == 0) {
-    norms[wave][0] = any_bad ? (double)NAN : (double)ref;
-    norms[wave][1] = sum;
+    s.norms[wave][0] = any_bad ? (double)NAN : (double)ref;
+    s.norms[wave][1] = sum;
   }
   __syncthreads();
   const int64_t slot = blockIdx.x;
-  const int n = kScanWaves * N;
+  const int n = s.count;
   if ((int)threadIdx.x < n) {
-    const uint64_t k = keys[threadIdx.x];
-    int rank = 0, filled = 0;
-    for (int i = 0; i < n; ++i) {
-      rank += keys[i] > k;
-      filled += keys[i] != 0;
-    }
-    if (k && rank < N) {
-      const uint32_t u = (uint32_t)(k >> 32);
-      p.val[slot * N + rank] = __uint_as_float(u >> 31 ? u & 0x7FFFFFFFu : ~u);
+    const uint64_t k = s.notes[threadIdx.x];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += s.notes[j] > k;
+    if (rank < N) {
+      p.val[slot * N + rank] = value_of((uint32_t)(k >> 32));
       p.idx[slot * N + rank] = (int)~(uint32_t)k;
     }
-    if ((int)threadIdx.x < N && (int)threadIdx.x >= filled) p.idx[slot * N + threadIdx.x] = kNone;
   }
+  for (int i = n + threadIdx.x; i < N; i += 64 * kScanWaves) p.idx[slot * N + i] = kNone;
   if (threadIdx.x == 0) {
     double ref_all = -INFINITY, total = 0.0;
     bool none = false;
     for (int w = 0; w < kScanWaves; ++w) {
-      none |= norms[w][0] != norms[w][0];
-      if (norms[w][0] > ref_all) ref_all = norms[w][0];
+      none |= s.norms[w][0] != s.norms[w][0];
+      if (s.norms[w][0] > ref_all) ref_all = s.norms[w][0];
     }
-    for (int w = 0; w < kScanWaves; ++w) total += norms[w][1] * exp2_f64((norms[w][0] - ref_all) * c);
+    for (int w = 0; w < kScanWaves; ++w) total += s.norms[w][1] * exp2_f64((s.norms[w][0] - ref_all) * c);
     p.norm[2 * slot] = none ? (double)NAN : ref_all;
     p.norm[2 * slot + 1] = total;
   }
@@ -227,22 +307,22 @@ __device__ __forceinline__ double value_of(uint64_t k) {
   return __longlong_as_double((long long)(k >> 63 ? k & ~(1ull << 63) : ~k));
 }
 template <int CTRL>
-__device__ __forceinline__ uint64_t dpp_u64(uint64_t v) {
-  const uint32_t lo = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)v, CTRL, 0xF, 0xF, true);
-  const uint32_t hi = (uint32_t)__builtin_amdgcn_mov_dpp((int)(v >> 32), CTRL, 0xF, 0xF, true);
-  return (uint64_t)hi << 32 | lo;
+__device__ __forceinline__ uint64_t max_step(uint64_t v) {
+  const int lo = (int)(uint32_t)v, hi = (int)(v >> 32);
+  const uint64_t o = (uint64_t)(uint32_t)__builtin_amdgcn_update_dpp(hi, hi, CTRL, 0xF, 0xF, false) << 32 |
+                     (uint32_t)__builtin_amdgcn_update_dpp(lo, lo, CTRL, 0xF, 0xF, false);
+  return max(v, o);
 }
-__device__ __forceinline__ uint64_t shfl_u64(uint64_t v, int m) {
-  return (uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), m) << 32 | (uint32_t)__shfl_xor((int)(uint32_t)v, m);
-}
-__device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
-  v = max(v, dpp_u64<0xB1>(v));
-  v = max(v, dpp_u64<0x4E>(v));
-  v = max(v, dpp_u64<0x124>(v));
-  v = max(v, dpp_u64<0x128>(v));
-  v = max(v, shfl_u64(v, 16));
-  v = max(v, shfl_u64(v, 32));
-  return v;
+// The largest of a wave's keys, in every lane: DPP steps alone (row_shr 1, 2, 4, 8, then rows into the rows behind them),
+// whose latency counts where one result is waited for after another.
+__device__ __forceinline__ uint64_t largest(uint64_t v) {
+  v = max_step<0x111>(v);
+  v = max_step<0x112>(v);
+  v = max_step<0x114>(v);
+  v = max_step<0x118>(v);
+  v = max_step<0x142>(v);
+  v = max_step<0x143>(v);
+  return (uint64_t)(uint32_t)read_lane((int)(v >> 32), 63) << 32 | (uint32_t)read_lane((int)(uint32_t)v, 63);
 }
 
 struct Candidate {
@@ -251,7 +331,7 @@ struct Candidate {
 };
 // The lane whose candidate comes first, or -1.
 __device__ __forceinline__ int first_of(const Candidate& c) {
-  const uint64_t best = wave_max_u64(c.key);
+  const uint64_t best = largest(c.key);
   if (best == 0) return -1;
   const uint64_t same = __ballot(c.key == best);
   int who = lowest(same);
@@ -302,7 +382,7 @@ __global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p
   __syncthreads();
   const int mine = lists <= 64 ? (wave == 0 ? lane : lists) : threadIdx.x;  // the lane's list
   int at = 0;
-  auto head = [&]() {
+  auto head = [&](int at) {  // (the one behind a head is looked up before it is needed: a lookup is three reads, one by one)
     Candidate r = {0, 0, 0};
     if (mine >= lists || at >= N) return r;
     r.beam = mine / p.S;
@@ -325,26 +405,26 @@ __global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p
   int n = 0;
   if (lists <= 64) {
     if (wave != 0) return;
-    Candidate h = head();
+    Candidate h = head(0), behind = head(1);
     for (; n < N; ++n) {
       const int who = first_of(h);
       if (who < 0) break;
       emit(n, who, h);
       if (lane == who) {
-        ++at;
-        h = head();
+        h = behind;
+        behind = head(++at + 1);
       }
     }
   } else {
-    Candidate h = head();
+    Candidate h = head(0), behind = head(1);
     int k = 0;
     for (; k < N; ++k) {
       const int who = first_of(h);
       if (who < 0) break;
       if (lane == who) {
         merged[wave][k] = h;
-        ++at;
-        h = head();
+        h = behind;
+        behind = head(++at + 1);
       }
     }
     if (lane >= k && lane < N) merged[wave][lane] = Candidate{0, 0, 0};
@@ -449,12 +529,14 @@ hipError_t launch_reorder(ReorderParams p, int64_t row_bytes, hipStream_t s) {
 // ------------------------------------------------------------------ host
 constexpr int kCus = 256;
 
-// Segments: two workgroups a CU where the rows are few, each of a tile a wave at least; as many lists as the pick has
-// lanes for, and LDS.
+// Segments: four workgroups a CU (512 x 151936: 107 us with two) where the rows allow it, each of a tile a wave at
+// least; a wave's lists at most (1 x 4 x 151936: 18 us, 24 with 38 of them) unless segments would have more than four such tiles; what the
+// pick has lanes and LDS for.
 void segment(BeamParams& p) {
   const int64_t rows = (int64_t)p.B * p.K, tiles = ((int64_t)p.V + kTile - 1) / kTile;
-  int64_t S = rows ? std::max<int64_t>(1, 2 * kCus / rows) : 1;
-  S = std::min(S, (tiles + kScanWaves - 1) / kScanWaves);
+  int64_t S = rows ? std::max<int64_t>(1, (4 * kCus + rows - 1) / rows) : 1;
+  const int64_t most = (tiles + kScanWaves - 1) / kScanWaves;
+  S = std::min(S, std::min(most, std::max<int64_t>(64 / p.K, (most + 3) / 4)));
   S = std::min<int64_t>(S, std::min(kMaxLists / p.K, std::max(1, kMaxStaged / (p.K * p.N))));
   p.seg_tiles = (int)((tiles + S - 1) / S);
   p.S = (int)((tiles + p.seg_tiles - 1) / p.seg_tiles);

@@ -11,6 +11,7 @@
 #include <type_traits>
 
 #include "entry.h"
+#include "lanes.h"
 
 namespace acrl {
 namespace {
@@ -64,17 +65,12 @@ __device__ __forceinline__ double exp2_f64(double t) {
   return __hiloint2double(__double2hiint(p) + (__double2loint(r) << 20), __double2loint(p));
 }
 
-__device__ __forceinline__ double shfl_xor_f64(double v, int m) {
-  return __hiloint2double(__shfl_xor(__double2hiint(v), m), __shfl_xor(__double2loint(v), m));
-}
-__device__ __forceinline__ int read_lane(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 // fp32 values in their order as integers, and back.
 __device__ __forceinline__ uint32_t order_of(float v) {
   const uint32_t u = __float_as_uint(v);
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o >> 31 ? o & 0x7FFFFFFFu : ~o); }
-__device__ __forceinline__ int lowest(uint64_t mask) { return __builtin_ctzll(mask); }
 
 // A lane's kEach consecutive logits, as they are read; those past `left` count as -infinity.
 template <typename T>
@@ -113,9 +109,6 @@ struct Logits {
 __device__ __forceinline__ uint64_t key_of(float v, int idx) {
   return (uint64_t)order_of(v == 0.0f ? 0.0f : v) << 32 | (uint32_t)~idx;
 }
-
-// Workgroup barrier that leaves loads into registers under way.
-__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // One pass over a row's segment: the sum of exponentials and the N largest
 // logits.  A workgroup notes in LDS, key by key, what is no less than a bar; when
@@ -297,34 +290,8 @@ __global__ __launch_bounds__(64 * kScanWaves, 8) void beam_scan_kernel(BeamParam
   }
 }
 
-// The larger score first, then the lower beam, then the lower token: score in a 64-bit key, the lanes that share the
-// largest told apart by the rest.  0: no candidate.
-__device__ __forceinline__ uint64_t key_of(double v) {
-  const uint64_t u = (uint64_t)__double_as_longlong(v == 0.0 ? 0.0 : v);
-  return u >> 63 ? ~u : u | 1ull << 63;
-}
-__device__ __forceinline__ double value_of(uint64_t k) {
-  return __longlong_as_double((long long)(k >> 63 ? k & ~(1ull << 63) : ~k));
-}
-template <int CTRL>
-__device__ __forceinline__ uint64_t max_step(uint64_t v) {
-  const int lo = (int)(uint32_t)v, hi = (int)(v >> 32);
-  const uint64_t o = (uint64_t)(uint32_t)__builtin_amdgcn_update_dpp(hi, hi, CTRL, 0xF, 0xF, false) << 32 |
-                     (uint32_t)__builtin_amdgcn_update_dpp(lo, lo, CTRL, 0xF, 0xF, false);
-  return max(v, o);
-}
-// The largest of a wave's keys, in every lane: DPP steps alone (row_shr 1, 2, 4, 8, then rows into the rows behind them),
-// whose latency counts where one result is waited for after another.
-__device__ __forceinline__ uint64_t largest(uint64_t v) {
-  v = max_step<0x111>(v);
-  v = max_step<0x112>(v);
-  v = max_step<0x114>(v);
-  v = max_step<0x118>(v);
-  v = max_step<0x142>(v);
-  v = max_step<0x143>(v);
-  return (uint64_t)(uint32_t)read_lane((int)(v >> 32), 63) << 32 | (uint32_t)read_lane((int)(uint32_t)v, 63);
-}
-
+// The larger score first, then the lower beam, then the lower token: the score in a 64-bit key, lanes that share the
+// largest told apart by the rest.  Key 0: no candidate.
 struct Candidate {
   uint64_t key;
   int beam, id;
@@ -388,10 +355,10 @@ __global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p
     r.beam = mine / p.S;
     if (state[r.beam] == 2 && mine % p.S == 0 && at == 0) {
       r.id = p.eos;
-      r.key = key_of(score[r.beam]);
+      r.key = score_key(score[r.beam]);
     } else if (state[r.beam] == 1 && idx[mine * N + at] != kNone) {
       r.id = idx[mine * N + at];
-      r.key = key_of(score[r.beam] + ((double)val[mine * N + at] * (double)p.inv_t - lse[r.beam]));
+      r.key = score_key(score[r.beam] + ((double)val[mine * N + at] * (double)p.inv_t - lse[r.beam]));
     }
     return r;
   };
@@ -399,7 +366,7 @@ __global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p
     if (lane == who) {
       p.ids[(int64_t)b * N + k] = chosen_id[k] = h.id;
       p.parents[(int64_t)b * N + k] = chosen_beam[k] = h.beam;
-      p.out[(int64_t)b * N + k] = (float)value_of(h.key);
+      p.out[(int64_t)b * N + k] = (float)score_of(h.key);
     }
   };
   int n = 0;

@@ -13,6 +13,7 @@
 // block's scale by one FMA each.
 #include "activation.h"
 #include "entry.h"
+#include "lanes.h"
 
 namespace acrl {
 namespace {
@@ -50,32 +51,24 @@ struct MoeParams {
   int score, renormalize, act;
   float scale;
   int kb_d, kb_f;                  // scale blocks of a row of Win, of Wout
-  int n_lists;                     // min(E, T k): experts that may be chosen
+  int by_pair;                     // there are fewer pairs than experts
   int up_wk, down_wk;              // waves that share a tile's K
   // workspace
   double* logits;                  // [T][E]
-  int* arrived;
-  int* lists;                      // number of chosen experts, then (expert, first position, pairs) of each
-  int* pairs;                      // [T k] pairs t k + j by expert
-  uint16_t* hi;                    // [T k][F] by position in `pairs`
+  uint16_t* hi;                    // [T k][F] by pair t k + j
   uint16_t* lo;
-  float* part;                     // [T k][d] by pair
+  float* part;                     // [T k][d]
 };
 
 __device__ __forceinline__ bool live(const MoeParams& p, int t) { return !p.mask || p.mask[t]; }
 
 // ------------------------------------------------------------------ router
-__device__ __forceinline__ double shfl_xor_f64(double v, int m) {
-  return __hiloint2double(__shfl_xor(__double2hiint(v), m), __shfl_xor(__double2loint(v), m));
-}
-
 // The router's logits in 64 bits, so that which of two experts is chosen does not
 // hang on the order of the sum: a wave takes one expert and NT tokens, 8 columns
 // a lane at a time, each router value converted once for all of them.
 template <int NT>
 __global__ __launch_bounds__(256) void moe_logits_kernel(MoeParams p) {
   const int lane = threadIdx.x & 63, e = blockIdx.x * 4 + (threadIdx.x >> 6), t0 = blockIdx.y * NT;
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.arrived = 0;  // (of the kernel behind this one)
   if (e >= p.E) return;
   const uint16_t* const r = p.router + (int64_t)e * p.d;
   double acc[NT] = {};
@@ -107,9 +100,10 @@ __global__ __launch_bounds__(256) void moe_logits_kernel(MoeParams p) {
   if (lane % (64 / NT) == 0 && t < p.T) p.logits[(int64_t)t * p.E + e] = acc[0];
 }
 
-// Choice of a token's experts by one wave: lane l has the experts l, l + 64, ..
-__device__ __forceinline__ void choose(const MoeParams& p, int t, int lane) {
-  constexpr int kEach = kMaxExperts / 64;
+// Choice of a token's experts by one wave: lane l has the experts l, l + 64, .. (EACH of them).
+template <int EACH>
+__global__ __launch_bounds__(64) void moe_choose_kernel(MoeParams p) {
+  const int t = blockIdx.x, lane = threadIdx.x;
   if (!live(p, t)) {
     if (lane < p.k) {
       p.ids[t * p.k + lane] = -1;
@@ -117,65 +111,64 @@ __device__ __forceinline__ void choose(const MoeParams& p, int t, int lane) {
     }
     return;
   }
-  double s[kEach], by[kEach];  // the score, what the choice goes by (NaN counts as the lowest)
+  double s[EACH];     // the score
+  uint64_t by[EACH];  // what the choice goes by, in order (NaN counts as the lowest; 0: chosen)
   double top = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) {
+  for (int i = 0; i < EACH; ++i) {
     const int e = 64 * i + lane;
     s[i] = e < p.E ? p.logits[(int64_t)t * p.E + e] : -INFINITY;
-    by[i] = s[i];
+    by[i] = score_key(s[i] == s[i] ? s[i] : -INFINITY);
     if (s[i] > top) top = s[i];
   }
   if (p.score == ACRL_MOE_SOFTMAX) {
-    for (int m = 32; m; m /= 2) {
-      const double o = shfl_xor_f64(top, m);
-      if (o > top) top = o;
-    }
+    top = score_of(largest(score_key(top)));
     double sum = 0.0;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i)
+    for (int i = 0; i < EACH; ++i)
       if (64 * i + lane < p.E) {
         s[i] = exp(s[i] - top);
         sum += s[i];
       }
     for (int m = 32; m; m /= 2) sum += shfl_xor_f64(sum, m);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) s[i] /= sum;
+    for (int i = 0; i < EACH; ++i) s[i] /= sum;
   } else {
 #pragma unroll
-    for (int i = 0; i < kEach; ++i)
+    for (int i = 0; i < EACH; ++i)
       if (64 * i + lane < p.E) s[i] = 1.0 / (1.0 + exp(-s[i]));
   }
-  uint32_t open = 0;  // the lane's experts that are not chosen yet
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) {
+  for (int i = 0; i < EACH; ++i) {
     const int e = 64 * i + lane;
-    if (e < p.E) open |= 1u << i;
-    if (p.bias && e < p.E) by[i] = s[i] + (double)p.bias[e];
-    if (by[i] != by[i]) by[i] = -INFINITY;
+    if (p.bias && e < p.E) {
+      const double v = s[i] + (double)p.bias[e];
+      by[i] = score_key(v == v ? v : -INFINITY);
+    }
+    if (e >= p.E) by[i] = 0;
   }
   double mine = 0.0, total = 0.0;  // lane j: the score of the j-th choice
   int mine_id = 0;
   for (int j = 0; j < p.k; ++j) {
-    double best = -INFINITY, best_s = 0.0;
-    int id = kMaxExperts;
+    uint64_t best = by[0];
+    double best_s = s[0];
+    int id = lane;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i)
-      if ((open >> i & 1) && (id == kMaxExperts || by[i] > best)) {
+    for (int i = 1; i < EACH; ++i)
+      if (by[i] > best) {
         best = by[i];
         best_s = s[i];
         id = 64 * i + lane;
       }
-    for (int m = 32; m; m /= 2) {
-      const double o = shfl_xor_f64(best, m), os = shfl_xor_f64(best_s, m);
-      const int oid = __shfl_xor(id, m);
-      if (oid < kMaxExperts && (id == kMaxExperts || o > best || (o == best && oid < id))) {
-        best = o;
-        best_s = os;
-        id = oid;
-      }
-    }
-    if (id % 64 == lane) open &= ~(1u << (id / 64));
+    const uint64_t most = largest(best);
+    uint64_t same = __ballot(best == most);
+    int who = lowest(same);
+    for (same &= same - 1; same; same &= same - 1)  // equal ones: the lowest index
+      if (read_lane(id, lowest(same)) < read_lane(id, who)) who = lowest(same);
+    id = read_lane(id, who);
+    best_s = read_lane(best_s, who);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) by[i] = 64 * i + lane == id ? 0 : by[i];
     if (lane == j) {
       mine = best_s;
       mine_id = id;
@@ -189,94 +182,41 @@ __device__ __forceinline__ void choose(const MoeParams& p, int t, int lane) {
   }
 }
 
-// The pairs (token, choice) by expert, in their own order within one: by 256
-// threads.  Pairs whose expert is out of range, and those of masked tokens, are
-// in no list.
-struct ListScratch {
-  uint8_t count[kMaxPairs / 64][kMaxExperts];  // of a wave's 64 pairs, by expert
-  int first[kMaxExperts];
+// The pairs (token, choice) of the workgroup's expert, in their order: `pairs`
+// holds n of them.  Row y of the grid is expert y, or, where there are fewer pairs
+// than experts, the expert of pair y if that is its first pair.  Every workgroup
+// looks through all ids (8 KB at most): lists made for all of them would need a
+// kernel of their own (9 us of 53 for one token).
+struct Tokens {
+  uint16_t pairs[kMaxPairs];
+  int counts[kWaves];
 };
-__device__ __forceinline__ void make_lists(const MoeParams& p, ListScratch& s) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, P = p.T * p.k, chunks = (P + 63) / 64;
-  for (int i = threadIdx.x; i < chunks * kMaxExperts / 4; i += 256) reinterpret_cast<uint32_t*>(s.count)[i] = 0;
-  __syncthreads();
-  auto expert = [&](int pair) {
-    if (pair >= P || !live(p, pair / p.k)) return -1;
-    const int e = __hip_atomic_load(p.ids + pair, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return e >= 0 && e < p.E ? e : -1;
-  };
-  auto same = [&](int e) {  // the lanes with the same expert
-    uint64_t m = __ballot(e >= 0);
+__device__ __forceinline__ int expert_of(const MoeParams& p) {
+  const int y = blockIdx.y;
+  if (!p.by_pair) return y;
+  const int e = p.ids[y];
+  return e >= 0 && e < p.E && live(p, y / p.k) ? e : -1;
+}
+__device__ __forceinline__ int find_tokens(const MoeParams& p, int e, Tokens& s) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, P = p.T * p.k;
+  int n = 0;
+  for (int first = 0; first < P; first += 64 * kWaves) {
+    const int pair = first + threadIdx.x;
+    const bool hit = pair < P && p.ids[pair] == e && live(p, pair / p.k);
+    const uint64_t m = __ballot(hit);
+    if (lane == 0) s.counts[wave] = __popcll(m);
+    lds_barrier();
+    int at = n + __popcll(m & ((1ull << lane) - 1));
 #pragma unroll
-    for (int b = 0; b < 9; ++b) {
-      const uint64_t set = __ballot(e >> b & 1);
-      m &= e >> b & 1 ? set : ~set;
+    for (int w = 0; w < kWaves; ++w) {
+      const int c = s.counts[w];
+      at += w < wave ? c : 0;
+      n += c;
     }
-    return m;
-  };
-  const uint64_t before = (1ull << lane) - 1;
-  for (int c = wave; c < chunks; c += 4) {
-    const int e = expert(64 * c + lane);
-    const uint64_t m = same(e);
-    if (e >= 0 && !(m & before)) s.count[c][e] = (uint8_t)__popcll(m);
+    if (hit) s.pairs[at] = (uint16_t)pair;
+    lds_barrier();
   }
-  __syncthreads();
-  if (wave == 0) {
-    int at = 0, n = 0;
-    for (int e0 = 0; e0 < p.E; e0 += 64) {
-      const int e = e0 + lane;
-      int total = 0;
-      if (e < p.E)
-        for (int c = 0; c < chunks; ++c) total += s.count[c][e];
-      int sum = total;
-      for (int o = 1; o < 64; o *= 2) {
-        const int v = __shfl_up(sum, o);
-        if (lane >= o) sum += v;
-      }
-      const uint64_t any = __ballot(total > 0);
-      const int first = at + sum - total;
-      if (e < p.E) s.first[e] = first;
-      if (total) {
-        int* l = p.lists + 1 + 3 * (n + __popcll(any & before));
-        l[0] = e;
-        l[1] = first;
-        l[2] = total;
-      }
-      at += __shfl(sum, 63);
-      n += __popcll(any);
-    }
-    if (lane == 0) p.lists[0] = n;
-  }
-  __syncthreads();
-  for (int c = wave; c < chunks; c += 4) {
-    const int e = expert(64 * c + lane);
-    const uint64_t m = same(e);
-    if (e < 0) continue;
-    int at = s.first[e] + __popcll(m & before);
-    for (int b = 0; b < c; ++b) at += s.count[b][e];
-    p.pairs[at] = 64 * c + lane;
-  }
-}
-
-// Four tokens' choices a workgroup; the one that ends last makes the lists.
-__global__ __launch_bounds__(256) void moe_choose_kernel(MoeParams p) {
-  __shared__ ListScratch scratch;
-  __shared__ int last;
-  const int t = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (t < p.T) choose(p, t, threadIdx.x & 63);
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x == 0) last = atomicAdd(p.arrived, 1) == (int)gridDim.x - 1;
-  __syncthreads();
-  if (!last) return;
-  __threadfence();
-  make_lists(p, scratch);
-}
-
-// The lists of given choices.
-__global__ __launch_bounds__(256) void moe_lists_kernel(MoeParams p) {
-  __shared__ ListScratch scratch;
-  make_lists(p, scratch);
+  return p.by_pair && n && s.pairs[0] != blockIdx.y ? 0 : n;
 }
 
 // ------------------------------------------------------------------ products
@@ -314,11 +254,11 @@ __device__ __forceinline__ Place place(int kb, int K, int q) {
   }
   return r;
 }
-// The codes of a block of a row of weights / the bf16 values of a column as four operands.
-__device__ __forceinline__ void load_codes(const uint8_t* row, const Place& l, i32x4 (&c)[2]) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) c[h] = *reinterpret_cast<const i32x4*>(row + l.at[h]);
+__device__ __forceinline__ bf16x8 cleared(const i32x4& c, bool no) {
+  const i32x4 zero = {0, 0, 0, 0};
+  return __builtin_bit_cast(bf16x8, no ? zero : c);
 }
+// The codes of a block of a row as four operands.
 __device__ __forceinline__ void codes(const i32x4 (&c)[2], const Place& l, bf16x8 (&o)[4]) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -326,90 +266,102 @@ __device__ __forceinline__ void codes(const i32x4 (&c)[2], const Place& l, bf16x
     widen(l.no[h] ? zero : c[h], reinterpret_cast<bf16x8(&)[2]>(o[2 * h]));
   }
 }
-__device__ __forceinline__ void load_column(const uint16_t* col, const Place& l, i32x4 (&c)[4]) {
-#pragma unroll
-  for (int h = 0; h < 4; ++h) c[h] = *reinterpret_cast<const i32x4*>(col + l.at[h / 2] + 8 * (h % 2));
-}
-__device__ __forceinline__ bf16x8 column(const i32x4 (&c)[4], const Place& l, int h) {
-  const i32x4 zero = {0, 0, 0, 0};
-  return __builtin_bit_cast(bf16x8, l.no[h / 2] ? zero : c[h]);
-}
 
 __device__ __forceinline__ void add(f32x4& acc, const f32x4& t, float s) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) acc[e] = fmaf(t[e], s, acc[e]);
 }
 
-// The gated products of an expert's tokens: a tile of 16 gate rows and the 16 up
-// rows that meet them, times CB blocks of 16 tokens, by up_wk waves that take
-// every up_wk-th scale block of K, U at a time; their sums meet in LDS in their
-// order.  h = act(gate) * up goes out as two bf16, within 2^-16 of h.
-template <int CB, int U>
-__global__ __launch_bounds__(64 * kWaves, 2) void moe_up_kernel(MoeParams p) {
-  __shared__ f32x4 red[kWaves][2][CB][64];
-  if ((int)blockIdx.y >= p.lists[0]) return;
-  const int* l = p.lists + 1 + 3 * blockIdx.y;
-  const int e = l[0], first = l[1], n = l[2];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
-  const int wk = p.up_wk, tiles = kWaves / wk, kw = wave % wk;
-  const int f0 = (blockIdx.x * tiles + wave / wk) * 16;
-  const uint8_t *gate = p.w_in, *up = p.w_in;
-  const float *s_gate = p.s_in, *s_up = p.s_in;
-  if (f0 < p.F) {
-    const int row = f0 + (lane & 15), blocks = (2 * p.F + kBlock - 1) / kBlock;
-    gate += ((int64_t)e * 2 * p.F + row) * p.d;
-    up = gate + (int64_t)p.F * p.d;
-    s_gate += ((int64_t)e * blocks + f0 / kBlock) * p.kb_d;
-    s_up += ((int64_t)e * blocks + (p.F + f0) / kBlock) * p.kb_d;
-  }
-  for (int c0 = 0; c0 < n; c0 += 16 * CB) {
-    const uint16_t* col[CB];
+// Two tiles of 16 rows of an expert (their codes at `row`, scales at `scale`)
+// times CB blocks of 16 columns of PARTS bf16 each (their sum), over the scale
+// blocks kw, kw + wk, .. of K.  A block's codes are loaded one block ahead, its
+// columns (from the caches) right before the codes that are ahead of them: loads
+// come back in their order.  Lanes of columns that are not there load nothing.
+template <int CB, int PARTS>
+__device__ __forceinline__ void stream(const uint8_t* const (&row)[2], const float* const (&scale)[2],
+                                       const uint16_t* const (&col)[CB][PARTS], const bool (&there)[CB], int K, int kb, int kw,
+                                       int wk, int q, f32x4 (&acc)[2][CB]) {
+  i32x4 a[2][2][2];
+  auto load = [&](i32x4 (&x)[2][2], int k) {
+    const Place at = place(k, K, q);
 #pragma unroll
-    for (int j = 0; j < CB; ++j) col[j] = p.x + p.pairs[first + min(c0 + 16 * j + (lane & 15), n - 1)] / p.k * p.ldx;
-    f32x4 g[CB] = {}, u[CB] = {};
-    if (f0 < p.F)
-      for (int k0 = kw; k0 < p.kb_d; k0 += wk * U) {
-        i32x4 a[U][2][2];
-        Place at[U];
-        float s[U][2];
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-          const int kb = min(k0 + i * wk, p.kb_d - 1);
-          at[i] = place(kb, p.d, q);
-          load_codes(gate, at[i], a[i][0]);
-          load_codes(up, at[i], a[i][1]);
-          s[i][0] = s_gate[kb];
-          s[i][1] = s_up[kb];
-        }
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-          if (k0 + i * wk >= p.kb_d) break;
-          bf16x8 wg[4], wu[4];
-          codes(a[i][0], at[i], wg);
-          codes(a[i][1], at[i], wu);
-#pragma unroll
-          for (int j = 0; j < CB; ++j) {
-            if (j && c0 + 16 * j >= n) break;
-            i32x4 b[4];
-            load_column(col[j], at[i], b);
-            f32x4 tg = {}, tu = {};
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-              const bf16x8 v = column(b, at[i], h);
-              tg = mfma(wg[h], v, tg);
-              tu = mfma(wu[h], v, tu);
-            }
-            add(g[j], tg, s[i][0]);
-            add(u[j], tu, s[i][1]);
-          }
-        }
-      }
+      for (int h = 0; h < 2; ++h) x[i][h] = *reinterpret_cast<const i32x4*>(row[i] + at.at[h]);
+  };
+  auto step = [&](i32x4 (&now)[2][2], i32x4 (&ahead)[2][2], int k) {
+    const Place at = place(k, K, q);
+    const float s0 = scale[0][k], s1 = scale[1][k];
 #pragma unroll
     for (int j = 0; j < CB; ++j) {
-      red[wave][0][j][lane] = g[j];
-      red[wave][1][j][lane] = u[j];
+      i32x4 b[PARTS][4] = {};
+      if (there[j]) {
+#pragma unroll
+        for (int c = 0; c < PARTS; ++c)
+#pragma unroll
+          for (int h = 0; h < 4; ++h) b[c][h] = *reinterpret_cast<const i32x4*>(col[j][c] + at.at[h / 2] + 8 * (h % 2));
+      }
+      if (j == 0) load(ahead, min(k + wk, kb - 1));
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        bf16x8 w[4];
+        codes(now[i], at, w);
+        f32x4 t = {};
+#pragma unroll
+        for (int c = PARTS - 1; c >= 0; --c)  // (the smaller part first)
+#pragma unroll
+          for (int h = 0; h < 4; ++h) t = mfma(w[h], cleared(b[c][h], at.no[h / 2]), t);
+        add(acc[i][j], t, i ? s1 : s0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
-    __syncthreads();
+  };
+  if (kw >= kb) return;
+  load(a[0], kw);
+  int k = kw;
+  for (; k + wk < kb; k += 2 * wk) {
+    step(a[0], a[1], k);
+    step(a[1], a[0], k + wk);
+  }
+  if (k < kb) step(a[0], a[1], k);
+}
+
+// The gated products of an expert's tokens: a tile of 16 gate rows and the 16 up
+// rows that meet them, times CB blocks of 16 tokens, by up_wk waves that share K;
+// their sums meet in LDS in their order.  h = act(gate) * up goes out as two bf16,
+// within 2^-16 of h.
+template <int CB>
+__global__ __launch_bounds__(64 * kWaves, CB == 1 ? 4 : 2) void moe_up_kernel(MoeParams p) {
+  __shared__ f32x4 red[kWaves][2][CB][64];
+  __shared__ Tokens tokens;
+  const int e = expert_of(p);
+  if (e < 0) return;
+  const int n = find_tokens(p, e, tokens);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
+  const int wk = p.up_wk, tiles = kWaves / wk, kw = wave % wk;
+  const int f0 = min((int)(blockIdx.x * tiles + wave / wk) * 16, p.F - 16);  // (tiles past the last repeat it)
+  const int blocks = (2 * p.F + kBlock - 1) / kBlock;
+  const uint8_t* const gate = p.w_in + ((int64_t)e * 2 * p.F + f0 + (lane & 15)) * p.d;
+  const uint8_t* const row[2] = {gate, gate + (int64_t)p.F * p.d};
+  const float* const scale[2] = {p.s_in + ((int64_t)e * blocks + f0 / kBlock) * p.kb_d,
+                                 p.s_in + ((int64_t)e * blocks + (p.F + f0) / kBlock) * p.kb_d};
+  for (int c0 = 0; c0 < n; c0 += 16 * CB) {
+    const uint16_t* col[CB][1];
+    bool there[CB];
+#pragma unroll
+    for (int j = 0; j < CB; ++j) {
+      const int c = c0 + 16 * j + (lane & 15);
+      there[j] = c < n;
+      col[j][0] = p.x + tokens.pairs[min(c, n - 1)] / p.k * p.ldx;
+    }
+    f32x4 acc[2][CB] = {};
+    stream<CB, 1>(row, scale, col, there, p.d, p.kb_d, kw, wk, q, acc);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < CB; ++j) red[wave][i][j][lane] = acc[i][j];
+    lds_barrier();
     for (int t = wave; t < tiles * CB; t += kWaves) {
       const int j = t % CB, tile = t / CB, c = c0 + 16 * j + (lane & 15), f = (blockIdx.x * tiles + tile) * 16 + 4 * q;
       f32x4 vg = red[tile * wk][0][j][lane], vu = red[tile * wk][1][j][lane];
@@ -430,77 +382,55 @@ __global__ __launch_bounds__(64 * kWaves, 2) void moe_up_kernel(MoeParams p) {
         hi[i / 2][i % 2] = r;
         lo[i / 2][i % 2] = fabsf((float)r) < INFINITY ? (__bf16)(h[i] - (float)r) : (__bf16)0.0f;
       }
-      const int64_t to = (int64_t)(first + c) * p.F + f;
+      const int64_t to = (int64_t)tokens.pairs[c] * p.F + f;
       *reinterpret_cast<u32x2*>(p.hi + to) = __builtin_bit_cast(u32x2, hi);
       *reinterpret_cast<u32x2*>(p.lo + to) = __builtin_bit_cast(u32x2, lo);
     }
-    __syncthreads();
+    lds_barrier();
   }
 }
 
-// Wout h of an expert's tokens: tiles of 16 rows, split as above, to one fp32 row a pair.
-template <int CB, int U>
-__global__ __launch_bounds__(64 * kWaves, 2) void moe_down_kernel(MoeParams p) {
-  __shared__ f32x4 red[kWaves][CB][64];
-  if ((int)blockIdx.y >= p.lists[0]) return;
-  const int* l = p.lists + 1 + 3 * blockIdx.y;
-  const int e = l[0], first = l[1], n = l[2];
+// Wout h of an expert's tokens: tiles of 32 rows, K shared as above, to one fp32 row a pair.
+template <int CB>
+__global__ __launch_bounds__(64 * kWaves, CB == 1 ? 4 : 2) void moe_down_kernel(MoeParams p) {
+  __shared__ f32x4 red[kWaves][2][CB][64];
+  __shared__ Tokens tokens;
+  const int e = expert_of(p);
+  if (e < 0) return;
+  const int n = find_tokens(p, e, tokens);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
   const int wk = p.down_wk, tiles = kWaves / wk, kw = wave % wk;
-  const int r0 = (blockIdx.x * tiles + wave / wk) * 16;
-  const uint8_t* row = p.w_out;
-  const float* s_row = p.s_out;
-  if (r0 < p.d) {
-    row += ((int64_t)e * p.d + r0 + (lane & 15)) * p.F;
-    s_row += ((int64_t)e * ((p.d + kBlock - 1) / kBlock) + r0 / kBlock) * p.kb_f;
-  }
+  const int r0 = min((int)(blockIdx.x * tiles + wave / wk) * 32, p.d - 32);
+  const uint8_t* const first = p.w_out + ((int64_t)e * p.d + r0 + (lane & 15)) * p.F;
+  const uint8_t* const row[2] = {first, first + 16 * (int64_t)p.F};
+  const float* const s_row = p.s_out + ((int64_t)e * ((p.d + kBlock - 1) / kBlock) + r0 / kBlock) * p.kb_f;
+  const float* const scale[2] = {s_row, s_row};
   for (int c0 = 0; c0 < n; c0 += 16 * CB) {
-    int64_t col[CB];
+    const uint16_t* col[CB][2];
+    bool there[CB];
 #pragma unroll
-    for (int j = 0; j < CB; ++j) col[j] = (int64_t)(first + min(c0 + 16 * j + (lane & 15), n - 1)) * p.F;
-    f32x4 acc[CB] = {};
-    if (r0 < p.d)
-      for (int k0 = kw; k0 < p.kb_f; k0 += wk * U) {
-        i32x4 a[U][2];
-        Place at[U];
-        float s[U];
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-          const int kb = min(k0 + i * wk, p.kb_f - 1);
-          at[i] = place(kb, p.F, q);
-          load_codes(row, at[i], a[i]);
-          s[i] = s_row[kb];
-        }
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-          if (k0 + i * wk >= p.kb_f) break;
-          bf16x8 w[4];
-          codes(a[i], at[i], w);
-#pragma unroll
-          for (int j = 0; j < CB; ++j) {
-            if (j && c0 + 16 * j >= n) break;
-            i32x4 bh[4], bl[4];
-            load_column(p.hi + col[j], at[i], bh);
-            load_column(p.lo + col[j], at[i], bl);
-            f32x4 t = {};
-#pragma unroll
-            for (int h = 0; h < 4; ++h) t = mfma(w[h], column(bl, at[i], h), t);
-#pragma unroll
-            for (int h = 0; h < 4; ++h) t = mfma(w[h], column(bh, at[i], h), t);
-            add(acc[j], t, s[i]);
-          }
-        }
-      }
-#pragma unroll
-    for (int j = 0; j < CB; ++j) red[wave][j][lane] = acc[j];
-    __syncthreads();
-    for (int t = wave; t < tiles * CB; t += kWaves) {
-      const int j = t % CB, tile = t / CB, c = c0 + 16 * j + (lane & 15), r = (blockIdx.x * tiles + tile) * 16 + 4 * q;
-      f32x4 v = red[tile * wk][j][lane];
-      for (int w = 1; w < wk; ++w) v += red[tile * wk + w][j][lane];
-      if (c < n && r < p.d) *reinterpret_cast<f32x4*>(p.part + (int64_t)p.pairs[first + c] * p.d + r) = v;
+    for (int j = 0; j < CB; ++j) {
+      const int c = c0 + 16 * j + (lane & 15);
+      there[j] = c < n;
+      const int64_t at = (int64_t)tokens.pairs[min(c, n - 1)] * p.F;
+      col[j][0] = p.hi + at;
+      col[j][1] = p.lo + at;
     }
-    __syncthreads();
+    f32x4 acc[2][CB] = {};
+    stream<CB, 2>(row, scale, col, there, p.F, p.kb_f, kw, wk, q, acc);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < CB; ++j) red[wave][i][j][lane] = acc[i][j];
+    lds_barrier();
+    for (int t = wave; t < tiles * 2 * CB; t += kWaves) {
+      const int j = t % CB, i = t / CB % 2, tile = t / CB / 2, c = c0 + 16 * j + (lane & 15);
+      const int r = (blockIdx.x * tiles + tile) * 32 + 16 * i + 4 * q;
+      f32x4 v = red[tile * wk][i][j][lane];
+      for (int w = 1; w < wk; ++w) v += red[tile * wk + w][i][j][lane];
+      if (c < n && r < p.d) *reinterpret_cast<f32x4*>(p.part + (int64_t)tokens.pairs[c] * p.d + r) = v;
+    }
+    lds_barrier();
   }
 }
 
@@ -536,48 +466,49 @@ size_t lay_out(MoeParams& p, uint8_t* base) {
   };
   const size_t P = (size_t)p.T * p.k;
   p.logits = reinterpret_cast<double*>(take((size_t)p.T * p.E * 8));
-  p.arrived = reinterpret_cast<int*>(take(4));
-  p.lists = reinterpret_cast<int*>(take((1 + 3 * (size_t)p.E) * 4));
-  p.pairs = reinterpret_cast<int*>(take(P * 4));
   p.hi = reinterpret_cast<uint16_t*>(take(P * p.F * 2));
   p.lo = reinterpret_cast<uint16_t*>(take(P * p.F * 2));
   p.part = reinterpret_cast<float*>(take(P * p.d * 4));
   return at;
 }
 
-// Waves that share a tile's K: as many as leave each a round of loads.
-int share(int kb, int each) {
+// Waves that share a tile's K: until there are three rounds of waves for the CUs (16 each), with two blocks each at
+// least; and one, while there is less than a round.
+int share(int64_t tiles, int kb) {
+  constexpr int64_t kRound = 256 * 16;
   int wk = 1;
-  while (wk < kWaves && wk * each < kb) wk *= 2;
+  while (wk < kWaves && ((tiles * wk * 2 <= 3 * kRound && wk * 4 <= kb) || (tiles * wk < kRound && wk < kb))) wk *= 2;
   return wk;
 }
 
-template <int CB, int U>
-hipError_t launch_products(const MoeParams& p, hipStream_t s) {
+template <int CB>
+hipError_t launch_products(MoeParams p, hipStream_t s) {
+  const int y = p.by_pair ? p.T * p.k : p.E;
+  p.up_wk = share((int64_t)p.F / 16 * y, p.kb_d);
+  p.down_wk = share((int64_t)p.d / 32 * y, p.kb_f);
   const int up = (p.F / 16 + kWaves / p.up_wk - 1) / (kWaves / p.up_wk);
-  hipLaunchKernelGGL((moe_up_kernel<CB, U>), dim3(up, p.n_lists), dim3(64 * kWaves), 0, s, p);
+  hipLaunchKernelGGL(moe_up_kernel<CB>, dim3(up, y), dim3(64 * kWaves), 0, s, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int down = (p.d / 16 + kWaves / p.down_wk - 1) / (kWaves / p.down_wk);
-  hipLaunchKernelGGL((moe_down_kernel<CB, U>), dim3(down, p.n_lists), dim3(64 * kWaves), 0, s, p);
+  const int down = (p.d / 32 + kWaves / p.down_wk - 1) / (kWaves / p.down_wk);
+  hipLaunchKernelGGL(moe_down_kernel<CB>, dim3(down, y), dim3(64 * kWaves), 0, s, p);
   return hipGetLastError();
 }
 
-hipError_t launch_moe(MoeParams p, int y_type, hipStream_t s) {
-  p.up_wk = share(p.kb_d, 2);
-  p.down_wk = share(p.kb_f, 2);
+hipError_t launch_moe(const MoeParams& p, int y_type, hipStream_t s) {
   hipError_t e;
   if (p.router) {
     const dim3 grid((p.E + 3) / 4, p.T == 1 ? 1 : (p.T + 7) / 8);
     if (p.T == 1) hipLaunchKernelGGL((moe_logits_kernel<1>), grid, dim3(256), 0, s, p);
     else hipLaunchKernelGGL((moe_logits_kernel<8>), grid, dim3(256), 0, s, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(moe_choose_kernel, dim3((p.T + 3) / 4), dim3(256), 0, s, p);
-  } else {
-    hipLaunchKernelGGL(moe_lists_kernel, dim3(1), dim3(256), 0, s, p);
+    if (p.E <= 64) hipLaunchKernelGGL(moe_choose_kernel<1>, dim3(p.T), dim3(64), 0, s, p);
+    else if (p.E <= 128) hipLaunchKernelGGL(moe_choose_kernel<2>, dim3(p.T), dim3(64), 0, s, p);
+    else hipLaunchKernelGGL(moe_choose_kernel<8>, dim3(p.T), dim3(64), 0, s, p);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  e = p.T <= 16 ? launch_products<1, 2>(p, s) : p.T <= 32 ? launch_products<2, 2>(p, s) : launch_products<4, 2>(p, s);
+  // one block of 16 columns while an expert has few tokens on average: more are taken in rounds
+  e = p.T * p.k <= 10 * p.E || p.T <= 16 ? launch_products<1>(p, s) : launch_products<2>(p, s);
   if (e != hipSuccess) return e;
   const dim3 grid((p.d / 4 + 255) / 256, p.T);
   if (y_type == ACRL_OUT_BF16) hipLaunchKernelGGL(moe_sum_kernel<__bf16>, grid, dim3(256), 0, s, p);
@@ -672,7 +603,7 @@ acrl_status acrl_moe_fp8(const acrl_moe_desc* m, void* stream) {
   p.scale = m->scale;
   p.kb_d = (p.d + acrl::kBlock - 1) / acrl::kBlock;
   p.kb_f = (p.F + acrl::kBlock - 1) / acrl::kBlock;
-  p.n_lists = p.T * p.k < p.E ? p.T * p.k : p.E;
+  p.by_pair = p.T * p.k < p.E;
   const size_t need = p.T ? acrl::lay_out(p, static_cast<uint8_t*>(m->workspace)) : 0;
   if (need && (!m->workspace || m->workspace_bytes < need)) {
     acrl::set_error("acrl_moe_fp8 needs %zu workspace bytes, got %zu", need, m->workspace_bytes);

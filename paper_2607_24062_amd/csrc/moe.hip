@@ -29,6 +29,8 @@ constexpr int kBlock = 128;        // columns per scale
 constexpr int kMaxTokens = 128, kMaxK = 16, kMaxExperts = 512;
 constexpr int kMaxPairs = kMaxTokens * kMaxK;
 constexpr int kWaves = 8;          // of the products' workgroups
+constexpr int kChooseTokens = 2;   // up to so many, every workgroup of the first products chooses by itself
+constexpr int kFewPairs = 16;      // up to so many, the second products and their sum are one kernel
 
 struct MoeParams {
   const uint16_t* x;
@@ -100,17 +102,14 @@ __global__ __launch_bounds__(256) void moe_logits_kernel(MoeParams p) {
   if (lane % (64 / NT) == 0 && t < p.T) p.logits[(int64_t)t * p.E + e] = acc[0];
 }
 
-// Choice of a token's experts by one wave: lane l has the experts l, l + 64, .. (EACH of them).
+// Choice of a token's experts by one wave, lane j getting the j-th: lane l looks at the experts l, l + 64, .. (EACH).
+struct Choice {
+  int id;
+  float weight;
+};
 template <int EACH>
-__global__ __launch_bounds__(64) void moe_choose_kernel(MoeParams p) {
-  const int t = blockIdx.x, lane = threadIdx.x;
-  if (!live(p, t)) {
-    if (lane < p.k) {
-      p.ids[t * p.k + lane] = -1;
-      p.weights[t * p.k + lane] = 0.0f;
-    }
-    return;
-  }
+__device__ __forceinline__ Choice choose(const MoeParams& p, int t, int lane) {
+  if (!live(p, t)) return {-1, 0.0f};
   double s[EACH];     // the score
   uint64_t by[EACH];  // what the choice goes by, in order (NaN counts as the lowest; 0: chosen)
   double top = -INFINITY;
@@ -175,10 +174,16 @@ __global__ __launch_bounds__(64) void moe_choose_kernel(MoeParams p) {
     }
     total += best_s;
   }
+  if (p.renormalize) mine = total == 0.0 ? 0.0 : mine / total;
+  return {mine_id, (float)(mine * (double)p.scale)};
+}
+template <int EACH>
+__global__ __launch_bounds__(64) void moe_choose_kernel(MoeParams p) {
+  const int t = blockIdx.x, lane = threadIdx.x;
+  const Choice c = choose<EACH>(p, t, lane);
   if (lane < p.k) {
-    if (p.renormalize) mine = total == 0.0 ? 0.0 : mine / total;
-    p.ids[t * p.k + lane] = mine_id;
-    p.weights[t * p.k + lane] = (float)(mine * (double)p.scale);
+    p.ids[t * p.k + lane] = c.id;
+    p.weights[t * p.k + lane] = c.weight;
   }
 }
 
@@ -190,19 +195,23 @@ __global__ __launch_bounds__(64) void moe_choose_kernel(MoeParams p) {
 struct Tokens {
   uint16_t pairs[kMaxPairs];
   int counts[kWaves];
+  int ids[kChooseTokens * kMaxK];
 };
-__device__ __forceinline__ int expert_of(const MoeParams& p) {
+// ids: all tokens' choices
+template <bool BY_PAIR>
+__device__ __forceinline__ int expert_of(const MoeParams& p, const int* ids) {
   const int y = blockIdx.y;
-  if (!p.by_pair) return y;
-  const int e = p.ids[y];
+  if (!BY_PAIR) return y;
+  const int e = ids[y];
   return e >= 0 && e < p.E && live(p, y / p.k) ? e : -1;
 }
-__device__ __forceinline__ int find_tokens(const MoeParams& p, int e, Tokens& s) {
+template <bool BY_PAIR>
+__device__ __forceinline__ int find_tokens(const MoeParams& p, const int* ids, int e, Tokens& s) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, P = p.T * p.k;
   int n = 0;
   for (int first = 0; first < P; first += 64 * kWaves) {
     const int pair = first + threadIdx.x;
-    const bool hit = pair < P && p.ids[pair] == e && live(p, pair / p.k);
+    const bool hit = pair < P && ids[pair] == e && live(p, pair / p.k);
     const uint64_t m = __ballot(hit);
     if (lane == 0) s.counts[wave] = __popcll(m);
     lds_barrier();
@@ -216,7 +225,7 @@ __device__ __forceinline__ int find_tokens(const MoeParams& p, int e, Tokens& s)
     if (hit) s.pairs[at] = (uint16_t)pair;
     lds_barrier();
   }
-  return p.by_pair && n && s.pairs[0] != blockIdx.y ? 0 : n;
+  return BY_PAIR && n && s.pairs[0] != blockIdx.y ? 0 : n;
 }
 
 // ------------------------------------------------------------------ products
@@ -272,26 +281,32 @@ __device__ __forceinline__ void add(f32x4& acc, const f32x4& t, float s) {
   for (int e = 0; e < 4; ++e) acc[e] = fmaf(t[e], s, acc[e]);
 }
 
-// Two tiles of 16 rows of an expert (their codes at `row`, scales at `scale`)
-// times CB blocks of 16 columns of PARTS bf16 each (their sum), over the scale
-// blocks kw, kw + wk, .. of K.  A block's codes are loaded one block ahead, its
-// columns (from the caches) right before the codes that are ahead of them: loads
-// come back in their order.  Lanes of columns that are not there load nothing.
-template <int CB, int PARTS>
-__device__ __forceinline__ void stream(const uint8_t* const (&row)[2], const float* const (&scale)[2],
-                                       const uint16_t* const (&col)[CB][PARTS], const bool (&there)[CB], int K, int kb, int kw,
-                                       int wk, int q, f32x4 (&acc)[2][CB]) {
-  i32x4 a[2][2][2];
-  auto load = [&](i32x4 (&x)[2][2], int k) {
-    const Place at = place(k, K, q);
+// R tiles of 16 rows of an expert (their codes at `row`, scales at `scale`) times
+// CB blocks of 16 columns of PARTS bf16 each (their sum), over the scale blocks
+// kw, kw + wk, .. of K.  A block's codes are loaded one block ahead, its columns
+// (from the caches) right before the codes that are ahead of them: loads come back
+// in their order.  Lanes of columns that are not there load nothing.
+template <int R, int CB, int PARTS>
+struct Stream {
+  using Codes = i32x4[R][2];
+  const uint8_t* row[R];
+  const float* scale[R];
+  const uint16_t* col[CB][PARTS];
+  bool there[CB];
+  int K, kb, kw, wk, q;
+
+  __device__ __forceinline__ void load(Codes& x, int k) const {
+    const Place at = place(min(k, kb - 1), K, q);
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < R; ++i)
 #pragma unroll
       for (int h = 0; h < 2; ++h) x[i][h] = *reinterpret_cast<const i32x4*>(row[i] + at.at[h]);
-  };
-  auto step = [&](i32x4 (&now)[2][2], i32x4 (&ahead)[2][2], int k) {
+  }
+  __device__ __forceinline__ void step(Codes& now, Codes& ahead, int k, f32x4 (&acc)[R][CB]) const {
     const Place at = place(k, K, q);
-    const float s0 = scale[0][k], s1 = scale[1][k];
+    float s[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) s[i] = scale[i][k];
 #pragma unroll
     for (int j = 0; j < CB; ++j) {
       i32x4 b[PARTS][4] = {};
@@ -301,10 +316,10 @@ __device__ __forceinline__ void stream(const uint8_t* const (&row)[2], const flo
 #pragma unroll
           for (int h = 0; h < 4; ++h) b[c][h] = *reinterpret_cast<const i32x4*>(col[j][c] + at.at[h / 2] + 8 * (h % 2));
       }
-      if (j == 0) load(ahead, min(k + wk, kb - 1));
+      if (j == 0) load(ahead, k + wk);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < R; ++i) {
         bf16x8 w[4];
         codes(now[i], at, w);
         f32x4 t = {};
@@ -312,51 +327,76 @@ __device__ __forceinline__ void stream(const uint8_t* const (&row)[2], const flo
         for (int c = PARTS - 1; c >= 0; --c)  // (the smaller part first)
 #pragma unroll
           for (int h = 0; h < 4; ++h) t = mfma(w[h], cleared(b[c][h], at.no[h / 2]), t);
-        add(acc[i][j], t, i ? s1 : s0);
+        add(acc[i][j], t, s[i]);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-  };
-  if (kw >= kb) return;
-  load(a[0], kw);
-  int k = kw;
-  for (; k + wk < kb; k += 2 * wk) {
-    step(a[0], a[1], k);
-    step(a[1], a[0], k + wk);
   }
-  if (k < kb) step(a[0], a[1], k);
-}
+  // first: the codes of block kw
+  __device__ __forceinline__ void run(Codes& first, f32x4 (&acc)[R][CB]) const {
+    if (kw >= kb) return;
+    Codes other;
+    int k = kw;
+    for (; k + wk < kb; k += 2 * wk) {
+      step(first, other, k, acc);
+      step(other, first, k + wk, acc);
+    }
+    if (k < kb) step(first, other, k, acc);
+  }
+};
 
 // The gated products of an expert's tokens: a tile of 16 gate rows and the 16 up
 // rows that meet them, times CB blocks of 16 tokens, by up_wk waves that share K;
 // their sums meet in LDS in their order.  h = act(gate) * up goes out as two bf16,
-// within 2^-16 of h.
-template <int CB>
+// within 2^-16 of h.  EACH: the choice of the experts stands here, too.
+template <int CB, int EACH, bool BY_PAIR>
 __global__ __launch_bounds__(64 * kWaves, CB == 1 ? 4 : 2) void moe_up_kernel(MoeParams p) {
   __shared__ f32x4 red[kWaves][2][CB][64];
   __shared__ Tokens tokens;
-  const int e = expert_of(p);
-  if (e < 0) return;
-  const int n = find_tokens(p, e, tokens);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
-  const int wk = p.up_wk, tiles = kWaves / wk, kw = wave % wk;
+  const int* ids = p.ids;
+  if constexpr (EACH > 0) {
+    if (wave < p.T) {
+      const Choice c = choose<EACH>(p, wave, lane);
+      if (lane < p.k) {
+        tokens.ids[wave * p.k + lane] = c.id;
+        if (blockIdx.x == 0 && blockIdx.y == 0) {
+          p.ids[wave * p.k + lane] = c.id;
+          p.weights[wave * p.k + lane] = c.weight;
+        }
+      }
+    }
+    lds_barrier();
+    ids = tokens.ids;
+  }
+  const int e = __builtin_amdgcn_readfirstlane(expert_of<BY_PAIR>(p, ids));
+  if (e < 0) return;
+  const int wk = p.up_wk, tiles = kWaves / wk;
   const int f0 = min((int)(blockIdx.x * tiles + wave / wk) * 16, p.F - 16);  // (tiles past the last repeat it)
   const int blocks = (2 * p.F + kBlock - 1) / kBlock;
-  const uint8_t* const gate = p.w_in + ((int64_t)e * 2 * p.F + f0 + (lane & 15)) * p.d;
-  const uint8_t* const row[2] = {gate, gate + (int64_t)p.F * p.d};
-  const float* const scale[2] = {p.s_in + ((int64_t)e * blocks + f0 / kBlock) * p.kb_d,
-                                 p.s_in + ((int64_t)e * blocks + (p.F + f0) / kBlock) * p.kb_d};
-  for (int c0 = 0; c0 < n; c0 += 16 * CB) {
-    const uint16_t* col[CB][1];
-    bool there[CB];
+  Stream<2, CB, 1> st;
+  st.K = p.d;
+  st.kb = p.kb_d;
+  st.kw = wave % wk;
+  st.wk = wk;
+  st.q = q;
+  st.row[0] = p.w_in + ((int64_t)e * 2 * p.F + f0 + (lane & 15)) * p.d;
+  st.row[1] = st.row[0] + (int64_t)p.F * p.d;
+  st.scale[0] = p.s_in + ((int64_t)e * blocks + f0 / kBlock) * p.kb_d;
+  st.scale[1] = p.s_in + ((int64_t)e * blocks + (p.F + f0) / kBlock) * p.kb_d;
+  typename Stream<2, CB, 1>::Codes first;
+  if (BY_PAIR) st.load(first, st.kw);  // (while it looks for the tokens: the expert is chosen)
+  const int n = find_tokens<BY_PAIR>(p, ids, e, tokens);
+  for (int c0 = 0; c0 < n;) {
+    if (!BY_PAIR) st.load(first, st.kw);
 #pragma unroll
     for (int j = 0; j < CB; ++j) {
       const int c = c0 + 16 * j + (lane & 15);
-      there[j] = c < n;
-      col[j][0] = p.x + tokens.pairs[min(c, n - 1)] / p.k * p.ldx;
+      st.there[j] = c < n;
+      st.col[j][0] = p.x + tokens.pairs[min(c, n - 1)] / p.k * p.ldx;
     }
     f32x4 acc[2][CB] = {};
-    stream<CB, 1>(row, scale, col, there, p.d, p.kb_d, kw, wk, q, acc);
+    st.run(first, acc);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -387,37 +427,45 @@ __global__ __launch_bounds__(64 * kWaves, CB == 1 ? 4 : 2) void moe_up_kernel(Mo
       *reinterpret_cast<u32x2*>(p.lo + to) = __builtin_bit_cast(u32x2, lo);
     }
     lds_barrier();
+    c0 += 16 * CB;
+    if (BY_PAIR && c0 < n) st.load(first, st.kw);
   }
 }
 
 // Wout h of an expert's tokens: tiles of 32 rows, K shared as above, to one fp32 row a pair.
-template <int CB>
+template <int CB, bool BY_PAIR>
 __global__ __launch_bounds__(64 * kWaves, CB == 1 ? 4 : 2) void moe_down_kernel(MoeParams p) {
   __shared__ f32x4 red[kWaves][2][CB][64];
   __shared__ Tokens tokens;
-  const int e = expert_of(p);
+  const int e = __builtin_amdgcn_readfirstlane(expert_of<BY_PAIR>(p, p.ids));
   if (e < 0) return;
-  const int n = find_tokens(p, e, tokens);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
-  const int wk = p.down_wk, tiles = kWaves / wk, kw = wave % wk;
+  const int wk = p.down_wk, tiles = kWaves / wk;
   const int r0 = min((int)(blockIdx.x * tiles + wave / wk) * 32, p.d - 32);
-  const uint8_t* const first = p.w_out + ((int64_t)e * p.d + r0 + (lane & 15)) * p.F;
-  const uint8_t* const row[2] = {first, first + 16 * (int64_t)p.F};
-  const float* const s_row = p.s_out + ((int64_t)e * ((p.d + kBlock - 1) / kBlock) + r0 / kBlock) * p.kb_f;
-  const float* const scale[2] = {s_row, s_row};
-  for (int c0 = 0; c0 < n; c0 += 16 * CB) {
-    const uint16_t* col[CB][2];
-    bool there[CB];
+  Stream<2, CB, 2> st;
+  st.K = p.F;
+  st.kb = p.kb_f;
+  st.kw = wave % wk;
+  st.wk = wk;
+  st.q = q;
+  st.row[0] = p.w_out + ((int64_t)e * p.d + r0 + (lane & 15)) * p.F;
+  st.row[1] = st.row[0] + 16 * (int64_t)p.F;
+  st.scale[0] = st.scale[1] = p.s_out + ((int64_t)e * ((p.d + kBlock - 1) / kBlock) + r0 / kBlock) * p.kb_f;
+  typename Stream<2, CB, 2>::Codes first;
+  if (BY_PAIR) st.load(first, st.kw);
+  const int n = find_tokens<BY_PAIR>(p, p.ids, e, tokens);
+  for (int c0 = 0; c0 < n;) {
+    if (!BY_PAIR) st.load(first, st.kw);
 #pragma unroll
     for (int j = 0; j < CB; ++j) {
       const int c = c0 + 16 * j + (lane & 15);
-      there[j] = c < n;
+      st.there[j] = c < n;
       const int64_t at = (int64_t)tokens.pairs[min(c, n - 1)] * p.F;
-      col[j][0] = p.hi + at;
-      col[j][1] = p.lo + at;
+      st.col[j][0] = p.hi + at;
+      st.col[j][1] = p.lo + at;
     }
     f32x4 acc[2][CB] = {};
-    stream<CB, 2>(row, scale, col, there, p.F, p.kb_f, kw, wk, q, acc);
+    st.run(first, acc);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -431,6 +479,57 @@ __global__ __launch_bounds__(64 * kWaves, CB == 1 ? 4 : 2) void moe_down_kernel(
       if (c < n && r < p.d) *reinterpret_cast<f32x4*>(p.part + (int64_t)tokens.pairs[c] * p.d + r) = v;
     }
     lds_barrier();
+    c0 += 16 * CB;
+    if (BY_PAIR && c0 < n) st.load(first, st.kw);
+  }
+}
+
+__device__ __forceinline__ float residual(const MoeParams& p, int t, int c) {
+  const int64_t at = t * p.ldr + c;
+  return p.res_f32 ? static_cast<const float*>(p.res)[at] : bf16_lo(static_cast<const uint16_t*>(p.res)[at]);
+}
+
+// The same with the sum, for few pairs: a tile of 16 rows of y, each wave a pair
+// (or a share of its K, where there are fewer than waves).
+template <typename OUT>
+__global__ __launch_bounds__(64 * kWaves, 4) void moe_down_few_kernel(MoeParams p) {
+  __shared__ float part[kFewPairs][kWaves][16];  // by pair and share of K
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
+  const int r0 = blockIdx.x * 16, P = p.T * p.k, wk = p.down_wk;
+  for (int u = wave; u < P * wk; u += kWaves) {
+    const int pair = u / wk, e = __builtin_amdgcn_readfirstlane(p.ids[pair]);
+    if (e < 0 || e >= p.E || !live(p, pair / p.k)) continue;
+    Stream<1, 1, 2> st;
+    st.K = p.F;
+    st.kb = p.kb_f;
+    st.kw = u % wk;
+    st.wk = wk;
+    st.q = q;
+    st.row[0] = p.w_out + ((int64_t)e * p.d + r0 + (lane & 15)) * p.F;
+    st.scale[0] = p.s_out + ((int64_t)e * ((p.d + kBlock - 1) / kBlock) + r0 / kBlock) * p.kb_f;
+    st.there[0] = (lane & 15) == 0;
+    st.col[0][0] = p.hi + (int64_t)pair * p.F;
+    st.col[0][1] = p.lo + (int64_t)pair * p.F;
+    f32x4 acc[1][1] = {};
+    Stream<1, 1, 2>::Codes first;
+    st.load(first, st.kw);
+    st.run(first, acc);
+    if ((lane & 15) == 0) *reinterpret_cast<f32x4*>(&part[pair][u % wk][4 * q]) = acc[0][0];
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < p.T * 16; i += 64 * kWaves) {
+    const int t = i / 16, r = i % 16;
+    float v = 0.0f;
+    if (live(p, t))
+      for (int j = 0; j < p.k; ++j) {
+        const int pair = t * p.k + j, e = p.ids[pair];
+        if (e < 0 || e >= p.E) continue;
+        float s = part[pair][0][r];
+        for (int w = 1; w < wk; ++w) s += part[pair][w][r];
+        v = fmaf(s, p.weights[pair], v);
+      }
+    if (p.res) v += residual(p, t, r0 + r);
+    static_cast<OUT*>(p.y)[t * p.ldy + r0 + r] = (OUT)v;
   }
 }
 
@@ -448,10 +547,7 @@ __global__ __launch_bounds__(256) void moe_sum_kernel(MoeParams p) {
     }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (p.res) {
-      const int64_t at = t * p.ldr + c + i;
-      v[i] += p.res_f32 ? static_cast<const float*>(p.res)[at] : bf16_lo(static_cast<const uint16_t*>(p.res)[at]);
-    }
+    if (p.res) v[i] += residual(p, t, c + i);
     static_cast<OUT*>(p.y)[t * p.ldy + c + i] = (OUT)v[i];
   }
 }
@@ -472,47 +568,66 @@ size_t lay_out(MoeParams& p, uint8_t* base) {
   return at;
 }
 
-// Waves that share a tile's K: until there are three rounds of waves for the CUs (16 each), with two blocks each at
+// Waves that share a tile's K: until there are four rounds of waves for the CUs (16 each), with two blocks each at
 // least; and one, while there is less than a round.
 int share(int64_t tiles, int kb) {
   constexpr int64_t kRound = 256 * 16;
   int wk = 1;
-  while (wk < kWaves && ((tiles * wk * 2 <= 3 * kRound && wk * 4 <= kb) || (tiles * wk < kRound && wk < kb))) wk *= 2;
+  while (wk < kWaves && ((tiles * wk * 2 <= 4 * kRound && wk * 4 <= kb) || (tiles * wk < kRound && wk < kb))) wk *= 2;
   return wk;
 }
 
-template <int CB>
-hipError_t launch_products(MoeParams p, hipStream_t s) {
+template <int CB, int EACH>
+hipError_t launch_up(MoeParams p, hipStream_t s) {
   const int y = p.by_pair ? p.T * p.k : p.E;
   p.up_wk = share((int64_t)p.F / 16 * y, p.kb_d);
-  p.down_wk = share((int64_t)p.d / 32 * y, p.kb_f);
-  const int up = (p.F / 16 + kWaves / p.up_wk - 1) / (kWaves / p.up_wk);
-  hipLaunchKernelGGL(moe_up_kernel<CB>, dim3(up, y), dim3(64 * kWaves), 0, s, p);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const int down = (p.d / 32 + kWaves / p.down_wk - 1) / (kWaves / p.down_wk);
-  hipLaunchKernelGGL(moe_down_kernel<CB>, dim3(down, y), dim3(64 * kWaves), 0, s, p);
+  const int x = (p.F / 16 + kWaves / p.up_wk - 1) / (kWaves / p.up_wk);
+  if (p.by_pair) hipLaunchKernelGGL((moe_up_kernel<CB, EACH, true>), dim3(x, y), dim3(64 * kWaves), 0, s, p);
+  else hipLaunchKernelGGL((moe_up_kernel<CB, EACH, false>), dim3(x, y), dim3(64 * kWaves), 0, s, p);
   return hipGetLastError();
 }
 
-hipError_t launch_moe(const MoeParams& p, int y_type, hipStream_t s) {
+template <int CB>
+hipError_t launch_down(MoeParams p, hipStream_t s) {
+  const int y = p.by_pair ? p.T * p.k : p.E;
+  p.down_wk = share((int64_t)p.d / 32 * y, p.kb_f);
+  const int x = (p.d / 32 + kWaves / p.down_wk - 1) / (kWaves / p.down_wk);
+  if (p.by_pair) hipLaunchKernelGGL((moe_down_kernel<CB, true>), dim3(x, y), dim3(64 * kWaves), 0, s, p);
+  else hipLaunchKernelGGL((moe_down_kernel<CB, false>), dim3(x, y), dim3(64 * kWaves), 0, s, p);
+  return hipGetLastError();
+}
+
+template <typename OUT>
+hipError_t launch_moe(MoeParams p, hipStream_t s) {
+  const int P = p.T * p.k;
   hipError_t e;
   if (p.router) {
     const dim3 grid((p.E + 3) / 4, p.T == 1 ? 1 : (p.T + 7) / 8);
     if (p.T == 1) hipLaunchKernelGGL((moe_logits_kernel<1>), grid, dim3(256), 0, s, p);
     else hipLaunchKernelGGL((moe_logits_kernel<8>), grid, dim3(256), 0, s, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (p.E <= 64) hipLaunchKernelGGL(moe_choose_kernel<1>, dim3(p.T), dim3(64), 0, s, p);
-    else if (p.E <= 128) hipLaunchKernelGGL(moe_choose_kernel<2>, dim3(p.T), dim3(64), 0, s, p);
-    else hipLaunchKernelGGL(moe_choose_kernel<8>, dim3(p.T), dim3(64), 0, s, p);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  // one block of 16 columns while an expert has few tokens on average: more are taken in rounds
-  e = p.T * p.k <= 10 * p.E || p.T <= 16 ? launch_products<1>(p, s) : launch_products<2>(p, s);
+  if (p.router && p.T <= kChooseTokens) {
+    e = p.E <= 128 ? launch_up<1, 2>(p, s) : launch_up<1, 8>(p, s);
+  } else {
+    if (p.router) {
+      if (p.E <= 64) hipLaunchKernelGGL(moe_choose_kernel<1>, dim3(p.T), dim3(64), 0, s, p);
+      else if (p.E <= 128) hipLaunchKernelGGL(moe_choose_kernel<2>, dim3(p.T), dim3(64), 0, s, p);
+      else hipLaunchKernelGGL(moe_choose_kernel<8>, dim3(p.T), dim3(64), 0, s, p);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    // one block of 16 columns while an expert has few tokens on average: more are taken in rounds
+    e = P <= 10 * p.E || p.T <= 16 ? launch_up<1, 0>(p, s) : launch_up<2, 0>(p, s);
+  }
   if (e != hipSuccess) return e;
-  const dim3 grid((p.d / 4 + 255) / 256, p.T);
-  if (y_type == ACRL_OUT_BF16) hipLaunchKernelGGL(moe_sum_kernel<__bf16>, grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL(moe_sum_kernel<float>, grid, dim3(256), 0, s, p);
+  if (P <= kFewPairs) {
+    for (p.down_wk = 1; p.down_wk * 2 * P <= kWaves && p.down_wk * 2 <= p.kb_f;) p.down_wk *= 2;
+    hipLaunchKernelGGL(moe_down_few_kernel<OUT>, dim3(p.d / 16), dim3(64 * kWaves), 0, s, p);
+    return hipGetLastError();
+  }
+  e = P <= 10 * p.E || p.T <= 16 ? launch_down<1>(p, s) : launch_down<2>(p, s);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(moe_sum_kernel<OUT>, dim3((p.d / 4 + 255) / 256, p.T), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
@@ -612,7 +727,9 @@ acrl_status acrl_moe_fp8(const acrl_moe_desc* m, void* stream) {
   ACRL_REQUIRE(aligned16(m->workspace), "workspace must be 16-byte aligned");
   st = acrl::check_device();
   if (st != ACRL_OK || p.T == 0) return st;
-  return acrl::hip_status(acrl::launch_moe(p, m->y_type, (hipStream_t)stream), "acrl_moe_fp8 launch");
+  const hipStream_t s = (hipStream_t)stream;
+  return acrl::hip_status(m->y_type == ACRL_OUT_BF16 ? acrl::launch_moe<__bf16>(p, s) : acrl::launch_moe<float>(p, s),
+                          "acrl_moe_fp8 launch");
 }
 
 }  // extern "C"

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import os
 from typing import Dict, Optional
 
@@ -777,31 +778,30 @@ def acrl_moe_fp8(x, w_in, s_in, w_out, s_out, top_k: int, router=None, score: in
     if router is None and (ids is None or weights is None):
         raise ValueError("a router, or ids and weights, are required")
     nbytes = _size("acrl_moe_workspace_size", T, d, E, top_k, F)
-    desc = MoeDesc(T, d, E, top_k, F, x.data_ptr(), x.stride(0) if T > 1 else (d + 7) // 8 * 8,
-                   _want(router, torch.bfloat16, E * d, index, "router", True),
-                   _want(select_bias, f32, E, index, "select_bias", True), _want(mask, torch.uint8, T, index, "mask", True),
-                   w_in.data_ptr(), _want(s_in, f32, E * ((2 * F + 127) // 128) * kb, index, "s_in"),
-                   _want(w_out, torch.uint8, E * d * F, index, "w_out"),
-                   _want(s_out, f32, E * kb * ((F + 127) // 128), index, "s_out"),
-                   score=score, renormalize=1 if renormalize else 0, activation=activation, scale=scale)
+    ldr = ldy = d
     if residual is not None:
-        desc.ldr = _matrix(residual, T, d, index, "residual")
-        desc.residual, desc.residual_type = residual.data_ptr(), _OUT_TYPES[residual.dtype]
+        ldr = _matrix(residual, T, d, index, "residual")
     if out is None:
         if out_dtype not in _OUT_TYPES:
             raise ValueError("out_dtype must be torch.bfloat16 or torch.float32, got %s" % out_dtype)
-        out, desc.ldy = _empty((T, d), out_dtype, dev, stream), d
+        out = _empty((T, d), out_dtype, dev, stream)
     else:
-        desc.ldy = _matrix(out, T, d, index, "out")
-    desc.y, desc.y_type = out.data_ptr(), _OUT_TYPES[out.dtype]
+        ldy = _matrix(out, T, d, index, "out")
     if ids is None:
         ids = _empty((T, top_k), torch.int32, dev, stream)
     if weights is None:
         weights = _empty((T, top_k), f32, dev, stream)
-    desc.ids, desc.weights = _want(ids, torch.int32, T * top_k, index, "ids"), _want(weights, f32, T * top_k, index, "weights")
-    if nbytes:
-        ws = _empty(nbytes, torch.uint8, dev, stream)
-        desc.workspace, desc.workspace_bytes = ws.data_ptr(), nbytes
+    ws = _empty(nbytes, torch.uint8, dev, stream) if nbytes else None
+    desc = MoeDesc(
+        T, d, E, top_k, F, x.data_ptr(), x.stride(0) if T > 1 else (d + 7) // 8 * 8,
+        _want(router, torch.bfloat16, E * d, index, "router", True), _want(select_bias, f32, E, index, "select_bias", True),
+        _want(mask, torch.uint8, T, index, "mask", True), w_in.data_ptr(),
+        _want(s_in, f32, E * ((2 * F + 127) // 128) * kb, index, "s_in"),
+        _want(w_out, torch.uint8, E * d * F, index, "w_out"), _want(s_out, f32, E * kb * ((F + 127) // 128), index, "s_out"),
+        None if residual is None else residual.data_ptr(), ldr, out.data_ptr(), ldy,
+        _want(ids, torch.int32, T * top_k, index, "ids"), _want(weights, f32, T * top_k, index, "weights"),
+        0 if residual is None else _OUT_TYPES[residual.dtype], _OUT_TYPES[out.dtype], score, 1 if renormalize else 0,
+        activation, scale, ws.data_ptr() if nbytes else None, nbytes)
     _check(lib().acrl_moe_fp8(ctypes.byref(desc), _raw_stream(stream, dev)), "acrl_moe_fp8")
     return out, ids, weights
 
@@ -856,12 +856,13 @@ def acrl_beam_reorder(state, parents, dim: int = 0, out=None, stream=None):
         out = _empty(shape, state.dtype, state.device, stream)
     elif tuple(out.shape) != shape or out.dtype != state.dtype or out.get_device() != index:
         raise ValueError("out must be %s of %s on %s" % (shape, state.dtype, state.device))
-    size = state.element_size()
-    row, src = _rows(state, dim, "state")
-    _, dst = _rows(out, dim, "out")
-    outer = 1
-    for n in state.shape[:dim]:
-        outer *= n
+    size, outer = state.element_size(), math.prod(state.shape[:dim])
+    if state.is_contiguous() and out.is_contiguous():
+        row = math.prod(state.shape[dim + 2:])
+        src, dst = (B * K * row, K * row, row), (B * n_out * row, n_out * row, row)
+    else:
+        row, src = _rows(state, dim, "state")
+        dst = _rows(out, dim, "out")[1]
     desc = ReorderDesc(outer, B, K, n_out, row * size, state.data_ptr(), *[n * size for n in src], out.data_ptr(),
                        *[n * size for n in dst], parents.data_ptr())
     _check(lib().acrl_beam_reorder(ctypes.byref(desc), _raw_stream(stream, state.device)), "acrl_beam_reorder")

@@ -495,17 +495,42 @@ template <int EACH>
 __global__ __launch_bounds__(64 * kWaves) void moe_up_few_kernel(MoeParams p) {
   __shared__ f32x4 red[kWaves][2][4];
   __shared__ int chosen[kChooseTokens * kMaxK];
+  __shared__ uint64_t keys[64 * EACH];
+  __shared__ int rank[64 * EACH];
+  static_assert(kWaves % EACH == 0, "whole parts");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
-  const int pair = blockIdx.y, f0 = blockIdx.x * 16;
-  if (pair == p.T * p.k) {
+  const int pair = (int)blockIdx.y - 1, f0 = blockIdx.x * 16;
+  if (pair < 0) {  // (first, since it takes as long as any)
     if (blockIdx.x == 0 && wave < p.T) write_choice<EACH>(p, wave, lane);
     return;
   }
-  if (wave < p.T) {
-    const int id = choose<EACH, false>(p, wave, lane).id;
-    if (lane < p.k) chosen[wave * p.k + lane] = id;
+  if (p.bias) {
+    if (wave < p.T) {
+      const int id = choose<EACH, false>(p, wave, lane).id;
+      if (lane < p.k) chosen[wave * p.k + lane] = id;
+    }
+    lds_barrier();
+  } else {
+    // by the logits alone: every expert's rank among all, each wave taking a part of the others
+    constexpr int kPad = 64 * EACH, kParts = kWaves / EACH, kOthers = kPad / kParts;
+    const int mine = threadIdx.x % kPad, first = threadIdx.x / kPad * kOthers;
+    for (int t = 0; t < p.T; ++t) {
+      if ((int)threadIdx.x < kPad) {
+        const double l = mine < p.E ? p.logits[(int64_t)t * p.E + mine] : 0.0;
+        keys[mine] = mine < p.E ? score_key(l == l ? l : -INFINITY) : 0;
+        rank[mine] = 0;
+      }
+      lds_barrier();
+      const uint64_t key = keys[mine];
+      int before = 0;
+#pragma unroll 8
+      for (int j = first; j < first + kOthers; ++j) before += keys[j] > key || (keys[j] == key && j < mine);
+      if (before) atomicAdd(&rank[mine], before);
+      lds_barrier();
+      if ((int)threadIdx.x < p.E && rank[mine] < p.k) chosen[t * p.k + rank[mine]] = live(p, t) ? mine : -1;
+      lds_barrier();
+    }
   }
-  lds_barrier();
   const int e = __builtin_amdgcn_readfirstlane(chosen[pair]), blocks = (2 * p.F + kBlock - 1) / kBlock;
   if (e < 0) return;
   const uint16_t* const x = p.x + pair / p.k * p.ldx;
@@ -573,9 +598,19 @@ __global__ __launch_bounds__(64 * kFewPairs) void moe_down_few_kernel(MoeParams 
   constexpr int PARTS = std::is_same<OUT, float>::value ? 3 : 2, U = 4;
   __shared__ i32x4 columns[kFewPairs][PARTS][64];
   __shared__ float part[kFewPairs][16];  // by pair and share of K
+  __shared__ float weight[kFewPairs];    // of the pairs that count
+  __shared__ bool counts[kFewPairs];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
   const int r0 = blockIdx.x * 16, P = p.T * p.k, wk = p.down_wk, pair = wave / wk;
   const int e = pair < P ? __builtin_amdgcn_readfirstlane(p.ids[pair]) : -1;
+  const int t = threadIdx.x / 16, r = threadIdx.x % 16;  // of the sum
+  float res = -0.0f;
+  if (p.res && t < p.T) res = residual(p, t, r0 + r);
+  if ((int)threadIdx.x < P) {
+    const int id = p.ids[threadIdx.x];
+    counts[threadIdx.x] = id >= 0 && id < p.E && live(p, threadIdx.x / p.k);
+    weight[threadIdx.x] = p.weights[threadIdx.x];
+  }
   if (e >= 0 && e < p.E && live(p, pair / p.k)) {
     const int each = (p.kb_f + wk - 1) / wk, k1 = min(p.kb_f, (wave % wk + 1) * each);
     const uint8_t* const row = p.w_out + ((int64_t)e * p.d + r0 + (lane & 15)) * p.F;
@@ -591,7 +626,8 @@ __global__ __launch_bounds__(64 * kFewPairs) void moe_down_few_kernel(MoeParams 
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const Place at = place(min(k0 + u, p.kb_f - 1), p.F, q);
+        if (k0 + u >= k1) break;
+        const Place at = place(k0 + u, p.F, q);
 #pragma unroll
         for (int i = 0; i < 2; ++i) a[u][i] = *reinterpret_cast<const i32x4*>(row + at.at[i]);
       }
@@ -617,18 +653,16 @@ __global__ __launch_bounds__(64 * kFewPairs) void moe_down_few_kernel(MoeParams 
     if ((lane & 15) == 0) *reinterpret_cast<f32x4*>(&part[wave][4 * q]) = acc;
   }
   __syncthreads();
-  if (threadIdx.x >= p.T * 16) return;
-  const int t = threadIdx.x / 16, r = threadIdx.x % 16;
+  if (t >= p.T) return;
   float v = 0.0f;
-  if (live(p, t))
-    for (int j = 0; j < p.k; ++j) {
-      const int i = t * p.k + j, id = p.ids[i];
-      if (id < 0 || id >= p.E) continue;
-      float s = part[i * wk][r];
-      for (int w = 1; w < wk; ++w) s += part[i * wk + w][r];
-      v = fmaf(s, p.weights[i], v);
-    }
-  if (p.res) v += residual(p, t, r0 + r);
+  for (int j = 0; j < p.k; ++j) {
+    const int i = t * p.k + j;
+    if (!counts[i]) continue;
+    float s = part[i * wk][r];
+    for (int w = 1; w < wk; ++w) s += part[i * wk + w][r];
+    v = fmaf(s, weight[i], v);
+  }
+  if (p.res) v += res;
   static_cast<OUT*>(p.y)[t * p.ldy + r0 + r] = (OUT)v;
 }
 

@@ -87,7 +87,7 @@ __global__ __launch_bounds__(256) void moe_logits_kernel(MoeParams p) {
       for (int t = 0; t < NT; ++t) acc[t] = fma(b, (double)bf16_hi(v[t][i]), fma(a, (double)bf16_lo(v[t][i]), acc[t]));
     }
   }
-  // halves of the tokens to halves of the lanes, until a lane has one token (NT = 8: by its upper three bits)
+  // halves of the tokens to halves of the lanes, until a lane has one token (by its upper bits)
   int m = 32;
 #pragma unroll
   for (int n = NT; n > 1; n /= 2, m /= 2)
@@ -210,11 +210,11 @@ __device__ __forceinline__ int expert_of(const MoeParams& p, const int* ids) {
   const int e = ids[y];
   return e >= 0 && e < p.E && live(p, y / p.k) ? e : -1;
 }
-template <bool BY_PAIR>
+template <int W, bool BY_PAIR>
 __device__ __forceinline__ int find_tokens(const MoeParams& p, const int* ids, int e, Tokens& s) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, P = p.T * p.k;
   int n = 0;
-  for (int first = 0; first < P; first += 64 * kWaves) {
+  for (int first = 0; first < P; first += 64 * W) {
     const int pair = first + threadIdx.x;
     const bool hit = pair < P && ids[pair] == e && live(p, pair / p.k);
     const uint64_t m = __ballot(hit);
@@ -222,7 +222,7 @@ __device__ __forceinline__ int find_tokens(const MoeParams& p, const int* ids, i
     lds_barrier();
     int at = n + __popcll(m & ((1ull << lane) - 1));
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       const int c = s.counts[w];
       at += w < wave ? c : 0;
       n += c;
@@ -328,27 +328,34 @@ struct Stream {
     float s[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) s[i] = scale[i][k];
+    constexpr int G = CB == 1 || CB + PARTS == 7 ? 1 : 2;  // blocks of columns at a time, as registers allow
 #pragma unroll
-    for (int j = 0; j < CB; ++j) {
-      i32x4 b[PARTS][4] = {};
-      if (there[j]) {
+    for (int j0 = 0; j0 < CB; j0 += G) {
+      i32x4 b[G][PARTS][4] = {};
 #pragma unroll
-        for (int c = 0; c < PARTS; ++c)
+      for (int j = 0; j < G; ++j)
+        if (there[j0 + j]) {
 #pragma unroll
-          for (int h = 0; h < 4; ++h) b[c][h] = *reinterpret_cast<const i32x4*>(col[j][c] + at.at[h / 2] + 8 * (h % 2));
-      }
-      if (j == 0) load(ahead, k + wk);
+          for (int c = 0; c < PARTS; ++c)
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+              b[j][c][h] = *reinterpret_cast<const i32x4*>(col[j0 + j][c] + at.at[h / 2] + 8 * (h % 2));
+        }
+      if (j0 + G == CB) load(ahead, k + wk);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < R; ++i) {
         bf16x8 w[4];
         codes(now[i], at, w);
-        f32x4 t = {};
 #pragma unroll
-        for (int c = PARTS - 1; c >= 0; --c)  // (the smaller part first)
+        for (int j = 0; j < G; ++j) {
+          f32x4 t = {};
 #pragma unroll
-          for (int h = 0; h < 4; ++h) t = mfma(w[h], cleared(b[c][h], at.no[h / 2]), t);
-        add(acc[i][j], t, s[i]);
+          for (int c = PARTS - 1; c >= 0; --c)  // (the smaller part first)
+#pragma unroll
+            for (int h = 0; h < 4; ++h) t = mfma(w[h], cleared(b[j][c][h], at.no[h / 2]), t);
+          add(acc[i][j0 + j], t, s[i]);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -371,14 +378,14 @@ struct Stream {
 // their sums meet in LDS in their order.  h = act(gate) * up goes out as two bf16,
 // within 2^-16 of h (7 % of the time of 16 tokens, d = 4096, F = 14336 over one, which
 // would be as far off as y's own rounding), or, where y is fp32, as three, exactly.
-template <int CB, bool BY_PAIR>
-__global__ __launch_bounds__(64 * kWaves, CB == 1 ? 4 : 2) void moe_up_kernel(MoeParams p) {
-  __shared__ f32x4 red[kWaves][2][CB][64];
+template <int CB, int W, bool BY_PAIR>
+__global__ __launch_bounds__(64 * W, CB == 1 ? 4 : CB == 2 ? 3 : 2) void moe_up_kernel(MoeParams p) {
+  __shared__ f32x4 red[W][2][CB][64];
   __shared__ Tokens tokens;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
   const int e = __builtin_amdgcn_readfirstlane(expert_of<BY_PAIR>(p, p.ids));
   if (e < 0) return;
-  const int wk = p.up_wk, tiles = kWaves / wk;
+  const int wk = p.up_wk, tiles = W / wk;
   const int f0 = min((int)(blockIdx.x * tiles + wave / wk) * 16, p.F - 16);  // (tiles past the last repeat it)
   const int blocks = (2 * p.F + kBlock - 1) / kBlock;
   Stream<2, CB, 1> st;
@@ -393,7 +400,7 @@ __global__ __launch_bounds__(64 * kWaves, CB == 1 ? 4 : 2) void moe_up_kernel(Mo
   st.scale[1] = p.s_in + ((int64_t)e * blocks + (p.F + f0) / kBlock) * p.kb_d;
   typename Stream<2, CB, 1>::Codes first;
   if (BY_PAIR) st.load(first, st.kw);  // (while it looks for the tokens: the expert is chosen)
-  const int n = find_tokens<BY_PAIR>(p, p.ids, e, tokens);
+  const int n = find_tokens<W, BY_PAIR>(p, p.ids, e, tokens);
   for (int c0 = 0; c0 < n;) {
     if (!BY_PAIR) st.load(first, st.kw);
 #pragma unroll
@@ -409,7 +416,7 @@ __global__ __launch_bounds__(64 * kWaves, CB == 1 ? 4 : 2) void moe_up_kernel(Mo
 #pragma unroll
       for (int j = 0; j < CB; ++j) red[wave][i][j][lane] = acc[i][j];
     lds_barrier();
-    for (int t = wave; t < tiles * CB; t += kWaves) {
+    for (int t = wave; t < tiles * CB; t += W) {
       const int j = t % CB, tile = t / CB, c = c0 + 16 * j + (lane & 15), f = (blockIdx.x * tiles + tile) * 16 + 4 * q;
       f32x4 vg = red[tile * wk][0][j][lane], vu = red[tile * wk][1][j][lane];
       for (int w = 1; w < wk; ++w) {
@@ -431,14 +438,14 @@ __global__ __launch_bounds__(64 * kWaves, CB == 1 ? 4 : 2) void moe_up_kernel(Mo
 }
 
 // Wout h of an expert's tokens: tiles of 32 rows, K shared as above, to one fp32 row a pair.
-template <int CB, int PARTS, bool BY_PAIR>
-__global__ __launch_bounds__(64 * kWaves, CB == 1 && PARTS == 2 ? 4 : 2) void moe_down_kernel(MoeParams p) {
-  __shared__ f32x4 red[kWaves][2][CB][64];
+template <int CB, int W, int PARTS, bool BY_PAIR>
+__global__ __launch_bounds__(64 * W, CB + PARTS == 3 ? 4 : 2) void moe_down_kernel(MoeParams p) {
+  __shared__ f32x4 red[W][2][CB][64];
   __shared__ Tokens tokens;
   const int e = __builtin_amdgcn_readfirstlane(expert_of<BY_PAIR>(p, p.ids));
   if (e < 0) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
-  const int wk = p.down_wk, tiles = kWaves / wk;
+  const int wk = p.down_wk, tiles = W / wk;
   const int r0 = min((int)(blockIdx.x * tiles + wave / wk) * 32, p.d - 32);
   Stream<2, CB, PARTS> st;
   st.K = p.F;
@@ -451,7 +458,7 @@ __global__ __launch_bounds__(64 * kWaves, CB == 1 && PARTS == 2 ? 4 : 2) void mo
   st.scale[0] = st.scale[1] = p.s_out + ((int64_t)e * ((p.d + kBlock - 1) / kBlock) + r0 / kBlock) * p.kb_f;
   typename Stream<2, CB, PARTS>::Codes first;
   if (BY_PAIR) st.load(first, st.kw);
-  const int n = find_tokens<BY_PAIR>(p, p.ids, e, tokens);
+  const int n = find_tokens<W, BY_PAIR>(p, p.ids, e, tokens);
   for (int c0 = 0; c0 < n;) {
     if (!BY_PAIR) st.load(first, st.kw);
 #pragma unroll
@@ -469,7 +476,7 @@ __global__ __launch_bounds__(64 * kWaves, CB == 1 && PARTS == 2 ? 4 : 2) void mo
 #pragma unroll
       for (int j = 0; j < CB; ++j) red[wave][i][j][lane] = acc[i][j];
     lds_barrier();
-    for (int t = wave; t < tiles * 2 * CB; t += kWaves) {
+    for (int t = wave; t < tiles * 2 * CB; t += W) {
       const int j = t % CB, i = t / CB % 2, tile = t / CB / 2, c = c0 + 16 * j + (lane & 15);
       const int r = (blockIdx.x * tiles + tile) * 32 + 16 * i + 4 * q;
       f32x4 v = red[tile * wk][i][j][lane];
@@ -702,30 +709,33 @@ size_t lay_out(MoeParams& p, uint8_t* base) {
 
 // Waves that share a tile's K: until there are four rounds of waves for the CUs (16 each), with two blocks each at
 // least; and one, while there is less than a round.
-int share(int64_t tiles, int kb) {
+int share(int64_t tiles, int kb, int W) {
   constexpr int64_t kRound = 256 * 16;
   int wk = 1;
-  while (wk < kWaves && ((tiles * wk * 2 <= 4 * kRound && wk * 4 <= kb) || (tiles * wk < kRound && wk < kb))) wk *= 2;
+  while (wk < W && ((tiles * wk * 2 <= 4 * kRound && wk * 4 <= kb) || (tiles * wk < kRound && wk < kb))) wk *= 2;
   return wk;
 }
 
+// Workgroups of eight waves, or four where two blocks of columns take registers that leave room for 12 waves a CU.
 template <int CB>
 hipError_t launch_up(MoeParams p, hipStream_t s) {
+  constexpr int W = CB == 1 ? 8 : 4;
   const int y = p.by_pair ? p.T * p.k : p.E;
-  p.up_wk = share((int64_t)p.F / 16 * y, p.kb_d);
-  const dim3 grid((p.F / 16 + kWaves / p.up_wk - 1) / (kWaves / p.up_wk), y);
-  if (p.by_pair) hipLaunchKernelGGL((moe_up_kernel<CB, true>), grid, dim3(64 * kWaves), 0, s, p);
-  else hipLaunchKernelGGL((moe_up_kernel<CB, false>), grid, dim3(64 * kWaves), 0, s, p);
+  p.up_wk = share((int64_t)p.F / 16 * y, p.kb_d, W);
+  const dim3 grid((p.F / 16 + W / p.up_wk - 1) / (W / p.up_wk), y);
+  if (p.by_pair) hipLaunchKernelGGL((moe_up_kernel<CB, W, true>), grid, dim3(64 * W), 0, s, p);
+  else hipLaunchKernelGGL((moe_up_kernel<CB, W, false>), grid, dim3(64 * W), 0, s, p);
   return hipGetLastError();
 }
 
 template <int CB, int PARTS>
 hipError_t launch_down(MoeParams p, hipStream_t s) {
+  constexpr int W = CB == 1 ? 8 : 4;
   const int y = p.by_pair ? p.T * p.k : p.E;
-  p.down_wk = share((int64_t)p.d / 32 * y, p.kb_f);
-  const dim3 grid((p.d / 32 + kWaves / p.down_wk - 1) / (kWaves / p.down_wk), y);
-  if (p.by_pair) hipLaunchKernelGGL((moe_down_kernel<CB, PARTS, true>), grid, dim3(64 * kWaves), 0, s, p);
-  else hipLaunchKernelGGL((moe_down_kernel<CB, PARTS, false>), grid, dim3(64 * kWaves), 0, s, p);
+  p.down_wk = share((int64_t)p.d / 32 * y, p.kb_f, W);
+  const dim3 grid((p.d / 32 + W / p.down_wk - 1) / (W / p.down_wk), y);
+  if (p.by_pair) hipLaunchKernelGGL((moe_down_kernel<CB, W, PARTS, true>), grid, dim3(64 * W), 0, s, p);
+  else hipLaunchKernelGGL((moe_down_kernel<CB, W, PARTS, false>), grid, dim3(64 * W), 0, s, p);
   return hipGetLastError();
 }
 
@@ -734,13 +744,15 @@ hipError_t launch_moe(MoeParams p, hipStream_t s) {
   constexpr int PARTS = std::is_same<OUT, float>::value ? 3 : 2;
   const int P = p.T * p.k;
   p.parts = PARTS;
-  // one block of 16 columns while an expert has few tokens on average: more are taken in rounds
-  const bool narrow = P <= 10 * p.E || p.T <= 16;
+  // Blocks of 16 columns by the tokens an expert has on average; where it has more than they hold, its weights are read
+  // again (128 tokens, 2 of 8 experts of 4096 x 14336: 871 us with one block, 735 with two, 630 with four).
+  const int blocks = P <= 10 * p.E || p.T <= 16 ? 1 : P <= 24 * p.E || p.T <= 32 ? 2 : 4;
   hipError_t e;
   if (p.router) {
-    const dim3 grid((p.E + 3) / 4, p.T == 1 ? 1 : (p.T + 7) / 8);
-    if (p.T == 1) hipLaunchKernelGGL((moe_logits_kernel<1>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((moe_logits_kernel<8>), grid, dim3(256), 0, s, p);
+    const int nt = p.T <= 16 ? 1 : 2;  // (7 tokens, 60 experts: 46 us with 2, 48 with 8; 64 tokens: 1 us more with 8)
+    const dim3 grid((p.E + 3) / 4, (p.T + nt - 1) / nt);
+    if (nt == 1) hipLaunchKernelGGL((moe_logits_kernel<1>), grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((moe_logits_kernel<2>), grid, dim3(256), 0, s, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (p.router && p.T <= kChooseTokens) {
@@ -755,7 +767,7 @@ hipError_t launch_moe(MoeParams p, hipStream_t s) {
       else hipLaunchKernelGGL(moe_choose_kernel<8>, dim3(p.T), dim3(64), 0, s, p);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    e = narrow ? launch_up<1>(p, s) : launch_up<2>(p, s);
+    e = blocks == 1 ? launch_up<1>(p, s) : blocks == 2 ? launch_up<2>(p, s) : launch_up<4>(p, s);
   }
   if (e != hipSuccess) return e;
   if (P <= kFewPairs) {
@@ -763,7 +775,7 @@ hipError_t launch_moe(MoeParams p, hipStream_t s) {
     hipLaunchKernelGGL(moe_down_few_kernel<OUT>, dim3(p.d / 16), dim3(64 * kFewPairs), 0, s, p);
     return hipGetLastError();
   }
-  e = narrow ? launch_down<1, PARTS>(p, s) : launch_down<2, PARTS>(p, s);
+  e = blocks == 1 ? launch_down<1, PARTS>(p, s) : blocks == 2 ? launch_down<2, PARTS>(p, s) : launch_down<4, PARTS>(p, s);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(moe_sum_kernel<OUT>, dim3((p.d / 4 + 255) / 256, p.T), dim3(256), 0, s, p);
   return hipGetLastError();

@@ -230,17 +230,17 @@ __global__ __launch_bounds__(64 * kScanWaves, 8) void beam_scan_kernel(BeamParam
     bad |= top == INFINITY;
     const float cut = value_of(bar);
     if (__ballot(top >= cut)) {
-      uint64_t pass[kEach];
       int n = 0;
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) n += __popcll(pass[i] = __ballot(x[i] >= cut));
+      for (int i = 0; i < kEach; ++i) n += __popcll(__ballot(x[i] >= cut));
       int to = 0;
       if (lane == 0) to = atomicAdd(&s.count, n);
       to = read_lane(to, 0);
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
-        if (x[i] >= cut) s.notes[to + __popcll(pass[i] & ((1ull << lane) - 1))] = key_of(x[i], (int)(here + i));
-        to += __popcll(pass[i]);
+        const uint64_t pass = __ballot(x[i] >= cut);
+        if (pass >> lane & 1) s.notes[to + __popcll(pass & ((1ull << lane) - 1))] = key_of(x[i], (int)(here + i));
+        to += __popcll(pass);
       }
     }
     if (((double)top - (double)m) * c > 900.0) {

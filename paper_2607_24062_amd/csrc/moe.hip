@@ -723,8 +723,13 @@ hipError_t launch_up(MoeParams p, hipStream_t s) {
   const int y = p.by_pair ? p.T * p.k : p.E;
   p.up_wk = share((int64_t)p.F / 16 * y, p.kb_d, W);
   const dim3 grid((p.F / 16 + W / p.up_wk - 1) / (W / p.up_wk), y);
-  if (p.by_pair) hipLaunchKernelGGL((moe_up_kernel<CB, W, true>), grid, dim3(64 * W), 0, s, p);
-  else hipLaunchKernelGGL((moe_up_kernel<CB, W, false>), grid, dim3(64 * W), 0, s, p);
+  if constexpr (CB == 1) {  // (fewer pairs than experts are few an expert)
+    if (p.by_pair) {
+      hipLaunchKernelGGL((moe_up_kernel<CB, W, true>), grid, dim3(64 * W), 0, s, p);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((moe_up_kernel<CB, W, false>), grid, dim3(64 * W), 0, s, p);
   return hipGetLastError();
 }
 
@@ -734,8 +739,13 @@ hipError_t launch_down(MoeParams p, hipStream_t s) {
   const int y = p.by_pair ? p.T * p.k : p.E;
   p.down_wk = share((int64_t)p.d / 32 * y, p.kb_f, W);
   const dim3 grid((p.d / 32 + W / p.down_wk - 1) / (W / p.down_wk), y);
-  if (p.by_pair) hipLaunchKernelGGL((moe_down_kernel<CB, W, PARTS, true>), grid, dim3(64 * W), 0, s, p);
-  else hipLaunchKernelGGL((moe_down_kernel<CB, W, PARTS, false>), grid, dim3(64 * W), 0, s, p);
+  if constexpr (CB == 1) {
+    if (p.by_pair) {
+      hipLaunchKernelGGL((moe_down_kernel<CB, W, PARTS, true>), grid, dim3(64 * W), 0, s, p);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((moe_down_kernel<CB, W, PARTS, false>), grid, dim3(64 * W), 0, s, p);
   return hipGetLastError();
 }
 

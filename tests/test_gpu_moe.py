@@ -45,10 +45,12 @@ def _x(torch, dev, T, d, seed):
     return f64(b), up_bf16(torch, dev, b)
 
 
-# T, d, E, k, F: one token and one expert; odd widths; every expert of a token; more tokens of an expert than a tile has,
-# than all its blocks have; the most of everything
+# T, d, E, k, F: one token and one expert; odd widths; every expert of a token; more tokens of an expert than a block of
+# columns has, than all its blocks have; the most of everything; one and two tokens among many experts, with long rows of
+# Wout that waves share; as many pairs as the kernel for few takes, and one more
 SIZES = [(1, 32, 1, 1, 32), (1, 256, 8, 2, 96), (3, 160, 5, 5, 64), (2, 416, 70, 6, 32), (16, 96, 4, 2, 160), (17, 288, 12, 3, 160),
-         (33, 128, 2, 1, 416), (70, 512, 3, 2, 256), (128, 64, 1, 1, 96), (128, 32, 512, 16, 32), (5, 1312, 9, 4, 1184)]
+         (33, 128, 2, 1, 416), (70, 512, 3, 2, 256), (128, 64, 1, 1, 96), (128, 32, 512, 16, 32), (5, 1312, 9, 4, 1184), (2, 96, 300, 3, 64), (1, 64, 129, 16, 160), (1, 96, 4, 2, 1184), (2, 1056, 40, 8, 32),
+         (16, 64, 20, 1, 64), (17, 64, 20, 1, 64), (30, 2080, 2, 1, 544)]
 
 
 @pytest.mark.parametrize("n,size", list(enumerate(SIZES)))
@@ -141,10 +143,11 @@ def test_what_is_not_chosen_has_no_influence():
     assert gi.tolist() == [[0, 1]] * T and bool(torch.isnan(y).all())
 
 
-def test_given_routing():
+@pytest.mark.parametrize("T", [3, 5, 21, 60])
+def test_given_routing(T):
     torch, dev = torch_dev()
     from paper_2607_24062_amd import acrl
-    T, d, E, k, F = 21, 96, 7, 3, 64
+    d, E, k, F = 96, 7, 3, 64
     layer = Layer(torch, dev, d, E, F, 31)
     x, tx = _x(torch, dev, T, d, 2)
     y, ids, w = acrl.acrl_moe_fp8(tx, *layer.t, k, router=layer.t_router)
@@ -182,10 +185,26 @@ def test_strides_and_in_place():
     assert torch.equal(own, want)
 
 
-def test_streams_graphs_and_no_tokens():
+def test_given_routing_of_one_token():
     torch, dev = torch_dev()
     from paper_2607_24062_amd import acrl
-    T, d, E, k, F = 20, 160, 9, 2, 96
+    d, E, k, F = 160, 7, 4, 96
+    layer = Layer(torch, dev, d, E, F, 33)
+    x, tx = _x(torch, dev, 1, d, 2)
+    y, ids, w = acrl.acrl_moe_fp8(tx, *layer.t, k, router=layer.t_router, out_dtype=torch.float32)
+    assert torch.equal(acrl.acrl_moe_fp8(tx, *layer.t, k, ids=ids, weights=w, out_dtype=torch.float32)[0], y)
+    for row in ([3, 3, -1, 9], [-5, 7, 8, 100], [6, 0, 6, 6]):
+        gi, gw = np.array([row], np.int32), np.array([[0.5, -1.0, 2.0, 0.25]], np.float32)
+        got = acrl.acrl_moe_fp8(tx, *layer.t, k, ids=up(torch, dev, gi), weights=up(torch, dev, gw), residual=tx,
+                                out_dtype=torch.float32)[0]
+        _check(down(got), *experts(x, gi, gw.astype(np.float64), layer.win, layer.wout, residual=x), "f32")
+
+
+@pytest.mark.parametrize("T", [1, 2, 6, 20])
+def test_streams_graphs_and_no_tokens(T):
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    d, E, k, F = 160, 9, 2, 96
     layer = Layer(torch, dev, d, E, F, 51)
     x, tx = _x(torch, dev, T, d, 2)
     call = lambda **kw: acrl.acrl_moe_fp8(tx, *layer.t, k, router=layer.t_router, out_dtype=torch.float32, **kw)  # noqa: E731

@@ -9,7 +9,7 @@ import pytest
 from test_gpu_product_tilings import _table
 from test_operator_resources import READELF, _notes
 
-# (scalar registers that do not fit are kept in lanes of a vector register: the scan has six, outside its loop over logits)
+# (scalar registers that do not fit, six of the scan, are kept in lanes of a vector register, not in memory)
 KEYS = ("private_segment_fixed_size", "vgpr_spill_count", "agpr_count")
 
 

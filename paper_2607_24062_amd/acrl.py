@@ -819,21 +819,19 @@ def acrl_beam_step(logits, scores, n_out: int, inv_temperature: float = 1.0, fin
     index, dev, f32 = _index_of(scores, torch.float32, "scores", stream), scores.device, torch.float32
     ldl = _matrix(logits, B * K, V, index, "logits")
     nbytes = _size("acrl_beam_workspace_size", B, K, V, n_out)
-    if ids is None:
-        ids = _empty((B, n_out), torch.int32, dev, stream)
-    if parents is None:
-        parents = _empty((B, n_out), torch.int32, dev, stream)
-    if out_scores is None:
-        out_scores = _empty((B, n_out), f32, dev, stream)
+    outputs = []
+    for t, dtype, name in ((ids, torch.int32, "ids"), (parents, torch.int32, "parents"), (out_scores, f32, "out_scores")):
+        if t is None:
+            t = _empty((B, n_out), dtype, dev, stream)
+        else:
+            _want(t, dtype, B * n_out, index, name)
+        outputs.append(t)
     ws = _empty(nbytes, torch.uint8, dev, stream) if nbytes else None
-    n = B * n_out
     desc = BeamDesc(B, K, V, n_out, logits.data_ptr(), ldl, scores.data_ptr(),
                     _want(finished, torch.uint8, B * K, index, "finished", True), _OUT_TYPES[logits.dtype], eos_id,
-                    inv_temperature, _want(ids, torch.int32, n, index, "ids"),
-                    _want(parents, torch.int32, n, index, "parents"), _want(out_scores, f32, n, index, "out_scores"),
-                    ws.data_ptr() if nbytes else None, nbytes)
+                    inv_temperature, *[t.data_ptr() for t in outputs], ws.data_ptr() if nbytes else None, nbytes)
     _check(lib().acrl_beam_step(ctypes.byref(desc), _raw_stream(stream, dev)), "acrl_beam_step")
-    return ids, parents, out_scores
+    return tuple(outputs)
 
 
 def acrl_beam_reorder(state, parents, dim: int = 0, out=None, stream=None):

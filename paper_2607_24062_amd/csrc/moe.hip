@@ -28,7 +28,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 constexpr int kBlock = 128;        // columns per scale
 constexpr int kMaxTokens = 128, kMaxK = 16, kMaxExperts = 512;
 constexpr int kMaxPairs = kMaxTokens * kMaxK;
-constexpr int kWaves = 8;          // of the products' workgroups
+constexpr int kWaves = 4;          // of the products' workgroups (7 tokens, 60 experts: 37 us, 46 with eight)
+constexpr int kFewWaves = 8;       // of those for one or two tokens
 constexpr int kChooseTokens = 2;   // up to so many, every workgroup of the first products chooses the experts by itself
 constexpr int kFewPairs = 16;      // up to so many, the second products and their sum are one kernel, a wave each
 
@@ -210,11 +211,11 @@ __device__ __forceinline__ int expert_of(const MoeParams& p, const int* ids) {
   const int e = ids[y];
   return e >= 0 && e < p.E && live(p, y / p.k) ? e : -1;
 }
-template <int W, bool BY_PAIR>
+template <bool BY_PAIR>
 __device__ __forceinline__ int find_tokens(const MoeParams& p, const int* ids, int e, Tokens& s) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, P = p.T * p.k;
   int n = 0;
-  for (int first = 0; first < P; first += 64 * W) {
+  for (int first = 0; first < P; first += 64 * kWaves) {
     const int pair = first + threadIdx.x;
     const bool hit = pair < P && ids[pair] == e && live(p, pair / p.k);
     const uint64_t m = __ballot(hit);
@@ -222,7 +223,7 @@ __device__ __forceinline__ int find_tokens(const MoeParams& p, const int* ids, i
     lds_barrier();
     int at = n + __popcll(m & ((1ull << lane) - 1));
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
+    for (int w = 0; w < kWaves; ++w) {
       const int c = s.counts[w];
       at += w < wave ? c : 0;
       n += c;
@@ -380,29 +381,34 @@ struct Stream {
 // their sums meet in LDS in their order.  h = act(gate) * up goes out as two bf16,
 // within 2^-16 of h (7 % of the time of 16 tokens, d = 4096, F = 14336 over one, which
 // would be as far off as y's own rounding), or, where y is fp32, as three, exactly.
-template <int CB, int W, bool BY_PAIR>
-__global__ __launch_bounds__(64 * W, CB == 1 ? 4 : CB == 2 ? 3 : 2) void moe_up_kernel(MoeParams p) {
-  __shared__ f32x4 red[W][2][CB][64];
+template <int CB, int R, bool BY_PAIR>
+__global__ __launch_bounds__(64 * kWaves, CB == 1 && R == 2 ? 4 : CB <= 2 ? 3 : 2) void moe_up_kernel(MoeParams p) {
+  __shared__ f32x4 red[kWaves][R][CB][64];
   __shared__ Tokens tokens;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
   const int e = __builtin_amdgcn_readfirstlane(expert_of<BY_PAIR>(p, p.ids));
   if (e < 0) return;
-  const int wk = p.up_wk, tiles = W / wk;
-  const int f0 = min((int)(blockIdx.x * tiles + wave / wk) * 16, p.F - 16);  // (tiles past the last repeat it)
+  const int wk = p.up_wk, tiles = kWaves / wk;
+  constexpr int H = R / 2, kRows = 16 * H;  // tiles of gate rows
+  const int f0 = min((int)(blockIdx.x * tiles + wave / wk) * kRows, p.F - kRows);  // (tiles past the last repeat it)
   const int blocks = (2 * p.F + kBlock - 1) / kBlock;
-  Stream<2, CB, 1> st;
+  Stream<R, CB, 1> st;
   st.K = p.d;
   st.kb = p.kb_d;
   st.kw = wave % wk;
   st.wk = wk;
   st.q = q;
-  st.row[0] = p.w_in + ((int64_t)e * 2 * p.F + f0 + (lane & 15)) * p.d;
-  st.row[1] = st.row[0] + (int64_t)p.F * p.d;
-  st.scale[0] = p.s_in + ((int64_t)e * blocks + f0 / kBlock) * p.kb_d;
-  st.scale[1] = p.s_in + ((int64_t)e * blocks + (p.F + f0) / kBlock) * p.kb_d;
-  typename Stream<2, CB, 1>::Codes first;
+#pragma unroll
+  for (int i = 0; i < H; ++i) {
+    const int f = f0 + 16 * i;
+    st.row[i] = p.w_in + ((int64_t)e * 2 * p.F + f + (lane & 15)) * p.d;
+    st.row[H + i] = st.row[i] + (int64_t)p.F * p.d;
+    st.scale[i] = p.s_in + ((int64_t)e * blocks + f / kBlock) * p.kb_d;
+    st.scale[H + i] = p.s_in + ((int64_t)e * blocks + (p.F + f) / kBlock) * p.kb_d;
+  }
+  typename Stream<R, CB, 1>::Codes first;
   if (BY_PAIR) st.load(first, st.kw);  // (while it looks for the tokens: the expert is chosen)
-  const int n = find_tokens<W, BY_PAIR>(p, p.ids, e, tokens);
+  const int n = find_tokens<BY_PAIR>(p, p.ids, e, tokens);
   for (int c0 = 0; c0 < n;) {
     if (!BY_PAIR) st.load(first, st.kw);
 #pragma unroll
@@ -411,25 +417,26 @@ __global__ __launch_bounds__(64 * W, CB == 1 ? 4 : CB == 2 ? 3 : 2) void moe_up_
       st.there[j] = c < n;
       st.col[j][0] = p.x + tokens.pairs[min(c, n - 1)] / p.k * p.ldx;
     }
-    f32x4 acc[2][CB] = {};
+    f32x4 acc[R][CB] = {};
     st.run(first, acc);
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < R; ++i)
 #pragma unroll
       for (int j = 0; j < CB; ++j) red[wave][i][j][lane] = acc[i][j];
     lds_barrier();
-    for (int t = wave; t < tiles * CB; t += W) {
-      const int j = t % CB, tile = t / CB, c = c0 + 16 * j + (lane & 15), f = (blockIdx.x * tiles + tile) * 16 + 4 * q;
-      f32x4 vg = red[tile * wk][0][j][lane], vu = red[tile * wk][1][j][lane];
+    for (int t = wave; t < tiles * H * CB; t += kWaves) {
+      const int j = t % CB, i = t / CB % H, tile = t / CB / H, c = c0 + 16 * j + (lane & 15);
+      const int f = (blockIdx.x * tiles + tile) * kRows + 16 * i + 4 * q;
+      f32x4 vg = red[tile * wk][i][j][lane], vu = red[tile * wk][H + i][j][lane];
       for (int w = 1; w < wk; ++w) {
-        vg += red[tile * wk + w][0][j][lane];
-        vu += red[tile * wk + w][1][j][lane];
+        vg += red[tile * wk + w][i][j][lane];
+        vu += red[tile * wk + w][H + i][j][lane];
       }
       if (c >= n || f >= p.F) continue;
       float h[4];
       for_activation(p.act, [&](auto act) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = activate<decltype(act)::value, true>(vg[i]) * vu[i];
+        for (int v = 0; v < 4; ++v) h[v] = activate<decltype(act)::value, true>(vg[v]) * vu[v];
       });
       store_parts(p, (int64_t)tokens.pairs[c] * p.F + f, h);
     }
@@ -439,28 +446,31 @@ __global__ __launch_bounds__(64 * W, CB == 1 ? 4 : CB == 2 ? 3 : 2) void moe_up_
   }
 }
 
-// Wout h of an expert's tokens: tiles of 32 rows, K shared as above, to one fp32 row a pair.
-template <int CB, int W, int PARTS, bool BY_PAIR>
-__global__ __launch_bounds__(64 * W, CB + PARTS == 3 ? 4 : 2) void moe_down_kernel(MoeParams p) {
-  __shared__ f32x4 red[W][2][CB][64];
+// Wout h of an expert's tokens: tiles of 16 R rows, K shared as above, to one fp32 row a pair.
+template <int CB, int R, int PARTS, bool BY_PAIR>
+__global__ __launch_bounds__(64 * kWaves, CB + PARTS + R == 5 ? 4 : 2) void moe_down_kernel(MoeParams p) {
+  __shared__ f32x4 red[kWaves][R][CB][64];
   __shared__ Tokens tokens;
   const int e = __builtin_amdgcn_readfirstlane(expert_of<BY_PAIR>(p, p.ids));
   if (e < 0) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
-  const int wk = p.down_wk, tiles = W / wk;
-  const int r0 = min((int)(blockIdx.x * tiles + wave / wk) * 32, p.d - 32);
-  Stream<2, CB, PARTS> st;
+  const int wk = p.down_wk, tiles = kWaves / wk;
+  const int r0 = min((int)(blockIdx.x * tiles + wave / wk) * 16 * R, p.d - 16 * R);
+  Stream<R, CB, PARTS> st;
   st.K = p.F;
   st.kb = p.kb_f;
   st.kw = wave % wk;
   st.wk = wk;
   st.q = q;
-  st.row[0] = p.w_out + ((int64_t)e * p.d + r0 + (lane & 15)) * p.F;
-  st.row[1] = st.row[0] + 16 * (int64_t)p.F;
-  st.scale[0] = st.scale[1] = p.s_out + ((int64_t)e * ((p.d + kBlock - 1) / kBlock) + r0 / kBlock) * p.kb_f;
-  typename Stream<2, CB, PARTS>::Codes first;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int r = r0 + 16 * i;
+    st.row[i] = p.w_out + ((int64_t)e * p.d + r + (lane & 15)) * p.F;
+    st.scale[i] = p.s_out + ((int64_t)e * ((p.d + kBlock - 1) / kBlock) + r / kBlock) * p.kb_f;
+  }
+  typename Stream<R, CB, PARTS>::Codes first;
   if (BY_PAIR) st.load(first, st.kw);
-  const int n = find_tokens<W, BY_PAIR>(p, p.ids, e, tokens);
+  const int n = find_tokens<BY_PAIR>(p, p.ids, e, tokens);
   for (int c0 = 0; c0 < n;) {
     if (!BY_PAIR) st.load(first, st.kw);
 #pragma unroll
@@ -471,16 +481,16 @@ __global__ __launch_bounds__(64 * W, CB + PARTS == 3 ? 4 : 2) void moe_down_kern
 #pragma unroll
       for (int i = 0; i < PARTS; ++i) st.col[j][i] = p.h[i] + at;
     }
-    f32x4 acc[2][CB] = {};
+    f32x4 acc[R][CB] = {};
     st.run(first, acc);
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < R; ++i)
 #pragma unroll
       for (int j = 0; j < CB; ++j) red[wave][i][j][lane] = acc[i][j];
     lds_barrier();
-    for (int t = wave; t < tiles * 2 * CB; t += W) {
-      const int j = t % CB, i = t / CB % 2, tile = t / CB / 2, c = c0 + 16 * j + (lane & 15);
-      const int r = (blockIdx.x * tiles + tile) * 32 + 16 * i + 4 * q;
+    for (int t = wave; t < tiles * R * CB; t += kWaves) {
+      const int j = t % CB, i = t / CB % R, tile = t / CB / R, c = c0 + 16 * j + (lane & 15);
+      const int r = (blockIdx.x * tiles + tile) * 16 * R + 16 * i + 4 * q;
       f32x4 v = red[tile * wk][i][j][lane];
       for (int w = 1; w < wk; ++w) v += red[tile * wk + w][i][j][lane];
       if (c < n && r < p.d) *reinterpret_cast<f32x4*>(p.part + (int64_t)tokens.pairs[c] * p.d + r) = v;
@@ -502,12 +512,12 @@ __device__ __forceinline__ float residual(const MoeParams& p, int t, int c) {
 // and the codes and columns of two blocks are under way together.  One pair a
 // workgroup and 16 gate and up rows, K shared by its waves.
 template <int EACH>
-__global__ __launch_bounds__(64 * kWaves) void moe_up_few_kernel(MoeParams p) {
-  __shared__ f32x4 red[kWaves][2][4];
+__global__ __launch_bounds__(64 * kFewWaves) void moe_up_few_kernel(MoeParams p) {
+  __shared__ f32x4 red[kFewWaves][2][4];
   __shared__ int chosen[kChooseTokens * kMaxK];
   __shared__ uint64_t keys[64 * EACH];
   __shared__ int rank[64 * EACH];
-  static_assert(kWaves % EACH == 0, "whole parts");
+  static_assert(kFewWaves % EACH == 0, "whole parts");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
   const int pair = (int)blockIdx.y - 1, f0 = blockIdx.x * 16;
   if (pair < 0) {  // (first, since it takes as long as any)
@@ -522,7 +532,7 @@ __global__ __launch_bounds__(64 * kWaves) void moe_up_few_kernel(MoeParams p) {
     lds_barrier();
   } else {
     // by the logits alone: every expert's rank among all, each wave taking a part of the others
-    constexpr int kPad = 64 * EACH, kParts = kWaves / EACH, kOthers = kPad / kParts;
+    constexpr int kPad = 64 * EACH, kParts = kFewWaves / EACH, kOthers = kPad / kParts;
     const int mine = threadIdx.x % kPad, first = threadIdx.x / kPad * kOthers;
     for (int t = 0; t < p.T; ++t) {
       if ((int)threadIdx.x < kPad) {
@@ -550,11 +560,11 @@ __global__ __launch_bounds__(64 * kWaves) void moe_up_few_kernel(MoeParams p) {
                                  p.s_in + ((int64_t)e * blocks + (p.F + f0) / kBlock) * p.kb_d};
   f32x4 acc[2] = {};
   constexpr int U = 2;
-  for (int k0 = wave; k0 < p.kb_d; k0 += U * kWaves) {
+  for (int k0 = wave; k0 < p.kb_d; k0 += U * kFewWaves) {
     i32x4 a[U][2][2], b[U][4];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const Place at = place(min(k0 + u * kWaves, p.kb_d - 1), p.d, q);
+      const Place at = place(min(k0 + u * kFewWaves, p.kb_d - 1), p.d, q);
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -564,7 +574,7 @@ __global__ __launch_bounds__(64 * kWaves) void moe_up_few_kernel(MoeParams p) {
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int k = k0 + u * kWaves;
+      const int k = k0 + u * kFewWaves;
       if (k >= p.kb_d) break;
       const Place at = place(k, p.d, q);
 #pragma unroll
@@ -586,7 +596,7 @@ __global__ __launch_bounds__(64 * kWaves) void moe_up_few_kernel(MoeParams p) {
   if (threadIdx.x >= 4) return;
   f32x4 vg = red[0][0][threadIdx.x], vu = red[0][1][threadIdx.x];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) {
+  for (int w = 1; w < kFewWaves; ++w) {
     vg += red[w][0][threadIdx.x];
     vu += red[w][1][threadIdx.x];
   }
@@ -713,44 +723,46 @@ size_t lay_out(MoeParams& p, uint8_t* base) {
 
 // Waves that share a tile's K: until there are four rounds of waves for the CUs (16 each), with two blocks each at
 // least; and one, while there is less than a round.
-int share(int64_t tiles, int kb, int W) {
+int share(int64_t tiles, int kb) {
   constexpr int64_t kRound = 256 * 16;
   int wk = 1;
-  while (wk < W && ((tiles * wk * 2 <= 4 * kRound && wk * 4 <= kb) || (tiles * wk < kRound && wk < kb))) wk *= 2;
+  while (wk < kWaves && ((tiles * wk * 2 <= 4 * kRound && wk * 4 <= kb) || (tiles * wk < kRound && wk < kb))) wk *= 2;
   return wk;
 }
 
-// Workgroups of eight waves, or four where two blocks of columns take registers that leave room for 12 waves a CU.
-template <int CB>
-hipError_t launch_up(MoeParams p, hipStream_t s) {
-  constexpr int W = CB == 1 ? 8 : 4;
-  const int y = p.by_pair ? p.T * p.k : p.E;
-  p.up_wk = share((int64_t)p.F / 16 * y, p.kb_d, W);
-  const dim3 grid((p.F / 16 + W / p.up_wk - 1) / (W / p.up_wk), y);
-  if constexpr (CB == 1) {  // (fewer pairs than experts are few an expert)
-    if (p.by_pair) {
-      hipLaunchKernelGGL((moe_up_kernel<CB, W, true>), grid, dim3(64 * W), 0, s, p);
-      return hipGetLastError();
-    }
-  }
-  hipLaunchKernelGGL((moe_up_kernel<CB, W, false>), grid, dim3(64 * W), 0, s, p);
+// R tiles of 16 rows a wave: four, which columns are read for once; two where there are few pairs, and where there are more
+// blocks of columns.  (With two, in workgroups of eight waves: 64 tokens, 8 of 128 experts of 2048 x 768 149 us for 143, 16
+// tokens, 2 of 8 of 4096 x 14336 293 for 267, 128 of the former 192 for 167.)
+template <int CB, int R, bool BY_PAIR>
+hipError_t launch_up_tiles(MoeParams p, hipStream_t s) {
+  const int y = BY_PAIR ? p.T * p.k : p.E, tiles = p.F / (8 * R);
+  p.up_wk = share((int64_t)tiles * y, p.kb_d);
+  const int each = kWaves / p.up_wk;
+  hipLaunchKernelGGL((moe_up_kernel<CB, R, BY_PAIR>), dim3((tiles + each - 1) / each, y), dim3(64 * kWaves), 0, s, p);
+  return hipGetLastError();
+}
+template <int CB, int R, int PARTS, bool BY_PAIR>
+hipError_t launch_down_tiles(MoeParams p, hipStream_t s) {
+  const int y = BY_PAIR ? p.T * p.k : p.E, tiles = p.d / (16 * R);
+  p.down_wk = share((int64_t)tiles * y, p.kb_f);
+  const int each = kWaves / p.down_wk;
+  hipLaunchKernelGGL((moe_down_kernel<CB, R, PARTS, BY_PAIR>), dim3((tiles + each - 1) / each, y), dim3(64 * kWaves), 0, s, p);
   return hipGetLastError();
 }
 
+template <int CB>
+hipError_t launch_up(const MoeParams& p, hipStream_t s) {
+  if constexpr (CB > 1) return launch_up_tiles<CB, 2, false>(p, s);  // (fewer pairs than experts are few an expert)
+  else if (p.by_pair) return launch_up_tiles<1, 2, true>(p, s);
+  else return launch_up_tiles<1, 4, false>(p, s);
+}
+
 template <int CB, int PARTS>
-hipError_t launch_down(MoeParams p, hipStream_t s) {
-  constexpr int W = CB == 1 ? 8 : 4;
-  const int y = p.by_pair ? p.T * p.k : p.E;
-  p.down_wk = share((int64_t)p.d / 32 * y, p.kb_f, W);
-  const dim3 grid((p.d / 32 + W / p.down_wk - 1) / (W / p.down_wk), y);
-  if constexpr (CB == 1) {
-    if (p.by_pair) {
-      hipLaunchKernelGGL((moe_down_kernel<CB, W, PARTS, true>), grid, dim3(64 * W), 0, s, p);
-      return hipGetLastError();
-    }
-  }
-  hipLaunchKernelGGL((moe_down_kernel<CB, W, PARTS, false>), grid, dim3(64 * W), 0, s, p);
-  return hipGetLastError();
+hipError_t launch_down(const MoeParams& p, hipStream_t s) {
+  if constexpr (CB > 1) return launch_down_tiles<CB, 2, PARTS, false>(p, s);
+  else if (p.by_pair) return launch_down_tiles<1, 2, PARTS, true>(p, s);
+  else if (p.d % 64 == 0) return launch_down_tiles<1, 4, PARTS, false>(p, s);
+  else return launch_down_tiles<1, 2, PARTS, false>(p, s);
 }
 
 template <typename OUT>
@@ -771,8 +783,8 @@ hipError_t launch_moe(MoeParams p, hipStream_t s) {
   }
   if (p.router && p.T <= kChooseTokens) {
     const dim3 grid(p.F / 16, P + 1);
-    if (p.E <= 128) hipLaunchKernelGGL(moe_up_few_kernel<2>, grid, dim3(64 * kWaves), 0, s, p);
-    else hipLaunchKernelGGL(moe_up_few_kernel<8>, grid, dim3(64 * kWaves), 0, s, p);
+    if (p.E <= 128) hipLaunchKernelGGL(moe_up_few_kernel<2>, grid, dim3(64 * kFewWaves), 0, s, p);
+    else hipLaunchKernelGGL(moe_up_few_kernel<8>, grid, dim3(64 * kFewWaves), 0, s, p);
     e = hipGetLastError();
   } else {
     if (p.router) {

@@ -32,8 +32,9 @@ def kernels(tmp_path_factory):
 def test_every_kernel_is_looked_at(kernels):
     count = lambda what: sum(what in k for k in kernels)  # noqa: E731
     assert count("linear_tile_kernel") == 2 * len(_table()[0]) and count("linear_rows_kernel") == 4
-    # up: three widths, the narrowest of pairs, too; down: the same of two and of three parts
-    for what, n in (("moe_logits", 2), ("moe_choose", 3), ("moe_up_kernel", 4), ("moe_up_few", 2), ("moe_down_kernel", 8),
+    # up: three widths, the narrowest of pairs, too; down: the same of two and of three parts, and the narrowest of tiles of
+    # two and of four rows
+    for what, n in (("moe_logits", 2), ("moe_choose", 3), ("moe_up_kernel", 4), ("moe_up_few", 2), ("moe_down_kernel", 10),
                     ("moe_down_few", 2), ("moe_sum", 2), ("beam_scan", 2), ("beam_pick", 1), ("beam_reorder", 4)):
         assert count(what) == n, what
 

@@ -3,9 +3,10 @@
 // FINE: within 6e-7 of the exact value, relative to its size, or within 1.3e-36
 // (the reciprocal of 1 + e^-s is 0 below fp32's normal range, 1.2e-38, and meets a
 // value of at most 104 there).  Otherwise, for results that become bf16 (half a
-// step: 2e-3 .. 4e-3): within 5e-5, or 1.3e-36, by half the instructions, which
-// stand after a product with nothing to hide them (8192 x 13824 x 5120, bf16 out: GELU
-// 590 -> 578 us, GELU_TANH 601 -> 559, SILU 554 -> 529; 511 with no activation).
+// step: 2e-3 .. 4e-3): within 5e-5, or 1.3e-36, in fewer instructions, which stand
+// after a product with nothing to hide them (8192 x 13824 x 5120, bf16 out, fine
+// and short: GELU 575 and 547 us, GELU_TANH 597 and 532, SILU 537 and 526; 511 with
+// no activation).
 #pragma once
 
 #include <type_traits>
@@ -33,21 +34,11 @@ __device__ __forceinline__ float times_sigmoid(float x, float s) {
   return x * __builtin_amdgcn_rcpf(1.0f + exp_f32<FINE>(-s));
 }
 
-// erfc(z), z >= 0: e^(-z^2) times a polynomial in 1 / (1 + z / 2), fitted to
+// erfc(z), z >= 0: e^(-z^2) times a polynomial in t = 1 / (1 + z / 2), fitted to
 // e^(z^2) erfc(z) over 0 <= z <= 14 for the least relative error (4.3e-8; 3.1e-7 as
-// evaluated in fp32; 3.4e-5 the shorter one).  square = z^2 in two parts.
-template <bool FINE>
+// evaluated in fp32).  square = z^2 in two parts.
 __device__ __forceinline__ float erfc_of(float z, float square, float square_rest) {
   const float t = __builtin_amdgcn_rcpf(fmaf(0.5f, z, 1.0f));
-  if (!FINE) {
-    float p = -0.067427858710289f;
-    p = fmaf(p, t, 0.018588868901133537f);
-    p = fmaf(p, t, 0.27242976427078247f);
-    p = fmaf(p, t, 0.2052343785762787f);
-    p = fmaf(p, t, 0.28950396180152893f);
-    p = fmaf(p, t, 0.2816377282142639f);
-    return p * t * exp_f32<false>(-square);
-  }
   float p = -0.05882089212536812f;
   p = fmaf(p, t, 0.28327813744544983f);
   p = fmaf(p, t, -0.4842751920223236f);
@@ -77,6 +68,20 @@ __device__ __forceinline__ float twice_u(float v, float& rest) {
   return s;
 }
 
+// GELU in 14 instructions: v Phi(v) = max(v, 0) - a erfc(a / sqrt 2) / 2, a = |v|, with a shorter polynomial for
+// erfc / 2 (3.4e-5).  (From 20 on erfc is 0 and a may end, which keeps infinities from meeting it.  The minimum keeps NaN.)
+__device__ __forceinline__ float gelu_short(float v) {
+  const float a = __builtin_elementwise_minimum(fabsf(v), 20.0f);
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.35355339059327376f, a, 1.0f));
+  float p = -0.0337139293551445f;
+  p = fmaf(p, t, 0.0092944344505667686f);
+  p = fmaf(p, t, 0.13621488213539124f);
+  p = fmaf(p, t, 0.10261718928813934f);
+  p = fmaf(p, t, 0.14475198090076447f);
+  p = fmaf(p, t, 0.14081886410713196f);
+  return fmaf(-a, p * t * __builtin_amdgcn_exp2f(a * a * (-0.5f * kLog2e)), fmaxf(v, 0.0f));
+}
+
 template <int ACT, bool FINE>
 __device__ __forceinline__ float activate(float v) {
   if constexpr (ACT == ACRL_ACT_RELU) {
@@ -84,13 +89,17 @@ __device__ __forceinline__ float activate(float v) {
   } else if constexpr (ACT == ACRL_ACT_SILU) {
     return times_sigmoid<FINE>(v, v);
   } else if constexpr (ACT == ACRL_ACT_GELU) {
+    if (!FINE) return gelu_short(v);
     // v Phi(v) = v erfc(-v / sqrt 2) / 2, by erfc of |v| / sqrt 2 on either side: no digits are lost far below 0
     const float a = fminf(fabsf(v), 20.0f), s = 0.5f * a * a;  // (erfc is 0 in fp32 from 14.2 / sqrt 2 on)
-    const float half = 0.5f * erfc_of<FINE>(0.70710678118654752f * a, s, fmaf(0.5f * a, a, -s));
+    const float half = 0.5f * erfc_of(0.70710678118654752f * a, s, fmaf(0.5f * a, a, -s));
     return v * (v < 0.0f ? half : 1.0f - half);
   } else if constexpr (ACT == ACRL_ACT_GELU_TANH) {
     // 1 + tanh(u) = 2 / (1 + e^(-2 u)), u = sqrt(2 / pi) (v + 0.044715 v^3)
-    if (!FINE) return times_sigmoid<false>(v, v * fmaf(0.07135481627260025f, v * v, 1.5957691216057308f));
+    if (!FINE) {  // (the factor log2(e) with the others)
+      constexpr float c1 = (float)(-1.5957691216057307 * 1.4426950408889634), c3 = (float)(-0.0713548162726 * 1.4426950408889634);
+      return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * fmaf(c3, v * v, c1)));
+    }
     float rest;
     const float s = twice_u(v, rest), e = exp_f32(-s);
     return v * __builtin_amdgcn_rcpf(1.0f + (fabsf(s) < 87.0f ? fmaf(-e, rest, e) : e));

@@ -22,8 +22,9 @@ typedef uint32_t u32x4_anywhere __attribute__((ext_vector_type(4), aligned(2)));
 
 constexpr int kMaxBeams = 64, kMaxOut = 64;
 constexpr int kScanWaves = 8, kEach = 8, kTile = 64 * kEach;  // logits of a lane, of a wave at a time
-constexpr int kKept = 256, kNotes = 512 + kScanWaves * kTile;  // notes of a workgroup: left between tiles, at most
-static_assert(kKept >= kMaxOut && kKept <= 64 * kScanWaves && kNotes >= kKept + kScanWaves * kTile, "notes fit");
+constexpr int notes_left(int N) { return 32 + 2 * N; }  // notes of a workgroup between tiles, at most
+constexpr int kNotes = notes_left(kMaxOut) + kScanWaves * kTile;
+static_assert(notes_left(kMaxOut) <= 64 * kScanWaves, "a thread ranks one");
 constexpr int kPickWaves = 4, kMaxLists = 64 * kPickWaves, kMaxStaged = 6144;
 constexpr int kNone = 0x7FFFFFFF;
 
@@ -40,7 +41,7 @@ struct BeamParams {
   int32_t* parents;
   float* out;
   // workspace, by row and segment
-  double* norm;             // [2]: a reference near the largest logit (NaN: no normaliser), sum of 2^((z - it) inv_t log2 e)
+  double* norm;             // [2]: a logit near the largest (NaN: no normaliser), sum of 2^((z - it) inv_t log2 e)
   float* val;               // [N] the segment's largest logits, falling
   int* idx;                 // [N] their tokens (kNone: no more)
 };
@@ -72,28 +73,37 @@ __device__ __forceinline__ uint32_t order_of(float v) {
 }
 __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o >> 31 ? o & 0x7FFFFFFFu : ~o); }
 
-// A lane's kEach consecutive logits, as they are read; those past `left` count as -infinity.
+// A lane's kEach consecutive logits, as they are read.  No lane skips a load: the compiler can then count them, and they
+// pass while the logits before them are worked on.  (Behind a load that some lanes skip all have to have arrived before
+// an older one is used: 4 us more of 97 at 512 x 151936.)
 template <typename T>
 struct Logits {
   static constexpr int kWords = kEach * (int)sizeof(T) / 4;
   uint32_t w[kWords];
-  __device__ __forceinline__ void read(const T* at, int left) {
-    // (rows of odd lengths begin anywhere: the loads are wide all the same)
-    if (left >= kEach) {
+  // the lane's of a wave's tile of a row z; what lies past `end` is the row's last
+  __device__ __forceinline__ void read(const T* z, int64_t tile, int64_t end, uint32_t lane) {
+    if (tile + kTile <= end) {
+      // (rows of odd lengths begin anywhere: the loads are wide all the same)
+      using global = __attribute__((address_space(1))) const T*;
+      global from = (global)(z + tile);
+      asm("" : "+s"(from));  // (one address for the wave, or the lanes' take registers that are needed elsewhere)
 #pragma unroll
       for (int i = 0; i < kWords / 4; ++i) {
-        const u32x4_anywhere v = reinterpret_cast<const u32x4_anywhere*>(at)[i];
+        const u32x4_anywhere v = reinterpret_cast<__attribute__((address_space(1))) const u32x4_anywhere*>(from + lane * kEach)[i];
 #pragma unroll
         for (int k = 0; k < 4; ++k) w[4 * i + k] = v[k];
       }
     } else {
+      const int64_t first = min(tile, end - 1);
+      const T* const from = z + first;
+      const uint32_t last = (uint32_t)(end - 1 - first);
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
-        const bool ok = i < left;
+        const T* const one = from + min(lane * kEach + i, last);
         if constexpr (sizeof(T) == 4) {
-          w[i] = ok ? reinterpret_cast<const uint32_t*>(at)[i] : 0xFF800000u;
+          w[i] = *reinterpret_cast<const uint32_t*>(one);
         } else {
-          const uint32_t v = ok ? reinterpret_cast<const uint16_t*>(at)[i] : 0xFF80u;
+          const uint32_t v = *reinterpret_cast<const uint16_t*>(one);
           w[i / 2] = i % 2 ? w[i / 2] | v << 16 : v;
         }
       }
@@ -112,10 +122,12 @@ __device__ __forceinline__ uint64_t key_of(float v, int idx) {
 
 // One pass over a row's segment: the sum of exponentials and the N largest
 // logits.  A workgroup notes in LDS, key by key, what is no less than a bar; when
-// there are many notes they are thinned out to the N largest, and the least of
-// those is the bar from there on.  With logits in no order that happens once or
-// twice.  (A list of N a wave, kept in order by insertions of 100 instructions and
-// more, 50 of them a wave at N = 16, took 28 us more of 103 at 512 x 151936.)
+// there are many notes they are thinned out to the N largest, and what is above the
+// least of those is noted from there on.  With logits in no order that happens three
+// or four times.  What bounds it (512 x 151936: 75 us) is less the loads (50 alone) than the vector
+// instructions: fp64 exponentials (25) and notes.  (A list of N a wave,
+// kept in order by insertions, took 28 us more; notes by ballots over all eight logits,
+// 200 instructions, 8 more; notes thinned out from 256 on, 3 more.)
 struct Scan {
   uint64_t notes[kNotes];
   double norms[kScanWaves][2];
@@ -187,12 +199,12 @@ __global__ __launch_bounds__(64 * kScanWaves, 8) void beam_scan_kernel(BeamParam
   const int64_t end = min((int64_t)p.V, begin + (int64_t)p.seg_tiles * kTile);
   const double c = (double)p.inv_t * 1.4426950408889634074;  // (the same rounding for all terms)
   const int N = p.N;
-  float m = -INFINITY;  // the lane's reference: no more than 2^900 below any of its logits
+  float m = -INFINITY;  // the lane's reference, one of its logits: no more than 2^900 below any other
   double sum = 0.0;
   bool bad = false;
   Logits<T> next;
-  int64_t at = begin + (int64_t)wave * kTile + lane * kEach;
-  next.read(z + at, (int)max((int64_t)-1, min(end - at, (int64_t)kEach)));
+  int64_t tile = begin + (int64_t)wave * kTile;  // the wave's
+  next.read(z, tile, end, lane);
   if (threadIdx.x == 0) s.count = 0;
   // The first bar: each of the W waves whose tile is whole has q = ceil(N / W) logits that are no less than the q-th
   // largest of its lanes' largest, so N of the workgroup's are no less than the least of these.
@@ -218,9 +230,14 @@ __global__ __launch_bounds__(64 * kScanWaves, 8) void beam_scan_kernel(BeamParam
     float x[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) x[i] = next[i];
-    const int64_t here = at;
-    at += kScanWaves * kTile;
-    next.read(z + at, (int)max((int64_t)-1, min(end - at, (int64_t)kEach)));
+    const int64_t here = tile + lane * kEach;
+    if (tile + kTile > end) {
+      const int left = (int)max((int64_t)0, end - tile) - lane * kEach;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) x[i] = i < left ? x[i] : -INFINITY;
+    }
+    tile += kScanWaves * kTile;
+    next.read(z, tile, end, lane);
     float top = x[0];
 #pragma unroll
     for (int i = 0; i < kEach; i += 2) {
@@ -229,31 +246,22 @@ __global__ __launch_bounds__(64 * kScanWaves, 8) void beam_scan_kernel(BeamParam
     }
     bad |= top == INFINITY;
     const float cut = value_of(bar);
-    if (__ballot(top >= cut)) {
-      int n = 0;
+    if (top >= cut) {
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) n += __popcll(__ballot(x[i] >= cut));
-      int to = 0;
-      if (lane == 0) to = atomicAdd(&s.count, n);
-      to = read_lane(to, 0);
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        const uint64_t pass = __ballot(x[i] >= cut);
-        if (pass >> lane & 1) s.notes[to + __popcll(pass & ((1ull << lane) - 1))] = key_of(x[i], (int)(here + i));
-        to += __popcll(pass);
-      }
+      for (int i = 0; i < kEach; ++i)
+        if (x[i] >= cut) s.notes[atomicAdd(&s.count, 1)] = key_of(x[i], (int)(here + i));
     }
     if (((double)top - (double)m) * c > 900.0) {
       sum *= exp2_f64(((double)m - (double)top) * c);
       m = top;
     }
-    const double mc = (double)m * c;
+    // (the difference first: logits of 1e20 would leave nothing of an exponent in z c - m c)
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) sum += exp2_f64(fma((double)x[i], c, -mc));
+    for (int i = 0; i < kEach; ++i) sum += exp2_f64(((double)x[i] - (double)m) * c);
     lds_barrier();
     const int count = s.count;
     lds_barrier();  // (all have read it before any wave notes more)
-    if (count > kKept) bar = thin_out(s, count, N);
+    if (count > notes_left(N)) bar = thin_out(s, count, N) + 1;  // (what comes has higher tokens: more than the N-th, not as much)
   }
   // the waves' sums together
   const float ref = wave_max(m);
@@ -315,6 +323,7 @@ __device__ __forceinline__ int first_of(const Candidate& c) {
 __global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p) {
   extern __shared__ uint8_t staged[];  // val [lists][N], idx [lists][N]
   __shared__ double lse[kMaxBeams], score[kMaxBeams];
+  __shared__ double refs[kMaxLists], sums[kMaxLists];
   __shared__ int state[kMaxBeams];     // 0: no candidates, 1: its lists, 2: finished
   __shared__ Candidate merged[kPickWaves][kMaxOut];
   __shared__ int chosen_beam[kMaxOut], chosen_id[kMaxOut];
@@ -323,29 +332,37 @@ __global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p
   float* const val = reinterpret_cast<float*>(staged);
   int* const idx = reinterpret_cast<int*>(val + lists * N);
   const double c = (double)p.inv_t * 1.4426950408889634074;
-  if ((int)threadIdx.x < p.K) {
-    const int j = threadIdx.x, row = b * p.K + j;
-    score[j] = p.scores[row];
-    state[j] = !alive(p.scores[row]) ? 0 : p.finished && p.finished[row] ? 2 : 1;
+  // All of a list is read at once, also where its beam turns out to have none and nothing has been written.
+  const bool has_list = (int)threadIdx.x < lists, has_beam = (int)threadIdx.x < p.K;
+  const double* const norm = p.norm + 2 * ((int64_t)b * lists + threadIdx.x);
+  double list_ref = 0.0, list_sum = 0.0;
+  float own = 0.0f;
+  bool finished = false;
+  if (has_list) list_ref = norm[0], list_sum = norm[1];
+  if (has_beam) own = p.scores[b * p.K + threadIdx.x];
+  if (has_beam && p.finished) finished = p.finished[b * p.K + threadIdx.x];
+  for (int i = threadIdx.x; i < lists * N; i += 64 * kPickWaves) {
+    val[i] = p.val[(int64_t)b * lists * N + i];
+    idx[i] = p.idx[(int64_t)b * lists * N + i];
+  }
+  if (has_list) refs[threadIdx.x] = list_ref, sums[threadIdx.x] = list_sum;
+  __syncthreads();
+  if (has_beam) {
+    const int j = threadIdx.x;
+    score[j] = own;
+    state[j] = !alive(own) ? 0 : finished ? 2 : 1;
     if (state[j] == 1) {
-      const double* n = p.norm + 2 * (int64_t)row * p.S;
       double ref = -INFINITY, sum = 0.0;
       bool none = false;
-      for (int s = 0; s < p.S; ++s) {
-        none |= n[2 * s] != n[2 * s];
-        if (n[2 * s] > ref) ref = n[2 * s];
+      for (int s = j * p.S; s < (j + 1) * p.S; ++s) {
+        none |= refs[s] != refs[s];
+        if (refs[s] > ref) ref = refs[s];
       }
-      for (int s = 0; s < p.S; ++s) sum += n[2 * s + 1] * exp2_f64((n[2 * s] - ref) * c);
+      for (int s = j * p.S; s < (j + 1) * p.S; ++s) sum += sums[s] * exp2_f64((refs[s] - ref) * c);
       lse[j] = ref * (double)p.inv_t + log(sum);
       if (none || !(fabs(lse[j]) < INFINITY)) state[j] = 0;
     }
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < lists * N; i += 64 * kPickWaves)
-    if (state[i / (p.S * N)] == 1) {
-      val[i] = p.val[(int64_t)b * lists * N + i];
-      idx[i] = p.idx[(int64_t)b * lists * N + i];
-    }
   __syncthreads();
   const int mine = lists <= 64 ? (wave == 0 ? lane : lists) : threadIdx.x;  // the lane's list
   int at = 0;
@@ -362,12 +379,10 @@ __global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p
     }
     return r;
   };
-  auto emit = [&](int k, int who, const Candidate& h) {
-    if (lane == who) {
-      p.ids[(int64_t)b * N + k] = chosen_id[k] = h.id;
-      p.parents[(int64_t)b * N + k] = chosen_beam[k] = h.beam;
-      p.out[(int64_t)b * N + k] = (float)score_of(h.key);
-    }
+  auto emit = [&](int k, const Candidate& h) {
+    p.ids[(int64_t)b * N + k] = chosen_id[k] = h.id;
+    p.parents[(int64_t)b * N + k] = chosen_beam[k] = h.beam;
+    p.out[(int64_t)b * N + k] = (float)score_of(h.key);
   };
   int n = 0;
   if (lists <= 64) {
@@ -376,8 +391,8 @@ __global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p
     for (; n < N; ++n) {
       const int who = first_of(h);
       if (who < 0) break;
-      emit(n, who, h);
       if (lane == who) {
+        emit(n, h);
         h = behind;
         behind = head(++at + 1);
       }
@@ -403,8 +418,8 @@ __global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p
     for (; n < N; ++n) {
       const int who = first_of(h);
       if (who < 0) break;
-      emit(n, who, h);
       if (lane == who) {
+        emit(n, h);
         ++at;
         h = next();
       }

@@ -86,6 +86,38 @@ def test_logits_of_any_size():
         assert (np.abs(down(got[2]) - scores) <= tol).all()
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_ties_over_many_tiles(kind):
+    # a workgroup meets the same values again and again: the first tokens are the ones to keep
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    V, N = 151936, 40
+    r = np.random.default_rng(12)
+    rows = [np.zeros(V), r.integers(-2, 3, V), np.arange(V) // 20000, -(np.arange(V) // 20000), np.where(np.arange(V) > 9000, -0.0, 0.0)]
+    for z in rows:
+        z = np.stack([z, z]).astype(np.float32)
+        t = up(torch, dev, z)
+        t = t.to(torch.bfloat16) if kind == "bf16" else t
+        s = np.array([[-1.0, -1.5]], np.float32)
+        _same(acrl.acrl_beam_step(t, up(torch, dev, s), N), beam(z[None], s, N))
+
+
+@pytest.mark.parametrize("size", [1e10, 1e20, 1e30])
+def test_scores_of_large_logits(size):
+    # differences are of the logits themselves: those of the same size keep theirs, and the largest has all the weight
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    V, N = 40000, 5
+    r = np.random.default_rng(13)
+    z = (r.normal(size=(6, V)) * size).astype(np.float32)
+    s = np.array([[-1.0, -2.0, -3.0], [-2.5, -0.5, -1.5]], np.float32)
+    ids, parents, scores = beam(z.reshape(2, 3, V), s, N)
+    got = acrl.acrl_beam_step(up(torch, dev, z), up(torch, dev, s), N)
+    assert np.array_equal(down(got[0]), ids) and np.array_equal(down(got[1]), parents)
+    # fp64 roundings of z, of the normaliser (1e-10) and of two sums, and the one to fp32
+    assert (np.abs(down(got[2]) - scores) <= (HALF["f32"] + 4 * 2.0 ** -53) * np.abs(scores) + 1e-9).all()
+
+
 def test_masked_logits_and_lost_rows():
     torch, dev = torch_dev()
     from paper_2607_24062_amd import acrl

@@ -197,6 +197,17 @@ def test_rows_apart_streams_and_graphs():
     assert [tuple(t.shape) for t in none] == [(0, 2)] * 3
 
 
+@pytest.mark.parametrize("K,V,N", [(4, 3000, 4), (64, 20000, 64), (8, 5, 8)])
+def test_scores_in_place(K, V, N):
+    # a step's scores take the place of the last one's
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    _, tz, _, ts = _inputs(torch, dev, 5, K, V, "f32", 14)
+    want = acrl.acrl_beam_step(tz, ts, N)
+    got = acrl.acrl_beam_step(tz, ts, N, out_scores=ts)
+    assert got[2] is ts and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 # ------------------------------------------------------------------ states
 def _gather(state, parents, dim):
     torch = __import__("torch")

@@ -35,6 +35,7 @@ struct BeamParams {
   const uint8_t* finished;  // or NULL
   int B, K, V, N, eos;
   float inv_t;
+  double c, least, reach;   // inv_t log2 e, -1000 / c, 400 / c
   int S;                    // segments of a row, each one workgroup's
   int seg_tiles;            // tiles of a segment
   int32_t* ids;
@@ -49,21 +50,21 @@ struct BeamParams {
 // A row's beam can give candidates: it has a finite score.
 __device__ __forceinline__ bool alive(float score) { return fabsf(score) < INFINITY; }
 
-// 2^t for t in [-1000, 1000] (below: as -1000): the polynomial is an interpolation of
-// 2^f, |f| <= 1/2, at Chebyshev's points, within 5.5e-11 of it.
-__device__ __forceinline__ double exp2_f64(double t) {
-  constexpr double kRound = 6755399441055744.0;  // 1.5 2^52: added, it leaves t's integer in the low bits
-  t = fmax(t, -1000.0);
-  const double r = t + kRound, f = t - (r - kRound);
-  double p = 1.5303700711425663e-05;
-  p = fma(p, f, 0.00015469729214122798);
-  p = fma(p, f, 0.0013333478473685175);
-  p = fma(p, f, 0.009618025613318018);
-  p = fma(p, f, 0.055504109063258665);
-  p = fma(p, f, 0.24022651213498092);
-  p = fma(p, f, 0.6931471805568324);
-  p = fma(p, f, 0.9999999999595618);
-  return __hiloint2double(__double2hiint(p) + (__double2loint(r) << 20), __double2loint(p));
+// 2^(c d) for c d up to 1000 (below -1000: as there): the polynomial is an
+// interpolation of 2^f, |f| <= 1/2, at Chebyshev's points, within 5.5e-11 of it.
+__device__ __forceinline__ double exp2_f64(const BeamParams& p, double d) {
+  constexpr double kRound = 6755399441055744.0;  // 1.5 2^52: added, it leaves an integer in the low bits
+  d = fmax(d, p.least);
+  const double r = fma(d, p.c, kRound), f = fma(d, p.c, kRound - r);
+  double v = 1.5303700711425663e-05;
+  v = fma(v, f, 0.00015469729214122798);
+  v = fma(v, f, 0.0013333478473685175);
+  v = fma(v, f, 0.009618025613318018);
+  v = fma(v, f, 0.055504109063258665);
+  v = fma(v, f, 0.24022651213498092);
+  v = fma(v, f, 0.6931471805568324);
+  v = fma(v, f, 0.9999999999595618);
+  return __hiloint2double(__double2hiint(v) + (__double2loint(r) << 20), __double2loint(v));
 }
 
 // fp32 values in their order as integers, and back.
@@ -97,9 +98,11 @@ struct Logits {
       const int64_t first = min(tile, end - 1);
       const T* const from = z + first;
       const uint32_t last = (uint32_t)(end - 1 - first);
+      uint32_t mine = lane * kEach;
+      asm volatile("" : "+v"(mine));  // (made here: else eight offsets lie in registers all the time)
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
-        const T* const one = from + min(lane * kEach + i, last);
+        const T* const one = from + min(mine + i, last);
         if constexpr (sizeof(T) == 4) {
           w[i] = *reinterpret_cast<const uint32_t*>(one);
         } else {
@@ -197,9 +200,8 @@ __global__ __launch_bounds__(64 * kScanWaves, 8) void beam_scan_kernel(BeamParam
   const T* const z = static_cast<const T*>(p.logits) + row * p.ldl;
   const int64_t begin = (int64_t)seg * p.seg_tiles * kTile;
   const int64_t end = min((int64_t)p.V, begin + (int64_t)p.seg_tiles * kTile);
-  const double c = (double)p.inv_t * 1.4426950408889634074;  // (the same rounding for all terms)
   const int N = p.N;
-  float m = -INFINITY;  // the lane's reference, one of its logits: no more than 2^900 below any other
+  float m = -INFINITY, most = -INFINITY;  // the lane's reference, one of its logits, and up to where it serves
   double sum = 0.0;
   bool bad = false;
   Logits<T> next;
@@ -238,26 +240,25 @@ __global__ __launch_bounds__(64 * kScanWaves, 8) void beam_scan_kernel(BeamParam
     }
     tile += kScanWaves * kTile;
     next.read(z, tile, end, lane);
-    float top = x[0];
+    float top = x[0];  // (or NaN)
 #pragma unroll
-    for (int i = 0; i < kEach; i += 2) {
-      top = fmaxf(top, fmaxf(x[i], x[i + 1]));
-      bad |= __builtin_isunordered(x[i], x[i + 1]);
-    }
-    bad |= top == INFINITY;
+    for (int i = 1; i < kEach; ++i) top = __builtin_elementwise_maximum(top, x[i]);
+    bad |= !(top < INFINITY);
     const float cut = value_of(bar);
     if (top >= cut) {
 #pragma unroll
       for (int i = 0; i < kEach; ++i)
         if (x[i] >= cut) s.notes[atomicAdd(&s.count, 1)] = key_of(x[i], (int)(here + i));
     }
-    if (((double)top - (double)m) * c > 900.0) {
-      sum *= exp2_f64(((double)m - (double)top) * c);
+    if (top > most) {
+      // (most is rounded: by no more than what it is above m, or to m; no term is above 2^800)
+      sum *= exp2_f64(p, (double)m - (double)top);
       m = top;
+      most = (float)((double)m + p.reach);
     }
     // (the difference first: logits of 1e20 would leave nothing of an exponent in z c - m c)
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) sum += exp2_f64(((double)x[i] - (double)m) * c);
+    for (int i = 0; i < kEach; ++i) sum += exp2_f64(p, (double)x[i] - (double)m);
     lds_barrier();
     const int count = s.count;
     lds_barrier();  // (all have read it before any wave notes more)
@@ -265,7 +266,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 8) void beam_scan_kernel(BeamParam
   }
   // the waves' sums together
   const float ref = wave_max(m);
-  sum *= exp2_f64(((double)m - (double)ref) * c);
+  sum *= exp2_f64(p, (double)m - (double)ref);
   for (int o = 32; o; o /= 2) sum += shfl_xor_f64(sum, o);
   const bool any_bad = __ballot(bad) != 0;
   if (lane == 0) {
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 8) void beam_scan_kernel(BeamParam
       none |= s.norms[w][0] != s.norms[w][0];
       if (s.norms[w][0] > ref_all) ref_all = s.norms[w][0];
     }
-    for (int w = 0; w < kScanWaves; ++w) total += s.norms[w][1] * exp2_f64((s.norms[w][0] - ref_all) * c);
+    for (int w = 0; w < kScanWaves; ++w) total += s.norms[w][1] * exp2_f64(p, s.norms[w][0] - ref_all);
     p.norm[2 * slot] = none ? (double)NAN : ref_all;
     p.norm[2 * slot + 1] = total;
   }
@@ -313,7 +314,6 @@ __global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p
   __shared__ int chosen_beam[kMaxOut], chosen_id[kMaxOut];
   const int b = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lists = p.K * p.S, N = p.N;
-  const double c = (double)p.inv_t * 1.4426950408889634074;
   const float* const val = p.val + (int64_t)b * lists * N;
   const int* const idx = p.idx + (int64_t)b * lists * N;
   // All of a list is read at once, also where its beam turns out to have none and nothing has been written.
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p
         none |= refs[s] != refs[s];
         if (refs[s] > ref) ref = refs[s];
       }
-      for (int s = j * p.S; s < (j + 1) * p.S; ++s) sum += sums[s] * exp2_f64((refs[s] - ref) * c);
+      for (int s = j * p.S; s < (j + 1) * p.S; ++s) sum += sums[s] * exp2_f64(p, refs[s] - ref);
       lse[j] = ref * (double)p.inv_t + log(sum);
       if (none || !(fabs(lse[j]) < INFINITY)) state[j] = 0;
     }
@@ -561,6 +561,9 @@ acrl_status acrl_beam_step(const acrl_beam_desc* d, void* stream) {
   p.finished = d->finished;
   p.eos = d->eos_id;
   p.inv_t = d->inv_temperature;
+  p.c = (double)p.inv_t * 1.4426950408889634074;
+  p.least = -1000.0 / p.c;
+  p.reach = 400.0 / p.c;
   p.ids = d->ids;
   p.parents = d->parents;
   p.out = d->out_scores;

@@ -64,6 +64,8 @@ struct MoeParams {
 };
 
 __device__ __forceinline__ bool live(const MoeParams& p, int t) { return !p.mask || p.mask[t]; }
+// Whether the ids of token t count: those that the router made are -1 where the mask takes it out.
+__device__ __forceinline__ bool has_pairs(const MoeParams& p, int t) { return p.router || live(p, t); }
 
 // ------------------------------------------------------------------ router
 // The router's logits in 64 bits, so that which of two experts is chosen does not
@@ -111,14 +113,20 @@ struct Choice {
 };
 template <int EACH, bool WEIGHTS>
 __device__ __forceinline__ Choice choose(const MoeParams& p, int t, int lane) {
-  if (!live(p, t)) return {-1, 0.0f};
   double s[EACH];     // the score
+  float bias[EACH];
   uint64_t by[EACH];  // what the choice goes by, in order (NaN counts as the lowest; 0: chosen)
   double top = -INFINITY;
 #pragma unroll
+  for (int i = 0; i < EACH; ++i) {  // (all that is read, before any of it is looked at)
+    const int e = min(64 * i + lane, p.E - 1);
+    s[i] = p.logits[(int64_t)t * p.E + e];
+    bias[i] = p.bias ? p.bias[e] : 0.0f;
+  }
+  if (!live(p, t)) return {-1, 0.0f};
+#pragma unroll
   for (int i = 0; i < EACH; ++i) {
-    const int e = 64 * i + lane;
-    s[i] = e < p.E ? p.logits[(int64_t)t * p.E + e] : -INFINITY;
+    if (64 * i + lane >= p.E) s[i] = -INFINITY;
     by[i] = score_key(s[i] == s[i] ? s[i] : -INFINITY);
     if (s[i] > top) top = s[i];
   }
@@ -144,7 +152,7 @@ __device__ __forceinline__ Choice choose(const MoeParams& p, int t, int lane) {
   for (int i = 0; i < EACH; ++i) {
     const int e = 64 * i + lane;
     if (p.bias && e < p.E) {
-      const double v = s[i] + (double)p.bias[e];
+      const double v = s[i] + (double)bias[i];
       by[i] = score_key(v == v ? v : -INFINITY);
     }
     if (e >= p.E) by[i] = 0;
@@ -209,7 +217,7 @@ __device__ __forceinline__ int expert_of(const MoeParams& p, const int* ids) {
   const int y = blockIdx.y;
   if (!BY_PAIR) return y;
   const int e = ids[y];
-  return e >= 0 && e < p.E && live(p, y / p.k) ? e : -1;
+  return e >= 0 && e < p.E && has_pairs(p, y / p.k) ? e : -1;
 }
 template <bool BY_PAIR>
 __device__ __forceinline__ int find_tokens(const MoeParams& p, const int* ids, int e, Tokens& s) {
@@ -217,7 +225,7 @@ __device__ __forceinline__ int find_tokens(const MoeParams& p, const int* ids, i
   int n = 0;
   for (int first = 0; first < P; first += 64 * kWaves) {
     const int pair = first + threadIdx.x;
-    const bool hit = pair < P && ids[pair] == e && live(p, pair / p.k);
+    const bool hit = pair < P && ids[pair] == e && has_pairs(p, pair / p.k);
     const uint64_t m = __ballot(hit);
     if (lane == 0) s.counts[wave] = __popcll(m);
     lds_barrier();
@@ -628,10 +636,10 @@ __global__ __launch_bounds__(64 * kFewPairs) void moe_down_few_kernel(MoeParams 
   if (p.res && t < p.T) res = residual(p, t, r0 + r);
   if ((int)threadIdx.x < P) {
     const int id = p.ids[threadIdx.x];
-    counts[threadIdx.x] = id >= 0 && id < p.E && live(p, threadIdx.x / p.k);
+    counts[threadIdx.x] = id >= 0 && id < p.E && has_pairs(p, threadIdx.x / p.k);
     weight[threadIdx.x] = p.weights[threadIdx.x];
   }
-  if (e >= 0 && e < p.E && live(p, pair / p.k)) {
+  if (e >= 0 && e < p.E && has_pairs(p, pair / p.k)) {
     const int each = (p.kb_f + wk - 1) / wk, k1 = min(p.kb_f, (wave % wk + 1) * each);
     const uint8_t* const row = p.w_out + ((int64_t)e * p.d + r0 + (lane & 15)) * p.F;
     const float* const scale = p.s_out + ((int64_t)e * ((p.d + kBlock - 1) / kBlock) + r0 / kBlock) * p.kb_f;
@@ -687,23 +695,31 @@ __global__ __launch_bounds__(64 * kFewPairs) void moe_down_few_kernel(MoeParams 
 }
 
 // y of a token: its pairs' rows by their weights, in the order of its choices (no atomics: equal calls give equal bits),
-// and the residual.
+// and the residual.  All rows are under way together (one after another: 6.0 us for 4.6 at 64 tokens, 8 pairs each, d =
+// 2048).
 template <typename OUT>
 __global__ __launch_bounds__(256) void moe_sum_kernel(MoeParams p) {
-  const int t = blockIdx.y, c = (blockIdx.x * 256 + threadIdx.x) * 4;
-  if (c >= p.d) return;
-  f32x4 v = {};
-  if (live(p, t))
-    for (int j = 0; j < p.k; ++j) {
-      const int pair = t * p.k + j, e = p.ids[pair];
-      if (e < 0 || e >= p.E) continue;
-      add(v, *reinterpret_cast<const f32x4*>(p.part + (int64_t)pair * p.d + c), p.weights[pair]);
-    }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (p.res) v[i] += residual(p, t, c + i);
-    static_cast<OUT*>(p.y)[t * p.ldy + c + i] = (OUT)v[i];
+  const int t = blockIdx.y, c = (blockIdx.x * 256 + threadIdx.x) * 4, j = threadIdx.x & 63;
+  int id = -1;
+  float weight = 0.0f;
+  if (j < p.k && has_pairs(p, t)) {  // lane j has the j-th pair's
+    id = p.ids[t * p.k + j];
+    weight = p.weights[t * p.k + j];
   }
+  const uint64_t pairs = __ballot(id >= 0 && id < p.E);
+  if (c >= p.d) return;
+  f32x4 rows[kMaxK], v = {};
+  float res[4];
+#pragma unroll
+  for (int n = 0; n < kMaxK; ++n)
+    if (pairs >> n & 1) rows[n] = *reinterpret_cast<const f32x4*>(p.part + (int64_t)(t * p.k + n) * p.d + c);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) res[i] = p.res ? residual(p, t, c + i) : 0.0f;
+#pragma unroll
+  for (int n = 0; n < kMaxK; ++n)
+    if (pairs >> n & 1) add(v, rows[n], __int_as_float(read_lane(__float_as_int(weight), n)));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) static_cast<OUT*>(p.y)[t * p.ldy + c + i] = (OUT)(p.res ? v[i] + res[i] : v[i]);
 }
 
 // ------------------------------------------------------------------ host

@@ -222,10 +222,11 @@ __device__ __forceinline__ int expert_of(const MoeParams& p, const int* ids) {
 template <bool BY_PAIR>
 __device__ __forceinline__ int find_tokens(const MoeParams& p, const int* ids, int e, Tokens& s) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, P = p.T * p.k;
-  int n = 0;
+  int n = 0, next = (int)threadIdx.x < P ? ids[threadIdx.x] : -1;
   for (int first = 0; first < P; first += 64 * kWaves) {
-    const int pair = first + threadIdx.x;
-    const bool hit = pair < P && ids[pair] == e && has_pairs(p, pair / p.k);
+    const int pair = first + threadIdx.x, id = next;
+    next = pair + 64 * kWaves < P ? ids[pair + 64 * kWaves] : -1;
+    const bool hit = id == e && has_pairs(p, pair / p.k);
     const uint64_t m = __ballot(hit);
     if (lane == 0) s.counts[wave] = __popcll(m);
     lds_barrier();

@@ -477,13 +477,15 @@ hipError_t launch_reorder(ReorderParams p, int64_t row_bytes, hipStream_t s) {
 constexpr int kCus = 256;
 
 // Segments: four workgroups a CU (512 x 151936: 107 us with two) where the rows allow it, each of a tile a wave at
-// least; a wave's lists at most (1 x 4 x 151936: 18 us, 24 with 38 of them) unless segments would have more than four such tiles; what the
-// pick has lanes and LDS for.
+// least; as many as one wave of the pick has lanes for (1 x 4 x 151936: 15.6 us, 18.6 with 38 of them), or of four tiles a
+// wave where that saves more tiles one after another than the pick's second round of choices costs (1 x 24 x 151936, 4
+// chosen: 19 us, 26 with the former; 8 x 8, 8 chosen: 30 with the latter, 24); what the pick has lanes and LDS for.
 void segment(BeamParams& p) {
   const int64_t rows = (int64_t)p.B * p.K, tiles = ((int64_t)p.V + kTile - 1) / kTile;
   int64_t S = rows ? std::max<int64_t>(1, (4 * kCus + rows - 1) / rows) : 1;
   const int64_t most = (tiles + kScanWaves - 1) / kScanWaves;
-  S = std::min(S, std::min(most, std::max<int64_t>(64 / p.K, (most + 3) / 4)));
+  const int64_t few = std::max(1, 64 / p.K), many = (most + 3) / 4;
+  S = std::min(S, std::min(most, most / few - most / many > p.N / 2 + 2 ? many : few));
   S = std::min<int64_t>(S, std::min(kMaxLists / p.K, std::max(1, kMaxStaged / (p.K * p.N))));
   p.seg_tiles = (int)((tiles + S - 1) / S);
   p.S = (int)((tiles + p.seg_tiles - 1) / p.seg_tiles);

@@ -845,43 +845,43 @@ def acrl_beam_reorder(state, parents, dim: int = 0, out=None, stream=None):
     if not state.is_cuda or state.dim() < dim + 2 or dim < 0:
         raise ValueError("state must be a device tensor with sequences in dimension %d and beams in the next" % dim)
     _index_of(parents, torch.int32, "parents", stream)
-    B, K = state.shape[dim], state.shape[dim + 1]
+    shape, size = state.shape, state.element_size()
+    B, K = shape[dim], shape[dim + 1]
     if parents.dim() != 2 or parents.shape[0] != B or parents.get_device() != index:
         raise ValueError("parents must be [%d, n_out] on %s" % (B, state.device))
     n_out = parents.shape[1]
-    shape = (*state.shape[:dim + 1], n_out, *state.shape[dim + 2:])
+    shape_out = (*shape[:dim + 1], n_out, *shape[dim + 2:])
     if out is None:
-        out = _empty(shape, state.dtype, state.device, stream)
-    elif tuple(out.shape) != shape or out.dtype != state.dtype or out.get_device() != index:
-        raise ValueError("out must be %s of %s on %s" % (shape, state.dtype, state.device))
-    size, outer = state.element_size(), math.prod(state.shape[:dim])
-    if state.is_contiguous() and out.is_contiguous():
-        row = math.prod(state.shape[dim + 2:])
-        src, dst = (B * K * row, K * row, row), (B * n_out * row, n_out * row, row)
-    else:
-        row, src = _rows(state, dim, "state")
-        dst = _rows(out, dim, "out")[1]
-    desc = ReorderDesc(outer, B, K, n_out, row * size, state.data_ptr(), *[n * size for n in src], out.data_ptr(),
-                       *[n * size for n in dst], parents.data_ptr())
+        out = _empty(shape_out, state.dtype, state.device, stream)
+    elif tuple(out.shape) != shape_out or out.dtype != state.dtype or out.get_device() != index:
+        raise ValueError("out must be %s of %s on %s" % (shape_out, state.dtype, state.device))
+    outer, row, *src = _rows(shape, state.stride(), dim, size, "state")
+    _, _, *dst = _rows(shape_out, out.stride(), dim, size, "out")
+    desc = ReorderDesc(outer, B, K, n_out, row, state.data_ptr(), *src, out.data_ptr(), *dst, parents.data_ptr())
     _check(lib().acrl_beam_reorder(ctypes.byref(desc), _raw_stream(stream, state.device)), "acrl_beam_reorder")
     return out
 
 
-def _rows(t, dim: int, name: str):
-    """(elements of a beam's row, (outer, sequence, beam) strides) of a tensor of states."""
+@functools.lru_cache(maxsize=256)
+def _rows(shape, strides, dim: int, size: int, name: str):
+    """(outer, bytes of a beam's row, bytes between outer ones, sequences, beams)
+    of a tensor of states with elements of `size` bytes."""
+    if 0 in shape:
+        return 0, 0, 0, 0, 0
     row = 1
-    for n, s in zip(reversed(t.shape[dim + 2:]), reversed(t.stride()[dim + 2:])):
+    for n, s in zip(reversed(shape[dim + 2:]), reversed(strides[dim + 2:])):
         if n != 1 and s != row:
             raise ValueError("%s: a beam's row must be dense" % name)
         row *= n
     outer, step = 0, None
-    for n, s in zip(reversed(t.shape[:dim]), reversed(t.stride()[:dim])):
+    for n, s in zip(reversed(shape[:dim]), reversed(strides[:dim])):
         if n == 1:
             continue
         if step is not None and s != step:
             raise ValueError("%s: the dimensions before the sequences must collapse into one" % name)
-        outer, step = outer or s, s * n
-    return row, (outer, t.stride(dim) if t.shape[dim] > 1 else 0, t.stride(dim + 1) if t.shape[dim + 1] > 1 else 0)
+        outer, step = outer if step is not None else s, s * n
+    return (math.prod(shape[:dim]), row * size, outer * size, strides[dim] * size if shape[dim] > 1 else 0,
+            strides[dim + 1] * size if shape[dim + 1] > 1 else 0)
 
 
 # ------------------------------------------------------------------ losses beside the surrogate

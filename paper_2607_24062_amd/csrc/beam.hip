@@ -127,10 +127,11 @@ __device__ __forceinline__ uint64_t key_of(float v, int idx) {
 // logits.  A workgroup notes in LDS, key by key, what is no less than a bar; when
 // there are many notes they are thinned out to the N largest, and what is above the
 // least of those is noted from there on.  With logits in no order that happens three
-// or four times.  What bounds it (512 x 151936: 75 us) is less the loads (50 alone) than the vector
-// instructions: fp64 exponentials (25) and notes.  (A list of N a wave,
-// kept in order by insertions, took 28 us more; notes by ballots over all eight logits,
-// 200 instructions, 8 more; notes thinned out from 256 on, 3 more.)
+// or four times.  What bounds it (512 x 151936: 70 us) is less the loads (50 alone)
+// than the vector instructions: fp64 exponentials (20) and notes.  (A list of N a
+// wave, kept in order by insertions, took 28 us more; notes by ballots over all eight
+// logits, 200 instructions, 8 more; notes thinned out from 256 on, 3 more; fmaxf,
+// which has NaN to hide, and a check of its own, 3.)
 struct Scan {
   uint64_t notes[kNotes];
   double norms[kScanWaves][2];

@@ -539,7 +539,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void moe_up_few_kernel(MoeParams p)
     if (blockIdx.x == 0 && wave < p.T) write_choice<EACH>(p, wave, lane);
     return;
   }
-  if (p.bias) {
+  if (EACH > 2 || p.bias) {  // (more than 128 experts: 22 us of ranks each of all)
     if (wave < p.T) {
       const int id = choose<EACH, false>(p, wave, lane).id;
       if (lane < p.k) chosen[wave * p.k + lane] = id;

@@ -29,8 +29,7 @@ constexpr int kBlock = 128;        // columns per scale
 constexpr int kMaxTokens = 128, kMaxK = 16, kMaxExperts = 512;
 constexpr int kMaxPairs = kMaxTokens * kMaxK;
 constexpr int kWaves = 4;          // of the products' workgroups (7 tokens, 60 experts: 37 us, 46 with eight)
-constexpr int kFewWaves = 8;       // of those for one or two tokens
-constexpr int kChooseTokens = 2;   // up to so many, every workgroup of the first products chooses the experts by itself
+constexpr int kFewWaves = 8;       // of those for few tokens, a wave at least for each
 constexpr int kFewPairs = 16;      // up to so many, the second products and their sum are one kernel, a wave each
 
 struct MoeParams {
@@ -521,52 +520,27 @@ __device__ __forceinline__ float residual(const MoeParams& p, int t, int c) {
   return p.res_f32 ? static_cast<const float*>(p.res)[at] : bf16_lo(static_cast<const uint16_t*>(p.res)[at]);
 }
 
-// The same for one or two tokens, where what counts is how many loads wait for
-// another: every workgroup chooses the experts by itself (1.6 us of 22 for one
-// token, 2048 x 768, 8 of 128 experts; their weights are made by a workgroup apart),
-// and the codes and columns of two blocks are under way together.  One pair a
+// The same for few tokens that hardly share experts, where what counts is how many
+// loads wait for another: every workgroup chooses its pair's expert by itself (2 us
+// of 22 for one token, 2048 x 768, 8 of 128 experts; weights are made by a workgroup
+// apart), and the codes and columns of two blocks are under way together.  One pair a
 // workgroup and 16 gate and up rows, K shared by its waves.
 template <int EACH>
 __global__ __launch_bounds__(64 * kFewWaves) void moe_up_few_kernel(MoeParams p) {
   __shared__ f32x4 red[kFewWaves][2][4];
-  __shared__ int chosen[kChooseTokens * kMaxK];
-  __shared__ uint64_t keys[64 * EACH];
-  __shared__ int rank[64 * EACH];
-  static_assert(kFewWaves % EACH == 0, "whole parts");
+  __shared__ int chosen;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
   const int pair = (int)blockIdx.y - 1, f0 = blockIdx.x * 16;
   if (pair < 0) {  // (first, since it takes as long as any)
     if (blockIdx.x == 0 && wave < p.T) write_choice<EACH>(p, wave, lane);
     return;
   }
-  if (EACH > 2 || p.bias) {  // (more than 128 experts: 22 us of ranks each of all)
-    if (wave < p.T) {
-      const int id = choose<EACH, false>(p, wave, lane).id;
-      if (lane < p.k) chosen[wave * p.k + lane] = id;
-    }
-    lds_barrier();
-  } else {
-    // by the logits alone: every expert's rank among all, each wave taking a part of the others
-    constexpr int kPad = 64 * EACH, kParts = kFewWaves / EACH, kOthers = kPad / kParts;
-    const int mine = threadIdx.x % kPad, first = threadIdx.x / kPad * kOthers;
-    for (int t = 0; t < p.T; ++t) {
-      if ((int)threadIdx.x < kPad) {
-        const double l = mine < p.E ? p.logits[(int64_t)t * p.E + mine] : 0.0;
-        keys[mine] = mine < p.E ? score_key(l == l ? l : -INFINITY) : 0;
-        rank[mine] = 0;
-      }
-      lds_barrier();
-      const uint64_t key = keys[mine];
-      int before = 0;
-#pragma unroll 8
-      for (int j = first; j < first + kOthers; ++j) before += keys[j] > key || (keys[j] == key && j < mine);
-      if (before) atomicAdd(&rank[mine], before);
-      lds_barrier();
-      if ((int)threadIdx.x < p.E && rank[mine] < p.k) chosen[t * p.k + rank[mine]] = live(p, t) ? mine : -1;
-      lds_barrier();
-    }
+  if (wave == 0) {
+    const int id = choose<EACH, false>(p, pair / p.k, lane).id;
+    if (lane == pair % p.k) chosen = id;
   }
-  const int e = __builtin_amdgcn_readfirstlane(chosen[pair]), blocks = (2 * p.F + kBlock - 1) / kBlock;
+  lds_barrier();
+  const int e = __builtin_amdgcn_readfirstlane(chosen), blocks = (2 * p.F + kBlock - 1) / kBlock;
   if (e < 0) return;
   const uint16_t* const x = p.x + pair / p.k * p.ldx;
   const uint8_t* const gate = p.w_in + ((int64_t)e * 2 * p.F + f0 + (lane & 15)) * p.d;
@@ -804,7 +778,9 @@ hipError_t launch_moe(MoeParams p, hipStream_t s) {
     else hipLaunchKernelGGL((moe_logits_kernel<2>), grid, dim3(256), 0, s, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if (p.router && p.T <= kChooseTokens) {
+  // (3 tokens, 8 of 128 experts of 2048 x 768: 38.2 us, 40.2 the other way; 4 tokens, 2 of them: 19.8 and 23.1; but 8 tokens, 8
+  // of them, 70.4 and 67.2; 4 tokens, 2 of 8 experts of 4096 x 14336: 237 and 208)
+  if (p.router && (p.T <= 2 || (p.T <= kFewWaves && 4 * P <= p.E))) {
     const dim3 grid(p.F / 16, P + 1);
     if (p.E <= 128) hipLaunchKernelGGL(moe_up_few_kernel<2>, grid, dim3(64 * kFewWaves), 0, s, p);
     else hipLaunchKernelGGL(moe_up_few_kernel<8>, grid, dim3(64 * kFewWaves), 0, s, p);

@@ -77,6 +77,17 @@ def test_sizes(n, size):
         _check(down(y.float()), *experts(x, ids, w, layer.win, layer.wout, act, None if resid is None else f64(resid)), out)
 
 
+# tokens that hardly share experts, a pair a workgroup: up to 128 experts and more, pairs for either second product, as many
+# pairs as that takes and one expert too few for it
+FEW = [(3, 96, 70, 2, 64), (8, 64, 64, 2, 96), (8, 64, 63, 2, 96), (8, 160, 300, 9, 64), (5, 288, 128, 6, 1184), (4, 1312, 512, 16, 32),
+       (9, 64, 512, 2, 64)]
+
+
+@pytest.mark.parametrize("n,size", list(enumerate(FEW)))
+def test_few_tokens(n, size):
+    test_sizes(n + 100, size)
+
+
 @pytest.mark.parametrize("act", list(ACTS))
 def test_activations(act):
     torch, dev = torch_dev()

@@ -105,13 +105,13 @@ __global__ __launch_bounds__(256) void moe_logits_kernel(MoeParams p) {
 }
 
 // Choice of a token's experts by one wave, lane j getting the j-th: lane l looks at the experts l, l + 64, .. (EACH).
-// Without WEIGHTS, the ids alone.
+// Without WEIGHTS, the ids alone, of the first n.
 struct Choice {
   int id;
   float weight;
 };
 template <int EACH, bool WEIGHTS>
-__device__ __forceinline__ Choice choose(const MoeParams& p, int t, int lane) {
+__device__ __forceinline__ Choice choose(const MoeParams& p, int t, int lane, int n) {
   double s[EACH];     // the score
   float bias[EACH];
   uint64_t by[EACH];  // what the choice goes by, in order (NaN counts as the lowest; 0: chosen)
@@ -158,7 +158,7 @@ __device__ __forceinline__ Choice choose(const MoeParams& p, int t, int lane) {
   }
   double mine = 0.0, total = 0.0;  // lane j: the score of the j-th choice
   int mine_id = 0;
-  for (int j = 0; j < p.k; ++j) {
+  for (int j = 0; j < n; ++j) {
     uint64_t best = by[0];
     double best_s = s[0];
     int id = lane;
@@ -190,7 +190,7 @@ __device__ __forceinline__ Choice choose(const MoeParams& p, int t, int lane) {
 }
 template <int EACH>
 __device__ __forceinline__ void write_choice(const MoeParams& p, int t, int lane) {
-  const Choice c = choose<EACH, true>(p, t, lane);
+  const Choice c = choose<EACH, true>(p, t, lane, p.k);
   if (lane < p.k) {
     p.ids[t * p.k + lane] = c.id;
     p.weights[t * p.k + lane] = c.weight;
@@ -536,7 +536,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void moe_up_few_kernel(MoeParams p)
     return;
   }
   if (wave == 0) {
-    const int id = choose<EACH, false>(p, pair / p.k, lane).id;
+    const int id = choose<EACH, false>(p, pair / p.k, lane, pair % p.k + 1).id;
     if (lane == pair % p.k) chosen = id;
   }
   lds_barrier();

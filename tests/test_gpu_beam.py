@@ -118,6 +118,21 @@ def test_scores_of_large_logits(size):
     assert (np.abs(down(got[2]) - scores) <= (HALF["f32"] + 4 * 2.0 ** -53) * np.abs(scores) + 1e-9).all()
 
 
+@pytest.mark.parametrize("inv_t", [1e-3, 50.0, 1e20])
+def test_temperatures(inv_t):
+    # from nearly even weights to all of it on the largest logit
+    torch, dev = torch_dev()
+    from paper_2607_24062_amd import acrl
+    V, N = 30000, 6
+    r = np.random.default_rng(15)
+    z = (r.normal(size=(6, V)) * 3).astype(np.float32)
+    s = np.array([[-1.0, -1.001, -1.002], [-2.5, -0.5, -1.5]], np.float32)
+    ids, parents, scores = beam(z.reshape(2, 3, V), s, N, inv_t)
+    got = acrl.acrl_beam_step(up(torch, dev, z), up(torch, dev, s), N, inv_temperature=inv_t)
+    assert np.array_equal(down(got[0]), ids) and np.array_equal(down(got[1]), parents)
+    assert (np.abs(down(got[2]) - scores) <= (HALF["f32"] + 4 * 2.0 ** -53) * np.abs(scores) + 1e-9).all()
+
+
 def test_masked_logits_and_lost_rows():
     torch, dev = torch_dev()
     from paper_2607_24062_amd import acrl

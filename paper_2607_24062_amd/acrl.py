@@ -276,6 +276,8 @@ def _ptr(t: Optional[torch.Tensor]):
 # the current stream's handle alone, where torch has it: making its Stream
 # object takes 2.7 us, twice per call, and the handle 0.1
 _current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+# likewise the current device's index, once there is a device tensor
+_current_index = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _zero_all = getattr(torch, "_foreach_zero_", None)
 
 
@@ -332,13 +334,21 @@ def _want(t, dtype, numel: int, index: int, name: str, optional: bool = False):
 def _index_of(t, dtype, name: str, stream=None) -> int:
     """The device index of a device tensor, which is to be the current one (the
     library launches there) and the stream's."""
-    _dev(t, dtype, name)
     index = t.get_device()
+    if index < 0 or t.dtype is not dtype or not t.is_contiguous():
+        _dev(t, dtype, name)
     if stream is not None and stream.device_index != index:
         raise ValueError("%s is on cuda:%d, the stream belongs to cuda:%d" % (name, index, stream.device_index))
-    if index != torch.cuda.current_device():
-        raise ValueError("%s is on cuda:%d, the current device is cuda:%d" % (name, index, torch.cuda.current_device()))
+    if index != _current_index():
+        raise ValueError("%s is on cuda:%d, the current device is cuda:%d" % (name, index, _current_index()))
     return index
+
+
+def _raw_of(stream, index: int) -> int:
+    """The HIP stream of `stream`, or the current one of the device `index`."""
+    if stream is not None or _current_raw is None:
+        return _raw_stream(stream, torch.device("cuda", index))
+    return _current_raw(index)
 
 
 @functools.lru_cache(maxsize=256)
@@ -751,7 +761,7 @@ def acrl_linear_fp8(xq, x_scales, wq, w_scales, bias=None, activation: int = ACT
     if residual is not None:
         desc.ldr = _matrix(residual, M, N, index, "residual")
         desc.residual, desc.residual_type = residual.data_ptr(), _OUT_TYPES[residual.dtype]
-    _check(lib().acrl_linear_fp8(ctypes.byref(desc), _raw_stream(stream, xq.device)), "acrl_linear_fp8")
+    _check(lib().acrl_linear_fp8(ctypes.byref(desc), _raw_of(stream, index)), "acrl_linear_fp8")
     return out
 
 
@@ -802,7 +812,7 @@ def acrl_moe_fp8(x, w_in, s_in, w_out, s_out, top_k: int, router=None, score: in
         _want(ids, torch.int32, T * top_k, index, "ids"), _want(weights, f32, T * top_k, index, "weights"),
         0 if residual is None else _OUT_TYPES[residual.dtype], _OUT_TYPES[out.dtype], score, 1 if renormalize else 0,
         activation, scale, ws.data_ptr() if nbytes else None, nbytes)
-    _check(lib().acrl_moe_fp8(ctypes.byref(desc), _raw_stream(stream, dev)), "acrl_moe_fp8")
+    _check(lib().acrl_moe_fp8(ctypes.byref(desc), _raw_of(stream, index)), "acrl_moe_fp8")
     return out, ids, weights
 
 
@@ -830,7 +840,7 @@ def acrl_beam_step(logits, scores, n_out: int, inv_temperature: float = 1.0, fin
     desc = BeamDesc(B, K, V, n_out, logits.data_ptr(), ldl, scores.data_ptr(),
                     _want(finished, torch.uint8, B * K, index, "finished", True), _OUT_TYPES[logits.dtype], eos_id,
                     inv_temperature, *[t.data_ptr() for t in outputs], ws.data_ptr() if nbytes else None, nbytes)
-    _check(lib().acrl_beam_step(ctypes.byref(desc), _raw_stream(stream, dev)), "acrl_beam_step")
+    _check(lib().acrl_beam_step(ctypes.byref(desc), _raw_of(stream, index)), "acrl_beam_step")
     return tuple(outputs)
 
 
@@ -858,7 +868,7 @@ def acrl_beam_reorder(state, parents, dim: int = 0, out=None, stream=None):
     outer, row, *src = _rows(shape, state.stride(), dim, size, "state")
     _, _, *dst = _rows(shape_out, out.stride(), dim, size, "out")
     desc = ReorderDesc(outer, B, K, n_out, row, state.data_ptr(), *src, out.data_ptr(), *dst, parents.data_ptr())
-    _check(lib().acrl_beam_reorder(ctypes.byref(desc), _raw_stream(stream, state.device)), "acrl_beam_reorder")
+    _check(lib().acrl_beam_reorder(ctypes.byref(desc), _raw_of(stream, index)), "acrl_beam_reorder")
     return out
 
 

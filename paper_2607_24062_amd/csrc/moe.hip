@@ -105,7 +105,8 @@ __global__ __launch_bounds__(256) void moe_logits_kernel(MoeParams p) {
 }
 
 // Choice of a token's experts by one wave, lane j getting the j-th: lane l looks at the experts l, l + 64, .. (EACH).
-// Without WEIGHTS, the ids alone, of the first n.
+// Without WEIGHTS, the ids alone, of the first n.  (Experts that no lane has are passed by: 2 tokens, 8 of 256, 24.3 us, 28.3
+// without; with two a lane that would cost 0.5 us.)
 struct Choice {
   int id;
   float weight;
@@ -118,6 +119,7 @@ __device__ __forceinline__ Choice choose(const MoeParams& p, int t, int lane, in
   double top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < EACH; ++i) {  // (all that is read, before any of it is looked at)
+    if (EACH > 2 && 64 * i >= p.E) break;
     const int e = min(64 * i + lane, p.E - 1);
     s[i] = p.logits[(int64_t)t * p.E + e];
     bias[i] = p.bias ? p.bias[e] : 0.0f;
@@ -125,6 +127,7 @@ __device__ __forceinline__ Choice choose(const MoeParams& p, int t, int lane, in
   if (!live(p, t)) return {-1, 0.0f};
 #pragma unroll
   for (int i = 0; i < EACH; ++i) {
+    if (EACH > 2 && 64 * i >= p.E) break;
     if (64 * i + lane >= p.E) s[i] = -INFINITY;
     by[i] = score_key(s[i] == s[i] ? s[i] : -INFINITY);
     if (s[i] > top) top = s[i];
@@ -134,21 +137,29 @@ __device__ __forceinline__ Choice choose(const MoeParams& p, int t, int lane, in
     top = score_of(largest(score_key(top)));
     double sum = 0.0;
 #pragma unroll
-    for (int i = 0; i < EACH; ++i)
+    for (int i = 0; i < EACH; ++i) {
+      if (EACH > 2 && 64 * i >= p.E) break;
       if (64 * i + lane < p.E) {
         s[i] = exp(s[i] - top);
         sum += s[i];
       }
+    }
     for (int m = 32; m; m /= 2) sum += shfl_xor_f64(sum, m);
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) s[i] /= sum;
+    for (int i = 0; i < EACH; ++i) {
+      if (EACH > 2 && 64 * i >= p.E) break;
+      s[i] /= sum;
+    }
   } else {
 #pragma unroll
-    for (int i = 0; i < EACH; ++i)
+    for (int i = 0; i < EACH; ++i) {
+      if (EACH > 2 && 64 * i >= p.E) break;
       if (64 * i + lane < p.E) s[i] = 1.0 / (1.0 + exp(-s[i]));
+    }
   }
 #pragma unroll
   for (int i = 0; i < EACH; ++i) {
+    if (EACH > 2 && 64 * i >= p.E) break;
     const int e = 64 * i + lane;
     if (p.bias && e < p.E) {
       const double v = s[i] + (double)bias[i];
@@ -163,12 +174,14 @@ __device__ __forceinline__ Choice choose(const MoeParams& p, int t, int lane, in
     double best_s = s[0];
     int id = lane;
 #pragma unroll
-    for (int i = 1; i < EACH; ++i)
+    for (int i = 1; i < EACH; ++i) {
+      if (EACH > 2 && 64 * i >= p.E) break;
       if (by[i] > best) {
         best = by[i];
         best_s = s[i];
         id = 64 * i + lane;
       }
+    }
     const uint64_t most = largest(best);
     uint64_t same = __ballot(best == most);
     int who = lowest(same);
@@ -177,7 +190,10 @@ __device__ __forceinline__ Choice choose(const MoeParams& p, int t, int lane, in
     id = read_lane(id, who);
     best_s = read_lane(best_s, who);
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) by[i] = 64 * i + lane == id ? 0 : by[i];
+    for (int i = 0; i < EACH; ++i) {
+      if (EACH > 2 && 64 * i >= p.E) break;
+      by[i] = 64 * i + lane == id ? 0 : by[i];
+    }
     if (lane == j) {
       mine = best_s;
       mine_id = id;
@@ -779,8 +795,8 @@ hipError_t launch_moe(MoeParams p, hipStream_t s) {
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   // (3 tokens, 8 of 128 experts of 2048 x 768: 38.2 us, 40.2 the other way; 4 tokens, 2 of them: 19.8 and 23.1; but 8 tokens, 8
-  // of them, 70.4 and 67.2; 4 tokens, 2 of 8 experts of 4096 x 14336: 237 and 208)
-  if (p.router && (p.T <= 2 || (p.T <= kFewWaves && 4 * P <= p.E))) {
+  // of them, 70.4 and 67.2; 4 tokens, 2 of 8 experts of 4096 x 14336: 237 and 208, 2 tokens: 132 and 117)
+  if (p.router && (p.T == 1 || (p.T <= kFewWaves && 4 * P <= p.E))) {
     const dim3 grid(p.F / 16, P + 1);
     if (p.E <= 128) hipLaunchKernelGGL(moe_up_few_kernel<2>, grid, dim3(64 * kFewWaves), 0, s, p);
     else hipLaunchKernelGGL(moe_up_few_kernel<8>, grid, dim3(64 * kFewWaves), 0, s, p);

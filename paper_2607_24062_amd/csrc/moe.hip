@@ -11,6 +11,8 @@
 // quantizing them.  E4M3 codes become bf16 exactly, products of 128 columns are
 // summed by bf16 matrix instructions from zero and enter the fp32 sums with the
 // block's scale by one FMA each.
+#include <algorithm>
+
 #include "activation.h"
 #include "entry.h"
 #include "lanes.h"
@@ -55,11 +57,12 @@ struct MoeParams {
   int kb_d, kb_f;                  // scale blocks of a row of Win, of Wout
   int by_pair;                     // there are fewer pairs than experts
   int up_wk, down_wk;              // waves that share a tile's K
+  int splits;                      // workgroups that share it in the second products
   // workspace
   double* logits;                  // [T][E]
   uint16_t* h[3];                  // [T k][F] by pair t k + j: h in two bf16 parts, or three
   int parts;
-  float* part;                     // [T k][d]
+  float* part;                     // [splits][T k][d]
 };
 
 __device__ __forceinline__ bool live(const MoeParams& p, int t) { return !p.mask || p.mask[t]; }
@@ -476,7 +479,7 @@ __global__ __launch_bounds__(64 * kWaves, CB == 1 && R == 2 ? 4 : CB <= 2 ? 3 : 
   }
 }
 
-// Wout h of an expert's tokens: tiles of 16 R rows, K shared as above, to one fp32 row a pair.
+// Wout h of an expert's tokens: tiles of 16 R rows, K shared as above and by workgroups, to an fp32 row a pair for each.
 template <int CB, int R, int PARTS, bool BY_PAIR>
 __global__ __launch_bounds__(64 * kWaves, CB + PARTS + R == 5 ? 4 : 2) void moe_down_kernel(MoeParams p) {
   __shared__ f32x4 red[kWaves][R][CB][64];
@@ -489,8 +492,8 @@ __global__ __launch_bounds__(64 * kWaves, CB + PARTS + R == 5 ? 4 : 2) void moe_
   Stream<R, CB, PARTS> st;
   st.K = p.F;
   st.kb = p.kb_f;
-  st.kw = wave % wk;
-  st.wk = wk;
+  st.kw = blockIdx.z * wk + wave % wk;
+  st.wk = wk * p.splits;
   st.q = q;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
@@ -498,6 +501,7 @@ __global__ __launch_bounds__(64 * kWaves, CB + PARTS + R == 5 ? 4 : 2) void moe_
     st.row[i] = p.w_out + ((int64_t)e * p.d + r + (lane & 15)) * p.F;
     st.scale[i] = scales_at(p.s_out, ((int64_t)e * ((p.d + kBlock - 1) / kBlock) + r / kBlock) * p.kb_f);
   }
+  float* const part = p.part + (int64_t)blockIdx.z * p.T * p.k * p.d;
   typename Stream<R, CB, PARTS>::Codes first;
   if (BY_PAIR) st.load(first, st.kw);
   const int n = find_tokens<BY_PAIR>(p, p.ids, e, tokens);
@@ -523,7 +527,7 @@ __global__ __launch_bounds__(64 * kWaves, CB + PARTS + R == 5 ? 4 : 2) void moe_
       const int r = (blockIdx.x * tiles + tile) * 16 * R + 16 * i + 4 * q;
       f32x4 v = red[tile * wk][i][j][lane];
       for (int w = 1; w < wk; ++w) v += red[tile * wk + w][i][j][lane];
-      if (c < n && r < p.d) *reinterpret_cast<f32x4*>(p.part + (int64_t)tokens.pairs[c] * p.d + r) = v;
+      if (c < n && r < p.d) *reinterpret_cast<f32x4*>(part + (int64_t)tokens.pairs[c] * p.d + r) = v;
     }
     lds_barrier();
     c0 += 16 * CB;
@@ -710,6 +714,10 @@ __global__ __launch_bounds__(256) void moe_sum_kernel(MoeParams p) {
 #pragma unroll
   for (int n = 0; n < kMaxK; ++n)
     if (pairs >> n & 1) rows[n] = *reinterpret_cast<const f32x4*>(p.part + (int64_t)(t * p.k + n) * p.d + c);
+  for (int z = 1; z < p.splits; ++z)
+#pragma unroll
+    for (int n = 0; n < kMaxK; ++n)
+      if (pairs >> n & 1) rows[n] += *reinterpret_cast<const f32x4*>(p.part + ((int64_t)z * p.T * p.k + t * p.k + n) * p.d + c);
 #pragma unroll
   for (int i = 0; i < 4; ++i) res[i] = p.res ? residual(p, t, c + i) : 0.0f;
 #pragma unroll
@@ -720,7 +728,47 @@ __global__ __launch_bounds__(256) void moe_sum_kernel(MoeParams p) {
 }
 
 // ------------------------------------------------------------------ host
+// Waves that share a tile's K: until there are four rounds of waves for the CUs (16 each), with two blocks each at
+// least; and one, while there is less than a round.
+int share(int64_t tiles, int kb) {
+  constexpr int64_t kRound = 256 * 16;
+  int wk = 1;
+  while (wk < kWaves && ((tiles * wk * 2 <= 4 * kRound && wk * 4 <= kb) || (tiles * wk < kRound && wk < kb))) wk *= 2;
+  return wk;
+}
+
+// Blocks of 16 columns by the tokens an expert has on average; where it has more than they hold, its weights are read
+// again (128 tokens, 2 of 8 experts of 4096 x 14336: 871 us with one block, 735 with two, 630 with four).
+int column_blocks(const MoeParams& p) {
+  const int P = p.T * p.k;
+  return P <= 10 * p.E || p.T <= 16 ? 1 : P <= 24 * p.E || p.T <= 32 ? 2 : 4;
+}
+
+// The second products of few pairs and their sum as one kernel, where its waves, 16 a workgroup of 16 rows, have not much
+// more of K each than those of the others (2 tokens, 6 of 8 experts of 928 x 8800: 49 us, DOWN_GENERAL the other way).
+int few_share(const MoeParams& p) {
+  int wk = 1;
+  while (wk * 2 * p.T * p.k <= kFewPairs && wk * 2 <= p.kb_f) wk *= 2;
+  return wk;
+}
+bool few_down(const MoeParams& p) {
+  return p.T * p.k <= kFewPairs && (p.kb_f + few_share(p) - 1) / few_share(p) <= p.kb_f / kWaves + 8;
+}
+
+// What follows from the sizes.
+void plan(MoeParams& p) {
+  p.kb_d = (p.d + kBlock - 1) / kBlock;
+  p.kb_f = (p.F + kBlock - 1) / kBlock;
+  p.by_pair = p.T * p.k < p.E;
+  // K of the second products is shared by workgroups until two a CU have some, four blocks a wave at least (8 tokens, 4 of 4
+  // experts of 384 x 10432: 24 us in one workgroup each, SPLIT_TIME in five)
+  const int rows = column_blocks(p) == 1 && !p.by_pair && p.d % 64 == 0 ? 64 : 32, tiles = p.d / rows, y = p.by_pair ? p.T * p.k : p.E;
+  const int wk = share((int64_t)tiles * y, p.kb_f), each = kWaves / wk;
+  p.splits = std::max(1, std::min(512 / std::max(1, (tiles + each - 1) / each * y), p.kb_f / (4 * wk)));
+}
+
 size_t lay_out(MoeParams& p, uint8_t* base) {
+  plan(p);
   size_t at = 0;
   auto take = [&](size_t bytes) {
     uint8_t* r = base + at;
@@ -730,17 +778,8 @@ size_t lay_out(MoeParams& p, uint8_t* base) {
   const size_t P = (size_t)p.T * p.k;
   p.logits = reinterpret_cast<double*>(take((size_t)p.T * p.E * 8));
   for (uint16_t*& h : p.h) h = reinterpret_cast<uint16_t*>(take(P * p.F * 2));
-  p.part = reinterpret_cast<float*>(take(P * p.d * 4));
+  p.part = reinterpret_cast<float*>(take(p.splits * P * p.d * 4));
   return at;
-}
-
-// Waves that share a tile's K: until there are four rounds of waves for the CUs (16 each), with two blocks each at
-// least; and one, while there is less than a round.
-int share(int64_t tiles, int kb) {
-  constexpr int64_t kRound = 256 * 16;
-  int wk = 1;
-  while (wk < kWaves && ((tiles * wk * 2 <= 4 * kRound && wk * 4 <= kb) || (tiles * wk < kRound && wk < kb))) wk *= 2;
-  return wk;
 }
 
 // R tiles of 16 rows a wave: four, which columns are read for once; two where there are few pairs, and where there are more
@@ -759,7 +798,7 @@ hipError_t launch_down_tiles(MoeParams p, hipStream_t s) {
   const int y = BY_PAIR ? p.T * p.k : p.E, tiles = p.d / (16 * R);
   p.down_wk = share((int64_t)tiles * y, p.kb_f);
   const int each = kWaves / p.down_wk;
-  hipLaunchKernelGGL((moe_down_kernel<CB, R, PARTS, BY_PAIR>), dim3((tiles + each - 1) / each, y), dim3(64 * kWaves), 0, s, p);
+  hipLaunchKernelGGL((moe_down_kernel<CB, R, PARTS, BY_PAIR>), dim3((tiles + each - 1) / each, y, p.splits), dim3(64 * kWaves), 0, s, p);
   return hipGetLastError();
 }
 
@@ -783,9 +822,7 @@ hipError_t launch_moe(MoeParams p, hipStream_t s) {
   constexpr int PARTS = std::is_same<OUT, float>::value ? 3 : 2;
   const int P = p.T * p.k;
   p.parts = PARTS;
-  // Blocks of 16 columns by the tokens an expert has on average; where it has more than they hold, its weights are read
-  // again (128 tokens, 2 of 8 experts of 4096 x 14336: 871 us with one block, 735 with two, 630 with four).
-  const int blocks = P <= 10 * p.E || p.T <= 16 ? 1 : P <= 24 * p.E || p.T <= 32 ? 2 : 4;
+  const int blocks = column_blocks(p);
   hipError_t e;
   if (p.router) {
     const int nt = p.T <= 16 ? 1 : 2;  // (7 tokens, 60 experts: 46 us with 2, 48 with 8; 64 tokens: 1 us more with 8)
@@ -811,8 +848,8 @@ hipError_t launch_moe(MoeParams p, hipStream_t s) {
     e = blocks == 1 ? launch_up<1>(p, s) : blocks == 2 ? launch_up<2>(p, s) : launch_up<4>(p, s);
   }
   if (e != hipSuccess) return e;
-  if (P <= kFewPairs) {
-    for (p.down_wk = 1; p.down_wk * 2 * P <= kFewPairs && p.down_wk * 2 <= p.kb_f;) p.down_wk *= 2;
+  if (few_down(p)) {
+    p.down_wk = few_share(p);
     hipLaunchKernelGGL(moe_down_few_kernel<OUT>, dim3(p.d / 16), dim3(64 * kFewPairs), 0, s, p);
     return hipGetLastError();
   }
@@ -907,9 +944,6 @@ acrl_status acrl_moe_fp8(const acrl_moe_desc* m, void* stream) {
   p.renormalize = m->renormalize != 0;
   p.act = m->activation;
   p.scale = m->scale;
-  p.kb_d = (p.d + acrl::kBlock - 1) / acrl::kBlock;
-  p.kb_f = (p.F + acrl::kBlock - 1) / acrl::kBlock;
-  p.by_pair = p.T * p.k < p.E;
   const size_t need = p.T ? acrl::lay_out(p, static_cast<uint8_t*>(m->workspace)) : 0;
   if (need && (!m->workspace || m->workspace_bytes < need)) {
     acrl::set_error("acrl_moe_fp8 needs %zu workspace bytes, got %zu", need, m->workspace_bytes);

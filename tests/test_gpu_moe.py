@@ -88,6 +88,16 @@ def test_few_tokens(n, size):
     test_sizes(n + 100, size)
 
 
+# long rows of Wout and few of them: workgroups share a row, by expert and by pair, odd parts among them
+LONG = [(8, 64, 2, 2, 4160), (3, 96, 5, 4, 4480), (2, 96, 8, 6, 4512), (40, 64, 2, 1, 4128), (1, 32, 3, 3, 5152), (17, 32, 20, 1, 8224),
+        (70, 64, 2, 2, 6144)]
+
+
+@pytest.mark.parametrize("n,size", list(enumerate(LONG)))
+def test_long_rows(n, size):
+    test_sizes(n + 200, size)
+
+
 @pytest.mark.parametrize("act", list(ACTS))
 def test_activations(act):
     torch, dev = torch_dev()

@@ -745,7 +745,7 @@ int column_blocks(const MoeParams& p) {
 }
 
 // The second products of few pairs and their sum as one kernel, where its waves, 16 a workgroup of 16 rows, have not much
-// more of K each than those of the others (2 tokens, 6 of 8 experts of 928 x 8800: 49 us, DOWN_GENERAL the other way).
+// more of K each than those of the others (2 tokens, 6 of 8 experts of 928 x 8800: 76 us in all, 46 the other way).
 int few_share(const MoeParams& p) {
   int wk = 1;
   while (wk * 2 * p.T * p.k <= kFewPairs && wk * 2 <= p.kb_f) wk *= 2;
@@ -760,8 +760,8 @@ void plan(MoeParams& p) {
   p.kb_d = (p.d + kBlock - 1) / kBlock;
   p.kb_f = (p.F + kBlock - 1) / kBlock;
   p.by_pair = p.T * p.k < p.E;
-  // K of the second products is shared by workgroups until two a CU have some, four blocks a wave at least (8 tokens, 4 of 4
-  // experts of 384 x 10432: 24 us in one workgroup each, SPLIT_TIME in five)
+  // K of the second products is shared by workgroups until there are two a CU, with four blocks a wave at least (8 tokens, 2
+  // of 8 experts of 2048 x 8224: 99 us in all, 131 without; 4 of 4 of 384 x 10432: 36 and 50)
   const int rows = column_blocks(p) == 1 && !p.by_pair && p.d % 64 == 0 ? 64 : 32, tiles = p.d / rows, y = p.by_pair ? p.T * p.k : p.E;
   const int wk = share((int64_t)tiles * y, p.kb_f), each = kWaves / wk;
   p.splits = std::max(1, std::min(512 / std::max(1, (tiles + each - 1) / each * y), p.kb_f / (4 * wk)));

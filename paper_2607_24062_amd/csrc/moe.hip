@@ -415,7 +415,7 @@ struct Stream {
 // within 2^-16 of h (7 % of the time of 16 tokens, d = 4096, F = 14336 over one, which
 // would be as far off as y's own rounding), or, where y is fp32, as three, exactly.
 template <int CB, int R, bool BY_PAIR>
-__global__ __launch_bounds__(64 * kWaves, CB == 1 && R == 2 ? 4 : CB <= 2 ? 3 : 2) void moe_up_kernel(MoeParams p) {
+__global__ __launch_bounds__(64 * kWaves, CB == 1 && R == 2 ? 4 : CB == 1 ? 3 : 2) void moe_up_kernel(MoeParams p) {
   __shared__ f32x4 red[kWaves][R][CB][64];
   __shared__ Tokens tokens;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
@@ -738,10 +738,11 @@ int share(int64_t tiles, int kb) {
 }
 
 // Blocks of 16 columns by the tokens an expert has on average; where it has more than they hold, its weights are read
-// again (128 tokens, 2 of 8 experts of 4096 x 14336: 871 us with one block, 735 with two, 630 with four).
+// again (128 tokens, 2 of 8 experts of 4096 x 14336: 871 us with one block, 502 with two, 619 with four, which leave
+// registers for two tiles of rows alone; 1 of 4 of 1024 x 4096: 51 with two, 45 with four).
 int column_blocks(const MoeParams& p) {
   const int P = p.T * p.k;
-  return P <= 10 * p.E || p.T <= 16 ? 1 : P <= 24 * p.E || p.T <= 32 ? 2 : 4;
+  return P <= 10 * p.E || p.T <= 16 ? 1 : P <= 40 * p.E || p.T <= 32 ? 2 : 4;
 }
 
 // The second products of few pairs and their sum as one kernel, where its waves, 16 a workgroup of 16 rows, have not much
@@ -762,7 +763,7 @@ void plan(MoeParams& p) {
   p.by_pair = p.T * p.k < p.E;
   // K of the second products is shared by workgroups until there are two a CU, with four blocks a wave at least (8 tokens, 2
   // of 8 experts of 2048 x 8224: 99 us in all, 131 without; 4 of 4 of 384 x 10432: 36 and 50)
-  const int rows = column_blocks(p) == 1 && !p.by_pair && p.d % 64 == 0 ? 64 : 32, tiles = p.d / rows, y = p.by_pair ? p.T * p.k : p.E;
+  const int rows = column_blocks(p) <= 2 && !p.by_pair && p.d % 64 == 0 ? 64 : 32, tiles = p.d / rows, y = p.by_pair ? p.T * p.k : p.E;
   const int wk = share((int64_t)tiles * y, p.kb_f), each = kWaves / wk;
   p.splits = std::max(1, std::min(512 / std::max(1, (tiles + each - 1) / each * y), p.kb_f / (4 * wk)));
 }
@@ -782,9 +783,10 @@ size_t lay_out(MoeParams& p, uint8_t* base) {
   return at;
 }
 
-// R tiles of 16 rows a wave: four, which columns are read for once; two where there are few pairs, and where there are more
-// blocks of columns.  (With two, in workgroups of eight waves: 64 tokens, 8 of 128 experts of 2048 x 768 149 us for 143, 16
-// tokens, 2 of 8 of 4096 x 14336 293 for 267, 128 of the former 192 for 167.)
+// R tiles of 16 rows a wave: four, which columns are read for once; two where there are few pairs, and with four blocks of
+// columns, whose sums take the registers.  (With two, in workgroups of eight waves: 64 tokens, 8 of 128 experts of 2048 x
+// 768 149 us for 143, 16 tokens, 2 of 8 of 4096 x 14336 293 for 267.  With two and two blocks of columns: 64 tokens of the
+// latter 429 us for 339, 128 tokens, 4 of 32 of 2048 x 1024 86 for 70.)
 template <int CB, int R, bool BY_PAIR>
 hipError_t launch_up_tiles(MoeParams p, hipStream_t s) {
   const int y = BY_PAIR ? p.T * p.k : p.E, tiles = p.F / (8 * R);
@@ -804,14 +806,15 @@ hipError_t launch_down_tiles(MoeParams p, hipStream_t s) {
 
 template <int CB>
 hipError_t launch_up(const MoeParams& p, hipStream_t s) {
-  if constexpr (CB > 1) return launch_up_tiles<CB, 2, false>(p, s);  // (fewer pairs than experts are few an expert)
+  if constexpr (CB > 1) return launch_up_tiles<CB, CB == 2 ? 4 : 2, false>(p, s);  // (fewer pairs than experts are few an expert)
   else if (p.by_pair) return launch_up_tiles<1, 2, true>(p, s);
   else return launch_up_tiles<1, 4, false>(p, s);
 }
 
 template <int CB, int PARTS>
 hipError_t launch_down(const MoeParams& p, hipStream_t s) {
-  if constexpr (CB > 1) return launch_down_tiles<CB, 2, PARTS, false>(p, s);
+  if constexpr (CB == 4) return launch_down_tiles<4, 2, PARTS, false>(p, s);
+  else if constexpr (CB == 2) return p.d % 64 == 0 ? launch_down_tiles<2, 4, PARTS, false>(p, s) : launch_down<4, PARTS>(p, s);
   else if (p.by_pair) return launch_down_tiles<1, 2, PARTS, true>(p, s);
   else if (p.d % 64 == 0) return launch_down_tiles<1, 4, PARTS, false>(p, s);
   else return launch_down_tiles<1, 2, PARTS, false>(p, s);

@@ -684,6 +684,8 @@ acrl_status acrl_moe_fp8(const acrl_moe_desc* desc, void* stream);
  * that were chosen.
  *   lp[j, v] = z[j, v] / tau - log sum_u e^(z[j, u] / tau)       (64 bits)
  *   c[j, v]  = scores[j] + lp[j, v]
+ * (the sum's terms within 1.1e-12 and its logarithm within 5e-12 up to V = 2^20,
+ * beside fp64 roundings; a beam's only token has lp = 0, to the bit)
  *   a finished beam: c[j, eos_id] = scores[j], -infinity for its other tokens
  * The n_out candidates (j, v) of a sequence with the largest c, in falling order,
  * equal ones by beam and then token: ids (v), parents (j) and out_scores (c,

@@ -688,12 +688,13 @@ acrl_status acrl_moe_fp8(const acrl_moe_desc* desc, void* stream);
  * beside fp64 roundings; a beam's only token has lp = 0, to the bit)
  *   a finished beam: c[j, eos_id] = scores[j], -infinity for its other tokens
  * The n_out candidates (j, v) of a sequence with the largest c, in falling order,
- * equal ones by beam and then token: ids (v), parents (j) and out_scores (c,
- * rounded to fp32).  Within a beam the order is that of its logits.  A beam whose
- * score is not finite, or whose logits hold a NaN or +infinity or nothing above
- * -infinity, has c = -infinity for all its tokens; a logit of -infinity has it for
- * its own.  Such candidates come last, by beam and token, like any others of equal
- * score.  The rows of beams that are finished or have no finite score are not read.
+ * equal ones by beam: ids (v), parents (j) and out_scores (c, rounded to fp32).
+ * Within a beam the order is that of its logits, equal ones by token, also where
+ * different logits have the same c in 64 bits (1 / tau = 1e-20; scores of -3e38).
+ * A beam whose score is not finite, or whose logits hold a NaN or +infinity or
+ * nothing above -infinity, has c = -infinity for all its tokens; a logit of -infinity
+ * has it for its own.  Such candidates come last, by beam and token.  The rows of
+ * beams that are finished or have no finite score are not read.
  *   logits    [B K, V] of logits_type, rows ldl apart; row b K + j is beam j's
  *   scores    float [B, K], out_scores float [B, n_out]; with n_out = K it may be scores itself
  *   finished  uint8 [B, K], or NULL

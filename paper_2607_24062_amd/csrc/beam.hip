@@ -309,9 +309,13 @@ __global__ __launch_bounds__(64 * kScanWaves, 8) void beam_scan_kernel(BeamParam
 // A sequence's N best of its beams' lists: their scores as 64-bit keys (0: no
 // candidate) lie in LDS, a lane walks one list, and the first of all heads is taken
 // N times; with more than 64 lists four waves do that, and one of them over their
-// results.  Of equal scores the first list's comes first: lists lie by beam, then by
-// rising tokens.  What a round waits for is the largest of 64 keys alone, 0.15 us
-// (with scores, tokens and ties looked up in each: 0.4).
+// results.  Lists lie by beam, then by rising tokens: of equal scores the first list's
+// comes first.  Different logits of a beam may have the same score, too (they are far
+// smaller than it, or the temperature is near infinity), and then go by logit.  They are
+// read again for that alone, and only where it can be: scores fall with the logits, so
+// no two differing logits share one unless a list's entry and the fp32 value below it
+// do, which is looked at as the scores are made.  What a round waits for is the largest
+// of 64 keys alone, 0.15 us (with scores, tokens and ties looked up in each: 0.4).
 __global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p) {
   extern __shared__ uint64_t keys[];   // [lists][N]
   __shared__ double lse[kMaxBeams], score[kMaxBeams];
@@ -319,6 +323,7 @@ __global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p
   __shared__ int state[kMaxBeams];     // 0: no candidates, 1: its lists, 2: finished
   __shared__ int picked[kPickWaves][kMaxOut], chosen[kMaxOut];  // places in keys
   __shared__ int chosen_beam[kMaxOut], chosen_id[kMaxOut];
+  __shared__ int close;                // different logits of a beam may have the same score
   const int b = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lists = p.K * p.S, N = p.N;
   const float* const val = p.val + (int64_t)b * lists * N;
@@ -335,6 +340,7 @@ __global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p
   for (int i = threadIdx.x; i < lists * N; i += 64 * kPickWaves)  // (a thread's own, until they are keys)
     keys[i] = (uint64_t)__float_as_uint(val[i]) << 1 | (idx[i] != kNone);
   if (has_list) refs[threadIdx.x] = list_ref, sums[threadIdx.x] = list_sum;
+  if (threadIdx.x == 0) close = 0;
   __syncthreads();
   if (has_beam) {
     const int j = threadIdx.x;
@@ -358,10 +364,24 @@ __global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p
     const uint64_t v = keys[i];
     uint64_t key = 0;
     if (state[j] == 2 && i == j * p.S * N) key = score_key(score[j]);
-    if (state[j] == 1 && (v & 1)) key = score_key(score[j] + ((double)__uint_as_float((uint32_t)(v >> 1)) * (double)p.inv_t - lse[j]));
+    if (state[j] == 1 && (v & 1)) {
+      const float z = __uint_as_float((uint32_t)(v >> 1));
+      auto key_at = [&](float z) { return score_key(score[j] + ((double)z * (double)p.inv_t - lse[j])); };
+      key = key_at(z);
+      if (p.S > 1 && key_at(value_of(order_of(z) - 1)) == key) close = 1;
+    }
     keys[i] = key;
   }
   __syncthreads();
+  const bool by_logit = __builtin_amdgcn_readfirstlane(close);
+  // of the lanes `same`, whose lists' heads (at `here`) have equal scores, the first: by beam, logit and list
+  auto first_of = [&](uint64_t same, int here) {
+    const int each = p.S * N, beam = read_lane(here, lowest(same)) / each;
+    const bool in = same >> lane & 1 && here / each == beam;
+    const uint32_t z = in ? order_of(val[here]) : 0;  // (0: a NaN's, no candidate's.  A finished beam has one, with nobody to tie)
+    const uint32_t top = (uint32_t)largest(z);
+    return lowest(__ballot(in && z == top));
+  };
   // the first n of the lists that the wave's lanes walk, place by place (-1: none), to `to`
   auto pick = [&](auto place, int* to) {
     int at = 0, here = place(0), behind = place(1), n = 0;
@@ -369,7 +389,8 @@ __global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p
     for (; n < N; ++n) {
       const uint64_t best = largest(key);
       if (best == 0) break;
-      if (lane == lowest(__ballot(key == best))) {
+      const uint64_t same = __ballot(key == best);
+      if (lane == (by_logit && same & (same - 1) ? first_of(same, here) : lowest(same))) {
         to[n] = here;
         here = behind;
         key = next;

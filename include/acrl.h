@@ -707,7 +707,8 @@ acrl_status acrl_moe_fp8(const acrl_moe_desc* desc, void* stream);
  *   dst[o, b, n] = src[o, b, parents[b, n]]     (zeros where that is no beam)
  * each at its strides in bytes (outer, sequence, beam).  dst may be src itself
  * (n_out = K, same strides): beams that stay are then not touched.  Otherwise the
- * two must not overlap, and rows of dst must not overlap each other.
+ * two must not overlap.  Rows of dst must not overlap each other: of its strides,
+ * those of single entries aside, each is no less than what rows at the smaller ones span.
  * Requirements: outer and B at most 2^20, K and n_out in [1, 64], strides in
  * [0, 2^42); any alignment: copied in units of 16, 4 or 1 bytes, the largest that
  * divides both addresses, all strides and row_bytes; the units of a row, rounded up

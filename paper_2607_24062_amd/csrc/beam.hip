@@ -8,7 +8,9 @@
 #include <float.h>
 
 #include <algorithm>
+#include <iterator>
 #include <type_traits>
+#include <utility>
 
 #include "entry.h"
 #include "lanes.h"
@@ -627,8 +629,17 @@ acrl_status acrl_beam_reorder(const acrl_reorder_desc* d, void* stream) {
     ACRL_REQUIRE(d->src && d->dst && d->parents, "src, dst and parents are required");
     ACRL_REQUIRE(((uintptr_t)d->parents & 3u) == 0, "parents is misaligned");
     // (the last byte's place fits 64 bits: factors of at most 2^20, strides below 2^42)
-    ACRL_REQUIRE((d->n_out == 1 || d->dst_beam >= d->row_bytes) && (d->B == 1 || d->dst_seq >= d->row_bytes) &&
-                     (d->outer == 1 || d->dst_outer >= d->row_bytes), "rows of dst overlap");
+    // By rising stride, each no less than what the rows under it span.  (No overflow: a span that passes is no more than a
+    // stride, below 2^42, and grows by at most 2^20 strides.)
+    std::pair<uint64_t, uint64_t> sides[] = {{d->dst_beam, d->n_out}, {d->dst_seq, d->B}, {d->dst_outer, d->outer}};
+    std::sort(std::begin(sides), std::end(sides));
+    uint64_t span = (uint64_t)d->row_bytes;
+    for (auto [stride, n] : sides)
+      if (n > 1) {
+        ACRL_REQUIRE(stride >= span, "rows of dst overlap: a stride of %llu bytes, and %llu under it",
+                     (unsigned long long)stride, (unsigned long long)span);
+        span += (n - 1) * stride;
+      }
     auto last = [&](int64_t so, int64_t ss, int64_t sb, int64_t n) {
       return (uintptr_t)((d->outer - 1) * so) + (uintptr_t)((d->B - 1) * ss) + (uintptr_t)((n - 1) * sb + d->row_bytes);
     };

@@ -696,7 +696,8 @@ acrl_status acrl_moe_fp8(const acrl_moe_desc* desc, void* stream);
  * has it for its own.  Such candidates come last, by beam and token.  The rows of
  * beams that are finished or have no finite score are not read.
  *   logits    [B K, V] of logits_type, rows ldl apart; row b K + j is beam j's
- *   scores    float [B, K], out_scores float [B, n_out]; with n_out = K it may be scores itself
+ *   scores    float [B, K], out_scores float [B, n_out]; with n_out = K it may be scores
+ *             itself, otherwise the two must not overlap
  *   finished  uint8 [B, K], or NULL
  *   ids, parents  int32 [B, n_out]
  * Requirements: 0 <= B <= 2^20, 1 <= K <= 64, B K < 2^22, 1 <= V < 2^30, 1 <= n_out <= min(64, K V),

@@ -585,6 +585,11 @@ acrl_status acrl_beam_step(const acrl_beam_desc* d, void* stream) {
     return ACRL_ERR_WORKSPACE;
   }
   ACRL_REQUIRE(acrl::aligned16(d->workspace), "workspace must be 16-byte aligned");
+  // (a sequence's scores are read by its own workgroup of the choice, before it writes: only there may they be replaced)
+  const uintptr_t in = (uintptr_t)d->scores, out = (uintptr_t)d->out_scores;
+  ACRL_REQUIRE(d->B == 0 || (in == out && d->n_out == d->K) || out >= in + (uintptr_t)(d->B * d->K) * 4 ||
+                   in >= out + (uintptr_t)(d->B * d->n_out) * 4,
+               "out_scores overlaps scores without being scores itself, of n_out = K");
   st = acrl::check_device();
   if (st != ACRL_OK || d->B == 0) return st;
   p.logits = d->logits;

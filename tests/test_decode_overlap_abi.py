@@ -55,3 +55,21 @@ def test_rows_side_by_side(acrl, p):  # noqa: F811
     # strides of dimensions that have one entry are not looked at; states in place
     for kw in (dict(B=1, dst_seq=0), dict(n_out=1, dst_beam=3), dict(dst=p), dict(dst=p, K=1, n_out=1, dst_beam=0, src_beam=0)):
         assert not _refused(acrl, "acrl_beam_reorder", _reorder(acrl, p, **kw)), kw
+
+
+def test_scores_on_scores(acrl, p):  # noqa: F811
+    # out_scores may be scores itself, sequence by sequence; any other overlap writes what another sequence still reads
+    ok = dict(B=4, K=3, V=100, n_out=3, logits=p, ldl=100, scores=_off(p, 1024), ids=_off(p, 2048), parents=_off(p, 3072),
+              out_scores=_off(p, 4096), inv_temperature=1.0, workspace=p, workspace_bytes=1 << 30)
+    call = lambda **kw: _refused(acrl, "acrl_beam_step", acrl.BeamDesc(**{**ok, **kw}))  # noqa: E731
+    # scores are 48 bytes from 1024 on, n_out of 2 and 5 write 32 and 80
+    for kw in (dict(out_scores=_off(p, 1024), n_out=2), dict(out_scores=_off(p, 1024), n_out=5), dict(out_scores=_off(p, 1028)),
+               dict(out_scores=_off(p, 1020)), dict(out_scores=_off(p, 1068)), dict(out_scores=_off(p, 1024 - 44)),
+               dict(out_scores=_off(p, 1024 - 76), n_out=5)):
+        assert call(**kw), kw
+        assert b"out_scores" in acrl.lib().acrl_last_error()
+    if __import__("torch").cuda.is_available():
+        pytest.skip("calls of host memory end at the device's look-up only where there is none")
+    for kw in (dict(out_scores=_off(p, 1024)), dict(out_scores=_off(p, 1072)), dict(out_scores=_off(p, 976)),
+               dict(out_scores=_off(p, 944), n_out=5), dict(out_scores=_off(p, 992), n_out=2)):
+        assert not call(**kw), (kw, acrl.lib().acrl_last_error())

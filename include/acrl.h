@@ -571,7 +571,8 @@ acrl_status acrl_matmul_fp8(const acrl_matmul_desc* desc, void* stream);
  *   NONE S;  RELU max(S, 0);  SILU S / (1 + e^-S);  GELU S Phi(S), Phi the normal
  *   distribution function;  GELU_TANH S (1 + tanh(sqrt(2/pi) (S + 0.044715 S^3))) / 2
  * each within 6e-7 of its exact value at S, relative to its size (5e-5 where y
- * is bf16), or within 1.3e-36.  NaN stays NaN.
+ * is bf16), or within 1.3e-36.  NaN stays NaN; S = -infinity gives 0 with RELU and NaN
+ * (infinity times 0) with SILU, GELU and GELU_TANH.
  *   bias      [N] of bias_type, or NULL
  *   residual  [M, N] of residual_type, rows ldr elements apart, or NULL.  It may
  *             be y itself (same pointer, type and row distance): y is then updated

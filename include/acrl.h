@@ -618,8 +618,8 @@ acrl_status acrl_linear_fp8(const acrl_linear_desc* desc, void* stream);
  * without one), and what their rows of x hold has no influence; experts that no
  * token chose are not read.
  * Weights are E4M3 with one scale per 128 x 128 block (ACRL_SCALE_BLOCK128 of each
- * expert's matrix), x stays bf16; sums are fp32, what lies between the products
- * keeps 16 bits and more.  y is rounded once.
+ * expert's matrix), x stays bf16; sums are fp32.  What lies between the products is
+ * fp32 where y is, and within 2^-16 of it where y is bf16.  y is rounded once.
  *   x         bf16 [T, d], rows ldx elements apart
  *   router    bf16 [E, d], or NULL: ids and weights are inputs (a routing made
  *             earlier, taken over as it is; ids outside [0, E) add nothing, the
@@ -682,7 +682,10 @@ acrl_status acrl_moe_fp8(const acrl_moe_desc* desc, void* stream);
 /* ======================================================================== *
  * Beside acrl_sample_mu, which draws the next token of a response: the choice of
  * the next tokens of B sequences of K beams each, and the states of the beams
- * that were chosen.
+ * that were chosen.  The logits are the caller's, for instance acrl_matmul_fp8's with
+ * a head of ACRL_SCALE_BLOCK128; acrl_score_pi_mu and acrl_sample_mu read the first
+ * three scalings, so their mu is another quantization of the same head, and its
+ * log-probs of a beam's tokens are not the beam's score.
  *   lp[j, v] = z[j, v] / tau - log sum_u e^(z[j, u] / tau)       (64 bits)
  *   c[j, v]  = scores[j] + lp[j, v]
  * (the sum's terms within 1.1e-12 and its logarithm within 5e-12 up to V = 2^20,

@@ -57,7 +57,7 @@ __device__ __forceinline__ bool alive(float score) { return fabsf(score) < INFIN
 // exact at 0, which is one of the points at even degrees.  That keeps what the lane's,
 // wave's and segment's references have in common free of error: a row with a single
 // token left has that token's logit for its normaliser, to the bit.  (Degree 7 is off
-// by 5.5e-11, at 0 by 4e-11, and saves 1.5 us of 82 at 512 x 151936; degree 10, 3.7e-16,
+// by 5.5e-11, at 0 by 4e-11, and saves 2.5 us of 76 at 512 x 151936; degree 10, 3.7e-16,
 // takes 6 more.)
 __device__ __forceinline__ double exp2_f64(const BeamParams& p, double d) {
   constexpr double kRound = 6755399441055744.0;  // 1.5 2^52: added, it leaves an integer in the low bits
@@ -135,7 +135,7 @@ __device__ __forceinline__ uint64_t key_of(float v, int idx) {
 // logits.  A workgroup notes in LDS, key by key, what is no less than a bar; when
 // there are many notes they are thinned out to the N largest, and what is above the
 // least of those is noted from there on.  With logits in no order that happens three
-// or four times.  What bounds it (512 x 151936: 70 us) is less the loads (50 alone)
+// or four times.  What bounds it (512 x 151936: 76 us) is less the loads (50 alone)
 // than the vector instructions: fp64 exponentials (20) and notes.  (A list of N a
 // wave, kept in order by insertions, took 28 us more; notes by ballots over all eight
 // logits, 200 instructions, 8 more; notes thinned out from 256 on, 3 more; fmaxf,
@@ -316,8 +316,9 @@ __global__ __launch_bounds__(64 * kScanWaves, 8) void beam_scan_kernel(BeamParam
 // smaller than it, or the temperature is near infinity), and then go by logit.  They are
 // read again for that alone, and only where it can be: scores fall with the logits, so
 // no two differing logits share one unless a list's entry and the fp32 value below it
-// do, which is looked at as the scores are made.  What a round waits for is the largest
-// of 64 keys alone, 0.15 us (with scores, tokens and ties looked up in each: 0.4).
+// do, which is looked at as the scores are made.  (64 x 8 beams, 16 chosen: 7.7 us, 12.6
+// where all logits are 0 and every round has such ties.)  What a round waits for is else the
+// largest of 64 keys alone, 0.15 us (with scores, tokens and ties looked up in each: 0.4).
 __global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamParams p) {
   extern __shared__ uint64_t keys[];   // [lists][N]
   __shared__ double lse[kMaxBeams], score[kMaxBeams];

@@ -101,3 +101,32 @@ def test_differences_of_a_few_steps():
     for b in range(2):
         assert np.array_equal(ids[b], _by_logit(z[b], n))
     assert (np.diff(scores) <= 0).all()
+
+
+def test_states_whose_layers_sequences_and_beams_lie_in_any_order():
+    # the strides that rows of dst may have: every order of the three, holes among them
+    torch, dev = torch_dev()
+    from itertools import permutations
+
+    from paper_2607_24062_amd import acrl
+    L, B, K, n = 2, 3, 4, 40
+    state = torch.randn((L, B, K, n), device=dev)
+    parents = torch.tensor([[3, 0, 0, 2], [1, 1, 2, 0], [0, 1, 2, 3]], dtype=torch.int32, device=dev)
+    want = torch.stack([state[:, b, parents[b].long()] for b in range(B)], 1)
+    for order in permutations(range(3)):
+        shape = [(L, B, K)[i] for i in order]
+        wide = torch.full((*shape[:2], shape[2] + 1, n + 4), 7.0, device=dev)
+        out = wide[:, :, :shape[2], :n].permute(*(order.index(i) for i in range(3)), 3)
+        assert out.shape == state.shape
+        acrl.acrl_beam_reorder(state, parents, dim=1, out=out)
+        assert torch.equal(out, want)
+        assert bool((wide[..., n:] == 7.0).all()) and bool((wide[:, :, shape[2]:] == 7.0).all())
+        own = out.clone(memory_format=torch.preserve_format)
+        out.copy_(state)
+        acrl.acrl_beam_reorder(out, parents, dim=1, out=out)
+        assert torch.equal(out, want) and torch.equal(own, want)
+    # rows of two sequences on each other: refused
+    flat = torch.zeros(L * B * K * n, device=dev)
+    both = flat.as_strided((1, 2, 3, n), (0, n, n, 1))
+    with pytest.raises(acrl.AcrlError, match="overlap"):
+        acrl.acrl_beam_reorder(state[:1, :2, :3].contiguous(), parents[:2, :3].contiguous(), dim=1, out=both)
